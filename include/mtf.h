@@ -455,6 +455,79 @@ mtf_status mtf_xent_backward(const mtf_layout_t* layout, const mtf_tensor* h, co
                              const mtf_tensor* lse, const mtf_tensor* dloss, mtf_tensor* dh, mtf_tensor* dwout, void* workspace, size_t workspace_bytes,
                              void* stream);
 
+/* ---- other losses on stored logits ----------------------------------------------------------------------
+ * Beside the cross-entropy above: distillation from a teacher's most likely words, the clipped policy loss
+ * with a divergence term, and the preference loss on pairs of sequences.  (The paper trains with maximum
+ * likelihood alone; these are the losses its models are tuned with, on the logits that mtf_einsum leaves.)
+ * Common to all:
+ *   logits   [*tokens, vocab], bf16 or f32, any vocab size, 16-byte aligned.  dlogits: the same dims and type, 16-byte
+ *            aligned; it may be `logits` itself, and overlaps nothing else.  With it dh and dwout are two einsums, as in
+ *            mtf_xent_backward.
+ *   targets  int32, one per token; a value outside [0, vocab) is treated as in mtf_softmax_xent_forward: the row's loss
+ *            and gradient are 0 and mtf_device_status reports it.
+ *   weight   f32 [*tokens], or NULL for ones: a factor of the token's loss.  A row of weight 0 (a prompt, padding) is not
+ *            read, nor are its targets and other inputs: all its results are 0.
+ *   f32 tensors "per token" have the dims of logits without the last one, in their order.  No output may overlap another
+ *   tensor of the call.  Row statistics are f32 sums of f32 exponentials with the maximum subtracted, what a row works out
+ *   from them is held in 64 bits, and each result is rounded once.  A logit of -infinity is a word of probability 0; a row
+ *   with a NaN or +infinity, or with no finite logit, has NaN for its results.  Results repeat bit for bit.
+ *   Vocab split over processors is free (the logits are stored once); split across RANKS it is refused, MTF_ERR_UNSUPPORTED.
+ * The forward calls leave what the backward calls read.  A step is both in one launch that reads the logits once: the gradient
+ * is that of the SUM of the losses it returns (weights carry the normalisation).  dloss: NULL, or factors that
+ * multiply the gradient, f32 per token (preference: per pair).
+ *
+ * Distillation.  teacher_ids int32 and teacher_logits (bf16 or f32) [*tokens, slots], 1 <= slots <= 512: a teacher's words and
+ * its logits for them, in any order; id -1 marks an empty slot (its logit is not used), other ids outside [0, vocab) are
+ * reported and left out, slots with the same id add up.  q = softmax over the used slots of teacher_logits / temperature:
+ *     loss = weight * ( soft_weight * temperature^2 * sum_k q_k (log q_k - log softmax(logits / temperature)[id_k])
+ *                       + hard_weight * (lse - logits[target]) )
+ * A token without a used slot has the second term alone.  targets may be NULL when hard_weight is 0.
+ * stats f32 [*tokens, 2]: the log-sum-exp of logits / temperature (0 when soft_weight is 0) and of logits (0 when
+ * hard_weight is 0).  temperature from 1e-4 to 1e4; weights >= 0, finite. */
+typedef struct { float temperature, soft_weight, hard_weight; } mtf_distill_params;
+mtf_status mtf_distill_forward(const mtf_layout_t* layout, const mtf_tensor* logits, const int32_t* teacher_ids, const mtf_tensor* teacher_logits,
+                               const int32_t* targets, const mtf_tensor* weight, const mtf_distill_params* params, mtf_tensor* stats,
+                               mtf_tensor* loss, void* stream);
+mtf_status mtf_distill_backward(const mtf_layout_t* layout, const mtf_tensor* logits, const int32_t* teacher_ids, const mtf_tensor* teacher_logits,
+                                const int32_t* targets, const mtf_tensor* weight, const mtf_distill_params* params, const mtf_tensor* stats,
+                                const mtf_tensor* dloss, mtf_tensor* dlogits, void* stream);
+mtf_status mtf_distill_step(const mtf_layout_t* layout, const mtf_tensor* logits, const int32_t* teacher_ids, const mtf_tensor* teacher_logits,
+                            const int32_t* targets, const mtf_tensor* weight, const mtf_distill_params* params, mtf_tensor* loss,
+                            mtf_tensor* dlogits, void* stream);
+/* Policy.  old_logp, ref_logp, advantage: f32 per token; ref_logp may be NULL when kl_weight is 0.
+ *     logp = logits[target] - lse;  r = exp(logp - old_logp);  e = ref_logp - logp
+ *     loss  = weight * ( -min(r * advantage, clip(r, 1 - clip_low, 1 + clip_high) * advantage) + kl_weight * (exp(e) - 1 - e) )
+ *     dlogp = d loss / d logp  (0 through the first term where the clipped product is the smaller one)
+ *     dlogits = dloss * dlogp * (onehot(target) - softmax(logits))
+ * lse, logp, dlogp, loss: f32 per token.  0 <= clip_low <= 1, clip_high >= 0, kl_weight >= 0 and finite (clip_high may be
+ * infinite: no limit above). */
+typedef struct { float clip_low, clip_high, kl_weight; } mtf_policy_params;
+mtf_status mtf_policy_forward(const mtf_layout_t* layout, const mtf_tensor* logits, const int32_t* targets, const mtf_tensor* old_logp,
+                              const mtf_tensor* ref_logp, const mtf_tensor* advantage, const mtf_tensor* weight, const mtf_policy_params* params,
+                              mtf_tensor* lse, mtf_tensor* logp, mtf_tensor* dlogp, mtf_tensor* loss, void* stream);
+mtf_status mtf_policy_backward(const mtf_layout_t* layout, const mtf_tensor* logits, const int32_t* targets, const mtf_tensor* lse,
+                               const mtf_tensor* dlogp, const mtf_tensor* dloss, mtf_tensor* dlogits, void* stream);
+mtf_status mtf_policy_step(const mtf_layout_t* layout, const mtf_tensor* logits, const int32_t* targets, const mtf_tensor* old_logp,
+                           const mtf_tensor* ref_logp, const mtf_tensor* advantage, const mtf_tensor* weight, const mtf_policy_params* params,
+                           mtf_tensor* logp, mtf_tensor* loss, mtf_tensor* dlogits, void* stream);
+/* Preference.  logits [branch = 2, *pairs, length, vocab]: the first dimension has size 2 (0: the answer preferred, 1: the
+ * other one), the last token dimension is the one along an answer; *pairs may be absent (one pair).
+ *     logp per token as above;  seq_logp[i, b] = sum over length of weight * logp     (weight 1 / length: the mean)
+ *     margin = (seq_logp[0] - ref_logp[0]) - (seq_logp[1] - ref_logp[1]);  h = beta * margin
+ *     sigmoid: loss = -(1 - smoothing) log sigmoid(h) - smoothing log sigmoid(-h);   hinge: loss = max(0, 1 - h)
+ *     squared: loss = (margin - 1 / (2 beta))^2
+ *     dseq = d loss / d seq_logp;   dlogits = dloss * dseq * weight * (onehot(target) - softmax(logits))
+ * ref_logp, seq_logp, dseq: f32 [branch, *pairs];  loss, dloss: f32 [*pairs] (one pair without *pairs: one element in any
+ * dims);  lse, logp: f32 per token.  beta > 0 and finite; 0 <= smoothing <= 0.5, and 0 unless the kind is sigmoid.  The branch
+ * and length dimensions may not be split across ranks (MTF_ERR_UNSUPPORTED). */
+typedef enum { MTF_PREFERENCE_SIGMOID = 0, MTF_PREFERENCE_HINGE = 1, MTF_PREFERENCE_SQUARED = 2 } mtf_preference_kind;
+typedef struct { int32_t kind; float beta, smoothing; } mtf_preference_params;
+mtf_status mtf_preference_forward(const mtf_layout_t* layout, const mtf_tensor* logits, const int32_t* targets, const mtf_tensor* weight,
+                                  const mtf_tensor* ref_logp, const mtf_preference_params* params, mtf_tensor* lse, mtf_tensor* logp,
+                                  mtf_tensor* seq_logp, mtf_tensor* dseq, mtf_tensor* loss, void* stream);
+mtf_status mtf_preference_backward(const mtf_layout_t* layout, const mtf_tensor* logits, const int32_t* targets, const mtf_tensor* weight,
+                                   const mtf_tensor* lse, const mtf_tensor* dseq, const mtf_tensor* dloss, mtf_tensor* dlogits, void* stream);
+
 /* ---- reductions (Section 6 "Reduction") --------------------------------------------------------- */
 /* out[out dims] = sum over the other dims of in (out dims a subset of in's).  Local reduction per
  * slice, then the group sum across the mesh dims of reduced-out split dims, in one launch. */
@@ -484,7 +557,7 @@ const char* mtf_last_error(void);
 /* Synchronises the current device and reads the sticky device status word: 0 = no kernel of this
  * library gave up on a bounded wait since the last call; non-zero = a code naming the wait.
  * Resets the word.  Returns MTF_ERR_TIMEOUT when it was non-zero, else MTF_ERR_INVALID_ARG when a
- * token id or target outside [0, vocab) was seen by the vocab kernels since the last call. */
+ * token id or target outside [0, vocab) was seen by the vocab and loss kernels since the last call. */
 mtf_status mtf_device_status(int32_t* code);
 /* Testing hook for the failure path of the bounded device-side waits.  limit_cycles > 0 sets how many SM
  * cycles a wait may take before it gives up (<= 0 restores the default of about two seconds);

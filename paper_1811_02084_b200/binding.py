@@ -82,6 +82,20 @@ class mtf_update_params(Structure):
     _fields_ = [("lr", c_float), ("momentum", c_float), ("weight_decay", c_float)]
 
 
+class mtf_distill_params(Structure):
+    _fields_ = [("temperature", c_float), ("soft_weight", c_float), ("hard_weight", c_float)]
+
+
+class mtf_policy_params(Structure):
+    _fields_ = [("clip_low", c_float), ("clip_high", c_float), ("kl_weight", c_float)]
+
+
+class mtf_preference_params(Structure):
+    _fields_ = [("kind", c_int32), ("beta", c_float), ("smoothing", c_float)]
+
+
+MTF_PREFERENCE_SIGMOID, MTF_PREFERENCE_HINGE, MTF_PREFERENCE_SQUARED = 0, 1, 2
+_PREFERENCE_KINDS = {"sigmoid": MTF_PREFERENCE_SIGMOID, "hinge": MTF_PREFERENCE_HINGE, "squared": MTF_PREFERENCE_SQUARED}
 MTF_RESHAPE_NONE, MTF_RESHAPE_ALLGATHER, MTF_RESHAPE_SLICE, MTF_RESHAPE_ALLTOALL = 0, 1, 2, 3
 
 
@@ -99,6 +113,7 @@ def _load():
             "`python paper_1811_02084_b200/build.py` (needs nvcc; there is no CPU fallback).")
     L = ctypes.CDLL(LIB_PATH)
     vp = c_void_p
+    _T = POINTER(mtf_tensor)
     sig = {
         "mtf_mesh_create": [c_int32, POINTER(mtf_dim), POINTER(vp)],
         "mtf_mesh_destroy": [vp],
@@ -155,6 +170,14 @@ def _load():
         "mtf_xent_forward": [vp, POINTER(mtf_tensor), POINTER(mtf_tensor), vp, POINTER(mtf_tensor), POINTER(mtf_tensor), POINTER(mtf_tensor), vp, c_size_t, vp],
         "mtf_xent_backward": [vp, POINTER(mtf_tensor), POINTER(mtf_tensor), vp, POINTER(mtf_tensor), POINTER(mtf_tensor), POINTER(mtf_tensor), POINTER(mtf_tensor),
                               POINTER(mtf_tensor), vp, c_size_t, vp],
+        "mtf_distill_forward": [vp, _T, vp, _T, vp, _T, POINTER(mtf_distill_params), _T, _T, vp],
+        "mtf_distill_backward": [vp, _T, vp, _T, vp, _T, POINTER(mtf_distill_params), _T, _T, _T, vp],
+        "mtf_distill_step": [vp, _T, vp, _T, vp, _T, POINTER(mtf_distill_params), _T, _T, vp],
+        "mtf_policy_forward": [vp, _T, vp, _T, _T, _T, _T, POINTER(mtf_policy_params), _T, _T, _T, _T, vp],
+        "mtf_policy_backward": [vp, _T, vp, _T, _T, _T, _T, vp],
+        "mtf_policy_step": [vp, _T, vp, _T, _T, _T, _T, POINTER(mtf_policy_params), _T, _T, _T, vp],
+        "mtf_preference_forward": [vp, _T, vp, _T, _T, POINTER(mtf_preference_params), _T, _T, _T, _T, _T, vp],
+        "mtf_preference_backward": [vp, _T, vp, _T, _T, _T, _T, _T, vp],
         "mtf_debug_wait_test": [c_int64, c_int32],
         "mtf_debug_contraction": [c_int32, c_int32, POINTER(c_int32), POINTER(c_int32)],
         "mtf_debug_pair_tiles": [c_int32, c_int32, POINTER(c_int32), POINTER(c_int32)],
@@ -622,6 +645,67 @@ def mtf_xent_backward(layout, h: Named, wout: Named, targets, logits: Named, lse
     wp, wb = _ws(workspace)
     _check(_lib.mtf_xent_backward(layout.handle, _p(h), _p(wout), c_void_p(targets.data_ptr()), _p(logits), _p(lse), _p(dloss), _p(dh), _p(dwout), wp, wb,
                                   _stream(stream)))
+
+
+def _ids(t):
+    """The pointer of an int32 tensor of ids (None: no tensor)."""
+    if t is None:
+        return c_void_p(0)
+    if str(t.dtype) != "torch.int32" or not t.is_contiguous():
+        raise MtfError(1, "ids and targets must be contiguous int32 tensors")
+    return c_void_p(t.data_ptr())
+
+
+def mtf_distill_forward(layout, logits: Named, teacher_ids, teacher_logits: Named, targets, weight: Named | None, temperature: float, soft_weight: float,
+                        hard_weight: float, stats: Named, loss: Named, stream=None) -> None:
+    """teacher_ids [*tokens, slots] and targets [*tokens] (None when hard_weight is 0): contiguous int32 device tensors."""
+    hp = mtf_distill_params(float(temperature), float(soft_weight), float(hard_weight))
+    _check(_lib.mtf_distill_forward(layout.handle, _p(logits), _ids(teacher_ids), _p(teacher_logits), _ids(targets), _p(weight), byref(hp), _p(stats), _p(loss),
+                                    _stream(stream)))
+
+
+def mtf_distill_backward(layout, logits: Named, teacher_ids, teacher_logits: Named, targets, weight: Named | None, temperature: float, soft_weight: float,
+                         hard_weight: float, stats: Named, dloss: Named | None, dlogits: Named, stream=None) -> None:
+    hp = mtf_distill_params(float(temperature), float(soft_weight), float(hard_weight))
+    _check(_lib.mtf_distill_backward(layout.handle, _p(logits), _ids(teacher_ids), _p(teacher_logits), _ids(targets), _p(weight), byref(hp), _p(stats), _p(dloss),
+                                     _p(dlogits), _stream(stream)))
+
+
+def mtf_distill_step(layout, logits: Named, teacher_ids, teacher_logits: Named, targets, weight: Named | None, temperature: float, soft_weight: float,
+                     hard_weight: float, loss: Named, dlogits: Named, stream=None) -> None:
+    hp = mtf_distill_params(float(temperature), float(soft_weight), float(hard_weight))
+    _check(_lib.mtf_distill_step(layout.handle, _p(logits), _ids(teacher_ids), _p(teacher_logits), _ids(targets), _p(weight), byref(hp), _p(loss), _p(dlogits),
+                                 _stream(stream)))
+
+
+def mtf_policy_forward(layout, logits: Named, targets, old_logp: Named, ref_logp: Named | None, advantage: Named, weight: Named | None, clip_low: float,
+                       clip_high: float, kl_weight: float, lse: Named, logp: Named, dlogp: Named, loss: Named, stream=None) -> None:
+    hp = mtf_policy_params(float(clip_low), float(clip_high), float(kl_weight))
+    _check(_lib.mtf_policy_forward(layout.handle, _p(logits), _ids(targets), _p(old_logp), _p(ref_logp), _p(advantage), _p(weight), byref(hp), _p(lse), _p(logp),
+                                   _p(dlogp), _p(loss), _stream(stream)))
+
+
+def mtf_policy_backward(layout, logits: Named, targets, lse: Named, dlogp: Named, dloss: Named | None, dlogits: Named, stream=None) -> None:
+    _check(_lib.mtf_policy_backward(layout.handle, _p(logits), _ids(targets), _p(lse), _p(dlogp), _p(dloss), _p(dlogits), _stream(stream)))
+
+
+def mtf_policy_step(layout, logits: Named, targets, old_logp: Named, ref_logp: Named | None, advantage: Named, weight: Named | None, clip_low: float,
+                    clip_high: float, kl_weight: float, logp: Named, loss: Named, dlogits: Named, stream=None) -> None:
+    hp = mtf_policy_params(float(clip_low), float(clip_high), float(kl_weight))
+    _check(_lib.mtf_policy_step(layout.handle, _p(logits), _ids(targets), _p(old_logp), _p(ref_logp), _p(advantage), _p(weight), byref(hp), _p(logp), _p(loss),
+                                _p(dlogits), _stream(stream)))
+
+
+def mtf_preference_forward(layout, logits: Named, targets, weight: Named | None, ref_logp: Named, kind, beta: float, smoothing: float, lse: Named, logp: Named,
+                           seq_logp: Named, dseq: Named, loss: Named, stream=None) -> None:
+    """kind: "sigmoid", "hinge", "squared" or the constants of the same names."""
+    hp = mtf_preference_params(_PREFERENCE_KINDS[kind] if kind in _PREFERENCE_KINDS else int(kind), float(beta), float(smoothing))
+    _check(_lib.mtf_preference_forward(layout.handle, _p(logits), _ids(targets), _p(weight), _p(ref_logp), byref(hp), _p(lse), _p(logp), _p(seq_logp), _p(dseq),
+                                       _p(loss), _stream(stream)))
+
+
+def mtf_preference_backward(layout, logits: Named, targets, weight: Named | None, lse: Named, dseq: Named, dloss: Named | None, dlogits: Named, stream=None) -> None:
+    _check(_lib.mtf_preference_backward(layout.handle, _p(logits), _ids(targets), _p(weight), _p(lse), _p(dseq), _p(dloss), _p(dlogits), _stream(stream)))
 
 
 def mtf_status_string(status: int) -> str:
