@@ -7,6 +7,7 @@
 #include <cuda_runtime.h>
 
 #include <algorithm>
+#include <atomic>
 
 #include "launch.cuh"
 #include "losses.h"
@@ -16,7 +17,6 @@ namespace {
 using mtf::LossRows;
 using mtf::kMaxTeacher;
 
-constexpr int kThreads = 256;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLowest = -3.402823466e38f;
 
@@ -26,22 +26,73 @@ __device__ __forceinline__ float ex2(float x) {
   return y;
 }
 
-template <typename T> struct Piece;      // 16 bytes of a row
+// Two f32 values side by side: one instruction works on both.
+typedef unsigned long long f32x2;
+__device__ __forceinline__ f32x2 pair(float lo, float hi) {
+  f32x2 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+  return r;
+}
+__device__ __forceinline__ f32x2 pair(float v) { return pair(v, v); }
+__device__ __forceinline__ float2 both(f32x2 v) {
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+  return r;
+}
+__device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) { f32x2 r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
+__device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b) { f32x2 r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
+__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) { f32x2 r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c)); return r; }
+
+// 2^y of both on the special-function unit, ...
+__device__ __forceinline__ f32x2 ex2_unit(f32x2 y) {
+  const float2 f = both(y);
+  return pair(ex2(f.x), ex2(f.y));
+}
+// ... and on the arithmetic pipes, for y <= 0 or NaN: y = i + f, i whole, |f| <= 1/2, and 2^f as the polynomial of degree 5 through
+// (0, 1) with the smallest largest relative error on [-1/2, 1/2] (found by linear programming: 9e-8; 1.7e-7 with f32 coefficients and sums).
+// Below -127 the result is exactly 0.  A NaN may come out as a number.
+__device__ __forceinline__ f32x2 ex2_fma(f32x2 y) {
+  float2 c = both(y);
+  y = pair(fmaxf(c.x, -127.f), fmaxf(c.y, -127.f));
+  const f32x2 whole = add2(y, pair(12582912.f));                  // 1.5 * 2^23: the sum's low bits are i
+  const f32x2 f = fma2(add2(whole, pair(-12582912.f)), pair(-1.f), y);
+  f32x2 v = fma2(f, pair(0.0013264727f), pair(0.009671513f));
+  v = fma2(f, v, pair(0.055507336f));
+  v = fma2(f, v, pair(0.24022242f));
+  v = fma2(f, v, pair(0.693147f));
+  v = fma2(f, v, pair(1.f));
+  const float2 w = both(whole);
+  c = both(v);
+  return pair(__uint_as_float(__float_as_uint(c.x) + (__float_as_uint(w.x) << 23)), __uint_as_float(__float_as_uint(c.y) + (__float_as_uint(w.y) << 23)));
+}
+
+template <typename T> struct Piece;      // 16 bytes of a row: kN values, two by two
 template <> struct Piece<__nv_bfloat16> {
   static constexpr int kN = 8;
-  static __device__ __forceinline__ void get(const uint4& u, float* f) {
+  static __device__ __forceinline__ void get(const uint4& u, f32x2* f) {
     const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      f[2 * e] = __uint_as_float(w[e] << 16);
-      f[2 * e + 1] = __uint_as_float(w[e] & 0xFFFF0000u);
-    }
+    for (int e = 0; e < 4; ++e) f[e] = pair(__uint_as_float(w[e] << 16), __uint_as_float(w[e] & 0xFFFF0000u));
   }
-  static __device__ __forceinline__ uint4 put(const float* f) {
+  static __device__ __forceinline__ uint32_t max2(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+  }
+  // the largest value of N pieces (NaN only if there is nothing else)
+  template <int N>
+  static __device__ __forceinline__ float largest(const uint4* u) {
+    uint32_t m = max2(max2(u[0].x, u[0].y), max2(u[0].z, u[0].w));
+#pragma unroll
+    for (int i = 1; i < N; ++i) m = max2(m, max2(max2(u[i].x, u[i].y), max2(u[i].z, u[i].w)));
+    return fmaxf(__uint_as_float(m << 16), __uint_as_float(m & 0xFFFF0000u));
+  }
+  static __device__ __forceinline__ uint4 put(const f32x2* f) {
     uint32_t w[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const __nv_bfloat162 h = __floats2bfloat162_rn(f[2 * e], f[2 * e + 1]);
+      const float2 v = both(f[e]);
+      const __nv_bfloat162 h = __floats2bfloat162_rn(v.x, v.y);
       w[e] = *reinterpret_cast<const uint32_t*>(&h);
     }
     return make_uint4(w[0], w[1], w[2], w[3]);
@@ -51,11 +102,21 @@ template <> struct Piece<__nv_bfloat16> {
 };
 template <> struct Piece<float> {
   static constexpr int kN = 4;
-  static __device__ __forceinline__ void get(const uint4& u, float* f) {
-    f[0] = __uint_as_float(u.x); f[1] = __uint_as_float(u.y); f[2] = __uint_as_float(u.z); f[3] = __uint_as_float(u.w);
+  static __device__ __forceinline__ void get(const uint4& u, f32x2* f) {
+    f[0] = pair(__uint_as_float(u.x), __uint_as_float(u.y));
+    f[1] = pair(__uint_as_float(u.z), __uint_as_float(u.w));
   }
-  static __device__ __forceinline__ uint4 put(const float* f) {
-    return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+  template <int N>
+  static __device__ __forceinline__ float largest(const uint4* u) {
+    float m = kLowest;
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      m = fmaxf(m, fmaxf(fmaxf(__uint_as_float(u[i].x), __uint_as_float(u[i].y)), fmaxf(__uint_as_float(u[i].z), __uint_as_float(u[i].w))));
+    return m;
+  }
+  static __device__ __forceinline__ uint4 put(const f32x2* f) {
+    const float2 a = both(f[0]), b = both(f[1]);
+    return make_uint4(__float_as_uint(a.x), __float_as_uint(a.y), __float_as_uint(b.x), __float_as_uint(b.y));
   }
   static __device__ __forceinline__ float one(const void* p, long long i) { return reinterpret_cast<const float*>(p)[i]; }
   static __device__ __forceinline__ void set(void* p, long long i, float v) { reinterpret_cast<float*>(p)[i] = v; }
@@ -70,68 +131,131 @@ template <typename T>
 __device__ __forceinline__ RowSpan row_span(long long row, int V) {
   constexpr int n = Piece<T>::kN;
   RowSpan s;
-  const int off = (int)((row * V) % n);
-  s.head = min(V, (n - off) % n);
-  s.pieces = (V - s.head) / n;
+  const int off = (int)(((uint32_t)row * (uint32_t)V) & (n - 1));
+  s.head = min(V, (n - off) & (n - 1));
+  s.pieces = (int)((uint32_t)(V - s.head) / n);
   s.tail = V - s.head - s.pieces * n;
   return s;
 }
 __device__ __forceinline__ int edge_element(const RowSpan& s, int i, int V) { return i < s.head ? i : V - s.tail + (i - s.head); }
 
-// Running maximum and sums of exponentials relative to it.  The maximum starts at the lowest finite number, so that entries of
-// -infinity add nothing and need no care, and a row of them alone leaves sums of 0.
+// 2^(z a0 - b0) and, with two temperatures, 2^(z a1 - b1), a0 being the softened one.  A temperature of 2 (NT = 3) has the second as the square of
+// the first (b1 = 2 b0).  For others (NT = 2) the special-function unit alone would bound a distillation's walks (4 exponentials an entry at 16
+// a cycle and SM): it takes three of four, the arithmetic pipes the fourth, which is a softened one, so that a NaN is never lost.
+template <int NT>
+__device__ __forceinline__ void exponentials(int e, f32x2 z, float a0, float nb0, float a1, float nb1, f32x2& e0, f32x2& e1) {
+  const f32x2 y = fma2(z, pair(a0), pair(nb0));
+  e0 = NT == 2 && (e & 1) ? ex2_fma(y) : ex2_unit(y);
+  if (NT == 2) e1 = ex2_unit(fma2(z, pair(a1), pair(nb1)));
+  if (NT == 3) e1 = mul2(e0, e0);
+}
+
+__device__ __forceinline__ float reference(float m, float a) { return __fmul_rn(m, a); }
+// What a row's exponents are formed from: the factors a0 and a1, and the size `huge` from which on logits have no room for the products (they would
+// be rounded by a whole exponent and more).  A row without an entry between -huge and huge, or with one above (a row that is masked as a whole by
+// the type's lowest value, say), is worked out from differences instead.
+struct Factors {
+  float a0, a1, huge;
+  __host__ __device__ __forceinline__ Factors(float a0_, float a1_) : a0(a0_), a1(a1_), huge(16777216.f / (a0_ > a1_ ? a0_ : a1_)) {}
+  __device__ __forceinline__ bool is_huge(float m) const { return !(fabsf(m) < huge); }
+};
+
+// Sums of exponentials relative to a reference m, an entry of the row: sums of 2^(z a - b) with b = fl(m a), the one rounding of which every use
+// of the sums allows for.  m starts at -huge (far lower entries, infinity among them, add nothing) and is raised to the largest entry seen only
+// where that lies 2^40 above it: an f32 sum has room for that, and nearly every entry is spared the rescaling (a thread that raises its
+// reference holds up its warp, and with a maximum that is always exact some thread of a warp nearly always does).
 template <int NT>
 struct RunningSum {
-  float m = kLowest, s0 = 0.f, s1 = 0.f;      // s0: exponents times a0, s1: times a1 (NT = 2)
-  template <int N>
-  __device__ __forceinline__ void add(const float* f, float a0, float a1) {
-    float pm = f[0];
-#pragma unroll
-    for (int e = 1; e < N; ++e) pm = fmaxf(pm, f[e]);
-    if (pm > m) {
-      s0 *= ex2((m - pm) * a0);
-      if (NT == 2) s1 *= ex2((m - pm) * a1);
+  float m, limit, nb0, nb1;
+  f32x2 p0 = 0ull, p1 = 0ull;      // p0: exponents times a0, p1: times a1 (two temperatures); two partial sums each
+  __device__ __forceinline__ explicit RunningSum(const Factors& F) : m(-F.huge), limit(-F.huge), nb0(reference(F.huge, F.a0)), nb1(reference(F.huge, F.a1)) {}
+  __device__ __forceinline__ void raise(float pm, const Factors& F) {
+    const float a0 = F.a0, a1 = F.a1;
+    if (pm > limit) {
+      const float b0 = reference(pm, a0), b1 = reference(pm, a1);
+      p0 = mul2(p0, pair(ex2(-nb0 - b0)));
+      if (NT >= 2) p1 = mul2(p1, pair(ex2(-nb1 - b1)));
       m = pm;
+      limit = pm + 40.f / (NT >= 2 ? fmaxf(a0, a1) : a0);
+      nb0 = -b0;
+      nb1 = -b1;
     }
+  }
+  template <typename T, int N>
+  __device__ __forceinline__ void add(const uint4* u, const Factors& F) {
+    raise(Piece<T>::template largest<N>(u), F);
+    add_below<T, N>(u, F);
+  }
+  template <typename T, int N>
+  __device__ __forceinline__ void add_below(const uint4* u, const Factors& F) {      // ... entries that the reference has been raised for
 #pragma unroll
-    for (int e = 0; e < N; ++e) {
-      s0 += ex2((f[e] - m) * a0);
-      if (NT == 2) s1 += ex2((f[e] - m) * a1);
+    for (int i = 0; i < N; ++i) {
+      f32x2 f[Piece<T>::kN / 2];
+      Piece<T>::get(u[i], f);
+#pragma unroll
+      for (int e = 0; e < Piece<T>::kN / 2; ++e) {
+        f32x2 e0, e1;
+        exponentials<NT>(e, f[e], F.a0, nb0, F.a1, nb1, e0, e1);
+        p0 = add2(p0, e0);
+        if (NT >= 2) p1 = add2(p1, e1);
+      }
     }
   }
-  __device__ __forceinline__ void join(float m2, float t0, float t1, float a0, float a1) {
-    const float mx = fmaxf(m, m2);
-    s0 = s0 * ex2((m - mx) * a0) + t0 * ex2((m2 - mx) * a0);
-    if (NT == 2) s1 = s1 * ex2((m - mx) * a1) + t1 * ex2((m2 - mx) * a1);
-    m = mx;
+  __device__ __forceinline__ void add_one(float f, const Factors& F) {
+    raise(f, F);
+    p0 = add2(p0, pair(ex2(fmaf(f, F.a0, nb0)), 0.f));
+    if (NT >= 2) p1 = add2(p1, pair(ex2(fmaf(f, F.a1, nb1)), 0.f));
   }
+  __device__ __forceinline__ void of_warp(float& t_m, float& t_0, float& t_1, const Factors& F) const;
 };
 
-struct RowResult {
-  float m;                     // the exponentials' shift in both sums
-  double s0, s1;
-};
+// a maximum over the warp: f32 values in the order of whole numbers
+__device__ __forceinline__ float warp_max(float v) {
+  int i = __float_as_int(v);
+  i = __reduce_max_sync(0xffffffffu, i >= 0 ? i : i ^ 0x7fffffff);
+  return __int_as_float(i >= 0 ? i : i ^ 0x7fffffff);
+}
+__device__ __forceinline__ float warp_add(float v) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  return v;
+}
+// what a sum relative to m is multiplied by to be relative to mx >= m
+__device__ __forceinline__ float to_reference(float m, float mx, float a, const Factors& F) { return ex2(F.is_huge(mx) ? (m - mx) * a : reference(m, a) - reference(mx, a)); }
+// the lanes' references and sums joined, the same in every lane
+template <int NT>
+__device__ __forceinline__ void warp_join(float& m, float& s0, float& s1, const Factors& F) {
+  const float mx = warp_max(m);
+  s0 = warp_add(s0 * to_reference(m, mx, F.a0, F));
+  if (NT >= 2) s1 = warp_add(s1 * to_reference(m, mx, F.a1, F));
+  m = mx;
+}
+template <int NT>
+__device__ __forceinline__ void RunningSum<NT>::of_warp(float& t_m, float& t_0, float& t_1, const Factors& F) const {
+  t_m = m;
+  t_0 = both(p0).x + both(p0).y;
+  t_1 = both(p1).x + both(p1).y;
+  warp_join<NT>(t_m, t_0, t_1, F);
+}
 
-// What a row's gradient is made of: k0 exp2((z - m0) a0) (+ k1 exp2((z - m1) a1)), and the entries that differ.
+// What a row's gradient is made of: k0 2^(z a0 + nb0) (+ k1 2^(z a1 + nb1)), or with huge logits k0 2^((z - m0) a0) (+ ...), and the entries
+// that differ.
 struct RowGrad {
-  float k0, m0, k1, m1;
+  float k0, nb0, k1, nb1, m0, m1;
   int zero;                    // the whole row is 0
-  int fix_id;                  // LOGP, POLICY: the label's entry and its value
-  float fix;
+  int huge;
+  float fix;                   // the label's entry
+  double lse0, lse1, cs, ch;   // distillation: log-sum-exps and the two parts' factors
 };
 
-struct Scratch {
-  float m[kThreads / 32], s0[kThreads / 32], s1[kThreads / 32];
-  RowGrad g;
-};
-// the teacher's list, and behind it the label
+// A teacher's list: arrays of `slots`, rounded up to 4.
 struct Slots {
-  double q[kMaxTeacher + 1];
-  int id[kMaxTeacher + 1];
-  float z[kMaxTeacher + 1];
-  float fix[kMaxTeacher + 1];      // the entry's gradient
-  int first[kMaxTeacher + 1];      // of the slots with this id it is the first, which writes
-  double red[2][kThreads / 32];
+  double* q;                   // its distribution
+  int* id;                     // -1: empty
+  float* z;                    // the student's logit; later the entry's gradient
+  static __host__ __device__ int room(int slots) { return (slots + 3) & ~3; }
+  static __host__ __device__ size_t bytes(int slots) { return (size_t)room(slots) * 16; }
+  __device__ Slots(unsigned char* at, int slots) : q(reinterpret_cast<double*>(at)), id(reinterpret_cast<int*>(q + room(slots))), z(reinterpret_cast<float*>(id + room(slots))) {}
 };
 
 __device__ __forceinline__ double warp_add(double v) {
@@ -144,294 +268,890 @@ __device__ __forceinline__ double warp_max(double v) {
   for (int o = 16; o > 0; o >>= 1) v = fmax(v, __shfl_xor_sync(0xffffffffu, v, o));
   return v;
 }
-// sum (or maximum) over the block, the same in every thread; red: a slot per warp
-template <bool kMax>
-__device__ __forceinline__ double block_all(double v, double* red) {
-  v = kMax ? warp_max(v) : warp_add(v);
-  __syncthreads();
-  if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = v;
-  __syncthreads();
-  double r = red[0];
-#pragma unroll
-  for (int w = 1; w < kThreads / 32; ++w) r = kMax ? fmax(r, red[w]) : r + red[w];
+
+// ---- what a row is worked out from, apart from the walks over its logits -------------------------------------------------------
+template <int OP> __device__ __forceinline__ bool soft_on(const LossRows& a) { return OP == mtf::LOSS_DISTILL && a.soft != 0.f; }
+template <int OP> __device__ __forceinline__ bool hard_on(const LossRows& a) { return OP == mtf::LOSS_DISTILL && a.hard != 0.f; }
+
+struct RowIn {
+  float w, scale;              // factors of the loss and (backward) of the gradient
+  int label;
+  bool skip, bad;              // nothing to be done but zeros; the label is out of range
+};
+// A row whose factor is 0 is not looked at: neither its label nor anything else of it.
+template <int OP, int PASS>
+__device__ __forceinline__ RowIn row_in(const LossRows& a, long long row) {
+  // (all loads at once; what a row's factor of 0 leaves out is loaded and not looked at)
+  RowIn r;
+  const bool wants_label = OP != mtf::LOSS_DISTILL || hard_on<OP>(a);
+  r.w = a.weight ? a.weight[row] : 1.f;
+  r.label = wants_label ? a.targets[row] : 0;
+  r.scale = 1.f;
+  if (PASS == mtf::LOSS_BACKWARD) {
+    long long at = row;
+    if (OP == mtf::LOSS_DISTILL) r.scale = r.w;
+    else if (a.dseq) {
+      const unsigned seq = (unsigned)row / (unsigned)a.length;
+      at = seq % (unsigned)a.pairs;
+      const float d = a.dseq[seq];
+      r.scale = r.w == 0.f ? 0.f : r.w * d;
+    } else {
+      r.scale = a.dlogp[row];
+    }
+    const float f = a.dloss ? a.dloss[at] : 1.f;
+    if (r.scale != 0.f) r.scale *= f;
+  }
+  r.skip = r.w == 0.f || (PASS == mtf::LOSS_BACKWARD && r.scale == 0.f);
+  r.bad = !r.skip && wants_label && (r.label < 0 || r.label >= a.V);
+  r.skip |= r.bad;
   return r;
 }
 
-// One block per row: the statistics in one walk over the row, the gradient in another.
-template <typename T, int OP, int PASS, int NT>
-__global__ void __launch_bounds__(kThreads) loss_rows_kernel(const LossRows a, int* __restrict__ bad) {
-  using P = Piece<T>;
-  mtf::chain_wait_only();
-  __shared__ Scratch sc;
-  extern __shared__ __align__(16) unsigned char dyn[];
-  Slots& sl = *reinterpret_cast<Slots*>(dyn);
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const long long row = blockIdx.x;
-  const int V = a.V;
-  const RowSpan sp = row_span<T>(row, V);
-  const char* const zr = reinterpret_cast<const char*>(a.z) + row * V * (long long)sizeof(T);
-  char* const dr = reinterpret_cast<char*>(a.d) + row * V * (long long)sizeof(T);
-  const uint4* const z16 = reinterpret_cast<const uint4*>(zr + sp.head * (int)sizeof(T));
-  uint4* const d16 = reinterpret_cast<uint4*>(dr + sp.head * (int)sizeof(T));
-  const bool soft_on = OP == mtf::LOSS_DISTILL && a.soft != 0.f, hard_on = OP == mtf::LOSS_DISTILL && a.hard != 0.f;
-  // the first sum is the softened one wherever there is one
-  const float tau = soft_on ? a.temperature : 1.f;
-  const float a0 = kLog2e / tau, a1 = kLog2e;
+// by one thread: the results of a row that is skipped
+template <int OP>
+__device__ __forceinline__ void zero_results(const LossRows& a, long long row) {
+  if (a.loss) a.loss[row] = 0.f;
+  if (a.logp) a.logp[row] = 0.f;
+  if (a.dlogp) a.dlogp[row] = 0.f;
+  if (!a.lse) return;
+  if (OP == mtf::LOSS_DISTILL) { a.lse[2 * row] = 0.f; a.lse[2 * row + 1] = 0.f; }
+  else a.lse[row] = 0.f;
+}
 
-  const float w = a.weight ? a.weight[row] : 1.f;
-  // a row whose factor is 0 is not looked at: neither its label nor anything else of it
-  bool skip = w == 0.f;
-  float scale = 1.f;           // of the gradient (backward)
-  if (PASS == mtf::LOSS_BACKWARD && !skip) {
-    long long at = row;
-    if (OP == mtf::LOSS_DISTILL) scale = w;
-    else if (a.dseq) { scale = w * a.dseq[row / a.length]; at = (row / a.length) % a.pairs; }
-    else scale = a.dlogp[row];
-    if (a.dloss && scale != 0.f) scale *= a.dloss[at];
-    skip = scale == 0.f;
+struct RowInputs {
+  float zy, old, ref, adv;
+  double kl, sum;              // the teacher's sum_k q_k (log q_k - z_k / tau), and sum_k q_k: 1, or 0 without a used slot
+};
+// By one warp, before anything of the row is overwritten; all lanes return the same.  The teacher's list, with its distribution over the used
+// slots, goes to `sl`.
+template <typename T, int OP>
+__device__ __forceinline__ RowInputs row_inputs(const LossRows& a, long long row, const char* zr, int label, const Slots& sl, int lane, int* bad, bool report = true) {
+  RowInputs r = {};
+  if (OP != mtf::LOSS_DISTILL || hard_on<OP>(a)) r.zy = Piece<T>::one(zr, label);
+  if (OP == mtf::LOSS_POLICY) {
+    r.old = a.old_logp[row];
+    r.adv = a.advantage[row];
+    if (a.kl_weight != 0.f) r.ref = a.ref_logp[row];
   }
-  int label = 0;
-  if (!skip && (OP != mtf::LOSS_DISTILL || hard_on)) {
-    label = a.targets[row];
-    if (label < 0 || label >= V) { skip = true; if (tid == 0) atomicExch(bad, 1); }
-  }
-  if (skip) {
-    if ((PASS & mtf::LOSS_FORWARD) && tid == 0) {
-      if (a.loss) a.loss[row] = 0.f;
-      if (a.logp) a.logp[row] = 0.f;
-      if (a.dlogp) a.dlogp[row] = 0.f;
-      if (a.lse) {
-        if (OP == mtf::LOSS_DISTILL) { a.lse[2 * row] = 0.f; a.lse[2 * row + 1] = 0.f; }
-        else a.lse[row] = 0.f;
+  if (OP != mtf::LOSS_DISTILL) return r;
+  const int K = a.slots;
+  constexpr int kB = 4;        // loads in flight a lane
+  double best = -INFINITY;
+  for (int k0 = lane; k0 < Slots::room(K); k0 += 32 * kB) {
+    int id[kB];
+    float t[kB], z[kB];
+#pragma unroll
+    for (int i = 0; i < kB; ++i) {
+      const int k = k0 + 32 * i;
+      id[i] = -1;
+      t[i] = 0.f;
+      if (k < K && soft_on<OP>(a)) {
+        id[i] = a.teacher_ids[row * K + k];
+        t[i] = a.teacher_bf16 ? Piece<__nv_bfloat16>::one(a.teacher, row * K + k) : Piece<float>::one(a.teacher, row * K + k);
       }
     }
-    if (PASS & mtf::LOSS_BACKWARD) {
-      for (int p = tid; p < sp.pieces; p += kThreads) d16[p] = make_uint4(0u, 0u, 0u, 0u);
-      if (tid < sp.head + sp.tail) P::set(dr, edge_element(sp, tid, V), 0.f);
+#pragma unroll
+    for (int i = 0; i < kB; ++i) {
+      if (id[i] < -1 || id[i] >= a.V) { if (report) atomicExch(bad, 1); id[i] = -1; }
+      z[i] = id[i] >= 0 ? Piece<T>::one(zr, id[i]) : 0.f;
     }
-    return;
+#pragma unroll
+    for (int i = 0; i < kB; ++i) {
+      const int k = k0 + 32 * i;
+      if (k >= Slots::room(K)) continue;
+      const double q = id[i] >= 0 ? (double)t[i] * a.inv_tau : -INFINITY;
+      sl.id[k] = id[i];
+      sl.z[k] = z[i];
+      sl.q[k] = q;
+      best = fmax(best, q != q ? INFINITY : q);      // (NaN: every difference to the maximum is NaN)
+    }
   }
+  best = warp_max(best);
+  const bool any = best != -INFINITY;
+  double sum = 0.0, kl = 0.0;
+  if (any) {
+    for (int k = lane; k < K; k += 32) {
+      const double d = sl.q[k] - best, e = exp(d);
+      sum += e;
+      if (e != 0.0) kl += e * (d - (double)sl.z[k] * a.inv_tau);      // (a word of probability 0 adds nothing, whatever the student says to it)
+      sl.q[k] = e;
+    }
+    sum = warp_add(sum);
+    const double inv = 1.0 / sum;
+    r.kl = warp_add(kl) * inv - log(sum);
+    for (int k = lane; k < K; k += 32) sl.q[k] *= inv;
+  } else {
+    for (int k = lane; k < K; k += 32) sl.id[k] = -1;
+  }
+  r.sum = any ? 1.0 : 0.0;
+  __syncwarp();
+  return r;
+}
 
-  // ---- statistics -------------------------------------------------------------------------------------------------
-  RowResult r;
-  r.m = 0.f; r.s0 = 1.0; r.s1 = 1.0;
+// log sum exp of z / tau, less m / tau, from a sum s relative to m
+__device__ __forceinline__ double log_sum(float m, double s, float af, const Factors& F) {
+  const double off = F.is_huge(m) ? 0.0 : ((double)reference(m, af) - (double)m * (double)af) * 0.6931471805599453;
+  return off + log(s);
+}
+
+// The row's numbers from its reference and sums, in 64 bits: they are differences of values near each other.  write: this thread stores the
+// results per row.
+template <int OP, int PASS, int NT>
+__device__ __forceinline__ RowGrad row_numbers(const LossRows& a, long long row, const RowIn& in, const RowInputs& x, float m, double s0, double s1, bool write,
+                                               const Factors& F) {
+  const float a0 = F.a0, a1 = F.a1;
+  RowGrad g = {};
+  const double w = (double)in.w;
+  double logp;                 // of the label
   if (PASS & mtf::LOSS_FORWARD) {
-    RunningSum<NT> rs;
-    for (int p = tid; p < sp.pieces; p += kThreads) {
-      float f[P::kN];
-      P::get(z16[p], f);
-      rs.template add<P::kN>(f, a0, a1);
-    }
-    if (tid < sp.head + sp.tail) {
-      const float f = P::one(zr, edge_element(sp, tid, V));
-      rs.template add<1>(&f, a0, a1);
-    }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-      const float m2 = __shfl_xor_sync(0xffffffffu, rs.m, o), t0 = __shfl_xor_sync(0xffffffffu, rs.s0, o);
-      const float t1 = NT == 2 ? __shfl_xor_sync(0xffffffffu, rs.s1, o) : 0.f;
-      rs.join(m2, t0, t1, a0, a1);
-    }
-    if (lane == 0) { sc.m[warp] = rs.m; sc.s0[warp] = rs.s0; sc.s1[warp] = rs.s1; }
-    __syncthreads();
-    r.m = kLowest;
-#pragma unroll
-    for (int i = 0; i < kThreads / 32; ++i) r.m = fmaxf(r.m, sc.m[i]);
-    r.s0 = r.s1 = 0.0;
-#pragma unroll
-    for (int i = 0; i < kThreads / 32; ++i) {
-      r.s0 += (double)(sc.s0[i] * ex2((sc.m[i] - r.m) * a0));
-      if (NT == 2) r.s1 += (double)(sc.s1[i] * ex2((sc.m[i] - r.m) * a1));
-    }
-    if (NT == 1) r.s1 = r.s0;
-  }
-
-  // ---- the row's numbers, in 64 bits: they are differences of values near each other ------------------------------------
-  if (OP != mtf::LOSS_DISTILL) {
-    if (tid == 0) {
-      RowGrad g = {};
-      g.fix_id = label;
-      double c, logp;
-      const double zy = (double)P::one(zr, label);
-      if (PASS & mtf::LOSS_FORWARD) {
-        const double log_s = log(r.s0);
-        logp = (zy - (double)r.m) - log_s;
-        if (a.lse) a.lse[row] = (float)((double)r.m + log_s);
-        if (a.logp) a.logp[row] = (float)logp;
-        c = 0.0;
-        if (OP == mtf::LOSS_POLICY) {
-          const double adv = (double)a.advantage[row], ratio = exp(logp - (double)a.old_logp[row]);
-          const double plain = ratio * adv, clipped = fmin(fmax(ratio, 1.0 - (double)a.clip_low), 1.0 + (double)a.clip_high) * adv;
-          const bool cut = plain > clipped;             // (not so for NaN, which both results then show)
-          double loss = cut ? -clipped : -plain, dl = cut ? 0.0 : -plain;
-          if (a.kl_weight != 0.f) {
-            const double e = (double)a.ref_logp[row] - logp, em1 = expm1(e);
-            loss += (double)a.kl_weight * (em1 - e);
-            dl -= (double)a.kl_weight * em1;
-          }
-          a.loss[row] = (float)((double)w * loss);
-          c = (double)w * dl;
-          if (a.dlogp) a.dlogp[row] = (float)c;
-        }
-        g.k0 = (float)(-c / r.s0);
-        g.m0 = r.m;
-      } else {
-        const float lse = a.lse[row];
-        logp = zy - (double)lse;
-        c = (double)scale;
-        g.k0 = -scale;
-        g.m0 = lse;
-      }
-      g.zero = c == 0.0;
-      g.fix = (float)(-c * expm1(logp));
-      sc.g = g;
-    }
+    const double inv_tau = OP == mtf::LOSS_DISTILL ? a.inv_tau : 1.0, l0 = log_sum(m, s0, a0, F), l1 = NT == 1 ? l0 : log_sum(m, s1, a1, F);
+    g.lse0 = (double)m * inv_tau + l0;
+    g.lse1 = NT == 1 ? g.lse0 : (double)m + l1;      // (one sum: tau is 1, or only one of the two is used)
+    g.m0 = g.m1 = m;
+    logp = ((double)x.zy - (double)m) - l1;
+  } else if (OP == mtf::LOSS_DISTILL) {
+    g.lse0 = (double)a.lse[2 * row];
+    g.lse1 = (double)a.lse[2 * row + 1];
+    g.m0 = (float)(soft_on<OP>(a) ? g.lse0 * (double)a.temperature : g.lse1);
+    g.m1 = NT == 1 ? g.m0 : (float)g.lse1;
+    logp = (double)x.zy - g.lse1;
   } else {
-    const int K = a.slots;
-    double lse0, lse1;           // of z / tau, of z
-    if (PASS & mtf::LOSS_FORWARD) {
-      lse0 = (double)r.m / (double)tau + log(r.s0);
-      lse1 = (double)r.m + log(r.s1);
-      if (tid == 0 && a.lse) {
-        a.lse[2 * row] = (float)(soft_on ? lse0 : 0.0);
-        a.lse[2 * row + 1] = (float)(hard_on ? lse1 : 0.0);
-      }
-    } else {
-      lse0 = (double)a.lse[2 * row];
-      lse1 = (double)a.lse[2 * row + 1];
-    }
-    // the teacher's distribution over its used slots
-    double best = -INFINITY;
-    if (soft_on) {
-      for (int k = tid; k < K; k += kThreads) {
-        int id = a.teacher_ids[row * K + k];
-        if (id < -1 || id >= V) { atomicExch(bad, 1); id = -1; }
-        double t = -INFINITY;
-        if (id >= 0) {
-          t = (double)(a.teacher_bf16 ? Piece<__nv_bfloat16>::one(a.teacher, row * K + k) : Piece<float>::one(a.teacher, row * K + k)) / (double)tau;
-          sl.z[k] = P::one(zr, id);
-        }
-        sl.id[k] = id;
-        sl.q[k] = t;
-        best = fmax(best, t != t ? INFINITY : t);      // (NaN: every difference to the maximum is NaN)
-      }
-      best = block_all<true>(best, sl.red[0]);
-    }
-    const bool any = soft_on && best != -INFINITY;
-    double sum = 0.0;
-    if (any)
-      for (int k = tid; k < K; k += kThreads) sum += exp(sl.q[k] - best);
-    sum = block_all<false>(sum, sl.red[1]);
-    const double log_norm = any ? best + log(sum) : 0.0;
-    double kl = 0.0;
-    if (any)
-      for (int k = tid; k < K; k += kThreads) {
-        const double t = sl.q[k] - log_norm, q = exp(t);
-        if (q != 0.0) kl += q * (t - ((double)sl.z[k] / (double)tau - lse0));      // (a word of probability 0 adds nothing, whatever the student says to it)
-        sl.q[k] = q;
-      }
-    if (PASS & mtf::LOSS_FORWARD) {
-      kl = block_all<false>(kl, sl.red[0]);
-      if (tid == 0) {
-        double loss = any ? (double)a.soft * (double)tau * (double)tau * kl : 0.0;
-        if (hard_on) loss += (double)a.hard * (lse1 - (double)P::one(zr, label));
-        a.loss[row] = (float)((double)w * loss);
-      }
-    }
-    if (PASS & mtf::LOSS_BACKWARD) {
-      const double g = PASS == mtf::LOSS_BACKWARD ? (double)scale : (double)w;
-      const double cs = any ? g * (double)a.soft * (double)tau : 0.0, ch = hard_on ? g * (double)a.hard : 0.0;
-      if (tid == 0) {
-        RowGrad gr = {};
-        if (PASS == mtf::LOSS_STEP) {
-          gr.m0 = gr.m1 = r.m;
-          gr.k0 = (float)(NT == 2 ? cs / r.s0 : (cs + ch) / r.s0);
-          gr.k1 = (float)(ch / r.s1);
-        } else {
-          gr.m0 = (float)(soft_on ? lse0 * (double)tau : lse1);
-          gr.m1 = (float)lse1;
-          gr.k0 = (float)(NT == 2 ? cs : cs + ch);
-          gr.k1 = (float)ch;
-        }
-        gr.zero = cs == 0.0 && ch == 0.0;
-        sc.g = gr;
-        sl.id[K] = hard_on ? label : -1;
-        sl.q[K] = 0.0;
-        if (hard_on) sl.z[K] = P::one(zr, label);
-      }
-      if (!any)
-        for (int k = tid; k < K; k += kThreads) sl.id[k] = -1;
-      __syncthreads();
-      // the entries that differ; of slots with one id the first takes care of all
-      for (int k = tid; k <= K; k += kThreads) {
-        const int id = sl.id[k];
-        bool first = id >= 0;
-        double q = 0.0;
-        for (int j = 0; first && j <= K; ++j)
-          if (sl.id[j] == id) {
-            first = j >= k;
-            q += sl.q[j];
-          }
-        sl.first[k] = first;
-        if (!first) continue;
-        const double z = (double)sl.z[k];
-        double v = 0.0;
-        if (any) v += cs * (exp(z / (double)tau - lse0) - q);
-        if (hard_on) v += ch * (exp(z - lse1) - (id == label ? 1.0 : 0.0));
-        sl.fix[k] = (float)v;
-      }
-    }
+    g.lse0 = g.lse1 = (double)a.lse[row];
+    g.m0 = g.m1 = (float)g.lse0;
+    logp = (double)x.zy - g.lse0;
   }
-  if (!(PASS & mtf::LOSS_BACKWARD)) return;
-  __syncthreads();
-
-  // ---- gradient -------------------------------------------------------------------------------------------------------
-  const RowGrad g = sc.g;
-  if (g.zero) {
-    for (int p = tid; p < sp.pieces; p += kThreads) d16[p] = make_uint4(0u, 0u, 0u, 0u);
-    if (tid < sp.head + sp.tail) P::set(dr, edge_element(sp, tid, V), 0.f);
-    return;
-  }
-  auto value = [&](float z) {
-    float v = g.k0 * ex2((z - g.m0) * a0);
-    if (NT == 2) v += g.k1 * ex2((z - g.m1) * a1);
-    return v;
-  };
-  for (int p = tid; p < sp.pieces; p += kThreads) {
-    float f[P::kN];
-    P::get(z16[p], f);
-#pragma unroll
-    for (int e = 0; e < P::kN; ++e) f[e] = value(f[e]);
-    d16[p] = P::put(f);
-  }
-  if (tid < sp.head + sp.tail) {
-    const int e = edge_element(sp, tid, V);
-    P::set(dr, e, value(P::one(zr, e)));
-  }
-  __syncthreads();
+  double c0, c1 = 0.0;         // factors of the two distributions in the gradient
   if (OP != mtf::LOSS_DISTILL) {
-    if (tid == 0) P::set(dr, g.fix_id, g.fix);
+    double c = (double)in.scale;
+    if (PASS & mtf::LOSS_FORWARD) {
+      const float hi = (float)logp;
+      // (preference: until the pairs' kernel has added the log-probabilities up, lse holds what rounding logp to f32 leaves over)
+      if (write && a.lse) a.lse[row] = OP == mtf::LOSS_LOGP && isfinite(hi) ? (float)(logp - (double)hi) : (float)g.lse0;
+      if (write && a.logp) a.logp[row] = hi;
+      c = 0.0;
+      if (OP == mtf::LOSS_POLICY) {
+        const double adv = (double)x.adv, ratio = exp(logp - (double)x.old), plain = ratio * adv;
+        const double clipped = fmin(fmax(ratio, 1.0 - (double)a.clip_low), 1.0 + (double)a.clip_high) * adv;
+        const bool cut = plain > clipped;             // (not so for NaN, which both results then show)
+        double loss = cut ? -clipped : -plain, dl = cut ? 0.0 : -plain;
+        if (a.kl_weight != 0.f) {
+          const double e = (double)x.ref - logp, em1 = expm1(e);
+          loss += (double)a.kl_weight * (em1 - e);
+          dl -= (double)a.kl_weight * em1;
+        }
+        if (write) a.loss[row] = (float)(w * loss);
+        c = w * dl;
+        if (write && a.dlogp) a.dlogp[row] = (float)c;
+      }
+    }
+    if (PASS == mtf::LOSS_FORWARD) return g;
+    c0 = -c;
+    g.fix = (float)(-c * expm1(logp));
   } else {
-    for (int k = tid; k <= a.slots; k += kThreads)
-      if (sl.first[k]) P::set(dr, sl.id[k], sl.fix[k]);
+    if (PASS & mtf::LOSS_FORWARD) {
+      double loss = 0.0;
+      if (x.sum != 0.0) loss = (double)a.soft * (double)a.temperature * (double)a.temperature * (x.kl + g.lse0);
+      if (hard_on<OP>(a)) loss -= (double)a.hard * logp;
+      if (write) {
+        a.loss[row] = (float)(w * loss);
+        if (a.lse) {
+          a.lse[2 * row] = (float)(soft_on<OP>(a) ? g.lse0 : 0.0);
+          a.lse[2 * row + 1] = (float)(hard_on<OP>(a) ? g.lse1 : 0.0);
+        }
+      }
+    }
+    if (PASS == mtf::LOSS_FORWARD) return g;
+    const double f = PASS == mtf::LOSS_BACKWARD ? (double)in.scale : w;
+    g.cs = x.sum != 0.0 ? f * (double)a.soft * (double)a.temperature : 0.0;
+    g.ch = hard_on<OP>(a) ? f * (double)a.hard : 0.0;
+    c0 = NT >= 2 ? g.cs : g.cs + g.ch;
+    c1 = g.ch;
+    // (the label's entry where no slot has it)
+    g.fix = (float)((g.cs != 0.0 ? g.cs * exp((double)x.zy * a.inv_tau - g.lse0) : 0.0) + g.ch * expm1(logp));
+  }
+  g.zero = c0 == 0.0 && (NT == 1 || c1 == 0.0);
+  g.huge = F.is_huge(g.m0) || F.is_huge(g.m1);
+  g.nb0 = -reference(g.m0, a0);
+  g.nb1 = NT == 3 ? 2.f * g.nb0 : -reference(g.m1, a1);
+  if (PASS == mtf::LOSS_STEP) {
+    g.k0 = (float)(c0 / s0);
+    g.k1 = NT >= 2 ? (float)(c1 / s1) : 0.f;
+  } else {
+    // 2^(z a - b) for exp of z / tau - lse: the rest of the exponent goes to the factor
+    const double l0 = soft_on<OP>(a) ? g.lse0 * (double)a.temperature : OP == mtf::LOSS_DISTILL ? g.lse1 : g.lse0;
+    g.k0 = (float)(g.huge ? c0 : c0 * exp2(-(double)g.nb0 - l0 * (double)a0));
+    g.k1 = (float)(g.huge || NT == 1 ? c1 : c1 * exp2(-(double)g.nb1 - g.lse1 * (double)a1));
+  }
+  return g;
+}
+
+// The entries of a distillation row's gradient that differ from the walk's, by one warp: their values take the place of sl.z, and slots that write
+// none get the id -1 (of slots with one id the first takes care of all).  True: a slot has the label's entry, too.
+__device__ __forceinline__ bool slot_values(const LossRows& a, const RowGrad& g, const Slots& sl, int label, int lane) {
+  const int K = a.slots;
+  const int4* const ids = reinterpret_cast<const int4*>(sl.id);
+  bool has_label = false;
+  unsigned later = 0u;         // bit k / 32: not the first of its id
+  for (int k = lane, bit = 0; k < K; k += 32, ++bit) {
+    const int id = sl.id[k];
+    if (id < 0) continue;
+    int first = K, same = 0;
+    for (int j = 0; 4 * j < K; ++j) {
+      const int4 v = ids[j];
+      if (v.w == id) { first = min(first, 4 * j + 3); ++same; }
+      if (v.z == id) { first = min(first, 4 * j + 2); ++same; }
+      if (v.y == id) { first = min(first, 4 * j + 1); ++same; }
+      if (v.x == id) { first = min(first, 4 * j); ++same; }
+    }
+    if (first != k) { later |= 1u << bit; continue; }
+    double q = sl.q[k];
+    for (int j = k + 1; same > 1 && j < K; ++j)
+      if (sl.id[j] == id) { q += sl.q[j]; --same; }
+    const double z = (double)sl.z[k];
+    double v = 0.0;
+    if (g.cs != 0.0) v += g.cs * (exp(z * a.inv_tau - g.lse0) - q);
+    if (g.ch != 0.0) {
+      v += g.ch * (exp(z - g.lse1) - (id == label ? 1.0 : 0.0));
+      has_label |= id == label;
+    }
+    sl.z[k] = (float)v;
+  }
+  __syncwarp();
+  for (int k = lane, bit = 0; k < K; k += 32, ++bit)
+    if ((later >> bit) & 1u) sl.id[k] = -1;
+  __syncwarp();
+  return __any_sync(0xffffffffu, has_label);
+}
+// ... behind the walk's stores, by threads `at` of n.  owned(id): this block writes that entry; label_alone: the label's entry is no slot's.
+template <typename T, typename F>
+__device__ __forceinline__ void write_slots(const LossRows& a, const RowGrad& g, const Slots& sl, int label, bool label_alone, char* dr, int at, int n, F owned) {
+  for (int k = at; k < a.slots; k += n) {
+    const int id = sl.id[k];
+    if (id >= 0 && owned(id)) Piece<T>::set(dr, id, sl.z[k]);
+  }
+  if (at == 0 && label_alone && owned(label)) Piece<T>::set(dr, label, g.fix);
+}
+
+template <typename T, int NT>
+struct GradValues {
+  float k0 = 0.f, nb0 = 0.f, k1 = 0.f, nb1 = 0.f;
+  __device__ __forceinline__ void set(const RowGrad& g) { k0 = g.k0; nb0 = g.nb0; k1 = g.k1; nb1 = g.nb1; }
+  __device__ __forceinline__ uint4 piece(const uint4& u, const Factors& F) const {
+    f32x2 f[Piece<T>::kN / 2];
+    Piece<T>::get(u, f);
+#pragma unroll
+    for (int e = 0; e < Piece<T>::kN / 2; ++e) {
+      f32x2 e0, e1;
+      exponentials<NT>(e, f[e], F.a0, nb0, F.a1, nb1, e0, e1);
+      f[e] = NT >= 2 ? fma2(e1, pair(k1), mul2(e0, pair(k0))) : mul2(e0, pair(k0));
+    }
+    return Piece<T>::put(f);
+  }
+};
+// one entry of a row's gradient, for the row's edges and for rows with huge logits
+template <int NT>
+__device__ __forceinline__ float gradient_of(float z, const RowGrad& g, const Factors& F) {
+  float v = g.k0 * ex2(g.huge ? (z - g.m0) * F.a0 : fmaf(z, F.a0, g.nb0));
+  if (NT >= 2) v += g.k1 * ex2(g.huge ? (z - g.m1) * F.a1 : fmaf(z, F.a1, g.nb1));
+  return v;
+}
+// pieces [first, last) of a row with huge logits, by threads `at` of n
+template <typename T, int NT>
+__device__ __noinline__ void huge_pieces(const uint4* from, uint4* to, int first, int last, int at, int n, const RowGrad& g, const Factors& F) {
+  for (int p = first + at; p < last; p += n) {
+    f32x2 f[Piece<T>::kN / 2];
+    Piece<T>::get(from[p], f);
+    for (int e = 0; e < Piece<T>::kN / 2; ++e) f[e] = pair(gradient_of<NT>(both(f[e]).x, g, F), gradient_of<NT>(both(f[e]).y, g, F));
+    to[p] = Piece<T>::put(f);
   }
 }
 
+// A row's part that one block works on: pieces [begin, end), and the row's edges with the first part.
+template <typename T>
+struct RowPart {
+  RowSpan sp;
+  const char* zr;
+  char* dr;
+  const uint4* z16;
+  uint4* d16;
+  int begin, end, edges, V;
+  // rank: which part, of `each` pieces
+  __device__ __forceinline__ RowPart(const LossRows& a, long long row, int each, int rank) : sp(row_span<T>(row, a.V)), V(a.V) {
+    zr = reinterpret_cast<const char*>(a.z) + row * a.V * (long long)sizeof(T);
+    dr = reinterpret_cast<char*>(a.d) + row * a.V * (long long)sizeof(T);
+    z16 = reinterpret_cast<const uint4*>(zr + sp.head * (int)sizeof(T));
+    d16 = reinterpret_cast<uint4*>(dr + sp.head * (int)sizeof(T));
+    begin = min(sp.pieces, rank * each);
+    end = min(sp.pieces, begin + each);
+    edges = rank == 0 ? sp.head + sp.tail : 0;
+  }
+  __device__ __forceinline__ int edge(int i) const { return edge_element(sp, i, V); }
+  __device__ __forceinline__ bool owned(int e) const {
+    constexpr int n = Piece<T>::kN;
+    return (e >= sp.head + begin * n && e < sp.head + end * n) || (edges && (e < sp.head || e >= V - sp.tail));
+  }
+  __device__ __forceinline__ void zeros(int tid, int n) const {
+    for (int p = begin + tid; p < end; p += n) d16[p] = make_uint4(0u, 0u, 0u, 0u);
+    if (tid < edges) Piece<T>::set(dr, edge(tid), 0.f);
+  }
+};
+
+// The part's largest entry and sums from differences to it, by one warp: for the rows that RunningSum leaves out.
+template <typename T, int NT>
+__device__ __noinline__ void sums_of_differences(const RowPart<T>& part, int lane, const Factors& F, float& m, float& s0, float& s1) {
+  constexpr int n = Piece<T>::kN;
+  const int first = part.sp.head + part.begin * n, last = part.sp.head + part.end * n;
+  auto each = [&](auto f) {
+    for (int e = first + lane; e < last; e += 32) f(Piece<T>::one(part.zr, e));
+    if (lane < part.edges) f(Piece<T>::one(part.zr, part.edge(lane)));
+  };
+  m = kLowest;
+  each([&](float z) { m = fmaxf(m, z); });
+  m = warp_max(m);
+  s0 = s1 = 0.f;
+  each([&](float z) {
+    s0 += ex2((z - m) * F.a0);
+    if (NT >= 2) s1 += ex2((z - m) * F.a1);
+  });
+  s0 = warp_add(s0);
+  s1 = warp_add(s1);
+}
+
+// ---- one block per row, which walks over it in global memory ---------------------------------------------------------------------
+constexpr int kRowWarps = 8;
+
+// pieces [begin, end) of a row, `n` threads side by side, U loads in flight a thread
+template <int U, typename F>
+__device__ __forceinline__ void walk(const uint4* z16, int begin, int end, F f) {
+  const int n = blockDim.x;
+  for (int p = begin + threadIdx.x; p < end; p += U * n) {
+    uint4 u[U];
+#pragma unroll
+    for (int i = 0; i < U; ++i)
+      if (p + i * n < end) u[i] = z16[p + i * n];
+#pragma unroll
+    for (int i = 0; i < U; ++i)
+      if (p + i * n < end) f(p + i * n, u[i]);
+  }
+}
+
+struct Scratch {
+  float m[kRowWarps], s0[kRowWarps], s1[kRowWarps];
+  float4 part;                 // this block's sums, for the other blocks of the row
+  RowGrad g;
+};
+static_assert(sizeof(Scratch) % 16 == 0, "the teacher's list lies behind it");
+
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+__device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ uint32_t in_peer(const void* p, uint32_t rank) {
+  uint32_t at;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem_u32(p)), "r"(rank));
+  return at;
+}
+
+// A row may be cut into `parts`, a block each.  Where sums are taken (few rows) the blocks are a cluster and read each other's sums.  A gradient on its own
+// needs nothing of the other parts: what a block reads of them it has no use for (they may be overwritten already).
+template <typename T, int OP, int PASS, int NT>
+__global__ void __launch_bounds__(kRowWarps * 32, PASS == mtf::LOSS_BACKWARD && OP != mtf::LOSS_DISTILL ? 6 : 4) loss_rows_kernel(const LossRows a, const Factors F, const int parts, const int each, int* __restrict__ bad) {
+  extern __shared__ __align__(128) unsigned char dyn[];
+  Scratch& sc = *reinterpret_cast<Scratch*>(dyn);
+  const Slots sl(dyn + sizeof(Scratch), a.slots);
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = blockDim.x >> 5;
+  const unsigned which = parts == 1 ? blockIdx.x : blockIdx.x / (unsigned)parts;
+  const int rank = blockIdx.x - which * parts;
+  const long long at = which, row = a.reverse ? a.rows - 1 - at : at;
+  constexpr bool kSums = (PASS & mtf::LOSS_FORWARD) != 0;
+  const RowPart<T> part(a, row, each, rank);
+  mtf::chain_wait_only();
+  const RowIn in = row_in<OP, PASS>(a, row);
+  if (in.skip) {               // (every block of the row)
+    if (tid == 0 && rank == 0 && in.bad) atomicExch(bad, 1);
+    if ((PASS & mtf::LOSS_FORWARD) && tid == 0 && rank == 0) zero_results<OP>(a, row);
+    if (PASS & mtf::LOSS_BACKWARD) part.zeros(tid, blockDim.x);
+    return;
+  }
+  RowInputs x = {};
+  if (warp == 0) x = row_inputs<T, OP>(a, row, part.zr, in.label, sl, lane, bad, rank == 0);
+
+  float m = 0.f, s0 = 1.f, s1 = 1.f;
+  if (PASS & mtf::LOSS_FORWARD) {
+    RunningSum<NT> rs(F);
+    // four pieces' loads in flight while the four before are worked on
+    const int n = blockDim.x, first = part.begin + tid, fours = first < part.end ? (part.end - first + n - 1) / n / 4 : 0;
+    const uint4* z = part.z16 + first;
+    uint4 u[4], w[4];
+    auto load = [&](uint4* to) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) to[i] = z[i * n];
+      z += 4 * n;
+    };
+    if (PASS == mtf::LOSS_FORWARD) {
+      if (fours) load(u);
+      for (int k = 1; k < fours; k += 2) {
+        load(w);
+        rs.template add<T, 4>(u, F);
+        if (k + 1 < fours) load(u);
+        rs.template add<T, 4>(w, F);
+      }
+      if (fours & 1) rs.template add<T, 4>(u, F);
+    } else {
+      for (int k = 0; k < fours; ++k) {
+        load(u);
+        rs.template add<T, 4>(u, F);
+      }
+    }
+    for (; z < part.z16 + part.end; z += n) {
+      const uint4 one = *z;
+      rs.template add<T, 1>(&one, F);
+    }
+    if (tid < part.edges) rs.add_one(Piece<T>::one(part.zr, part.edge(tid)), F);
+    float t_m, t_0, t_1;
+    rs.of_warp(t_m, t_0, t_1, F);
+    if (lane == 0) { sc.m[warp] = t_m; sc.s0[warp] = t_0; sc.s1[warp] = t_1; }
+    __syncthreads();
+    if (warp == 0) {
+      m = lane < warps ? sc.m[lane] : -F.huge;
+      s0 = lane < warps ? sc.s0[lane] : 0.f;
+      s1 = lane < warps ? sc.s1[lane] : 0.f;
+      warp_join<NT>(m, s0, s1, F);
+      if (F.is_huge(m)) sums_of_differences<T, NT>(part, lane, F, m, s0, s1);
+      if (lane == 0) sc.part = make_float4(m, s0, s1, 0.f);
+    }
+  }
+  if (kSums && parts > 1) {
+    __syncwarp();
+    cluster_arrive();
+    cluster_wait();            // (from here on a block may overwrite its part of the row)
+    if (warp == 0) {
+      m = kLowest;
+      s0 = s1 = 0.f;
+      if (lane < parts)
+        asm volatile("{\n\t.reg .f32 none;\n\tld.shared::cluster.v4.f32 {%0, %1, %2, none}, [%3];\n\t}" : "=f"(m), "=f"(s0), "=f"(s1) : "r"(in_peer(&sc.part, lane)) : "memory");
+      warp_join<NT>(m, s0, s1, F);
+    }
+    __syncwarp();
+    cluster_arrive();          // this block has read the others' sums: they may end once all have
+  }
+  RowGrad g = {};
+  if (warp == 0) {
+    g = row_numbers<OP, PASS, NT>(a, row, in, x, m, (double)s0, (double)(NT >= 2 ? s1 : s0), rank == 0 && lane == 0, F);
+    if ((PASS & mtf::LOSS_BACKWARD) && lane == 0) sc.g = g;
+  }
+  if (PASS & mtf::LOSS_BACKWARD) {
+    __syncthreads();
+    if (sc.g.zero) {
+      part.zeros(tid, blockDim.x);
+    } else {
+      if (sc.g.huge) {
+        huge_pieces<T, NT>(part.z16, part.d16, part.begin, part.end, tid, blockDim.x, sc.g, F);
+      } else {
+        GradValues<T, NT> v;
+        v.set(sc.g);
+        walk<4>(part.z16, part.begin, part.end, [&](int p, const uint4& u) { part.d16[p] = v.piece(u, F); });
+      }
+      if (tid < part.edges) Piece<T>::set(part.dr, part.edge(tid), gradient_of<NT>(Piece<T>::one(part.zr, part.edge(tid)), sc.g, F));
+      bool alone = true;
+      if (OP == mtf::LOSS_DISTILL && warp == 0) alone = !slot_values(a, g, sl, in.label, lane) && hard_on<OP>(a);
+      __syncthreads();
+      if (warp == 0) {
+        if (OP == mtf::LOSS_DISTILL) write_slots<T>(a, g, sl, in.label, alone, part.dr, lane, 32, [&](int e) { return part.owned(e); });
+        else if (lane == 0 && part.owned(in.label)) Piece<T>::set(part.dr, in.label, g.fix);
+      }
+    }
+  }
+  if (kSums && parts > 1) {
+    __syncwarp();
+    cluster_wait();
+  }
+}
+
+// ---- rows streamed through shared memory: statistics and gradient from one read ------------------------------------------------------
+// A block (or a cluster of them, each with a part of every row) takes every n-th row.  One warp keeps a ring of chunks filled by bulk copies.
+// Sixteen warps walk over the chunks twice, for the statistics and, `lead` chunks later, for the gradient, taking a chunk of each walk in turn:
+// chunks are read, freed and written at one steady rate.  Three more warps work out the rows' numbers, a row each; a row's are wanted `lead`
+// chunks behind its first, that is some chunks behind its last.  Rows are numbered by those that are not skipped (o); row o has slot o mod 3.
+constexpr int kWalkers = 16, kNumberWarps = 3, kStreamThreads = 32 * (1 + kNumberWarps + kWalkers);
+constexpr int kChunk = 16384, kChunkPieces = kChunk / 16, kMaxChunks = 13, kMaxParts = 8, kRowSlots = kNumberWarps;
+constexpr long long kWaitCycles = 4000000000LL;
+__device__ int g_loss_status = 0;
+
+struct Stream {
+  uint64_t full[kMaxChunks], empty[kMaxChunks];      // a chunk has landed / every walking warp is through with it
+  uint64_t sums[kRowSlots];                          // the walking warps' sums of the slot's row are there
+  uint64_t ready[kRowSlots];                         // ... its numbers are
+  uint64_t done[kRowSlots];                          // ... its gradient is, but for the entries that differ
+  uint64_t peers[kRowSlots], heard[kRowSlots];       // the other parts' sums are there; the other blocks have read this one's
+  int abort;
+  int pad[3];
+  float4 sum[kRowSlots][kWalkers];
+  float4 peer[kRowSlots][kMaxParts];
+  RowGrad g[kRowSlots];
+};
+static_assert(sizeof(Stream) % 16 == 0, "lists lie behind it");
+
+__device__ __forceinline__ void bar_init(uint64_t* bar, uint32_t count) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(bar)), "r"(count) : "memory"); }
+__device__ __forceinline__ void bar_arrive(uint64_t* bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(bar)) : "memory"); }
+__device__ __forceinline__ void bar_expect(uint64_t* bar, uint32_t bytes) { asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(smem_u32(bar)), "r"(bytes) : "memory"); }
+__device__ __forceinline__ bool bar_try(uint64_t* bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok) : "r"(smem_u32(bar)), "r"(parity) : "memory");
+  return ok != 0;
+}
+// Gives up after about two seconds: a code for mtf_device_status, and from then on no wait of the block waits (its rows' results are unspecified).
+__device__ __noinline__ void bar_wait_slow(uint64_t* bar, uint32_t parity, int code, volatile int* abort) {
+  const long long t0 = clock64();
+  while (!bar_try(bar, parity)) {
+    if (*abort) return;
+    if (clock64() - t0 > kWaitCycles) {
+      atomicCAS(&g_loss_status, 0, code);
+      *abort = 1;
+      return;
+    }
+  }
+}
+__device__ __forceinline__ void bar_wait(uint64_t* bar, uint32_t parity, int code, int* abort) {
+  if (!bar_try(bar, parity)) bar_wait_slow(bar, parity, code, abort);
+}
+template <typename T, int OP, int NT>
+__global__ void __launch_bounds__(kStreamThreads, 1) loss_stream_kernel(const LossRows a, const Factors F, const int parts, const int each, const int chunks, const int lead, int* __restrict__ bad) {
+  constexpr int PASS = mtf::LOSS_STEP;
+  extern __shared__ __align__(128) unsigned char dyn[];
+  const size_t list = OP == mtf::LOSS_DISTILL ? Slots::bytes(a.slots) : 0;
+  uint4* const ring = reinterpret_cast<uint4*>(dyn);
+  Stream& st = *reinterpret_cast<Stream*>(dyn + (size_t)chunks * kChunk);
+  unsigned char* const lists = dyn + (size_t)chunks * kChunk + sizeof(Stream);
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int rank = blockIdx.x % parts;
+  const long long first = blockIdx.x / parts, stride = gridDim.x / parts;
+  const int n = (int)((a.rows - first + stride - 1) / stride);        // rows of this block, each known by its number i
+  auto row_of = [&](int i) { return first + i * stride; };
+  if (tid == 0) {
+    for (int c = 0; c < chunks; ++c) { bar_init(&st.full[c], 1); bar_init(&st.empty[c], kWalkers); }
+    for (int s = 0; s < kRowSlots; ++s) {
+      bar_init(&st.sums[s], kWalkers);
+      bar_init(&st.ready[s], 1);
+      bar_init(&st.done[s], kWalkers);
+      bar_init(&st.peers[s], 1);
+      bar_init(&st.heard[s], parts);
+    }
+    st.abort = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  __syncthreads();
+  if (parts > 1) {             // the others' barriers are set up as well
+    cluster_arrive();
+    cluster_wait();
+  }
+  mtf::chain_wait_only();
+
+  // Which rows are skipped is found out 32 rows at a time, a row a lane, by every warp for itself.
+  uint32_t live = 0u;
+  auto look = [&](uint32_t& mask, int i) {
+    if ((i & 31) == 0) mask = __ballot_sync(0xffffffffu, i + lane < n && !row_in<OP, PASS>(a, row_of(i + lane)).skip);
+    return ((mask >> (i & 31)) & 1u) != 0u;
+  };
+
+  if (warp == 0) {
+    // ------------------------------- copies -------------------------------
+    int slot = 0;
+    uint32_t phase = 1u;
+    for (int i = 0; i < n; ++i) {
+      if (!look(live, i)) continue;
+      if (lane == 0) {
+        const RowPart<T> part(a, row_of(i), each, rank);
+        for (int p = part.begin; p < part.end; p += kChunkPieces) {
+          bar_wait(&st.empty[slot], phase, 0xA01, &st.abort);
+          const uint32_t bytes = (uint32_t)min(kChunkPieces, part.end - p) * 16u;
+          bar_expect(&st.full[slot], bytes);
+          asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                       ::"r"(smem_u32(ring + slot * kChunkPieces)), "l"(part.z16 + p), "r"(bytes), "r"(smem_u32(&st.full[slot])) : "memory");
+          if (++slot == chunks) { slot = 0; phase ^= 1u; }
+        }
+      }
+      __syncwarp();
+    }
+  } else if (warp <= kNumberWarps) {
+    // ------------------------------- the rows' numbers -------------------------------
+    const int s = warp - 1;
+    uint32_t phase = 1u;
+    int turn = -1, uses = 0, i = -1;                 // slot of row i; rows of this warp so far
+    // to this warp's next row, with the results of skipped rows on the way; false behind the last
+    auto next = [&] {
+      while (++i < n) {
+        if (look(live, i)) {
+          if (++turn == kRowSlots) turn = 0;
+          if (turn == s) return true;
+        } else if (i % kNumberWarps == s && rank == 0 && lane == 0) {
+          const long long row = row_of(i);
+          if (row_in<OP, PASS>(a, row).bad) atomicExch(bad, 1);
+          zero_results<OP>(a, row);
+        }
+      }
+      return false;
+    };
+    // What is read of a row is read while the walks still have the row before in hand: two lists a warp.
+    RowIn in = {};
+    RowInputs x = {};
+    auto list_of = [&](int use) { return Slots(lists + (2 * s + (use & 1)) * list, a.slots); };
+    auto read = [&] {
+      in = row_in<OP, PASS>(a, row_of(i));
+      x = row_inputs<T, OP>(a, row_of(i), RowPart<T>(a, row_of(i), each, rank).zr, in.label, list_of(uses), lane, bad);
+    };
+    bool more = next();
+    if (more) read();
+    while (more) {
+      const long long row = row_of(i);
+      const RowPart<T> part(a, row, each, rank);
+      const Slots sl = list_of(uses);
+      phase ^= 1u;
+      float m = -F.huge, s0 = 0.f, s1 = 0.f;
+      bar_wait(&st.sums[s], phase, 0xA02, &st.abort);
+      if (lane < kWalkers) { const float4 v = st.sum[s][lane]; m = v.x; s0 = v.y; s1 = v.z; }
+      warp_join<NT>(m, s0, s1, F);
+      if (F.is_huge(m)) sums_of_differences<T, NT>(part, lane, F, m, s0, s1);
+      if (parts > 1) {
+        // to every block of the row, and from there
+        if (uses) bar_wait(&st.heard[s], phase ^ 1u, 0xA03, &st.abort);
+        if (lane == 0) bar_expect(&st.peers[s], (uint32_t)parts * 16u);
+        __syncwarp();
+        if (lane < parts)
+          asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [%0], {%1, %2, %3, %4}, [%5];"
+                       ::"r"(in_peer(&st.peer[s][rank], lane)), "f"(m), "f"(s0), "f"(s1), "f"(0.f), "r"(in_peer(&st.peers[s], lane)) : "memory");
+        bar_wait(&st.peers[s], phase, 0xA04, &st.abort);
+        m = kLowest;
+        s0 = s1 = 0.f;
+        if (lane < parts) { const float4 v = st.peer[s][lane]; m = v.x; s0 = v.y; s1 = v.z; }
+        __syncwarp();
+        if (lane < parts) asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(in_peer(&st.heard[s], lane)) : "memory");
+        warp_join<NT>(m, s0, s1, F);
+      }
+      const RowGrad g = row_numbers<OP, PASS, NT>(a, row, in, x, m, (double)s0, (double)(NT >= 2 ? s1 : s0), rank == 0 && lane == 0, F);
+      __syncwarp();            // (every lane has read the sums)
+      if (lane == 0) {
+        st.g[s] = g;
+        bar_arrive(&st.ready[s]);
+      }
+      const int label = in.label;
+      bool alone = true;
+      if (OP == mtf::LOSS_DISTILL) alone = !slot_values(a, g, sl, label, lane) && hard_on<OP>(a);
+      const float fix = g.fix;
+      const bool zero = g.zero;
+      ++uses;
+      more = next();
+      if (more) read();
+      bar_wait(&st.done[s], phase, 0xA05, &st.abort);
+      if (!zero) {
+        if (OP == mtf::LOSS_DISTILL) write_slots<T>(a, st.g[s], sl, label, alone, part.dr, lane, 32, [&](int e) { return part.owned(e); });
+        else if (lane == 0 && part.owned(label)) Piece<T>::set(part.dr, label, fix);
+      }
+      __syncwarp();
+    }
+  } else {
+    // ------------------------------- walks -------------------------------
+    const int at = tid - 32 * (1 + kNumberWarps);
+    constexpr int nt = 32 * kWalkers, kEach = kChunkPieces / nt;
+    // the statistics' walk: row i, with slot s1; pieces [p, end) of its part are to come, the next of them in chunk c1
+    int i = -1, s1 = -1, p = 0, end = 0, c1 = 0;
+    uint32_t phase1 = 0u;
+    float edge = 0.f;
+    bool has_edge = false;
+    RunningSum<NT> rs(F);
+    auto next = [&] {                                // to the next row; false behind the last
+      do {
+        if (++i >= n) return false;
+      } while (!look(live, i));
+      if (++s1 == kRowSlots) s1 = 0;
+      const RowPart<T> part(a, row_of(i), each, rank);
+      p = part.begin;
+      end = part.end;
+      has_edge = at < part.edges;
+      if (has_edge) edge = Piece<T>::one(part.zr, part.edge(at));      // (wanted at the row's end)
+      rs = RunningSum<NT>(F);
+      return true;
+    };
+    auto count = [&] {                               // a chunk
+      bar_wait(&st.full[c1], phase1, 0xA11, &st.abort);
+      const uint4* const c = ring + c1 * kChunkPieces;
+      if (end - p >= kChunkPieces) {
+        uint4 u[kEach];
+#pragma unroll
+        for (int k = 0; k < kEach; ++k) u[k] = c[at + k * nt];
+        rs.template add<T, kEach>(u, F);
+      } else {
+        for (int k = at; k < end - p; k += nt) {
+          const uint4 u = c[k];
+          rs.template add<T, 1>(&u, F);
+        }
+      }
+      if (++c1 == chunks) { c1 = 0; phase1 ^= 1u; }
+      p += kChunkPieces;
+    };
+    auto finish = [&] {                              // the row's sums are complete
+      if (has_edge) rs.add_one(edge, F);
+      float t_m, t_0, t_1;
+      rs.of_warp(t_m, t_0, t_1, F);
+      if (lane == 0) {
+        st.sum[s1][warp - 1 - kNumberWarps] = make_float4(t_m, t_0, t_1, 0.f);
+        bar_arrive(&st.sums[s1]);
+      }
+      __syncwarp();
+    };
+    // the gradient's walk: row j, slot s2; `left` pieces to come, to `to` and behind, from chunk c2
+    int j = -1, s2 = -1, left = 0, c2 = 0;
+    uint32_t live_j = 0u, phase2 = 1u;
+    uint4* to = nullptr;
+    float edge_j = 0.f;
+    bool has_edge_j = false, no_chunk = false, plain = false;      // plain: neither zeros nor huge logits
+    GradValues<T, NT> v;
+    auto next_j = [&] {                              // to the next row that is not skipped, writing the zeros of those between; false behind the last
+      while (true) {
+        if (++j >= n) return false;
+        const bool alive = look(live_j, j);
+        const RowPart<T> part(a, row_of(j), each, rank);
+        if (!alive) { part.zeros(at, nt); continue; }
+        if (++s2 == kRowSlots) s2 = 0;
+        if (s2 == 0) phase2 ^= 1u;
+        to = part.d16 + part.begin;
+        left = part.end - part.begin;
+        no_chunk = left == 0;
+        has_edge_j = at < part.edges;
+        if (has_edge_j) edge_j = Piece<T>::one(part.zr, part.edge(at));
+        return true;
+      }
+    };
+    auto put = [&] {                                 // a chunk
+      const uint4* const c = ring + c2 * kChunkPieces;
+      const int here = min(left, kChunkPieces);
+      if (!plain) {
+        if (!st.g[s2].zero) huge_pieces<T, NT>(c, to, 0, here, at, nt, st.g[s2], F);
+        else
+          for (int k = at; k < here; k += nt) to[k] = make_uint4(0u, 0u, 0u, 0u);
+      } else if (here == kChunkPieces) {
+#pragma unroll
+        for (int k = 0; k < kEach; ++k) to[at + k * nt] = v.piece(c[at + k * nt], F);
+      } else {
+        for (int k = at; k < here; k += nt) to[k] = v.piece(c[k], F);
+      }
+      __syncwarp();
+      if (lane == 0) bar_arrive(&st.empty[c2]);
+      if (++c2 == chunks) c2 = 0;
+      to += kChunkPieces;
+      left -= kChunkPieces;
+    };
+    auto finish_j = [&] {
+      if (has_edge_j) {
+        const RowPart<T> part(a, row_of(j), each, rank);
+        Piece<T>::set(part.dr, part.edge(at), st.g[s2].zero ? 0.f : gradient_of<NT>(edge_j, st.g[s2], F));
+      }
+      __syncwarp();
+      if (lane == 0) bar_arrive(&st.done[s2]);
+    };
+    // `ahead`: chunks that the first walk is ahead by.  A row may be without a chunk (fewer entries than a piece): it counts as one.
+    int ahead = 0;
+    bool more = next(), more_j = next_j(), begun = false;
+    while (more_j) {
+      if (more && ahead < lead) {
+        if (p < end) count();
+        ++ahead;
+        if (p >= end) { finish(); more = next(); }
+        continue;
+      }
+      if (!begun) {                                  // the row's numbers
+        bar_wait(&st.ready[s2], phase2, 0xA12, &st.abort);
+        plain = !st.g[s2].zero && !st.g[s2].huge;
+        v.set(st.g[s2]);
+        begun = true;
+      }
+      if (more && plain) {
+        // both walks at once: their chains of instructions fill each other's waits
+        const int both_full = min(end - p, left) / kChunkPieces;
+#pragma unroll 1
+        for (int c = 0; c < both_full; ++c) {
+          bar_wait(&st.full[c1], phase1, 0xA11, &st.abort);
+          uint4 u[kEach], w[kEach];
+#pragma unroll
+          for (int k = 0; k < kEach; ++k) { u[k] = ring[c1 * kChunkPieces + at + k * nt]; w[k] = ring[c2 * kChunkPieces + at + k * nt]; }
+          rs.raise(Piece<T>::template largest<kEach>(u), F);
+          rs.template add_below<T, kEach>(u, F);
+#pragma unroll
+          for (int k = 0; k < kEach; ++k) to[at + k * nt] = v.piece(w[k], F);
+          __syncwarp();
+          if (lane == 0) bar_arrive(&st.empty[c2]);
+          if (++c1 == chunks) { c1 = 0; phase1 ^= 1u; }
+          if (++c2 == chunks) c2 = 0;
+          p += kChunkPieces;
+          to += kChunkPieces;
+          left -= kChunkPieces;
+        }
+        if (both_full) {
+          if (p >= end) { finish(); more = next(); }
+          if (left > 0) continue;
+        }
+      }
+      if (left > 0) {
+        put();
+        --ahead;
+      }
+      if (left <= 0) {
+        if (no_chunk) --ahead;
+        finish_j();
+        more_j = next_j();
+        begun = false;
+      }
+    }
+  }
+
+  if (*(volatile int*)&st.abort)
+    for (int i = 0; i < 2000; ++i) __nanosleep(1000);      // copies in flight get time to land
+  if (parts > 1) {             // nobody leaves while another block may still write to its shared memory
+    __syncwarp();
+    cluster_arrive();
+    cluster_wait();
+  }
+}
+
+// ---- the pairs of the preference loss ----------------------------------------------------------------------------------------------------
+constexpr int kPairThreads = 1024;
+// sum over the block, the same in every thread
+__device__ __forceinline__ double block_sum(double v, double* red) {
+  v = warp_add(v);
+  __syncthreads();
+  if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = v;
+  __syncthreads();
+  double r = 0.0;
+#pragma unroll
+  for (int w = 0; w < kPairThreads / 32; ++w) r += red[w];
+  return r;
+}
+
 // One block per pair: both sequences' log-probabilities added up in a fixed order, in 64 bits, then the loss of the pair and its
-// derivative by each of the two sums.
-__global__ void __launch_bounds__(kThreads) preference_pairs_kernel(const mtf::PreferencePairs a) {
+// derivative by each of the two sums.  A sum of hundreds of log-probabilities that are each rounded to f32 would be off by more than its
+// own rounding (the loss goes by the difference of two): the rows' kernel has left the rest of each in lse's place, and lse itself, the
+// label's logit less the log-probability, is written here.
+template <typename T>
+__global__ void __launch_bounds__(kPairThreads) preference_pairs_kernel(const mtf::PreferencePairs a) {
   mtf::chain_wait();
-  __shared__ double red[kThreads / 32];
+  __shared__ double red[kPairThreads / 32];
   const long long b = blockIdx.x;
   double s[2];
   for (int i = 0; i < 2; ++i) {
-    const long long at = (i * a.pairs + b) * a.length;
+    const long long from = (i * a.pairs + b) * a.length;
     double v = 0.0;
-    for (long long t = threadIdx.x; t < a.length; t += kThreads) {
-      const float w = a.weight ? a.weight[at + t] : 1.f;
-      if (w != 0.f) v += (double)w * (double)a.logp[at + t];
+    for (long long t = from + threadIdx.x; t < from + a.length; t += kPairThreads) {
+      const float w = a.weight ? a.weight[t] : 1.f, hi = a.logp[t], lo = a.lse[t];
+      const int label = a.targets[t];
+      if (w == 0.f || label < 0 || label >= a.V) continue;                // (both 0)
+      if (isfinite(hi)) {
+        const double logp = (double)hi + (double)lo;
+        v += (double)w * logp;
+        a.lse[t] = (float)((double)Piece<T>::one(a.z, t * a.V + label) - logp);
+      } else {
+        v += (double)w * (double)hi;
+      }
     }
-    s[i] = block_all<false>(v, red);
+    s[i] = block_sum(v, red);
   }
   if (threadIdx.x) return;
   const double margin = (s[0] - (double)a.ref[b]) - (s[1] - (double)a.ref[a.pairs + b]), beta = (double)a.beta, h = beta * margin;
@@ -457,19 +1177,102 @@ __global__ void __launch_bounds__(kThreads) preference_pairs_kernel(const mtf::P
   a.loss[b] = (float)loss;
 }
 
+// the first sum is the softened one wherever there is one
+Factors factors(const LossRows& a) { return Factors(kLog2e * (float)a.inv_tau, kLog2e); }
+template <typename T>
+int pieces_each(const LossRows& a, int parts) { return (a.V / Piece<T>::kN + parts - 1) / parts; }
+
+// Clusters of `parts` blocks of the stream kernel, one block to an SM, that the GPU holds at once (the SMs of a cluster lie in one group of
+// them, so this is less than SMs / parts); asked for once per process.
+template <typename K>
+int resident_clusters(K kernel, const cudaLaunchConfig_t& cfg, int parts, std::atomic<int>* known) {
+  int n = known[parts].load(std::memory_order_relaxed);
+  if (n > 0) return n;
+  if (cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess || n < 1) { (void)cudaGetLastError(); n = 1; }
+  known[parts].store(n, std::memory_order_relaxed);
+  return n;
+}
+
+template <typename T, int OP, int NT>
+bool launch_stream(const LossRows& a, size_t list, cudaLaunchConfig_t cfg, cudaLaunchAttribute* at, int* bad) {
+  const long long pieces = (long long)a.V * (a.bf16 ? 2 : 4) / 16;
+  const size_t fixed = sizeof(Stream) + 2 * kNumberWarps * list;
+  const int chunks = std::min<int>(kMaxChunks, (int)((227 * 1024 - fixed) / kChunk));
+  auto part_chunks = [&](int parts) { return (int)(((pieces + parts - 1) / parts + kChunkPieces - 1) / kChunkPieces); };
+  // The ring holds the lead and three chunks on their way; the lead is more than a row's part, and two at most (their slots).
+  int parts = 1;
+  while (parts < kMaxParts && part_chunks(parts) + 2 > chunks - 3) parts *= 2;
+  const int lead = std::min(chunks - 3, 2 * part_chunks(parts));
+  if (lead < part_chunks(parts) + 1) return false;
+  auto kernel = loss_stream_kernel<T, OP, NT>;
+  cfg.dynamicSmemBytes = fixed + (size_t)chunks * kChunk;
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)cfg.dynamicSmemBytes) != cudaSuccess) return true;
+  cfg.blockDim = dim3(kStreamThreads, 1, 1);
+  long long at_once = mtf::device_sm_count();
+  if (parts > 1) {
+    static std::atomic<int> known[kMaxParts + 1];
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = (unsigned)parts; at[1].val.clusterDim.y = 1; at[1].val.clusterDim.z = 1;
+    cfg.numAttrs = 2;
+    cfg.gridDim = dim3((unsigned)parts, 1, 1);
+    at_once = resident_clusters(kernel, cfg, parts, known);
+  }
+  cfg.gridDim = dim3((unsigned)(std::min(a.rows, at_once) * parts), 1, 1);
+  (void)cudaLaunchKernelEx(&cfg, kernel, a, factors(a), parts, pieces_each<T>(a, parts), chunks, lead, bad);
+  return true;
+}
+
 template <typename T, int OP, int PASS, int NT>
-void launch(const LossRows& a, int* bad, cudaStream_t st) {
-  const size_t smem = OP == mtf::LOSS_DISTILL ? sizeof(Slots) : 0;
-  mtf::launch_chained(loss_rows_kernel<T, OP, PASS, NT>, (unsigned)a.rows, kThreads, smem, st, a, bad);
+void launch(const LossRows& b, int* bad, cudaStream_t st) {
+  LossRows a = b;
+  a.inv_tau = a.soft != 0.f ? 1.0 / (double)a.temperature : 1.0;
+  // (a gradient that is asked for later begins where the statistics ended: those rows are still in the L2 cache)
+  a.reverse = PASS == mtf::LOSS_BACKWARD;
+  const size_t list = OP == mtf::LOSS_DISTILL ? Slots::bytes(a.slots) : 0;
+  cudaLaunchConfig_t cfg = {};
+  cudaLaunchAttribute at[2];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.stream = st; cfg.attrs = at; cfg.numAttrs = 1;
+  const long long bytes = (long long)a.V * (a.bf16 ? 2 : 4), pieces = bytes / 16, sms = mtf::device_sm_count();
+  int parts = 1, threads = 32;
+  if (PASS == mtf::LOSS_BACKWARD) {
+    // independent blocks of 32 KB (a teacher's list is worked out by every block of its row, so there only with few rows)
+    if (OP != mtf::LOSS_DISTILL) parts = (int)std::min<long long>(64, (bytes + 32767) / 32768);
+    while (parts < 64 && a.rows * parts * 2 <= 4 * sms && bytes / parts > 2048) parts *= 2;
+    while (threads < kRowWarps * 32 && threads * 8 < pieces / parts) threads *= 2;
+  } else {
+    if constexpr (PASS == mtf::LOSS_STEP)
+      if (bytes > 32768 && a.rows * bytes > (48LL << 20) && launch_stream<T, OP, NT>(a, list, cfg, at, bad)) return;
+    while (parts < kMaxParts && a.rows * parts * 2 <= sms && bytes / parts > 4096) parts *= 2;
+    const int each = PASS == mtf::LOSS_STEP ? 16 : a.bf16 ? 32 : 256;      // pieces a thread, while there are rows enough
+    while (threads < kRowWarps * 32 && (threads * each < pieces / parts || a.rows * parts * threads * 2 <= (PASS == mtf::LOSS_STEP ? 1024 : 2048) * sms)) threads *= 2;
+    if (parts > 1) {
+      at[1].id = cudaLaunchAttributeClusterDimension;
+      at[1].val.clusterDim.x = (unsigned)parts; at[1].val.clusterDim.y = 1; at[1].val.clusterDim.z = 1;
+      cfg.numAttrs = 2;
+    }
+  }
+  cfg.blockDim = dim3((unsigned)threads, 1, 1);
+  cfg.dynamicSmemBytes = sizeof(Scratch) + list;
+  cfg.gridDim = dim3((unsigned)(a.rows * parts), 1, 1);
+  (void)cudaLaunchKernelEx(&cfg, loss_rows_kernel<T, OP, PASS, NT>, a, factors(a), parts, pieces_each<T>(a, parts), bad);
+}
+
+template <typename T, int OP, int PASS>
+void launch_sums(int sums, const LossRows& a, int* bad, cudaStream_t st) {
+  if (OP != mtf::LOSS_DISTILL || sums == 1) launch<T, OP, PASS, 1>(a, bad, st);
+  else if (sums == 2) launch<T, OP, PASS, OP == mtf::LOSS_DISTILL ? 2 : 1>(a, bad, st);
+  else launch<T, OP, PASS, OP == mtf::LOSS_DISTILL ? 3 : 1>(a, bad, st);
 }
 
 template <typename T>
 void dispatch(mtf::LossOp op, mtf::LossPass pass, int sums, const LossRows& a, int* bad, cudaStream_t st) {
   using namespace mtf;
   if (op == LOSS_DISTILL) {
-    if (pass == LOSS_FORWARD) { if (sums == 2) launch<T, LOSS_DISTILL, LOSS_FORWARD, 2>(a, bad, st); else launch<T, LOSS_DISTILL, LOSS_FORWARD, 1>(a, bad, st); }
-    else if (pass == LOSS_BACKWARD) { if (sums == 2) launch<T, LOSS_DISTILL, LOSS_BACKWARD, 2>(a, bad, st); else launch<T, LOSS_DISTILL, LOSS_BACKWARD, 1>(a, bad, st); }
-    else { if (sums == 2) launch<T, LOSS_DISTILL, LOSS_STEP, 2>(a, bad, st); else launch<T, LOSS_DISTILL, LOSS_STEP, 1>(a, bad, st); }
+    if (pass == LOSS_FORWARD) launch_sums<T, LOSS_DISTILL, LOSS_FORWARD>(sums, a, bad, st);
+    else if (pass == LOSS_BACKWARD) launch_sums<T, LOSS_DISTILL, LOSS_BACKWARD>(sums, a, bad, st);
+    else launch_sums<T, LOSS_DISTILL, LOSS_STEP>(sums, a, bad, st);
   } else if (pass == LOSS_BACKWARD) {
     launch<T, LOSS_LOGP, LOSS_BACKWARD, 1>(a, bad, st);
   } else if (op == LOSS_LOGP) {
@@ -493,14 +1296,24 @@ static mtf_status after(const char* what) {
 }
 
 mtf_status launch_loss_rows(LossOp op, LossPass pass, const LossRows& a, void* stream) {
-  const int sums = op == LOSS_DISTILL && a.soft != 0.f && a.hard != 0.f && a.temperature != 1.f ? 2 : 1;
+  const int sums = op == LOSS_DISTILL && a.soft != 0.f && a.hard != 0.f && a.temperature != 1.f ? (a.temperature == 2.f ? 3 : 2) : 1;
   if (a.bf16) dispatch<__nv_bfloat16>(op, pass, sums, a, bad_index_flag(), (cudaStream_t)stream);
   else dispatch<float>(op, pass, sums, a, bad_index_flag(), (cudaStream_t)stream);
   return after("loss_rows_kernel");
 }
 
+mtf_status read_loss_status(int* code) {
+  int v = 0;
+  cudaError_t e = cudaMemcpyFromSymbol(&v, g_loss_status, sizeof(int));
+  if (e != cudaSuccess) return fail(MTF_ERR_CUDA, "cudaMemcpyFromSymbol: %s", cudaGetErrorString(e));
+  if (v) { int z = 0; cudaMemcpyToSymbol(g_loss_status, &z, sizeof(int)); }
+  *code = v;
+  return MTF_OK;
+}
+
 mtf_status launch_preference_pairs(const PreferencePairs& a, void* stream) {
-  launch_chained(preference_pairs_kernel, (unsigned)a.pairs, kThreads, 0, (cudaStream_t)stream, a);
+  if (a.bf16) launch_chained(preference_pairs_kernel<__nv_bfloat16>, (unsigned)a.pairs, kPairThreads, 0, (cudaStream_t)stream, a);
+  else launch_chained(preference_pairs_kernel<float>, (unsigned)a.pairs, kPairThreads, 0, (cudaStream_t)stream, a);
   return after("preference_pairs_kernel");
 }
 

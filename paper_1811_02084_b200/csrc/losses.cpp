@@ -321,6 +321,11 @@ mtf_status mtf_preference_forward(const mtf_layout_t* layout, const mtf_tensor* 
     p.dseq = per_sequence(c, dseq, logits, "dseq", true);
     p.loss = per_pair(c, loss, logits, "loss", true);
     if (!c.ok()) return c.st;
+    p.z = a.z;
+    p.V = a.V;
+    p.bf16 = a.bf16;
+    p.targets = a.targets;
+    p.lse = a.lse;
     p.logp = a.logp;
     p.weight = a.weight;
     p.pairs = a.pairs;

@@ -33,6 +33,8 @@ struct LossRows {
   const void* teacher = nullptr;
   int teacher_bf16 = 0, slots = 0;
   float temperature = 1.f, soft = 0.f, hard = 0.f;
+  double inv_tau = 1.0;               // 1 / temperature where the softened term is on
+  int reverse = 0;                    // rows from the last to the first
   const float* dloss = nullptr;       // backward: one per row (preference: per pair); NULL = 1
 };
 
@@ -42,8 +44,11 @@ enum LossPass { LOSS_FORWARD = 1, LOSS_BACKWARD = 2, LOSS_STEP = 3 };
 mtf_status launch_loss_rows(LossOp op, LossPass pass, const LossRows& a, void* stream);
 
 struct PreferencePairs {
+  const void* z = nullptr;            // logits
+  int V = 0, bf16 = 0;
+  const int32_t* targets = nullptr;
   const float *logp = nullptr, *weight = nullptr, *ref = nullptr;
-  float *seq = nullptr, *dseq = nullptr, *loss = nullptr;
+  float *lse = nullptr, *seq = nullptr, *dseq = nullptr, *loss = nullptr;
   long long pairs = 0, length = 0;
   int kind = 0;
   float beta = 0.f, smoothing = 0.f;

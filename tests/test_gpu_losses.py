@@ -472,7 +472,7 @@ def test_ids_out_of_range_are_reported(mtf, op):
 
 # ---- shapes of a launch: few rows, many rows, one launch behind another ---------------------------------------------------------------------------
 
-@pytest.mark.parametrize("B,L,V", [(1, 1, 200000), (1, 2, 131072), (1, 9, 70001), (1, 40, 50000), (1, 75, 40000), (4, 90, 1111), (9, 333, 515), (2, 100, 120000)])
+@pytest.mark.parametrize("B,L,V", [(1, 1, 200000), (1, 2, 131072), (1, 9, 70001), (1, 40, 50000), (1, 75, 40000), (4, 90, 1111), (9, 333, 515), (2, 100, 120000), (148, 64, 2100), (66, 148, 1030), (33, 63, 70001)])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_rows_and_vocabularies_in_bulk(mtf, B, L, V, dtype):
     """Against torch in 64 bits on the GPU: numbers of rows on both sides of what fills the GPU, rows on both sides of what an SM keeps."""
