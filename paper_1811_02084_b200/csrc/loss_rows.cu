@@ -238,14 +238,18 @@ __device__ __forceinline__ void RunningSum<NT>::of_warp(float& t_m, float& t_0, 
   warp_join<NT>(t_m, t_0, t_1, F);
 }
 
-// What a row's gradient is made of: k0 2^(z a0 + nb0) (+ k1 2^(z a1 + nb1)), or with huge logits k0 2^((z - m0) a0) (+ ...), and the entries
-// that differ.
+// What a row's gradient is made of: k0 2^(z a0 + nb0) (+ k1 2^(z a1 + nb1)), or with huge logits k0 2^((z - m0) a0) (+ ...).
 struct RowGrad {
   float k0, nb0, k1, nb1, m0, m1;
   int zero;                    // the whole row is 0
   int huge;
-  float fix;                   // the label's entry
-  double lse0, lse1, cs, ch;   // distillation: log-sum-exps and the two parts' factors
+};
+// What else a row comes to, in 64 bits.
+struct RowNumbers {
+  double c;                    // LOGP, POLICY: derivative by the label's log-probability
+  double plain, clipped, em1;  // POLICY: both sides of the limit, and exp(ref - logp) - 1
+  double cs, ch;               // distillation: factors of the two distributions in the gradient
+  double lse0, lse1;           // log-sum-exp of z / tau and of z
 };
 
 // A teacher's list: arrays of `slots`, rounded up to 4.
@@ -263,11 +267,10 @@ __device__ __forceinline__ double warp_add(double v) {
   for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
   return v;
 }
-__device__ __forceinline__ double warp_max(double v) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) v = fmax(v, __shfl_xor_sync(0xffffffffu, v, o));
-  return v;
-}
+// (The rows' numbers are long stretches of code that run once a row beside the walks, at the rate at which their instructions come in: one
+// copy each of the functions that they call more than once.)
+__device__ __noinline__ double exp64(double x) { return exp(x); }
+__device__ __noinline__ double log64(double x) { return log(x); }
 
 // ---- what a row is worked out from, apart from the walks over its logits -------------------------------------------------------
 template <int OP> __device__ __forceinline__ bool soft_on(const LossRows& a) { return OP == mtf::LOSS_DISTILL && a.soft != 0.f; }
@@ -322,10 +325,29 @@ struct RowInputs {
   float zy, old, ref, adv;
   double kl, sum;              // the teacher's sum_k q_k (log q_k - z_k / tau), and sum_k q_k: 1, or 0 without a used slot
 };
-// By one warp, before anything of the row is overwritten; all lanes return the same.  The teacher's list, with its distribution over the used
-// slots, goes to `sl`.
+// The first slots of a teacher's list as they are loaded, kB a lane.
+constexpr int kB = 4;
+struct Fetched {
+  int id[kB];
+  float t[kB];
+};
+__device__ __forceinline__ void fetch_slots(const LossRows& a, long long row, int first, int lane, bool on, Fetched& f) {
+#pragma unroll
+  for (int i = 0; i < kB; ++i) {
+    const int k = first + lane + 32 * i;
+    f.id[i] = -1;
+    f.t[i] = 0.f;
+    if (on && k < a.slots) {
+      f.id[i] = a.teacher_ids[row * a.slots + k];
+      f.t[i] = a.teacher_bf16 ? Piece<__nv_bfloat16>::one(a.teacher, row * a.slots + k) : Piece<float>::one(a.teacher, row * a.slots + k);
+    }
+  }
+}
+
+// By one warp, before anything of the row is overwritten; all lanes return the same.  The teacher's list (f: its first slots), with its
+// distribution over the used slots, goes to `sl`.
 template <typename T, int OP>
-__device__ __forceinline__ RowInputs row_inputs(const LossRows& a, long long row, const char* zr, int label, const Slots& sl, int lane, int* bad, bool report = true) {
+__device__ __forceinline__ RowInputs row_inputs(const LossRows& a, long long row, const char* zr, int label, Fetched& f, const Slots& sl, int lane, int* bad, bool report) {
   RowInputs r = {};
   if (OP != mtf::LOSS_DISTILL || hard_on<OP>(a)) r.zy = Piece<T>::one(zr, label);
   if (OP == mtf::LOSS_POLICY) {
@@ -335,50 +357,44 @@ __device__ __forceinline__ RowInputs row_inputs(const LossRows& a, long long row
   }
   if (OP != mtf::LOSS_DISTILL) return r;
   const int K = a.slots;
-  constexpr int kB = 4;        // loads in flight a lane
-  double best = -INFINITY;
-  for (int k0 = lane; k0 < Slots::room(K); k0 += 32 * kB) {
-    int id[kB];
-    float t[kB], z[kB];
+  float best = -INFINITY;      // of the logits as they are: f32 values
+  for (int first = 0; first < K; first += 32 * kB) {
+    float z[kB];
+    if (first) fetch_slots(a, row, first, lane, soft_on<OP>(a), f);
 #pragma unroll
     for (int i = 0; i < kB; ++i) {
-      const int k = k0 + 32 * i;
-      id[i] = -1;
-      t[i] = 0.f;
-      if (k < K && soft_on<OP>(a)) {
-        id[i] = a.teacher_ids[row * K + k];
-        t[i] = a.teacher_bf16 ? Piece<__nv_bfloat16>::one(a.teacher, row * K + k) : Piece<float>::one(a.teacher, row * K + k);
-      }
+      if (f.id[i] < -1 || f.id[i] >= a.V) { if (report) atomicExch(bad, 1); f.id[i] = -1; }
+      z[i] = f.id[i] >= 0 ? Piece<T>::one(zr, f.id[i]) : 0.f;
     }
 #pragma unroll
     for (int i = 0; i < kB; ++i) {
-      if (id[i] < -1 || id[i] >= a.V) { if (report) atomicExch(bad, 1); id[i] = -1; }
-      z[i] = id[i] >= 0 ? Piece<T>::one(zr, id[i]) : 0.f;
-    }
-#pragma unroll
-    for (int i = 0; i < kB; ++i) {
-      const int k = k0 + 32 * i;
+      const int k = first + lane + 32 * i;
       if (k >= Slots::room(K)) continue;
-      const double q = id[i] >= 0 ? (double)t[i] * a.inv_tau : -INFINITY;
-      sl.id[k] = id[i];
+      const float t = f.id[i] >= 0 ? f.t[i] : -INFINITY;
+      sl.id[k] = f.id[i];
       sl.z[k] = z[i];
-      sl.q[k] = q;
-      best = fmax(best, q != q ? INFINITY : q);      // (NaN: every difference to the maximum is NaN)
+      sl.q[k] = (double)t;
+      best = fmaxf(best, t != t ? INFINITY : t);      // (NaN: every difference to the maximum is NaN)
     }
   }
   best = warp_max(best);
   const bool any = best != -INFINITY;
   double sum = 0.0, kl = 0.0;
   if (any) {
+#pragma unroll 1
     for (int k = lane; k < K; k += 32) {
-      const double d = sl.q[k] - best, e = exp(d);
+      const double d = (sl.q[k] - (double)best) * a.inv_tau, e = exp64(d);
       sum += e;
       if (e != 0.0) kl += e * (d - (double)sl.z[k] * a.inv_tau);      // (a word of probability 0 adds nothing, whatever the student says to it)
       sl.q[k] = e;
     }
-    sum = warp_add(sum);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+      sum += __shfl_xor_sync(0xffffffffu, sum, o);
+      kl += __shfl_xor_sync(0xffffffffu, kl, o);
+    }
     const double inv = 1.0 / sum;
-    r.kl = warp_add(kl) * inv - log(sum);
+    r.kl = kl * inv - log64(sum);
     for (int k = lane; k < K; k += 32) sl.q[k] *= inv;
   } else {
     for (int k = lane; k < K; k += 32) sl.id[k] = -1;
@@ -388,114 +404,139 @@ __device__ __forceinline__ RowInputs row_inputs(const LossRows& a, long long row
   return r;
 }
 
-// log sum exp of z / tau, less m / tau, from a sum s relative to m
-__device__ __forceinline__ double log_sum(float m, double s, float af, const Factors& F) {
-  const double off = F.is_huge(m) ? 0.0 : ((double)reference(m, af) - (double)m * (double)af) * 0.6931471805599453;
-  return off + log(s);
+// what log(s) + m / tau is off by as log-sum-exp of z / tau, s being relative to m: the rounding of the reference
+__device__ __forceinline__ double reference_off(float m, float af, const Factors& F) {
+  return F.is_huge(m) ? 0.0 : ((double)reference(m, af) - (double)m * (double)af) * 0.6931471805599453;
 }
 
-// The row's numbers from its reference and sums, in 64 bits: they are differences of values near each other.  write: this thread stores the
-// results per row.
+// First what the gradient's walk waits for: the row's factors, from its reference m and sums.  (POLICY: the ratio is
+// exp(z_y - m - old) / s, so that the logarithm can wait, too.)
 template <int OP, int PASS, int NT>
-__device__ __forceinline__ RowGrad row_numbers(const LossRows& a, long long row, const RowIn& in, const RowInputs& x, float m, double s0, double s1, bool write,
-                                               const Factors& F) {
+__device__ __forceinline__ RowGrad row_gradient(const LossRows& a, long long row, const RowIn& in, const RowInputs& x, float m, float s0, float s1, const Factors& F,
+                                                RowNumbers& r) {
   const float a0 = F.a0, a1 = F.a1;
   RowGrad g = {};
+  r = {};
   const double w = (double)in.w;
-  double logp;                 // of the label
-  if (PASS & mtf::LOSS_FORWARD) {
-    const double inv_tau = OP == mtf::LOSS_DISTILL ? a.inv_tau : 1.0, l0 = log_sum(m, s0, a0, F), l1 = NT == 1 ? l0 : log_sum(m, s1, a1, F);
-    g.lse0 = (double)m * inv_tau + l0;
-    g.lse1 = NT == 1 ? g.lse0 : (double)m + l1;      // (one sum: tau is 1, or only one of the two is used)
-    g.m0 = g.m1 = m;
-    logp = ((double)x.zy - (double)m) - l1;
-  } else if (OP == mtf::LOSS_DISTILL) {
-    g.lse0 = (double)a.lse[2 * row];
-    g.lse1 = (double)a.lse[2 * row + 1];
-    g.m0 = (float)(soft_on<OP>(a) ? g.lse0 * (double)a.temperature : g.lse1);
-    g.m1 = NT == 1 ? g.m0 : (float)g.lse1;
-    logp = (double)x.zy - g.lse1;
-  } else {
-    g.lse0 = g.lse1 = (double)a.lse[row];
-    g.m0 = g.m1 = (float)g.lse0;
-    logp = (double)x.zy - g.lse0;
-  }
+  g.m0 = g.m1 = m;
   double c0, c1 = 0.0;         // factors of the two distributions in the gradient
   if (OP != mtf::LOSS_DISTILL) {
-    double c = (double)in.scale;
+    r.c = (double)in.scale;
     if (PASS & mtf::LOSS_FORWARD) {
-      const float hi = (float)logp;
-      // (preference: until the pairs' kernel has added the log-probabilities up, lse holds what rounding logp to f32 leaves over)
-      if (write && a.lse) a.lse[row] = OP == mtf::LOSS_LOGP && isfinite(hi) ? (float)(logp - (double)hi) : (float)g.lse0;
-      if (write && a.logp) a.logp[row] = hi;
-      c = 0.0;
+      r.c = 0.0;
       if (OP == mtf::LOSS_POLICY) {
-        const double adv = (double)x.adv, ratio = exp(logp - (double)x.old), plain = ratio * adv;
-        const double clipped = fmin(fmax(ratio, 1.0 - (double)a.clip_low), 1.0 + (double)a.clip_high) * adv;
-        const bool cut = plain > clipped;             // (not so for NaN, which both results then show)
-        double loss = cut ? -clipped : -plain, dl = cut ? 0.0 : -plain;
+        const double base = ((double)x.zy - (double)m) - reference_off(m, a0, F), adv = (double)x.adv;
+        const double ratio = exp64(base - (double)x.old) / (double)s0;
+        r.plain = ratio * adv;
+        r.clipped = fmin(fmax(ratio, 1.0 - (double)a.clip_low), 1.0 + (double)a.clip_high) * adv;
+        double dl = r.plain > r.clipped ? 0.0 : -r.plain;             // (NaN: not cut, and both results show it)
         if (a.kl_weight != 0.f) {
-          const double e = (double)x.ref - logp, em1 = expm1(e);
-          loss += (double)a.kl_weight * (em1 - e);
-          dl -= (double)a.kl_weight * em1;
+          r.em1 = exp64((double)x.ref - base) * (double)s0 - 1.0;
+          dl -= (double)a.kl_weight * r.em1;
         }
-        if (write) a.loss[row] = (float)(w * loss);
-        c = w * dl;
-        if (write && a.dlogp) a.dlogp[row] = (float)c;
+        r.c = w * dl;
       }
     }
-    if (PASS == mtf::LOSS_FORWARD) return g;
-    c0 = -c;
-    g.fix = (float)(-c * expm1(logp));
+    c0 = -r.c;
   } else {
-    if (PASS & mtf::LOSS_FORWARD) {
-      double loss = 0.0;
-      if (x.sum != 0.0) loss = (double)a.soft * (double)a.temperature * (double)a.temperature * (x.kl + g.lse0);
-      if (hard_on<OP>(a)) loss -= (double)a.hard * logp;
-      if (write) {
-        a.loss[row] = (float)(w * loss);
-        if (a.lse) {
-          a.lse[2 * row] = (float)(soft_on<OP>(a) ? g.lse0 : 0.0);
-          a.lse[2 * row + 1] = (float)(hard_on<OP>(a) ? g.lse1 : 0.0);
-        }
-      }
-    }
-    if (PASS == mtf::LOSS_FORWARD) return g;
     const double f = PASS == mtf::LOSS_BACKWARD ? (double)in.scale : w;
-    g.cs = x.sum != 0.0 ? f * (double)a.soft * (double)a.temperature : 0.0;
-    g.ch = hard_on<OP>(a) ? f * (double)a.hard : 0.0;
-    c0 = NT >= 2 ? g.cs : g.cs + g.ch;
-    c1 = g.ch;
-    // (the label's entry where no slot has it)
-    g.fix = (float)((g.cs != 0.0 ? g.cs * exp((double)x.zy * a.inv_tau - g.lse0) : 0.0) + g.ch * expm1(logp));
+    r.cs = x.sum != 0.0 ? f * (double)a.soft * (double)a.temperature : 0.0;
+    r.ch = hard_on<OP>(a) ? f * (double)a.hard : 0.0;
+    c0 = NT >= 2 ? r.cs : r.cs + r.ch;
+    c1 = r.ch;
   }
+  if (PASS == mtf::LOSS_FORWARD) return g;
   g.zero = c0 == 0.0 && (NT == 1 || c1 == 0.0);
+  if (PASS == mtf::LOSS_STEP) {
+    g.huge = F.is_huge(m);
+    g.nb0 = -reference(m, a0);
+    g.nb1 = -reference(m, a1);
+    g.k0 = (float)c0 / s0;
+    g.k1 = NT >= 2 ? (float)c1 / s1 : 0.f;
+    return g;
+  }
+  // from the stored log-sum-exps: 2^(z a - b) for exp of z / tau - lse, the rest of the exponent goes to the factor
+  if (OP == mtf::LOSS_DISTILL) {
+    r.lse0 = (double)a.lse[2 * row];
+    r.lse1 = (double)a.lse[2 * row + 1];
+  } else {
+    r.lse0 = r.lse1 = (double)a.lse[row];
+  }
+  const double l0 = soft_on<OP>(a) ? r.lse0 * (double)a.temperature : OP == mtf::LOSS_DISTILL ? r.lse1 : r.lse0;
+  g.m0 = (float)l0;
+  g.m1 = NT == 1 ? g.m0 : (float)r.lse1;
   g.huge = F.is_huge(g.m0) || F.is_huge(g.m1);
   g.nb0 = -reference(g.m0, a0);
   g.nb1 = NT == 3 ? 2.f * g.nb0 : -reference(g.m1, a1);
-  if (PASS == mtf::LOSS_STEP) {
-    g.k0 = (float)(c0 / s0);
-    g.k1 = NT >= 2 ? (float)(c1 / s1) : 0.f;
-  } else {
-    // 2^(z a - b) for exp of z / tau - lse: the rest of the exponent goes to the factor
-    const double l0 = soft_on<OP>(a) ? g.lse0 * (double)a.temperature : OP == mtf::LOSS_DISTILL ? g.lse1 : g.lse0;
-    g.k0 = (float)(g.huge ? c0 : c0 * exp2(-(double)g.nb0 - l0 * (double)a0));
-    g.k1 = (float)(g.huge || NT == 1 ? c1 : c1 * exp2(-(double)g.nb1 - g.lse1 * (double)a1));
-  }
+  g.k0 = (float)(g.huge ? c0 : c0 * exp2(-(double)g.nb0 - l0 * (double)a0));
+  g.k1 = (float)(g.huge || NT == 1 ? c1 : c1 * exp2(-(double)g.nb1 - r.lse1 * (double)a1));
   return g;
+}
+
+// Then the rest.  write: this thread stores the results per row.
+template <int OP, int PASS, int NT>
+__device__ __forceinline__ void row_results(const LossRows& a, long long row, const RowIn& in, const RowInputs& x, float m, float s0, float s1, bool write, const Factors& F,
+                                            RowNumbers& r) {
+  const double w = (double)in.w;
+  double logp = 0.0;           // of the label
+  if (PASS & mtf::LOSS_FORWARD) {
+    const double inv_tau = OP == mtf::LOSS_DISTILL ? a.inv_tau : 1.0, l0 = reference_off(m, F.a0, F) + log64((double)s0);
+    const double l1 = NT == 1 ? l0 : reference_off(m, F.a1, F) + log64((double)s1);
+    r.lse0 = (double)m * inv_tau + l0;
+    r.lse1 = NT == 1 ? r.lse0 : (double)m + l1;      // (one sum: tau is 1, or only one of the two is used)
+    logp = ((double)x.zy - (double)m) - l1;
+  }
+  if (OP != mtf::LOSS_DISTILL) {
+    if (PASS & mtf::LOSS_FORWARD) {
+      const float hi = (float)logp;
+      // (preference: until the pairs' kernel has added the log-probabilities up, lse holds what rounding logp to f32 leaves over)
+      if (write && a.lse) a.lse[row] = OP == mtf::LOSS_LOGP && isfinite(hi) ? (float)(logp - (double)hi) : (float)r.lse0;
+      if (write && a.logp) a.logp[row] = hi;
+      if (OP == mtf::LOSS_POLICY) {
+        double loss = r.plain > r.clipped ? -r.clipped : -r.plain;
+        if (a.kl_weight != 0.f) loss += (double)a.kl_weight * (r.em1 - ((double)x.ref - logp));
+        if (write) a.loss[row] = (float)(w * loss);
+        if (write && a.dlogp) a.dlogp[row] = (float)r.c;
+      }
+    }
+    return;
+  }
+  if (PASS & mtf::LOSS_FORWARD) {
+    double loss = 0.0;
+    if (x.sum != 0.0) loss = (double)a.soft * (double)a.temperature * (double)a.temperature * (x.kl + r.lse0);
+    if (hard_on<OP>(a)) loss -= (double)a.hard * logp;
+    if (write) {
+      a.loss[row] = (float)(w * loss);
+      if (a.lse) {
+        a.lse[2 * row] = (float)(soft_on<OP>(a) ? r.lse0 : 0.0);
+        a.lse[2 * row + 1] = (float)(hard_on<OP>(a) ? r.lse1 : 0.0);
+      }
+    }
+  }
+}
+
+// one entry of a row's gradient as a walk writes it: for the row's edges, for rows with huge logits and for the entries that differ
+template <int NT>
+__device__ __forceinline__ float gradient_of(float z, const RowGrad& g, const Factors& F) {
+  float v = g.k0 * ex2(g.huge ? (z - g.m0) * F.a0 : fmaf(z, F.a0, g.nb0));
+  if (NT >= 2) v += g.k1 * ex2(g.huge ? (z - g.m1) * F.a1 : fmaf(z, F.a1, g.nb1));
+  return v;
 }
 
 // The entries of a distillation row's gradient that differ from the walk's, by one warp: their values take the place of sl.z, and slots that write
 // none get the id -1 (of slots with one id the first takes care of all).  True: a slot has the label's entry, too.
-__device__ __forceinline__ bool slot_values(const LossRows& a, const RowGrad& g, const Slots& sl, int label, int lane) {
+template <int NT>
+__device__ __forceinline__ bool slot_values(const LossRows& a, const RowGrad& g, const RowNumbers& r, const Slots& sl, int label, int lane, const Factors& F) {
   const int K = a.slots;
   const int4* const ids = reinterpret_cast<const int4*>(sl.id);
   bool has_label = false;
   unsigned later = 0u;         // bit k / 32: not the first of its id
+#pragma unroll 1
   for (int k = lane, bit = 0; k < K; k += 32, ++bit) {
     const int id = sl.id[k];
     if (id < 0) continue;
     int first = K, same = 0;
+#pragma unroll 2
     for (int j = 0; 4 * j < K; ++j) {
       const int4 v = ids[j];
       if (v.w == id) { first = min(first, 4 * j + 3); ++same; }
@@ -505,16 +546,12 @@ __device__ __forceinline__ bool slot_values(const LossRows& a, const RowGrad& g,
     }
     if (first != k) { later |= 1u << bit; continue; }
     double q = sl.q[k];
+#pragma unroll 1
     for (int j = k + 1; same > 1 && j < K; ++j)
       if (sl.id[j] == id) { q += sl.q[j]; --same; }
-    const double z = (double)sl.z[k];
-    double v = 0.0;
-    if (g.cs != 0.0) v += g.cs * (exp(z * a.inv_tau - g.lse0) - q);
-    if (g.ch != 0.0) {
-      v += g.ch * (exp(z - g.lse1) - (id == label ? 1.0 : 0.0));
-      has_label |= id == label;
-    }
-    sl.z[k] = (float)v;
+    const bool is_label = r.ch != 0.0 && id == label;
+    has_label |= is_label;
+    sl.z[k] = (float)((double)gradient_of<NT>(sl.z[k], g, F) - r.cs * q - (is_label ? r.ch : 0.0));
   }
   __syncwarp();
   for (int k = lane, bit = 0; k < K; k += 32, ++bit)
@@ -523,13 +560,18 @@ __device__ __forceinline__ bool slot_values(const LossRows& a, const RowGrad& g,
   return __any_sync(0xffffffffu, has_label);
 }
 // ... behind the walk's stores, by threads `at` of n.  owned(id): this block writes that entry; label_alone: the label's entry is no slot's.
-template <typename T, typename F>
-__device__ __forceinline__ void write_slots(const LossRows& a, const RowGrad& g, const Slots& sl, int label, bool label_alone, char* dr, int at, int n, F owned) {
+template <typename T, typename O>
+__device__ __forceinline__ void write_slots(const LossRows& a, float fix, const Slots& sl, int label, bool label_alone, char* dr, int at, int n, O owned) {
   for (int k = at; k < a.slots; k += n) {
     const int id = sl.id[k];
     if (id >= 0 && owned(id)) Piece<T>::set(dr, id, sl.z[k]);
   }
-  if (at == 0 && label_alone && owned(label)) Piece<T>::set(dr, label, g.fix);
+  if (at == 0 && label_alone && owned(label)) Piece<T>::set(dr, label, fix);
+}
+// the label's entry (distillation: where no slot has it)
+template <int OP, int NT>
+__device__ __forceinline__ float label_value(const RowGrad& g, const RowNumbers& r, float zy, const Factors& F) {
+  return (float)((double)gradient_of<NT>(zy, g, F) + (OP == mtf::LOSS_DISTILL ? -r.ch : r.c));
 }
 
 template <typename T, int NT>
@@ -548,13 +590,6 @@ struct GradValues {
     return Piece<T>::put(f);
   }
 };
-// one entry of a row's gradient, for the row's edges and for rows with huge logits
-template <int NT>
-__device__ __forceinline__ float gradient_of(float z, const RowGrad& g, const Factors& F) {
-  float v = g.k0 * ex2(g.huge ? (z - g.m0) * F.a0 : fmaf(z, F.a0, g.nb0));
-  if (NT >= 2) v += g.k1 * ex2(g.huge ? (z - g.m1) * F.a1 : fmaf(z, F.a1, g.nb1));
-  return v;
-}
 // pieces [first, last) of a row with huge logits, by threads `at` of n
 template <typename T, int NT>
 __device__ __noinline__ void huge_pieces(const uint4* from, uint4* to, int first, int last, int at, int n, const RowGrad& g, const Factors& F) {
@@ -673,7 +708,11 @@ __global__ void __launch_bounds__(kRowWarps * 32, PASS == mtf::LOSS_BACKWARD && 
     return;
   }
   RowInputs x = {};
-  if (warp == 0) x = row_inputs<T, OP>(a, row, part.zr, in.label, sl, lane, bad, rank == 0);
+  if (warp == 0) {
+    Fetched f = {};
+    if (OP == mtf::LOSS_DISTILL) fetch_slots(a, row, 0, lane, soft_on<OP>(a), f);
+    x = row_inputs<T, OP>(a, row, part.zr, in.label, f, sl, lane, bad, rank == 0);
+  }
 
   float m = 0.f, s0 = 1.f, s1 = 1.f;
   if (PASS & mtf::LOSS_FORWARD) {
@@ -734,14 +773,16 @@ __global__ void __launch_bounds__(kRowWarps * 32, PASS == mtf::LOSS_BACKWARD && 
     __syncwarp();
     cluster_arrive();          // this block has read the others' sums: they may end once all have
   }
-  RowGrad g = {};
+  RowNumbers r = {};
   if (warp == 0) {
-    g = row_numbers<OP, PASS, NT>(a, row, in, x, m, (double)s0, (double)(NT >= 2 ? s1 : s0), rank == 0 && lane == 0, F);
+    const RowGrad g = row_gradient<OP, PASS, NT>(a, row, in, x, m, s0, s1, F, r);
     if ((PASS & mtf::LOSS_BACKWARD) && lane == 0) sc.g = g;
+    if (PASS == mtf::LOSS_FORWARD) row_results<OP, PASS, NT>(a, row, in, x, m, s0, s1, rank == 0 && lane == 0, F, r);
   }
   if (PASS & mtf::LOSS_BACKWARD) {
     __syncthreads();
-    if (sc.g.zero) {
+    const bool zero = sc.g.zero;
+    if (zero) {
       part.zeros(tid, blockDim.x);
     } else {
       if (sc.g.huge) {
@@ -752,13 +793,18 @@ __global__ void __launch_bounds__(kRowWarps * 32, PASS == mtf::LOSS_BACKWARD && 
         walk<4>(part.z16, part.begin, part.end, [&](int p, const uint4& u) { part.d16[p] = v.piece(u, F); });
       }
       if (tid < part.edges) Piece<T>::set(part.dr, part.edge(tid), gradient_of<NT>(Piece<T>::one(part.zr, part.edge(tid)), sc.g, F));
-      bool alone = true;
-      if (OP == mtf::LOSS_DISTILL && warp == 0) alone = !slot_values(a, g, sl, in.label, lane) && hard_on<OP>(a);
-      __syncthreads();
-      if (warp == 0) {
-        if (OP == mtf::LOSS_DISTILL) write_slots<T>(a, g, sl, in.label, alone, part.dr, lane, 32, [&](int e) { return part.owned(e); });
-        else if (lane == 0 && part.owned(in.label)) Piece<T>::set(part.dr, in.label, g.fix);
-      }
+    }
+    bool alone = true;
+    float fix = 0.f;
+    if (warp == 0) {
+      if (PASS & mtf::LOSS_FORWARD) row_results<OP, PASS, NT>(a, row, in, x, m, s0, s1, rank == 0 && lane == 0, F, r);
+      fix = label_value<OP, NT>(sc.g, r, x.zy, F);
+      if (OP == mtf::LOSS_DISTILL) alone = !slot_values<NT>(a, sc.g, r, sl, in.label, lane, F) && hard_on<OP>(a);
+    }
+    __syncthreads();
+    if (warp == 0 && !zero) {
+      if (OP == mtf::LOSS_DISTILL) write_slots<T>(a, fix, sl, in.label, alone, part.dr, lane, 32, [&](int e) { return part.owned(e); });
+      else if (lane == 0 && part.owned(in.label)) Piece<T>::set(part.dr, in.label, fix);
     }
   }
   if (kSums && parts > 1) {
@@ -891,19 +937,27 @@ __global__ void __launch_bounds__(kStreamThreads, 1) loss_stream_kernel(const Lo
       }
       return false;
     };
-    // What is read of a row is read while the walks still have the row before in hand: two lists a warp.
-    RowIn in = {};
+    // What is read of a row is read while the walks still have the row before in hand: two lists a warp, and the loads a row earlier still.
+    RowIn in = {}, in_next = {};
     RowInputs x = {};
+    Fetched f = {};
     auto list_of = [&](int use) { return Slots(lists + (2 * s + (use & 1)) * list, a.slots); };
+    auto fetch = [&] {
+      in_next.w = a.weight ? a.weight[row_of(i)] : 1.f;      // (a row that is not skipped: its label is good)
+      in_next.label = OP != mtf::LOSS_DISTILL || hard_on<OP>(a) ? a.targets[row_of(i)] : 0;
+      if (OP == mtf::LOSS_DISTILL) fetch_slots(a, row_of(i), 0, lane, soft_on<OP>(a), f);
+    };
     auto read = [&] {
-      in = row_in<OP, PASS>(a, row_of(i));
-      x = row_inputs<T, OP>(a, row_of(i), RowPart<T>(a, row_of(i), each, rank).zr, in.label, list_of(uses), lane, bad);
+      in = in_next;
+      x = row_inputs<T, OP>(a, row_of(i), RowPart<T>(a, row_of(i), each, rank).zr, in.label, f, list_of(uses), lane, bad, rank == 0);
     };
     bool more = next();
-    if (more) read();
+    if (more) { fetch(); read(); }
     while (more) {
       const long long row = row_of(i);
       const RowPart<T> part(a, row, each, rank);
+      more = next();
+      if (more) fetch();
       const Slots sl = list_of(uses);
       phase ^= 1u;
       float m = -F.huge, s0 = 0.f, s1 = 0.f;
@@ -927,23 +981,24 @@ __global__ void __launch_bounds__(kStreamThreads, 1) loss_stream_kernel(const Lo
         if (lane < parts) asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(in_peer(&st.heard[s], lane)) : "memory");
         warp_join<NT>(m, s0, s1, F);
       }
-      const RowGrad g = row_numbers<OP, PASS, NT>(a, row, in, x, m, (double)s0, (double)(NT >= 2 ? s1 : s0), rank == 0 && lane == 0, F);
+      RowNumbers r;
+      const RowGrad g = row_gradient<OP, PASS, NT>(a, row, in, x, m, s0, s1, F, r);
       __syncwarp();            // (every lane has read the sums)
       if (lane == 0) {
         st.g[s] = g;
         bar_arrive(&st.ready[s]);
       }
+      if (rank == 0) row_results<OP, PASS, NT>(a, row, in, x, m, s0, s1, lane == 0, F, r);
       const int label = in.label;
       bool alone = true;
-      if (OP == mtf::LOSS_DISTILL) alone = !slot_values(a, g, sl, label, lane) && hard_on<OP>(a);
-      const float fix = g.fix;
+      if (OP == mtf::LOSS_DISTILL) alone = !slot_values<NT>(a, g, r, sl, label, lane, F) && hard_on<OP>(a);
+      const float fix = label_value<OP, NT>(g, r, x.zy, F);
       const bool zero = g.zero;
       ++uses;
-      more = next();
       if (more) read();
       bar_wait(&st.done[s], phase, 0xA05, &st.abort);
       if (!zero) {
-        if (OP == mtf::LOSS_DISTILL) write_slots<T>(a, st.g[s], sl, label, alone, part.dr, lane, 32, [&](int e) { return part.owned(e); });
+        if (OP == mtf::LOSS_DISTILL) write_slots<T>(a, fix, sl, label, alone, part.dr, lane, 32, [&](int e) { return part.owned(e); });
         else if (lane == 0 && part.owned(label)) Piece<T>::set(part.dr, label, fix);
       }
       __syncwarp();
@@ -1114,18 +1169,6 @@ __global__ void __launch_bounds__(kStreamThreads, 1) loss_stream_kernel(const Lo
 
 // ---- the pairs of the preference loss ----------------------------------------------------------------------------------------------------
 constexpr int kPairThreads = 1024;
-// sum over the block, the same in every thread
-__device__ __forceinline__ double block_sum(double v, double* red) {
-  v = warp_add(v);
-  __syncthreads();
-  if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = v;
-  __syncthreads();
-  double r = 0.0;
-#pragma unroll
-  for (int w = 0; w < kPairThreads / 32; ++w) r += red[w];
-  return r;
-}
-
 // One block per pair: both sequences' log-probabilities added up in a fixed order, in 64 bits, then the loss of the pair and its
 // derivative by each of the two sums.  A sum of hundreds of log-probabilities that are each rounded to f32 would be off by more than its
 // own rounding (the loss goes by the difference of two): the rows' kernel has left the rest of each in lse's place, and lse itself, the
@@ -1135,24 +1178,34 @@ __global__ void __launch_bounds__(kPairThreads) preference_pairs_kernel(const mt
   mtf::chain_wait();
   __shared__ double red[kPairThreads / 32];
   const long long b = blockIdx.x;
-  double s[2];
-  for (int i = 0; i < 2; ++i) {
-    const long long from = (i * a.pairs + b) * a.length;
-    double v = 0.0;
-    for (long long t = from + threadIdx.x; t < from + a.length; t += kPairThreads) {
-      const float w = a.weight ? a.weight[t] : 1.f, hi = a.logp[t], lo = a.lse[t];
-      const int label = a.targets[t];
-      if (w == 0.f || label < 0 || label >= a.V) continue;                // (both 0)
-      if (isfinite(hi)) {
-        const double logp = (double)hi + (double)lo;
-        v += (double)w * logp;
-        a.lse[t] = (float)((double)Piece<T>::one(a.z, t * a.V + label) - logp);
-      } else {
-        v += (double)w * (double)hi;
-      }
+  // half of the threads to each of the two
+  constexpr int half = kPairThreads / 2;
+  const int side = threadIdx.x / half;
+  const long long from = (side * a.pairs + b) * a.length;
+  double v = 0.0;
+#pragma unroll 2
+  for (long long t = from + threadIdx.x % half; t < from + a.length; t += half) {
+    const float w = a.weight ? a.weight[t] : 1.f, hi = a.logp[t], lo = a.lse[t];
+    const int label = a.targets[t];
+    if (w == 0.f || label < 0 || label >= a.V) continue;                // (both 0)
+    if (isfinite(hi)) {
+      const double logp = (double)hi + (double)lo;
+      v += (double)w * logp;
+      a.lse[t] = (float)((double)Piece<T>::one(a.z, t * a.V + label) - logp);
+    } else {
+      v += (double)w * (double)hi;
     }
-    s[i] = block_sum(v, red);
   }
+  v = warp_add(v);
+  if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = v;
+  __syncthreads();
+  if (threadIdx.x >= 32) return;
+  double s[2];
+  v = red[threadIdx.x];
+#pragma unroll
+  for (int o = half / 64; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  s[0] = __shfl_sync(0xffffffffu, v, 0);
+  s[1] = __shfl_sync(0xffffffffu, v, half / 32);
   if (threadIdx.x) return;
   const double margin = (s[0] - (double)a.ref[b]) - (s[1] - (double)a.ref[a.pairs + b]), beta = (double)a.beta, h = beta * margin;
   double loss, d;
@@ -1201,8 +1254,8 @@ bool launch_stream(const LossRows& a, size_t list, cudaLaunchConfig_t cfg, cudaL
   auto part_chunks = [&](int parts) { return (int)(((pieces + parts - 1) / parts + kChunkPieces - 1) / kChunkPieces); };
   // The ring holds the lead and three chunks on their way; the lead is more than a row's part, and two at most (their slots).
   int parts = 1;
-  while (parts < kMaxParts && part_chunks(parts) + 2 > chunks - 3) parts *= 2;
-  const int lead = std::min(chunks - 3, 2 * part_chunks(parts));
+  while (parts < kMaxParts && part_chunks(parts) + 1 > chunks - (parts == 1 ? 4 : 3)) parts *= 2;
+  const int lead = std::min(chunks - (parts == 1 ? 4 : 3), 2 * part_chunks(parts));
   if (lead < part_chunks(parts) + 1) return false;
   auto kernel = loss_stream_kernel<T, OP, NT>;
   cfg.dynamicSmemBytes = fixed + (size_t)chunks * kChunk;
