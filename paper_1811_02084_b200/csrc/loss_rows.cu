@@ -139,13 +139,16 @@ __device__ __forceinline__ RowSpan row_span(long long row, int V) {
 }
 __device__ __forceinline__ int edge_element(const RowSpan& s, int i, int V) { return i < s.head ? i : V - s.tail + (i - s.head); }
 
-// 2^(z a0 - b0) and, with two temperatures, 2^(z a1 - b1), a0 being the softened one.  A temperature of 2 (NT = 3) has the second as the square of
-// the first (b1 = 2 b0).  For others (NT = 2) the special-function unit alone would bound a distillation's walks (4 exponentials an entry at 16
-// a cycle and SM): it takes three of four, the arithmetic pipes the fourth, which is a softened one, so that a NaN is never lost.
-template <int NT>
+// 2^(z a0 - b0) and, with two temperatures, 2^(z a1 - b1), a0 being the softened one, of pair e of a piece.  A temperature of 2 (NT = 3) has the second
+// as the square of the first (b1 = 2 b0).  The special-function unit takes an exponential every 8 cycles a scheduler, which alone would bound the
+// walks with two exponentials an entry; the arithmetic pipes take every other softened one of the sums and every fourth of the gradient, where the
+// factors want more of them (with one exponential an entry the walks are as long either way, and nothing is taken over).  Of the sums only softened
+// ones: a NaN may come out as a number there, and the other exponential of its entry shows it.  A gradient's factors are NaN where its row has one.
+template <int NT, bool kGradient>
 __device__ __forceinline__ void exponentials(int e, f32x2 z, float a0, float nb0, float a1, float nb1, f32x2& e0, f32x2& e1) {
   const f32x2 y = fma2(z, pair(a0), pair(nb0));
-  e0 = NT == 2 && (e & 1) ? ex2_fma(y) : ex2_unit(y);
+  const bool fma = NT == 2 && (kGradient ? (e & 3) == 3 : (e & 1) == 1);
+  e0 = fma ? ex2_fma(y) : ex2_unit(y);
   if (NT == 2) e1 = ex2_unit(fma2(z, pair(a1), pair(nb1)));
   if (NT == 3) e1 = mul2(e0, e0);
 }
@@ -160,55 +163,6 @@ struct Factors {
   __device__ __forceinline__ bool is_huge(float m) const { return !(fabsf(m) < huge); }
 };
 
-// Sums of exponentials relative to a reference m, an entry of the row: sums of 2^(z a - b) with b = fl(m a), the one rounding of which every use
-// of the sums allows for.  m starts at -huge (far lower entries, infinity among them, add nothing) and is raised to the largest entry seen only
-// where that lies 2^40 above it: an f32 sum has room for that, and nearly every entry is spared the rescaling (a thread that raises its
-// reference holds up its warp, and with a maximum that is always exact some thread of a warp nearly always does).
-template <int NT>
-struct RunningSum {
-  float m, limit, nb0, nb1;
-  f32x2 p0 = 0ull, p1 = 0ull;      // p0: exponents times a0, p1: times a1 (two temperatures); two partial sums each
-  __device__ __forceinline__ explicit RunningSum(const Factors& F) : m(-F.huge), limit(-F.huge), nb0(reference(F.huge, F.a0)), nb1(reference(F.huge, F.a1)) {}
-  __device__ __forceinline__ void raise(float pm, const Factors& F) {
-    const float a0 = F.a0, a1 = F.a1;
-    if (pm > limit) {
-      const float b0 = reference(pm, a0), b1 = reference(pm, a1);
-      p0 = mul2(p0, pair(ex2(-nb0 - b0)));
-      if (NT >= 2) p1 = mul2(p1, pair(ex2(-nb1 - b1)));
-      m = pm;
-      limit = pm + 40.f / (NT >= 2 ? fmaxf(a0, a1) : a0);
-      nb0 = -b0;
-      nb1 = -b1;
-    }
-  }
-  template <typename T, int N>
-  __device__ __forceinline__ void add(const uint4* u, const Factors& F) {
-    raise(Piece<T>::template largest<N>(u), F);
-    add_below<T, N>(u, F);
-  }
-  template <typename T, int N>
-  __device__ __forceinline__ void add_below(const uint4* u, const Factors& F) {      // ... entries that the reference has been raised for
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      f32x2 f[Piece<T>::kN / 2];
-      Piece<T>::get(u[i], f);
-#pragma unroll
-      for (int e = 0; e < Piece<T>::kN / 2; ++e) {
-        f32x2 e0, e1;
-        exponentials<NT>(e, f[e], F.a0, nb0, F.a1, nb1, e0, e1);
-        p0 = add2(p0, e0);
-        if (NT >= 2) p1 = add2(p1, e1);
-      }
-    }
-  }
-  __device__ __forceinline__ void add_one(float f, const Factors& F) {
-    raise(f, F);
-    p0 = add2(p0, pair(ex2(fmaf(f, F.a0, nb0)), 0.f));
-    if (NT >= 2) p1 = add2(p1, pair(ex2(fmaf(f, F.a1, nb1)), 0.f));
-  }
-  __device__ __forceinline__ void of_warp(float& t_m, float& t_0, float& t_1, const Factors& F) const;
-};
-
 // a maximum over the warp: f32 values in the order of whole numbers
 __device__ __forceinline__ float warp_max(float v) {
   int i = __float_as_int(v);
@@ -220,6 +174,54 @@ __device__ __forceinline__ float warp_add(float v) {
   for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
   return v;
 }
+// Sums of exponentials relative to a reference m, an entry of the row: sums of 2^(z a - b) with b = fl(m a), the one rounding of which every use
+// of the sums allows for.  m starts at -huge (far lower entries, infinity among them, add nothing) and is raised to the largest entry seen only
+// where that lies 2^40 above it: an f32 sum has room for that, and nearly every entry is spared the rescaling (with a maximum that is always
+// exact some thread of a warp has to rescale at nearly every step, and holds up the others).
+template <int NT>
+struct RunningSum {
+  float m, limit, nb0, nb1;
+  f32x2 p0 = 0ull, p1 = 0ull;      // p0: exponents times a0, p1: times a1 (two temperatures); two partial sums each
+  __device__ __forceinline__ explicit RunningSum(const Factors& F) : m(-F.huge), limit(-F.huge), nb0(reference(F.huge, F.a0)), nb1(reference(F.huge, F.a1)) {}
+  __device__ __forceinline__ void raise(float pm, const Factors& F) {
+    if (pm > limit) {
+      const float b0 = reference(pm, F.a0), b1 = reference(pm, F.a1);
+      p0 = mul2(p0, pair(ex2(-nb0 - b0)));
+      if (NT >= 2) p1 = mul2(p1, pair(ex2(-nb1 - b1)));
+      m = pm;
+      limit = pm + 40.f / (NT >= 2 ? fmaxf(F.a0, F.a1) : F.a0);
+      nb0 = -b0;
+      nb1 = -b1;
+    }
+  }
+  template <typename T, int N>
+  __device__ __forceinline__ void add_below(const uint4* u, const Factors& F) {      // entries that the reference has been raised for
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      f32x2 f[Piece<T>::kN / 2];
+      Piece<T>::get(u[i], f);
+#pragma unroll
+      for (int e = 0; e < Piece<T>::kN / 2; ++e) {
+        f32x2 e0, e1;
+        exponentials<NT, false>(e, f[e], F.a0, nb0, F.a1, nb1, e0, e1);
+        p0 = add2(p0, e0);
+        if (NT >= 2) p1 = add2(p1, e1);
+      }
+    }
+  }
+  template <typename T, int N>
+  __device__ __forceinline__ void add(const uint4* u, const Factors& F) {
+    raise(Piece<T>::template largest<N>(u), F);
+    add_below<T, N>(u, F);
+  }
+  __device__ __forceinline__ void add_one(float f, const Factors& F) {
+    raise(f, F);
+    p0 = add2(p0, pair(ex2(fmaf(f, F.a0, nb0)), 0.f));
+    if (NT >= 2) p1 = add2(p1, pair(ex2(fmaf(f, F.a1, nb1)), 0.f));
+  }
+  __device__ __forceinline__ void of_warp(float& t_m, float& t_0, float& t_1, const Factors& F) const;
+};
+
 // what a sum relative to m is multiplied by to be relative to mx >= m
 __device__ __forceinline__ float to_reference(float m, float mx, float a, const Factors& F) { return ex2(F.is_huge(mx) ? (m - mx) * a : reference(m, a) - reference(mx, a)); }
 // the lanes' references and sums joined, the same in every lane
@@ -578,13 +580,14 @@ template <typename T, int NT>
 struct GradValues {
   float k0 = 0.f, nb0 = 0.f, k1 = 0.f, nb1 = 0.f;
   __device__ __forceinline__ void set(const RowGrad& g) { k0 = g.k0; nb0 = g.nb0; k1 = g.k1; nb1 = g.nb1; }
+  template <int kPair = 0>     // the first pair's number (of pieces of two pairs the second of two is numbered on)
   __device__ __forceinline__ uint4 piece(const uint4& u, const Factors& F) const {
     f32x2 f[Piece<T>::kN / 2];
     Piece<T>::get(u, f);
 #pragma unroll
     for (int e = 0; e < Piece<T>::kN / 2; ++e) {
       f32x2 e0, e1;
-      exponentials<NT>(e, f[e], F.a0, nb0, F.a1, nb1, e0, e1);
+      exponentials<NT, true>(kPair + e, f[e], F.a0, nb0, F.a1, nb1, e0, e1);
       f[e] = NT >= 2 ? fma2(e1, pair(k1), mul2(e0, pair(k0))) : mul2(e0, pair(k0));
     }
     return Piece<T>::put(f);
@@ -655,11 +658,10 @@ __device__ __noinline__ void sums_of_differences(const RowPart<T>& part, int lan
 // ---- one block per row, which walks over it in global memory ---------------------------------------------------------------------
 constexpr int kRowWarps = 8;
 
-// pieces [begin, end) of a row, `n` threads side by side, U loads in flight a thread
+// pieces [begin, end) of a row, by threads `at` of n, U loads in flight a thread
 template <int U, typename F>
-__device__ __forceinline__ void walk(const uint4* z16, int begin, int end, F f) {
-  const int n = blockDim.x;
-  for (int p = begin + threadIdx.x; p < end; p += U * n) {
+__device__ __forceinline__ void walk(const uint4* z16, int begin, int end, int at, int n, F f) {
+  for (int p = begin + at; p < end; p += U * n) {
     uint4 u[U];
 #pragma unroll
     for (int i = 0; i < U; ++i)
@@ -688,12 +690,15 @@ __device__ __forceinline__ uint32_t in_peer(const void* p, uint32_t rank) {
 
 // A row may be cut into `parts`, a block each.  Where sums are taken (few rows) the blocks are a cluster and read each other's sums.  A gradient on its own
 // needs nothing of the other parts: what a block reads of them it has no use for (they may be overwritten already).
+// A distillation's teacher is worked out by a warp of its own beside the walk.
 template <typename T, int OP, int PASS, int NT>
-__global__ void __launch_bounds__(kRowWarps * 32, PASS == mtf::LOSS_BACKWARD && OP != mtf::LOSS_DISTILL ? 6 : 4) loss_rows_kernel(const LossRows a, const Factors F, const int parts, const int each, int* __restrict__ bad) {
+__global__ void __launch_bounds__((kRowWarps + (OP == mtf::LOSS_DISTILL)) * 32, OP == mtf::LOSS_DISTILL ? 3 : PASS == mtf::LOSS_BACKWARD ? 6 : 4) loss_rows_kernel(const LossRows a, const Factors F, const int parts, const int each, int* __restrict__ bad) {
   extern __shared__ __align__(128) unsigned char dyn[];
   Scratch& sc = *reinterpret_cast<Scratch*>(dyn);
   const Slots sl(dyn + sizeof(Scratch), a.slots);
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = blockDim.x >> 5;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int n = OP == mtf::LOSS_DISTILL ? blockDim.x - 32 : blockDim.x, warps = n >> 5;      // of the walk
+  const bool walks = tid < n, numbers = warp == (OP == mtf::LOSS_DISTILL ? warps : 0);
   const unsigned which = parts == 1 ? blockIdx.x : blockIdx.x / (unsigned)parts;
   const int rank = blockIdx.x - which * parts;
   const long long at = which, row = a.reverse ? a.rows - 1 - at : at;
@@ -708,7 +713,7 @@ __global__ void __launch_bounds__(kRowWarps * 32, PASS == mtf::LOSS_BACKWARD && 
     return;
   }
   RowInputs x = {};
-  if (warp == 0) {
+  if (numbers) {
     Fetched f = {};
     if (OP == mtf::LOSS_DISTILL) fetch_slots(a, row, 0, lane, soft_on<OP>(a), f);
     x = row_inputs<T, OP>(a, row, part.zr, in.label, f, sl, lane, bad, rank == 0);
@@ -718,7 +723,7 @@ __global__ void __launch_bounds__(kRowWarps * 32, PASS == mtf::LOSS_BACKWARD && 
   if (PASS & mtf::LOSS_FORWARD) {
     RunningSum<NT> rs(F);
     // four pieces' loads in flight while the four before are worked on
-    const int n = blockDim.x, first = part.begin + tid, fours = first < part.end ? (part.end - first + n - 1) / n / 4 : 0;
+    const int first = walks ? part.begin + tid : part.end, fours = first < part.end ? (part.end - first + n - 1) / n / 4 : 0;
     const uint4* z = part.z16 + first;
     uint4 u[4], w[4];
     auto load = [&](uint4* to) {
@@ -748,9 +753,9 @@ __global__ void __launch_bounds__(kRowWarps * 32, PASS == mtf::LOSS_BACKWARD && 
     if (tid < part.edges) rs.add_one(Piece<T>::one(part.zr, part.edge(tid)), F);
     float t_m, t_0, t_1;
     rs.of_warp(t_m, t_0, t_1, F);
-    if (lane == 0) { sc.m[warp] = t_m; sc.s0[warp] = t_0; sc.s1[warp] = t_1; }
+    if (lane == 0 && walks) { sc.m[warp] = t_m; sc.s0[warp] = t_0; sc.s1[warp] = t_1; }
     __syncthreads();
-    if (warp == 0) {
+    if (numbers) {
       m = lane < warps ? sc.m[lane] : -F.huge;
       s0 = lane < warps ? sc.s0[lane] : 0.f;
       s1 = lane < warps ? sc.s1[lane] : 0.f;
@@ -763,7 +768,7 @@ __global__ void __launch_bounds__(kRowWarps * 32, PASS == mtf::LOSS_BACKWARD && 
     __syncwarp();
     cluster_arrive();
     cluster_wait();            // (from here on a block may overwrite its part of the row)
-    if (warp == 0) {
+    if (numbers) {
       m = kLowest;
       s0 = s1 = 0.f;
       if (lane < parts)
@@ -774,7 +779,7 @@ __global__ void __launch_bounds__(kRowWarps * 32, PASS == mtf::LOSS_BACKWARD && 
     cluster_arrive();          // this block has read the others' sums: they may end once all have
   }
   RowNumbers r = {};
-  if (warp == 0) {
+  if (numbers) {
     const RowGrad g = row_gradient<OP, PASS, NT>(a, row, in, x, m, s0, s1, F, r);
     if ((PASS & mtf::LOSS_BACKWARD) && lane == 0) sc.g = g;
     if (PASS == mtf::LOSS_FORWARD) row_results<OP, PASS, NT>(a, row, in, x, m, s0, s1, rank == 0 && lane == 0, F, r);
@@ -784,25 +789,25 @@ __global__ void __launch_bounds__(kRowWarps * 32, PASS == mtf::LOSS_BACKWARD && 
     const bool zero = sc.g.zero;
     if (zero) {
       part.zeros(tid, blockDim.x);
-    } else {
+    } else if (walks) {
       if (sc.g.huge) {
-        huge_pieces<T, NT>(part.z16, part.d16, part.begin, part.end, tid, blockDim.x, sc.g, F);
+        huge_pieces<T, NT>(part.z16, part.d16, part.begin, part.end, tid, n, sc.g, F);
       } else {
         GradValues<T, NT> v;
         v.set(sc.g);
-        walk<4>(part.z16, part.begin, part.end, [&](int p, const uint4& u) { part.d16[p] = v.piece(u, F); });
+        walk<4>(part.z16, part.begin, part.end, tid, n, [&](int p, const uint4& u) { part.d16[p] = v.piece(u, F); });
       }
       if (tid < part.edges) Piece<T>::set(part.dr, part.edge(tid), gradient_of<NT>(Piece<T>::one(part.zr, part.edge(tid)), sc.g, F));
     }
     bool alone = true;
     float fix = 0.f;
-    if (warp == 0) {
+    if (numbers) {
       if (PASS & mtf::LOSS_FORWARD) row_results<OP, PASS, NT>(a, row, in, x, m, s0, s1, rank == 0 && lane == 0, F, r);
       fix = label_value<OP, NT>(sc.g, r, x.zy, F);
       if (OP == mtf::LOSS_DISTILL) alone = !slot_values<NT>(a, sc.g, r, sl, in.label, lane, F) && hard_on<OP>(a);
     }
     __syncthreads();
-    if (warp == 0 && !zero) {
+    if (numbers && !zero) {
       if (OP == mtf::LOSS_DISTILL) write_slots<T>(a, fix, sl, in.label, alone, part.dr, lane, 32, [&](int e) { return part.owned(e); });
       else if (lane == 0 && part.owned(in.label)) Piece<T>::set(part.dr, in.label, fix);
     }
@@ -909,6 +914,7 @@ __global__ void __launch_bounds__(kStreamThreads, 1) loss_stream_kernel(const Lo
         const RowPart<T> part(a, row_of(i), each, rank);
         for (int p = part.begin; p < part.end; p += kChunkPieces) {
           bar_wait(&st.empty[slot], phase, 0xA01, &st.abort);
+          if (*(volatile int*)&st.abort) break;      // (a chunk may be on its way into the slot, still)
           const uint32_t bytes = (uint32_t)min(kChunkPieces, part.end - p) * 16u;
           bar_expect(&st.full[slot], bytes);
           asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
@@ -1007,6 +1013,9 @@ __global__ void __launch_bounds__(kStreamThreads, 1) loss_stream_kernel(const Lo
     // ------------------------------- walks -------------------------------
     const int at = tid - 32 * (1 + kNumberWarps);
     constexpr int nt = 32 * kWalkers, kEach = kChunkPieces / nt;
+    // Rows whose length is a whole number of pieces all have the same part, without edges.
+    const bool aligned = a.V % Piece<T>::kN == 0;
+    const int begin0 = min(a.V / Piece<T>::kN, rank * each), end0 = min(a.V / Piece<T>::kN, begin0 + each);
     // the statistics' walk: row i, with slot s1; pieces [p, end) of its part are to come, the next of them in chunk c1
     int i = -1, s1 = -1, p = 0, end = 0, c1 = 0;
     uint32_t phase1 = 0u;
@@ -1018,12 +1027,15 @@ __global__ void __launch_bounds__(kStreamThreads, 1) loss_stream_kernel(const Lo
         if (++i >= n) return false;
       } while (!look(live, i));
       if (++s1 == kRowSlots) s1 = 0;
+      rs = RunningSum<NT>(F);
+      p = begin0;
+      end = end0;
+      if (aligned) return true;
       const RowPart<T> part(a, row_of(i), each, rank);
       p = part.begin;
       end = part.end;
       has_edge = at < part.edges;
       if (has_edge) edge = Piece<T>::one(part.zr, part.edge(at));      // (wanted at the row's end)
-      rs = RunningSum<NT>(F);
       return true;
     };
     auto count = [&] {                               // a chunk
@@ -1064,10 +1076,18 @@ __global__ void __launch_bounds__(kStreamThreads, 1) loss_stream_kernel(const Lo
       while (true) {
         if (++j >= n) return false;
         const bool alive = look(live_j, j);
+        if (alive) {
+          if (++s2 == kRowSlots) s2 = 0;
+          if (s2 == 0) phase2 ^= 1u;
+          if (aligned) {
+            to = reinterpret_cast<uint4*>(reinterpret_cast<char*>(a.d) + row_of(j) * a.V * (long long)sizeof(T)) + begin0;
+            left = end0 - begin0;
+            no_chunk = left == 0;
+            return true;
+          }
+        }
         const RowPart<T> part(a, row_of(j), each, rank);
         if (!alive) { part.zeros(at, nt); continue; }
-        if (++s2 == kRowSlots) s2 = 0;
-        if (s2 == 0) phase2 ^= 1u;
         to = part.d16 + part.begin;
         left = part.end - part.begin;
         no_chunk = left == 0;
@@ -1131,7 +1151,7 @@ __global__ void __launch_bounds__(kStreamThreads, 1) loss_stream_kernel(const Lo
           rs.raise(Piece<T>::template largest<kEach>(u), F);
           rs.template add_below<T, kEach>(u, F);
 #pragma unroll
-          for (int k = 0; k < kEach; ++k) to[at + k * nt] = v.piece(w[k], F);
+          for (int k = 0; k < kEach; ++k) to[at + k * nt] = (k & 1) && Piece<T>::kN == 4 ? v.template piece<2>(w[k], F) : v.piece(w[k], F);
           __syncwarp();
           if (lane == 0) bar_arrive(&st.empty[c2]);
           if (++c1 == chunks) { c1 = 0; phase1 ^= 1u; }
@@ -1306,7 +1326,7 @@ void launch(const LossRows& b, int* bad, cudaStream_t st) {
       cfg.numAttrs = 2;
     }
   }
-  cfg.blockDim = dim3((unsigned)threads, 1, 1);
+  cfg.blockDim = dim3((unsigned)(threads + (OP == mtf::LOSS_DISTILL ? 32 : 0)), 1, 1);
   cfg.dynamicSmemBytes = sizeof(Scratch) + list;
   cfg.gridDim = dim3((unsigned)(a.rows * parts), 1, 1);
   (void)cudaLaunchKernelEx(&cfg, loss_rows_kernel<T, OP, PASS, NT>, a, factors(a), parts, pieces_each<T>(a, parts), bad);
