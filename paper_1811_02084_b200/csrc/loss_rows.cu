@@ -325,7 +325,8 @@ __device__ __forceinline__ void zero_results(const LossRows& a, long long row) {
 
 struct RowInputs {
   float zy, old, ref, adv;
-  double kl, sum;              // the teacher's sum_k q_k (log q_k - z_k / tau), and sum_k q_k: 1, or 0 without a used slot
+  float zr;                    // the largest of the student's logits to the teacher's words, or 0
+  double kl, sum;              // the teacher's sum_k q_k (log q_k - (z_k - zr) / tau), and sum_k q_k: 1, or 0 without a used slot
 };
 // The first slots of a teacher's list as they are loaded, kB a lane.
 constexpr int kB = 4;
@@ -359,7 +360,7 @@ __device__ __forceinline__ RowInputs row_inputs(const LossRows& a, long long row
   }
   if (OP != mtf::LOSS_DISTILL) return r;
   const int K = a.slots;
-  float best = -INFINITY;      // of the logits as they are: f32 values
+  float best = -INFINITY, top = -INFINITY;      // of the logits as they are: f32 values
   for (int first = 0; first < K; first += 32 * kB) {
     float z[kB];
     if (first) fetch_slots(a, row, first, lane, soft_on<OP>(a), f);
@@ -377,9 +378,12 @@ __device__ __forceinline__ RowInputs row_inputs(const LossRows& a, long long row
       sl.z[k] = z[i];
       sl.q[k] = (double)t;
       best = fmaxf(best, t != t ? INFINITY : t);      // (NaN: every difference to the maximum is NaN)
+      if (f.id[i] >= 0) top = fmaxf(top, z[i]);
     }
   }
   best = warp_max(best);
+  top = warp_max(top);
+  r.zr = top != -INFINITY ? top : 0.f;
   const bool any = best != -INFINITY;
   double sum = 0.0, kl = 0.0;
   if (any) {
@@ -387,7 +391,7 @@ __device__ __forceinline__ RowInputs row_inputs(const LossRows& a, long long row
     for (int k = lane; k < K; k += 32) {
       const double d = (sl.q[k] - (double)best) * a.inv_tau, e = exp64(d);
       sum += e;
-      if (e != 0.0) kl += e * (d - (double)sl.z[k] * a.inv_tau);      // (a word of probability 0 adds nothing, whatever the student says to it)
+      if (e != 0.0) kl += e * (d - ((double)sl.z[k] - (double)r.zr) * a.inv_tau);      // (a word of probability 0 adds nothing, whatever the student says to it)
       sl.q[k] = e;
     }
 #pragma unroll
@@ -481,12 +485,14 @@ __device__ __forceinline__ void row_results(const LossRows& a, long long row, co
                                             RowNumbers& r) {
   const double w = (double)in.w;
   double logp = 0.0;           // of the label
+  double above = 0.0;          // log-sum-exp of z / tau less zr / tau
   if (PASS & mtf::LOSS_FORWARD) {
     const double inv_tau = OP == mtf::LOSS_DISTILL ? a.inv_tau : 1.0, l0 = reference_off(m, F.a0, F) + log64((double)s0);
     const double l1 = NT == 1 ? l0 : reference_off(m, F.a1, F) + log64((double)s1);
     r.lse0 = (double)m * inv_tau + l0;
     r.lse1 = NT == 1 ? r.lse0 : (double)m + l1;      // (one sum: tau is 1, or only one of the two is used)
     logp = ((double)x.zy - (double)m) - l1;
+    above = ((double)m - (double)x.zr) * inv_tau + l0;
   }
   if (OP != mtf::LOSS_DISTILL) {
     if (PASS & mtf::LOSS_FORWARD) {
@@ -505,7 +511,8 @@ __device__ __forceinline__ void row_results(const LossRows& a, long long row, co
   }
   if (PASS & mtf::LOSS_FORWARD) {
     double loss = 0.0;
-    if (x.sum != 0.0) loss = (double)a.soft * (double)a.temperature * (double)a.temperature * (x.kl + r.lse0);
+    // (differences first: in a row of the type's lowest values the log-sum-exp has no digits left for anything else)
+    if (x.sum != 0.0) loss = (double)a.soft * (double)a.temperature * (double)a.temperature * (x.kl + above);
     if (hard_on<OP>(a)) loss -= (double)a.hard * logp;
     if (write) {
       a.loss[row] = (float)(w * loss);

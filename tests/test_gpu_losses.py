@@ -8,6 +8,7 @@ exponential: with weights p the arguments' part is 3 u sum p X <= 3 u (log V + 1
     delta = (N + 3 (log V + 1) + 8) u   relative, and log-sum-exp and logp by delta, absolute.
 A gradient's entry k exp2((z - m) a) is off by delta (in k) + (3 X + 8) u of itself.  What is worked out from these in 64 bits and rounded once adds u (f32)
 or 2^-8 (bf16) of the value."""
+import gc
 import itertools
 import threading
 
@@ -511,6 +512,197 @@ def test_rows_and_vocabularies_in_bulk(mtf, B, L, V, dtype):
     assert bool(((loss.double() - want_loss).abs() <= 2.5 * d * w + U * want_loss.abs()).all())
     assert bool(((dz2.double() - want).abs() <= tol + U * 30 * (tol > 0) * want.abs() + (STEP[dtype] + 34 * U) * want.abs() + 30 * U * (0.5 * tau * p2.exp() + 0.5 * p1.exp())).all())
     guard.check()
+
+
+def rows_of_every_kind(dtype, T, V, seed, skipped):
+    """Logits on the GPU, row t of kind t * 7 % 16: masked by infinity (1) and by the type's lowest value (2), all lowest (3), all -infinity (4), with a NaN (5)
+    and an infinity (6), far from zero (7), one word far above the rest (8), all alike (9), and ordinary ones; targets among the words that are not masked;
+    weights, a share of them 0 (those rows hold NaN)."""
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    z = (2 * torch.randn(T, V, generator=g, device="cuda")).to(t_dtype(dtype))
+    kind = torch.arange(T, device="cuda") * 7 % 16
+    low = torch.finfo(z.dtype).min
+    half = V // 2
+    z[kind == 1, half:] = float("-inf")
+    z[kind == 2, half:] = low
+    z[kind == 3] = low
+    z[kind == 4] = float("-inf")
+    z[kind == 5, V // 3] = float("nan")
+    z[kind == 6, V - 1] = float("inf")
+    z[kind == 7] += 3.0e4
+    z[kind == 8] *= 1.0e30
+    z[kind == 9] = 1.5
+    y = torch.randint(0, half, (T,), generator=g, device="cuda")
+    y[kind == 8] = z[kind == 8].argmax(-1)
+    w = 0.5 + torch.rand(T, generator=g, device="cuda")
+    w[torch.rand(T, generator=g, device="cuda") < skipped] = 0.0
+    z[w == 0, V // 2] = float("nan")
+    return g, z, kind, y, w
+
+
+# few rows and short ones (blocks and clusters of the rows' kernel), and numbers of rows and words for which rows are streamed: one block a row
+# and clusters of 2 to 8, whole pieces and ragged ones, more than 32 and 64 rows a block
+KINDS = [("f32", 30, 5003), ("bf16", 40, 40000), ("bf16", 300, 2000), ("f32", 1600, 9000), ("bf16", 1600, 17001), ("bf16", 9600, 16411), ("f32", 700, 20480),
+         ("f32", 400, 36001), ("bf16", 250, 140001), ("f32", 90, 150000), ("f32", 60, 270000)]
+
+
+def in_guard(guard, t, dtype, in_place):
+    d = guard.empty(list(t.shape), dtype)
+    if not in_place:
+        return t, d
+    d.copy_(t)
+    return d, d
+
+
+def all_within(got, want, tol, what):
+    """Entries alike, or NaN in both."""
+    off = (got.double() - want).abs() > tol.nan_to_num(nan=0.0) + 1e-37
+    off &= ~(got.isnan() & want.isnan())
+    off |= got.isnan() != want.isnan()
+    off &= ~((got.double() == want) & want.isinf())
+    assert not bool(off.any()), (what, off.nonzero()[:5].tolist())
+
+
+@pytest.mark.parametrize("dtype,T,V", KINDS)
+@pytest.mark.parametrize("skipped", [0.1, 0.95])
+def test_policy_rows_of_every_kind(mtf, dtype, T, V, skipped):
+    """Every fifth row's gradient is 0 by a cut ratio.  Against torch in 64 bits on the GPU."""
+    import torch
+    g, z, kind, y, w = rows_of_every_kind(dtype, T, V, T + V, skipped)
+    z64, d = z.double(), delta(V)
+    lp = torch.log_softmax(z64, -1)
+    logp = lp.gather(-1, y[:, None])[:, 0]
+    ratio = torch.tensor([0.4, 0.7, 0.9, 1.1, 2.5], dtype=torch.float64, device="cuda")[torch.randint(0, 5, (T,), generator=g, device="cuda")]
+    old = torch.where(logp.isnan(), 0.0, logp - ratio.log()).float()
+    adv = torch.randn(T, generator=g, device="cuda")
+    adv[::5], old[::5] = adv[::5].abs(), torch.where(logp.isnan(), 0.0, logp - 1.0)[::5].float()      # ratio e, cut at 1.25
+    guard = Guarded()
+    zin, dz = in_guard(guard, z, dtype, T % 3 == 0)
+    out_logp, loss = guard.empty([1, T], "f32"), guard.empty([1, T], "f32")
+    N, lay = mtf.named, layout(mtf)
+    row, mat = lambda t: N(t.view(1, T), TOK), lambda t: N(t.view(1, T, V), TOK + ["vocab"])
+    mtf.mtf_policy_step(lay, mat(zin), y.int().view(1, T), row(old), None, row(adv), row(w), 0.2, 0.25, 0.0, row(out_logp), row(loss), mat(dz))
+    mtf.mtf_device_status()
+    guard.check()
+    rat = (logp - old.double()).exp()
+    plain, clipped = rat * adv, rat.clamp(0.8, 1.25) * adv
+    cut = plain > clipped
+    live = w != 0
+    slope = w * adv.abs() * rat
+    want_loss = torch.where(live, -w * torch.where(cut, clipped, plain), 0.0)
+    coef = torch.where(cut, 0.0, -w * plain)
+    all_within(out_logp[0], torch.where(live, logp, 0.0), d + U * logp.abs(), "logp")
+    all_within(loss[0], want_loss, slope * d + 2 * U * want_loss.abs(), "loss")
+    p = lp.exp()
+    x = torch.where(z64.isfinite(), z64.amax(-1, keepdim=True) - z64, 0.0)
+    want = -coef[:, None] * p
+    tol = coef.abs()[:, None] * p * (d + (3 * x + 8) * U)
+    want.scatter_add_(-1, y[:, None], coef[:, None])
+    want = torch.where((live & ~cut)[:, None], want, 0.0)
+    # (the label's entry is the difference c - c p: where p is 1 it is 0 with the error of c p, |c| p (d + ...), which a bound on its own size would leave out)
+    all_within(dz, want, torch.where((live & ~cut)[:, None], tol + (d + STEP[dtype] + 4 * U) * want.abs(), 0.0), "dlogits")
+
+
+@pytest.mark.parametrize("dtype,T,V", KINDS)
+@pytest.mark.parametrize("mix,K", [((1.0, 0.5, 0.5), 3), ((2.0, 0.75, 0.25), 40), ((1.5, 0.5, 0.5), 130), ((0.7, 1.0, 0.0), 512)], ids=str)
+def test_distillation_rows_of_every_kind(mtf, dtype, T, V, mix, K):
+    """Lists with empty slots, words more than once, the label among the words, and no word at all.  Against torch in 64 bits on the GPU."""
+    import torch
+    tau, soft, hard = (float(np.float32(v)) for v in mix)            # (as the call takes them)
+    g, z, kind, y, w = rows_of_every_kind(dtype, T, V, T + V + K, 0.15)
+    ids = torch.randint(0, V // 2, (T, K), generator=g, device="cuda")
+    ids[::3, K // 2:] = ids[::3, :K - K // 2]                        # words twice
+    ids[1::4, 0] = y[1::4]
+    ids[torch.rand(T, K, generator=g, device="cuda") < 0.1] = -1
+    ids[5::11] = -1
+    teacher = (2 * torch.randn(T, K, generator=g, device="cuda")).to(t_dtype(dtype))
+    teacher[ids < 0] = float("nan")                                  # (not looked at)
+    z64, d = z.double(), delta(V)
+    p1, p2 = torch.log_softmax(z64, -1), torch.log_softmax(z64 / tau, -1)
+    used = ids >= 0
+    at, some = ids.clamp(min=0), used.any(-1, keepdim=True)
+    q = torch.softmax(torch.where(used, teacher.double() / tau, float("-inf")), -1)
+    q = torch.where(used, q, 0.0)
+    term = torch.where(used & (q > 0), q * (q.log() - p2.gather(-1, at)), 0.0)
+    live = w != 0
+    want_loss = torch.where(live, w * (soft * tau ** 2 * term.sum(-1) - (hard * p1.gather(-1, y[:, None])[:, 0] if hard else 0.0)), 0.0)
+    s = soft * some
+    x = torch.where(z64.isfinite(), z64.amax(-1, keepdim=True) - z64, 0.0)
+    want, tol = s * tau * p2.exp(), s * tau * p2.exp() * (d + (3 * x / tau + 8) * U)
+    if hard:
+        want, tol = want + hard * p1.exp(), tol + hard * p1.exp() * (d + (3 * x + 8) * U)
+    del x, p1, p2
+    want.scatter_add_(-1, at, -s * tau * q)
+    want.scatter_add_(-1, y[:, None], torch.full((T, 1), -hard, dtype=torch.float64, device="cuda"))
+    want, tol = want * w[:, None], tol * w[:, None]
+    want = torch.where(live[:, None], want, 0.0)
+    nothing = ~(some[:, 0] | bool(hard)) | ~live
+    want[nothing], want_loss[nothing] = 0.0, 0.0
+    guard = Guarded()
+    zin, dz = in_guard(guard, z, dtype, T % 3 == 0)
+    loss = guard.empty([1, T], "f32")
+    N, lay = mtf.named, layout(mtf)
+    row, mat = lambda t: N(t.view(1, T), TOK), lambda t: N(t.view(1, T, -1), TOK + ["vocab"])
+    mtf.mtf_distill_step(lay, mat(zin), ids.int().view(1, T, K), N(teacher.view(1, T, K), TOK + ["slot"]), y.int().view(1, T), row(w), tau, soft, hard, row(loss), mat(dz))
+    mtf.mtf_device_status()
+    guard.check()
+    all_within(loss[0], want_loss, w * (soft * tau * tau + hard) * d + 2 * U * want_loss.abs(), "loss")
+    all_within(dz, want, torch.where(live[:, None], tol + (STEP[dtype] + 4 * U) * want.abs(), 0.0), "dlogits")
+
+
+@pytest.mark.parametrize("op", ["policy", "distill"])
+@pytest.mark.parametrize("V", [20001, 150000])
+def test_streamed_rows_repeat_captured_and_side_by_side(mtf, op, V):
+    """Rows of which two launches on two streams share the GPU, a captured launch, and targets out of range among them: the same bits each time."""
+    import torch
+    T = -(-(52 << 20) // (2 * V))
+    g, z, kind, y, w = rows_of_every_kind("bf16", T, V, V, 0.1)
+    w[3], y[3] = 1.0, V                                               # reported, its row 0
+    N, lay = mtf.named, layout(mtf)
+    row, mat = lambda t: N(t.view(1, T), TOK), lambda t: N(t.view(1, T, -1), TOK + ["vocab"])
+    old, adv = torch.full((T,), -9.0, device="cuda"), torch.randn(T, generator=g, device="cuda")
+    ids, teacher = torch.randint(0, V, (1, T, 16), generator=g, device="cuda").int(), torch.randn(1, T, 16, generator=g, device="cuda")
+    y32 = y.int().view(1, T)
+
+    def call():
+        loss, logp, dz = torch.full((T,), 7.0, device="cuda"), torch.full((T,), 7.0, device="cuda"), torch.full_like(z, 7.0)
+
+        def run():
+            if op == "policy":
+                mtf.mtf_policy_step(lay, mat(z), y32, row(old), row(old), row(adv), row(w), 0.2, 0.25, 0.1, row(logp), row(loss), mat(dz))
+            else:
+                mtf.mtf_distill_step(lay, mat(z), ids, N(teacher, TOK + ["slot"]), y32, row(w), 1.5, 0.5, 0.5, row(loss), mat(dz))
+        return run, [loss, logp, dz]
+
+    run, outs = call()
+    run()
+    with pytest.raises(mtf.MtfError, match="MTF_ERR_INVALID_ARG"):
+        mtf.mtf_device_status()
+    want = bits(outs)
+    assert float(outs[0][3]) == 0 and not outs[2][3].any()
+    for t in outs:
+        t.fill_(7.0)
+    gc.collect()                                                      # (an older graph that is collected during a capture ends it)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run()
+    graph.replay()
+    graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(bits(outs), want))
+    both = [call() for _ in range(2)]
+    streams = [torch.cuda.Stream() for _ in both]
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for (r, _), st in zip(both, streams):
+            with torch.cuda.stream(st):
+                r()
+    torch.cuda.synchronize()
+    for _, o in both:
+        assert all(torch.equal(a, b) for a, b in zip(bits(o), want))
+    with pytest.raises(mtf.MtfError):
+        mtf.mtf_device_status()
 
 
 def test_offsets_behind_two_to_the_31(mtf):
