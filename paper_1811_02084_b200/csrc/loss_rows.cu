@@ -139,22 +139,39 @@ __device__ __forceinline__ RowSpan row_span(long long row, int V) {
 }
 __device__ __forceinline__ int edge_element(const RowSpan& s, int i, int V) { return i < s.head ? i : V - s.tail + (i - s.head); }
 
-// 2^(z a0 - b0) and, with two temperatures, 2^(z a1 - b1), a0 being the softened one, of pair e of a piece.  A temperature of 2 (NT = 3) has the second
-// as the square of the first (b1 = 2 b0).  The special-function unit takes an exponential every 8 cycles a scheduler, which alone would bound the
-// walks with two exponentials an entry; the arithmetic pipes take every other softened one of the sums and every fourth of the gradient, where the
-// factors want more of them (with one exponential an entry the walks are as long either way, and nothing is taken over).  Of the sums only softened
-// ones: a NaN may come out as a number there, and the other exponential of its entry shows it.  A gradient's factors are NaN where its row has one.
+// How a row's exponentials are formed; NT of the kernels below.
+//   one       2^(z a0 - b0)
+//   two       and 2^(z a1 - b1): a temperature and none, a0 being the softened one
+//   powers    of one exponential t = 2^(z a0 - b0): t^soft for the temperature hard / soft, and t^hard without one
+// The special-function unit takes an exponential every 8 cycles a scheduler and bounds the walks: a power in place of a second one takes
+// 8192 x 32768 bf16 logits at temperature 1.5 in one call from 321 to 231 us, 2000 x 131072 in a forward call from 105 to 80 (temperatures that are no
+// such quotient take 321 and 105).
+constexpr int kOne = 1, kTwo = 2;
+constexpr int powers(int soft, int hard) { return 16 * soft + hard; }
+__host__ __device__ constexpr bool is_powers(int nt) { return nt >= 16; }
+__host__ __device__ constexpr int soft_power(int nt) { return is_powers(nt) ? nt / 16 : 1; }
+__host__ __device__ constexpr int hard_power(int nt) { return is_powers(nt) ? nt % 16 : 1; }
+
+// The first exponential, and the second if it is one of its own, of pair e of a piece.  Where there are two the arithmetic pipes take over every
+// other softened one of the sums and every fourth of the gradient, whose factors want more of them.  (Of the sums only softened ones: a NaN may
+// come out as a number there, and the other exponential of its entry shows it.  A gradient's factors are NaN where its row has one.)
 template <int NT, bool kGradient>
 __device__ __forceinline__ void exponentials(int e, f32x2 z, float a0, float nb0, float a1, float nb1, f32x2& e0, f32x2& e1) {
   const f32x2 y = fma2(z, pair(a0), pair(nb0));
-  const bool fma = NT == 2 && (kGradient ? (e & 3) == 3 : (e & 1) == 1);
+  const bool fma = NT == kTwo && (kGradient ? (e & 3) == 3 : (e & 1) == 1);
   e0 = fma ? ex2_fma(y) : ex2_unit(y);
-  if (NT == 2) e1 = ex2_unit(fma2(z, pair(a1), pair(nb1)));
-  if (NT == 3) e1 = mul2(e0, e0);
+  if (NT == kTwo) e1 = ex2_unit(fma2(z, pair(a1), pair(nb1)));
+}
+// t^n
+template <int N>
+__device__ __forceinline__ f32x2 power(f32x2 t) {
+  if constexpr (N == 1) return t;
+  else if constexpr (N % 2 == 0) return power<N / 2>(mul2(t, t));
+  else return mul2(t, power<N - 1>(t));
 }
 
 __device__ __forceinline__ float reference(float m, float a) { return __fmul_rn(m, a); }
-// What a row's exponents are formed from: the factors a0 and a1, and the size `huge` from which on logits have no room for the products (they would
+// What a row's exponents are formed from: the factors a0 and a1 (powers: that of the highest power), and the size `huge` from which on logits have no room for the products (they would
 // be rounded by a whole exponent and more).  A row without an entry between -huge and huge, or with one above (a row that is masked as a whole by
 // the type's lowest value, say), is worked out from differences instead.
 struct Factors {
@@ -186,10 +203,11 @@ struct RunningSum {
   __device__ __forceinline__ void raise(float pm, const Factors& F) {
     if (pm > limit) {
       const float b0 = reference(pm, F.a0), b1 = reference(pm, F.a1);
-      p0 = mul2(p0, pair(ex2(-nb0 - b0)));
-      if (NT >= 2) p1 = mul2(p1, pair(ex2(-nb1 - b1)));
+      p0 = mul2(p0, pair(ex2(soft_power(NT) * (-nb0 - b0))));
+      if (NT == kTwo) p1 = mul2(p1, pair(ex2(-nb1 - b1)));
+      if (is_powers(NT)) p1 = mul2(p1, pair(ex2(hard_power(NT) * (-nb0 - b0))));
       m = pm;
-      limit = pm + 40.f / (NT >= 2 ? fmaxf(F.a0, F.a1) : F.a0);
+      limit = pm + 40.f / (NT != kOne ? fmaxf(F.a0, F.a1) : F.a0);
       nb0 = -b0;
       nb1 = -b1;
     }
@@ -204,8 +222,14 @@ struct RunningSum {
       for (int e = 0; e < Piece<T>::kN / 2; ++e) {
         f32x2 e0, e1;
         exponentials<NT, false>(e, f[e], F.a0, nb0, F.a1, nb1, e0, e1);
-        p0 = add2(p0, e0);
-        if (NT >= 2) p1 = add2(p1, e1);
+        if (is_powers(NT)) {
+          const f32x2 soft = power<soft_power(NT)>(e0);
+          p0 = add2(p0, soft);
+          p1 = fma2(soft, power<hard_power(NT) - soft_power(NT)>(e0), p1);
+        } else {
+          p0 = add2(p0, e0);
+          if (NT == kTwo) p1 = add2(p1, e1);
+        }
       }
     }
   }
@@ -216,20 +240,23 @@ struct RunningSum {
   }
   __device__ __forceinline__ void add_one(float f, const Factors& F) {
     raise(f, F);
-    p0 = add2(p0, pair(ex2(fmaf(f, F.a0, nb0)), 0.f));
-    if (NT >= 2) p1 = add2(p1, pair(ex2(fmaf(f, F.a1, nb1)), 0.f));
+    const float y = fmaf(f, F.a0, nb0);
+    p0 = add2(p0, pair(ex2(soft_power(NT) * y), 0.f));
+    if (NT != kOne) p1 = add2(p1, pair(ex2(NT == kTwo ? fmaf(f, F.a1, nb1) : hard_power(NT) * y), 0.f));
   }
   __device__ __forceinline__ void of_warp(float& t_m, float& t_0, float& t_1, const Factors& F) const;
 };
 
-// what a sum relative to m is multiplied by to be relative to mx >= m
-__device__ __forceinline__ float to_reference(float m, float mx, float a, const Factors& F) { return ex2(F.is_huge(mx) ? (m - mx) * a : reference(m, a) - reference(mx, a)); }
+// what a sum (of powers n) relative to m is multiplied by to be relative to mx >= m
+__device__ __forceinline__ float to_reference(float m, float mx, float a, int n, const Factors& F) {
+  return ex2(n * (F.is_huge(mx) ? (m - mx) * a : reference(m, a) - reference(mx, a)));
+}
 // the lanes' references and sums joined, the same in every lane
 template <int NT>
 __device__ __forceinline__ void warp_join(float& m, float& s0, float& s1, const Factors& F) {
   const float mx = warp_max(m);
-  s0 = warp_add(s0 * to_reference(m, mx, F.a0, F));
-  if (NT >= 2) s1 = warp_add(s1 * to_reference(m, mx, F.a1, F));
+  s0 = warp_add(s0 * to_reference(m, mx, F.a0, soft_power(NT), F));
+  if (NT != kOne) s1 = warp_add(s1 * to_reference(m, mx, NT == kTwo ? F.a1 : F.a0, hard_power(NT), F));
   m = mx;
 }
 template <int NT>
@@ -240,7 +267,8 @@ __device__ __forceinline__ void RunningSum<NT>::of_warp(float& t_m, float& t_0, 
   warp_join<NT>(t_m, t_0, t_1, F);
 }
 
-// What a row's gradient is made of: k0 2^(z a0 + nb0) (+ k1 2^(z a1 + nb1)), or with huge logits k0 2^((z - m0) a0) (+ ...).
+// What a row's gradient is made of: k0 2^(z a0 + nb0) (+ k1 2^(z a1 + nb1)), or with huge logits k0 2^((z - m0) a0) (+ ...); k0 t^soft + k1 t^hard
+// with t the first of the two exponentials.
 struct RowGrad {
   float k0, nb0, k1, nb1, m0, m1;
   int zero;                    // the whole row is 0
@@ -411,8 +439,8 @@ __device__ __forceinline__ RowInputs row_inputs(const LossRows& a, long long row
 }
 
 // what log(s) + m / tau is off by as log-sum-exp of z / tau, s being relative to m: the rounding of the reference
-__device__ __forceinline__ double reference_off(float m, float af, const Factors& F) {
-  return F.is_huge(m) ? 0.0 : ((double)reference(m, af) - (double)m * (double)af) * 0.6931471805599453;
+__device__ __forceinline__ double reference_off(float m, float af, int n, const Factors& F) {
+  return F.is_huge(m) ? 0.0 : ((double)reference(m, af) - (double)m * (double)af) * n * 0.6931471805599453;
 }
 
 // First what the gradient's walk waits for: the row's factors, from its reference m and sums.  (POLICY: the ratio is
@@ -431,7 +459,7 @@ __device__ __forceinline__ RowGrad row_gradient(const LossRows& a, long long row
     if (PASS & mtf::LOSS_FORWARD) {
       r.c = 0.0;
       if (OP == mtf::LOSS_POLICY) {
-        const double base = ((double)x.zy - (double)m) - reference_off(m, a0, F), adv = (double)x.adv;
+        const double base = ((double)x.zy - (double)m) - reference_off(m, a0, 1, F), adv = (double)x.adv;
         const double ratio = exp64(base - (double)x.old) / (double)s0;
         r.plain = ratio * adv;
         r.clipped = fmin(fmax(ratio, 1.0 - (double)a.clip_low), 1.0 + (double)a.clip_high) * adv;
@@ -448,17 +476,17 @@ __device__ __forceinline__ RowGrad row_gradient(const LossRows& a, long long row
     const double f = PASS == mtf::LOSS_BACKWARD ? (double)in.scale : w;
     r.cs = x.sum != 0.0 ? f * (double)a.soft * (double)a.temperature : 0.0;
     r.ch = hard_on<OP>(a) ? f * (double)a.hard : 0.0;
-    c0 = NT >= 2 ? r.cs : r.cs + r.ch;
+    c0 = NT != kOne ? r.cs : r.cs + r.ch;
     c1 = r.ch;
   }
   if (PASS == mtf::LOSS_FORWARD) return g;
-  g.zero = c0 == 0.0 && (NT == 1 || c1 == 0.0);
+  g.zero = c0 == 0.0 && (NT == kOne || c1 == 0.0);
   if (PASS == mtf::LOSS_STEP) {
     g.huge = F.is_huge(m);
     g.nb0 = -reference(m, a0);
     g.nb1 = -reference(m, a1);
     g.k0 = (float)c0 / s0;
-    g.k1 = NT >= 2 ? (float)c1 / s1 : 0.f;
+    g.k1 = NT != kOne ? (float)c1 / s1 : 0.f;
     return g;
   }
   // from the stored log-sum-exps: 2^(z a - b) for exp of z / tau - lse, the rest of the exponent goes to the factor
@@ -470,12 +498,12 @@ __device__ __forceinline__ RowGrad row_gradient(const LossRows& a, long long row
   }
   const double l0 = soft_on<OP>(a) ? r.lse0 * (double)a.temperature : OP == mtf::LOSS_DISTILL ? r.lse1 : r.lse0;
   g.m0 = (float)l0;
-  g.m1 = NT == 1 ? g.m0 : (float)r.lse1;
+  g.m1 = NT == kOne ? g.m0 : (float)r.lse1;
   g.huge = F.is_huge(g.m0) || F.is_huge(g.m1);
-  g.nb0 = -reference(g.m0, a0);
-  g.nb1 = NT == 3 ? 2.f * g.nb0 : -reference(g.m1, a1);
-  g.k0 = (float)(g.huge ? c0 : c0 * exp2(-(double)g.nb0 - l0 * (double)a0));
-  g.k1 = (float)(g.huge || NT == 1 ? c1 : c1 * exp2(-(double)g.nb1 - r.lse1 * (double)a1));
+  g.nb0 = -reference(is_powers(NT) ? g.m1 : g.m0, a0);      // (powers: t^hard is the probability, and nothing above it overflows or is lost below)
+  g.nb1 = -reference(g.m1, a1);
+  g.k0 = (float)(g.huge ? c0 : c0 * exp2((-(double)g.nb0 - l0 * (double)a0) * soft_power(NT)));
+  g.k1 = (float)(g.huge || NT == kOne ? c1 : c1 * exp2(NT == kTwo ? -(double)g.nb1 - r.lse1 * (double)a1 : (-(double)g.nb0 - r.lse1 * (double)a0) * hard_power(NT)));
   return g;
 }
 
@@ -487,10 +515,10 @@ __device__ __forceinline__ void row_results(const LossRows& a, long long row, co
   double logp = 0.0;           // of the label
   double above = 0.0;          // log-sum-exp of z / tau less zr / tau
   if (PASS & mtf::LOSS_FORWARD) {
-    const double inv_tau = OP == mtf::LOSS_DISTILL ? a.inv_tau : 1.0, l0 = reference_off(m, F.a0, F) + log64((double)s0);
-    const double l1 = NT == 1 ? l0 : reference_off(m, F.a1, F) + log64((double)s1);
+    const double inv_tau = OP == mtf::LOSS_DISTILL ? a.inv_tau : 1.0, l0 = reference_off(m, F.a0, soft_power(NT), F) + log64((double)s0);
+    const double l1 = NT == kOne ? l0 : reference_off(m, NT == kTwo ? F.a1 : F.a0, hard_power(NT), F) + log64((double)s1);
     r.lse0 = (double)m * inv_tau + l0;
-    r.lse1 = NT == 1 ? r.lse0 : (double)m + l1;      // (one sum: tau is 1, or only one of the two is used)
+    r.lse1 = NT == kOne ? r.lse0 : (double)m + l1;      // (one sum: tau is 1, or only one of the two is used)
     logp = ((double)x.zy - (double)m) - l1;
     above = ((double)m - (double)x.zr) * inv_tau + l0;
   }
@@ -527,8 +555,10 @@ __device__ __forceinline__ void row_results(const LossRows& a, long long row, co
 // one entry of a row's gradient as a walk writes it: for the row's edges, for rows with huge logits and for the entries that differ
 template <int NT>
 __device__ __forceinline__ float gradient_of(float z, const RowGrad& g, const Factors& F) {
-  float v = g.k0 * ex2(g.huge ? (z - g.m0) * F.a0 : fmaf(z, F.a0, g.nb0));
-  if (NT >= 2) v += g.k1 * ex2(g.huge ? (z - g.m1) * F.a1 : fmaf(z, F.a1, g.nb1));
+  const float y = fmaf(z, F.a0, g.nb0);
+  float v = g.k0 * ex2(soft_power(NT) * (g.huge ? (z - g.m0) * F.a0 : y));
+  if (NT == kTwo) v += g.k1 * ex2(g.huge ? (z - g.m1) * F.a1 : fmaf(z, F.a1, g.nb1));
+  if (is_powers(NT)) v += g.k1 * ex2(hard_power(NT) * (g.huge ? (z - g.m1) * F.a0 : y));
   return v;
 }
 
@@ -595,7 +625,8 @@ struct GradValues {
     for (int e = 0; e < Piece<T>::kN / 2; ++e) {
       f32x2 e0, e1;
       exponentials<NT, true>(kPair + e, f[e], F.a0, nb0, F.a1, nb1, e0, e1);
-      f[e] = NT >= 2 ? fma2(e1, pair(k1), mul2(e0, pair(k0))) : mul2(e0, pair(k0));
+      if (is_powers(NT)) f[e] = mul2(power<soft_power(NT)>(e0), fma2(power<hard_power(NT) - soft_power(NT)>(e0), pair(k1), pair(k0)));      // (k0 and k1 have one sign)
+      else f[e] = NT == kTwo ? fma2(e1, pair(k1), mul2(e0, pair(k0))) : mul2(e0, pair(k0));
     }
     return Piece<T>::put(f);
   }
@@ -655,8 +686,8 @@ __device__ __noinline__ void sums_of_differences(const RowPart<T>& part, int lan
   m = warp_max(m);
   s0 = s1 = 0.f;
   each([&](float z) {
-    s0 += ex2((z - m) * F.a0);
-    if (NT >= 2) s1 += ex2((z - m) * F.a1);
+    s0 += ex2(soft_power(NT) * ((z - m) * F.a0));
+    if (NT != kOne) s1 += ex2(hard_power(NT) * ((z - m) * (NT == kTwo ? F.a1 : F.a0)));
   });
   s0 = warp_add(s0);
   s1 = warp_add(s1);
@@ -1258,7 +1289,11 @@ __global__ void __launch_bounds__(kPairThreads) preference_pairs_kernel(const mt
 }
 
 // the first sum is the softened one wherever there is one
-Factors factors(const LossRows& a) { return Factors(kLog2e * (float)a.inv_tau, kLog2e); }
+template <int NT>
+Factors factors(const LossRows& a) {
+  if (is_powers(NT)) return Factors(kLog2e / hard_power(NT), kLog2e);
+  return Factors(kLog2e * (float)a.inv_tau, kLog2e);
+}
 template <typename T>
 int pieces_each(const LossRows& a, int parts) { return (a.V / Piece<T>::kN + parts - 1) / parts; }
 
@@ -1298,7 +1333,7 @@ bool launch_stream(const LossRows& a, size_t list, cudaLaunchConfig_t cfg, cudaL
     at_once = resident_clusters(kernel, cfg, parts, known);
   }
   cfg.gridDim = dim3((unsigned)(std::min(a.rows, at_once) * parts), 1, 1);
-  (void)cudaLaunchKernelEx(&cfg, kernel, a, factors(a), parts, pieces_each<T>(a, parts), chunks, lead, bad);
+  (void)cudaLaunchKernelEx(&cfg, kernel, a, factors<NT>(a), parts, pieces_each<T>(a, parts), chunks, lead, bad);
   return true;
 }
 
@@ -1336,31 +1371,34 @@ void launch(const LossRows& b, int* bad, cudaStream_t st) {
   cfg.blockDim = dim3((unsigned)(threads + (OP == mtf::LOSS_DISTILL ? 32 : 0)), 1, 1);
   cfg.dynamicSmemBytes = sizeof(Scratch) + list;
   cfg.gridDim = dim3((unsigned)(a.rows * parts), 1, 1);
-  (void)cudaLaunchKernelEx(&cfg, loss_rows_kernel<T, OP, PASS, NT>, a, factors(a), parts, pieces_each<T>(a, parts), bad);
+  (void)cudaLaunchKernelEx(&cfg, loss_rows_kernel<T, OP, PASS, NT>, a, factors<NT>(a), parts, pieces_each<T>(a, parts), bad);
 }
 
-template <typename T, int OP, int PASS>
-void launch_sums(int sums, const LossRows& a, int* bad, cudaStream_t st) {
-  if (OP != mtf::LOSS_DISTILL || sums == 1) launch<T, OP, PASS, 1>(a, bad, st);
-  else if (sums == 2) launch<T, OP, PASS, OP == mtf::LOSS_DISTILL ? 2 : 1>(a, bad, st);
-  else launch<T, OP, PASS, OP == mtf::LOSS_DISTILL ? 3 : 1>(a, bad, st);
+template <typename T, int PASS>
+void launch_distill(const LossRows& a, int* bad, cudaStream_t st) {
+  if (a.soft == 0.f || a.hard == 0.f || a.temperature == 1.f) launch<T, mtf::LOSS_DISTILL, PASS, kOne>(a, bad, st);
+  else if (a.temperature == 1.5f) launch<T, mtf::LOSS_DISTILL, PASS, powers(2, 3)>(a, bad, st);
+  else if (a.temperature == 2.f) launch<T, mtf::LOSS_DISTILL, PASS, powers(1, 2)>(a, bad, st);
+  else if (a.temperature == 3.f) launch<T, mtf::LOSS_DISTILL, PASS, powers(1, 3)>(a, bad, st);
+  else if (a.temperature == 4.f) launch<T, mtf::LOSS_DISTILL, PASS, powers(1, 4)>(a, bad, st);
+  else launch<T, mtf::LOSS_DISTILL, PASS, kTwo>(a, bad, st);
 }
 
 template <typename T>
-void dispatch(mtf::LossOp op, mtf::LossPass pass, int sums, const LossRows& a, int* bad, cudaStream_t st) {
+void dispatch(mtf::LossOp op, mtf::LossPass pass, const LossRows& a, int* bad, cudaStream_t st) {
   using namespace mtf;
   if (op == LOSS_DISTILL) {
-    if (pass == LOSS_FORWARD) launch_sums<T, LOSS_DISTILL, LOSS_FORWARD>(sums, a, bad, st);
-    else if (pass == LOSS_BACKWARD) launch_sums<T, LOSS_DISTILL, LOSS_BACKWARD>(sums, a, bad, st);
-    else launch_sums<T, LOSS_DISTILL, LOSS_STEP>(sums, a, bad, st);
+    if (pass == LOSS_FORWARD) launch_distill<T, LOSS_FORWARD>(a, bad, st);
+    else if (pass == LOSS_BACKWARD) launch_distill<T, LOSS_BACKWARD>(a, bad, st);
+    else launch_distill<T, LOSS_STEP>(a, bad, st);
   } else if (pass == LOSS_BACKWARD) {
-    launch<T, LOSS_LOGP, LOSS_BACKWARD, 1>(a, bad, st);
+    launch<T, LOSS_LOGP, LOSS_BACKWARD, kOne>(a, bad, st);
   } else if (op == LOSS_LOGP) {
-    launch<T, LOSS_LOGP, LOSS_FORWARD, 1>(a, bad, st);
+    launch<T, LOSS_LOGP, LOSS_FORWARD, kOne>(a, bad, st);
   } else if (pass == LOSS_FORWARD) {
-    launch<T, LOSS_POLICY, LOSS_FORWARD, 1>(a, bad, st);
+    launch<T, LOSS_POLICY, LOSS_FORWARD, kOne>(a, bad, st);
   } else {
-    launch<T, LOSS_POLICY, LOSS_STEP, 1>(a, bad, st);
+    launch<T, LOSS_POLICY, LOSS_STEP, kOne>(a, bad, st);
   }
 }
 
@@ -1376,9 +1414,8 @@ static mtf_status after(const char* what) {
 }
 
 mtf_status launch_loss_rows(LossOp op, LossPass pass, const LossRows& a, void* stream) {
-  const int sums = op == LOSS_DISTILL && a.soft != 0.f && a.hard != 0.f && a.temperature != 1.f ? (a.temperature == 2.f ? 3 : 2) : 1;
-  if (a.bf16) dispatch<__nv_bfloat16>(op, pass, sums, a, bad_index_flag(), (cudaStream_t)stream);
-  else dispatch<float>(op, pass, sums, a, bad_index_flag(), (cudaStream_t)stream);
+  if (a.bf16) dispatch<__nv_bfloat16>(op, pass, a, bad_index_flag(), (cudaStream_t)stream);
+  else dispatch<float>(op, pass, a, bad_index_flag(), (cudaStream_t)stream);
   return after("loss_rows_kernel");
 }
 

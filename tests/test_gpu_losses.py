@@ -264,6 +264,21 @@ def test_distillation(mtf, V, dtype, mix):
     check_distill(mtf, Case("distill", dtype, V, K=min(6, V), seed=V), *mix, targets="given" if mix[2] else None)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("V", [2, 9, 1003, 40000])
+@pytest.mark.parametrize("mix", [(1.5, 0.25, 0.75), (3.0, 0.5, 0.5), (4.0, 0.75, 0.25), (2.5, 0.5, 0.5), (100.0, 0.5, 0.5)], ids=str)
+def test_distillation_at_other_temperatures(mtf, V, dtype, mix):
+    check_distill(mtf, Case("distill", dtype, V, K=min(6, V), seed=V + 2), *mix)
+
+
+@pytest.mark.parametrize("tau", [1.5, 2.0, 3.0, 4.0, 2.5])
+def test_a_term_of_little_weight_keeps_its_rows(mtf, tau):
+    """Rows whose words lie far apart, and one of the two terms alone but for a weight of 2^-30 of the other."""
+    for soft, hard in ((1.0, 2.0 ** -30), (2.0 ** -30, 1.0)):
+        c = Case("distill", "f32", 5000, K=6, seed=17, masked=False, logits=8.0 * np.random.RandomState(17).randn(15, 5000))
+        check_distill(mtf, c, tau, soft, hard)
+
+
 @pytest.mark.parametrize("K", [1, 2, 31, 32, 33, 100, 256, 257, 512])
 def test_distillation_lists(mtf, K):
     c = Case("distill", "f32", 2000, K=K, seed=K, B=2, L=3)
