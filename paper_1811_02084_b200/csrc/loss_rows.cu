@@ -742,7 +742,8 @@ __global__ void __launch_bounds__((kRowWarps + (OP == mtf::LOSS_DISTILL)) * 32, 
   const long long at = which, row = a.reverse ? a.rows - 1 - at : at;
   constexpr bool kSums = (PASS & mtf::LOSS_FORWARD) != 0;
   const RowPart<T> part(a, row, each, rank);
-  mtf::chain_wait_only();
+  if (OP == mtf::LOSS_LOGP && PASS == mtf::LOSS_FORWARD) mtf::chain_wait();      // (the pairs' kernel reads its inputs meanwhile)
+  else mtf::chain_wait_only();
   const RowIn in = row_in<OP, PASS>(a, row);
   if (in.skip) {               // (every block of the row)
     if (tid == 0 && rank == 0 && in.bad) atomicExch(bad, 1);
@@ -1233,26 +1234,47 @@ constexpr int kPairThreads = 1024;
 // label's logit less the log-probability, is written here.
 template <typename T>
 __global__ void __launch_bounds__(kPairThreads) preference_pairs_kernel(const mtf::PreferencePairs a) {
-  mtf::chain_wait();
   __shared__ double red[kPairThreads / 32];
   const long long b = blockIdx.x;
   // half of the threads to each of the two
   constexpr int half = kPairThreads / 2;
   const int side = threadIdx.x / half;
-  const long long from = (side * a.pairs + b) * a.length;
-  double v = 0.0;
-#pragma unroll 2
-  for (long long t = from + threadIdx.x % half; t < from + a.length; t += half) {
-    const float w = a.weight ? a.weight[t] : 1.f, hi = a.logp[t], lo = a.lse[t];
+  const long long end = (side * a.pairs + b + 1) * a.length, first = end - a.length + threadIdx.x % half;
+  // What the rows' kernel only reads, too, is read while that still runs: the first tokens' weights, targets and labels' logits.  (Blocks of this
+  // kernel start when all of that one's have waited for what came before it.)
+  constexpr int ahead = 2;
+  float w[ahead], z[ahead];
+  auto input = [&](long long t, float& wt, float& zt) {
     const int label = a.targets[t];
-    if (w == 0.f || label < 0 || label >= a.V) continue;                // (both 0)
+    const bool good = label >= 0 && label < a.V;
+    wt = good ? (a.weight ? a.weight[t] : 1.f) : 0.f;
+    zt = good ? Piece<T>::one(a.z, t * a.V + label) : 0.f;
+  };
+#pragma unroll
+  for (int i = 0; i < ahead; ++i) {
+    w[i] = 0.f;
+    if (first + i * half < end) input(first + i * half, w[i], z[i]);
+  }
+  mtf::chain_wait();
+  double v = 0.0;
+  auto add = [&](long long t, float wt, float zt) {
+    const float hi = a.logp[t], lo = a.lse[t];
+    if (wt == 0.f) return;       // (both 0)
     if (isfinite(hi)) {
       const double logp = (double)hi + (double)lo;
-      v += (double)w * logp;
-      a.lse[t] = (float)((double)Piece<T>::one(a.z, t * a.V + label) - logp);
+      v += (double)wt * logp;
+      a.lse[t] = (float)((double)zt - logp);
     } else {
-      v += (double)w * (double)hi;
+      v += (double)wt * (double)hi;
     }
+  };
+#pragma unroll
+  for (int i = 0; i < ahead; ++i)
+    if (first + i * half < end) add(first + i * half, w[i], z[i]);
+  for (long long t = first + ahead * half; t < end; t += half) {
+    float wt, zt;
+    input(t, wt, zt);
+    add(t, wt, zt);
   }
   v = warp_add(v);
   if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = v;
