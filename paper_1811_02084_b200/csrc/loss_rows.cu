@@ -353,6 +353,7 @@ __device__ __forceinline__ void zero_results(const LossRows& a, long long row) {
 
 struct RowInputs {
   float zy, old, ref, adv;
+  float best;                  // the teacher's largest logit
   float zr;                    // the largest of the student's logits to the teacher's words, or 0
   double kl, sum;              // the teacher's sum_k q_k (log q_k - (z_k - zr) / tau), and sum_k q_k: 1, or 0 without a used slot
 };
@@ -375,8 +376,8 @@ __device__ __forceinline__ void fetch_slots(const LossRows& a, long long row, in
   }
 }
 
-// By one warp, before anything of the row is overwritten; all lanes return the same.  The teacher's list (f: its first slots), with its
-// distribution over the used slots, goes to `sl`.
+// By one warp, before anything of the row is overwritten; all lanes return the same.  The teacher's list (f: its first slots) goes to `sl`; its
+// distribution is for teacher() to work out.
 template <typename T, int OP>
 __device__ __forceinline__ RowInputs row_inputs(const LossRows& a, long long row, const char* zr, int label, Fetched& f, const Slots& sl, int lane, int* bad, bool report) {
   RowInputs r = {};
@@ -411,13 +412,20 @@ __device__ __forceinline__ RowInputs row_inputs(const LossRows& a, long long row
   }
   best = warp_max(best);
   top = warp_max(top);
+  r.best = best;
   r.zr = top != -INFINITY ? top : 0.f;
-  const bool any = best != -INFINITY;
+  r.sum = best != -INFINITY ? 1.0 : 0.0;
+  __syncwarp();
+  return r;
+}
+// Its distribution over the used slots, to sl.q.
+__device__ __forceinline__ void teacher(const LossRows& a, RowInputs& r, const Slots& sl, int lane) {
+  const int K = a.slots;
   double sum = 0.0, kl = 0.0;
-  if (any) {
+  if (r.sum != 0.0) {
 #pragma unroll 1
     for (int k = lane; k < K; k += 32) {
-      const double d = (sl.q[k] - (double)best) * a.inv_tau, e = exp64(d);
+      const double d = (sl.q[k] - (double)r.best) * a.inv_tau, e = exp64(d);
       sum += e;
       if (e != 0.0) kl += e * (d - ((double)sl.z[k] - (double)r.zr) * a.inv_tau);      // (a word of probability 0 adds nothing, whatever the student says to it)
       sl.q[k] = e;
@@ -433,9 +441,7 @@ __device__ __forceinline__ RowInputs row_inputs(const LossRows& a, long long row
   } else {
     for (int k = lane; k < K; k += 32) sl.id[k] = -1;
   }
-  r.sum = any ? 1.0 : 0.0;
   __syncwarp();
-  return r;
 }
 
 // what log(s) + m / tau is off by as log-sum-exp of z / tau, s being relative to m: the rounding of the reference
@@ -756,7 +762,14 @@ __global__ void __launch_bounds__((kRowWarps + (OP == mtf::LOSS_DISTILL)) * 32, 
     Fetched f = {};
     if (OP == mtf::LOSS_DISTILL) fetch_slots(a, row, 0, lane, soft_on<OP>(a), f);
     x = row_inputs<T, OP>(a, row, part.zr, in.label, f, sl, lane, bad, rank == 0);
+    if (OP == mtf::LOSS_DISTILL && PASS != mtf::LOSS_BACKWARD) teacher(a, x, sl, lane);
   }
+  // a gradient on its own: the first pieces are on their way while the row's factors are worked out
+  uint4 early[4];
+  if (PASS == mtf::LOSS_BACKWARD && walks)
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (part.begin + tid + i * n < part.end) early[i] = part.z16[part.begin + tid + i * n];
 
   float m = 0.f, s0 = 1.f, s1 = 1.f;
   if (PASS & mtf::LOSS_FORWARD) {
@@ -834,7 +847,14 @@ __global__ void __launch_bounds__((kRowWarps + (OP == mtf::LOSS_DISTILL)) * 32, 
       } else {
         GradValues<T, NT> v;
         v.set(sc.g);
-        walk<4>(part.z16, part.begin, part.end, tid, n, [&](int p, const uint4& u) { part.d16[p] = v.piece(u, F); });
+        int from = part.begin;
+        if (PASS == mtf::LOSS_BACKWARD) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (from + tid + i * n < part.end) part.d16[from + tid + i * n] = v.piece(early[i], F);
+          from += 4 * n;
+        }
+        walk<4>(part.z16, from, part.end, tid, n, [&](int p, const uint4& u) { part.d16[p] = v.piece(u, F); });
       }
       if (tid < part.edges) Piece<T>::set(part.dr, part.edge(tid), gradient_of<NT>(Piece<T>::one(part.zr, part.edge(tid)), sc.g, F));
     }
@@ -842,6 +862,7 @@ __global__ void __launch_bounds__((kRowWarps + (OP == mtf::LOSS_DISTILL)) * 32, 
     float fix = 0.f;
     if (numbers) {
       if (PASS & mtf::LOSS_FORWARD) row_results<OP, PASS, NT>(a, row, in, x, m, s0, s1, rank == 0 && lane == 0, F, r);
+      if (OP == mtf::LOSS_DISTILL && PASS == mtf::LOSS_BACKWARD) teacher(a, x, sl, lane);
       fix = label_value<OP, NT>(sc.g, r, x.zy, F);
       if (OP == mtf::LOSS_DISTILL) alone = !slot_values<NT>(a, sc.g, r, sl, in.label, lane, F) && hard_on<OP>(a);
     }
@@ -995,6 +1016,7 @@ __global__ void __launch_bounds__(kStreamThreads, 1) loss_stream_kernel(const Lo
     auto read = [&] {
       in = in_next;
       x = row_inputs<T, OP>(a, row_of(i), RowPart<T>(a, row_of(i), each, rank).zr, in.label, f, list_of(uses), lane, bad, rank == 0);
+      if (OP == mtf::LOSS_DISTILL) teacher(a, x, list_of(uses), lane);
     };
     bool more = next();
     if (more) { fetch(); read(); }
