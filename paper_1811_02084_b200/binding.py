@@ -647,12 +647,17 @@ def mtf_xent_backward(layout, h: Named, wout: Named, targets, logits: Named, lse
                                   _stream(stream)))
 
 
+_int32 = None                                    # the type's object, once a call has come with it (its name takes longer to ask for)
+
+
 def _ids(t):
     """The pointer of an int32 tensor of ids (None: no tensor)."""
+    global _int32
     if t is None:
         return c_void_p(0)
-    if str(t.dtype) != "torch.int32" or not t.is_contiguous():
+    if (t.dtype is not _int32 and str(t.dtype) != "torch.int32") or not t.is_contiguous():
         raise MtfError(1, "ids and targets must be contiguous int32 tensors")
+    _int32 = t.dtype
     return c_void_p(t.data_ptr())
 
 

@@ -25,6 +25,7 @@ mtf_status read_attention_bwd_status(int* code);
 mtf_status read_attention_rows_status(int* code);
 mtf_status read_f32_status(int* code);
 mtf_status read_loss_status(int* code);
+mtf_status read_loss_bad_id(int* seen);
 bool tap_is_open();
 bool ffn_small_pays(int64_t T, int64_t D, int64_t F, int64_t E, bool backward);
 mtf_status launch_ffn_small_forward(int64_t T, int64_t D, int64_t F, int64_t E, const float* x, const float* w, const float* bias, const float* v, float* h, float* y,
@@ -813,7 +814,9 @@ mtf_status mtf_device_status(int32_t* code) {
   }
   int bad = 0;
   if ((st = mtf::read_bad_index(&bad)) != MTF_OK) return st;
-  if (bad) return fail(MTF_ERR_INVALID_ARG, "a token id or target outside [0, vocab) was seen by the vocab or loss kernels");
+  int bad_too = 0;
+  if ((st = mtf::read_loss_bad_id(&bad_too)) != MTF_OK) return st;
+  if (bad || bad_too) return fail(MTF_ERR_INVALID_ARG, "a token id or target outside [0, vocab) was seen by the vocab or loss kernels");
   return MTF_OK;
 }
 

@@ -17,6 +17,9 @@ namespace {
 using mtf::LossRows;
 using mtf::kMaxTeacher;
 
+__device__ int g_bad_id = 0;         // an id outside [0, V) was seen
+__device__ int g_loss_status = 0;    // a wait was given up
+
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLowest = -3.402823466e38f;
 
@@ -379,7 +382,7 @@ __device__ __forceinline__ void fetch_slots(const LossRows& a, long long row, in
 // By one warp, before anything of the row is overwritten; all lanes return the same.  The teacher's list (f: its first slots) goes to `sl`; its
 // distribution is for teacher() to work out.
 template <typename T, int OP>
-__device__ __forceinline__ RowInputs row_inputs(const LossRows& a, long long row, const char* zr, int label, Fetched& f, const Slots& sl, int lane, int* bad, bool report) {
+__device__ __forceinline__ RowInputs row_inputs(const LossRows& a, long long row, const char* zr, int label, Fetched& f, const Slots& sl, int lane, bool report) {
   RowInputs r = {};
   if (OP != mtf::LOSS_DISTILL || hard_on<OP>(a)) r.zy = Piece<T>::one(zr, label);
   if (OP == mtf::LOSS_POLICY) {
@@ -395,7 +398,7 @@ __device__ __forceinline__ RowInputs row_inputs(const LossRows& a, long long row
     if (first) fetch_slots(a, row, first, lane, soft_on<OP>(a), f);
 #pragma unroll
     for (int i = 0; i < kB; ++i) {
-      if (f.id[i] < -1 || f.id[i] >= a.V) { if (report) atomicExch(bad, 1); f.id[i] = -1; }
+      if (f.id[i] < -1 || f.id[i] >= a.V) { if (report) atomicExch(&g_bad_id, 1); f.id[i] = -1; }
       z[i] = f.id[i] >= 0 ? Piece<T>::one(zr, f.id[i]) : 0.f;
     }
 #pragma unroll
@@ -736,7 +739,7 @@ __device__ __forceinline__ uint32_t in_peer(const void* p, uint32_t rank) {
 // needs nothing of the other parts: what a block reads of them it has no use for (they may be overwritten already).
 // A distillation's teacher is worked out by a warp of its own beside the walk.
 template <typename T, int OP, int PASS, int NT>
-__global__ void __launch_bounds__((kRowWarps + (OP == mtf::LOSS_DISTILL)) * 32, OP == mtf::LOSS_DISTILL ? 3 : PASS == mtf::LOSS_BACKWARD ? 6 : 4) loss_rows_kernel(const LossRows a, const Factors F, const int parts, const int each, int* __restrict__ bad) {
+__global__ void __launch_bounds__((kRowWarps + (OP == mtf::LOSS_DISTILL)) * 32, OP == mtf::LOSS_DISTILL ? 3 : PASS == mtf::LOSS_BACKWARD ? 6 : 4) loss_rows_kernel(const LossRows a, const Factors F, const int parts, const int each) {
   extern __shared__ __align__(128) unsigned char dyn[];
   Scratch& sc = *reinterpret_cast<Scratch*>(dyn);
   const Slots sl(dyn + sizeof(Scratch), a.slots);
@@ -752,7 +755,7 @@ __global__ void __launch_bounds__((kRowWarps + (OP == mtf::LOSS_DISTILL)) * 32, 
   else mtf::chain_wait_only();
   const RowIn in = row_in<OP, PASS>(a, row);
   if (in.skip) {               // (every block of the row)
-    if (tid == 0 && rank == 0 && in.bad) atomicExch(bad, 1);
+    if (tid == 0 && rank == 0 && in.bad) atomicExch(&g_bad_id, 1);
     if ((PASS & mtf::LOSS_FORWARD) && tid == 0 && rank == 0) zero_results<OP>(a, row);
     if (PASS & mtf::LOSS_BACKWARD) part.zeros(tid, blockDim.x);
     return;
@@ -761,7 +764,7 @@ __global__ void __launch_bounds__((kRowWarps + (OP == mtf::LOSS_DISTILL)) * 32, 
   if (numbers) {
     Fetched f = {};
     if (OP == mtf::LOSS_DISTILL) fetch_slots(a, row, 0, lane, soft_on<OP>(a), f);
-    x = row_inputs<T, OP>(a, row, part.zr, in.label, f, sl, lane, bad, rank == 0);
+    x = row_inputs<T, OP>(a, row, part.zr, in.label, f, sl, lane, rank == 0);
     if (OP == mtf::LOSS_DISTILL && PASS != mtf::LOSS_BACKWARD) teacher(a, x, sl, lane);
   }
   // a gradient on its own: the first pieces are on their way while the row's factors are worked out
@@ -886,7 +889,6 @@ __global__ void __launch_bounds__((kRowWarps + (OP == mtf::LOSS_DISTILL)) * 32, 
 constexpr int kWalkers = 16, kNumberWarps = 3, kStreamThreads = 32 * (1 + kNumberWarps + kWalkers);
 constexpr int kChunk = 16384, kChunkPieces = kChunk / 16, kMaxChunks = 13, kMaxParts = 8, kRowSlots = kNumberWarps;
 constexpr long long kWaitCycles = 4000000000LL;
-__device__ int g_loss_status = 0;
 
 struct Stream {
   uint64_t full[kMaxChunks], empty[kMaxChunks];      // a chunk has landed / every walking warp is through with it
@@ -926,7 +928,7 @@ __device__ __forceinline__ void bar_wait(uint64_t* bar, uint32_t parity, int cod
   if (!bar_try(bar, parity)) bar_wait_slow(bar, parity, code, abort);
 }
 template <typename T, int OP, int NT>
-__global__ void __launch_bounds__(kStreamThreads, 1) loss_stream_kernel(const LossRows a, const Factors F, const int parts, const int each, const int chunks, const int lead, int* __restrict__ bad) {
+__global__ void __launch_bounds__(kStreamThreads, 1) loss_stream_kernel(const LossRows a, const Factors F, const int parts, const int each, const int chunks, const int lead) {
   constexpr int PASS = mtf::LOSS_STEP;
   extern __shared__ __align__(128) unsigned char dyn[];
   const size_t list = OP == mtf::LOSS_DISTILL ? Slots::bytes(a.slots) : 0;
@@ -997,7 +999,7 @@ __global__ void __launch_bounds__(kStreamThreads, 1) loss_stream_kernel(const Lo
           if (turn == s) return true;
         } else if (i % kNumberWarps == s && rank == 0 && lane == 0) {
           const long long row = row_of(i);
-          if (row_in<OP, PASS>(a, row).bad) atomicExch(bad, 1);
+          if (row_in<OP, PASS>(a, row).bad) atomicExch(&g_bad_id, 1);
           zero_results<OP>(a, row);
         }
       }
@@ -1015,7 +1017,7 @@ __global__ void __launch_bounds__(kStreamThreads, 1) loss_stream_kernel(const Lo
     };
     auto read = [&] {
       in = in_next;
-      x = row_inputs<T, OP>(a, row_of(i), RowPart<T>(a, row_of(i), each, rank).zr, in.label, f, list_of(uses), lane, bad, rank == 0);
+      x = row_inputs<T, OP>(a, row_of(i), RowPart<T>(a, row_of(i), each, rank).zr, in.label, f, list_of(uses), lane, rank == 0);
       if (OP == mtf::LOSS_DISTILL) teacher(a, x, list_of(uses), lane);
     };
     bool more = next();
@@ -1353,7 +1355,7 @@ int resident_clusters(K kernel, const cudaLaunchConfig_t& cfg, int parts, std::a
 }
 
 template <typename T, int OP, int NT>
-bool launch_stream(const LossRows& a, size_t list, cudaLaunchConfig_t cfg, cudaLaunchAttribute* at, int* bad) {
+bool launch_stream(const LossRows& a, size_t list, cudaLaunchConfig_t cfg, cudaLaunchAttribute* at) {
   const long long pieces = (long long)a.V * (a.bf16 ? 2 : 4) / 16;
   const size_t fixed = sizeof(Stream) + 2 * kNumberWarps * list;
   const int chunks = std::min<int>(kMaxChunks, (int)((227 * 1024 - fixed) / kChunk));
@@ -1377,12 +1379,12 @@ bool launch_stream(const LossRows& a, size_t list, cudaLaunchConfig_t cfg, cudaL
     at_once = resident_clusters(kernel, cfg, parts, known);
   }
   cfg.gridDim = dim3((unsigned)(std::min(a.rows, at_once) * parts), 1, 1);
-  (void)cudaLaunchKernelEx(&cfg, kernel, a, factors<NT>(a), parts, pieces_each<T>(a, parts), chunks, lead, bad);
+  (void)cudaLaunchKernelEx(&cfg, kernel, a, factors<NT>(a), parts, pieces_each<T>(a, parts), chunks, lead);
   return true;
 }
 
 template <typename T, int OP, int PASS, int NT>
-void launch(const LossRows& b, int* bad, cudaStream_t st) {
+void launch(const LossRows& b, cudaStream_t st) {
   LossRows a = b;
   a.inv_tau = a.soft != 0.f ? 1.0 / (double)a.temperature : 1.0;
   // (a gradient that is asked for later begins where the statistics ended: those rows are still in the L2 cache)
@@ -1402,7 +1404,7 @@ void launch(const LossRows& b, int* bad, cudaStream_t st) {
     while (threads < kRowWarps * 32 && threads * 8 < pieces / parts) threads *= 2;
   } else {
     if constexpr (PASS == mtf::LOSS_STEP)
-      if (bytes > 32768 && a.rows * bytes > (48LL << 20) && launch_stream<T, OP, NT>(a, list, cfg, at, bad)) return;
+      if (bytes > 32768 && a.rows * bytes > (48LL << 20) && launch_stream<T, OP, NT>(a, list, cfg, at)) return;
     while (parts < kMaxParts && a.rows * parts * 2 <= sms && bytes / parts > 4096) parts *= 2;
     const int each = PASS == mtf::LOSS_STEP ? 16 : a.bf16 ? 32 : 256;      // pieces a thread, while there are rows enough
     while (threads < kRowWarps * 32 && (threads * each < pieces / parts || a.rows * parts * threads * 2 <= (PASS == mtf::LOSS_STEP ? 1024 : 2048) * sms)) threads *= 2;
@@ -1415,34 +1417,34 @@ void launch(const LossRows& b, int* bad, cudaStream_t st) {
   cfg.blockDim = dim3((unsigned)(threads + (OP == mtf::LOSS_DISTILL ? 32 : 0)), 1, 1);
   cfg.dynamicSmemBytes = sizeof(Scratch) + list;
   cfg.gridDim = dim3((unsigned)(a.rows * parts), 1, 1);
-  (void)cudaLaunchKernelEx(&cfg, loss_rows_kernel<T, OP, PASS, NT>, a, factors<NT>(a), parts, pieces_each<T>(a, parts), bad);
+  (void)cudaLaunchKernelEx(&cfg, loss_rows_kernel<T, OP, PASS, NT>, a, factors<NT>(a), parts, pieces_each<T>(a, parts));
 }
 
 template <typename T, int PASS>
-void launch_distill(const LossRows& a, int* bad, cudaStream_t st) {
-  if (a.soft == 0.f || a.hard == 0.f || a.temperature == 1.f) launch<T, mtf::LOSS_DISTILL, PASS, kOne>(a, bad, st);
-  else if (a.temperature == 1.5f) launch<T, mtf::LOSS_DISTILL, PASS, powers(2, 3)>(a, bad, st);
-  else if (a.temperature == 2.f) launch<T, mtf::LOSS_DISTILL, PASS, powers(1, 2)>(a, bad, st);
-  else if (a.temperature == 3.f) launch<T, mtf::LOSS_DISTILL, PASS, powers(1, 3)>(a, bad, st);
-  else if (a.temperature == 4.f) launch<T, mtf::LOSS_DISTILL, PASS, powers(1, 4)>(a, bad, st);
-  else launch<T, mtf::LOSS_DISTILL, PASS, kTwo>(a, bad, st);
+void launch_distill(const LossRows& a, cudaStream_t st) {
+  if (a.soft == 0.f || a.hard == 0.f || a.temperature == 1.f) launch<T, mtf::LOSS_DISTILL, PASS, kOne>(a, st);
+  else if (a.temperature == 1.5f) launch<T, mtf::LOSS_DISTILL, PASS, powers(2, 3)>(a, st);
+  else if (a.temperature == 2.f) launch<T, mtf::LOSS_DISTILL, PASS, powers(1, 2)>(a, st);
+  else if (a.temperature == 3.f) launch<T, mtf::LOSS_DISTILL, PASS, powers(1, 3)>(a, st);
+  else if (a.temperature == 4.f) launch<T, mtf::LOSS_DISTILL, PASS, powers(1, 4)>(a, st);
+  else launch<T, mtf::LOSS_DISTILL, PASS, kTwo>(a, st);
 }
 
 template <typename T>
-void dispatch(mtf::LossOp op, mtf::LossPass pass, const LossRows& a, int* bad, cudaStream_t st) {
+void dispatch(mtf::LossOp op, mtf::LossPass pass, const LossRows& a, cudaStream_t st) {
   using namespace mtf;
   if (op == LOSS_DISTILL) {
-    if (pass == LOSS_FORWARD) launch_distill<T, LOSS_FORWARD>(a, bad, st);
-    else if (pass == LOSS_BACKWARD) launch_distill<T, LOSS_BACKWARD>(a, bad, st);
-    else launch_distill<T, LOSS_STEP>(a, bad, st);
+    if (pass == LOSS_FORWARD) launch_distill<T, LOSS_FORWARD>(a, st);
+    else if (pass == LOSS_BACKWARD) launch_distill<T, LOSS_BACKWARD>(a, st);
+    else launch_distill<T, LOSS_STEP>(a, st);
   } else if (pass == LOSS_BACKWARD) {
-    launch<T, LOSS_LOGP, LOSS_BACKWARD, kOne>(a, bad, st);
+    launch<T, LOSS_LOGP, LOSS_BACKWARD, kOne>(a, st);
   } else if (op == LOSS_LOGP) {
-    launch<T, LOSS_LOGP, LOSS_FORWARD, kOne>(a, bad, st);
+    launch<T, LOSS_LOGP, LOSS_FORWARD, kOne>(a, st);
   } else if (pass == LOSS_FORWARD) {
-    launch<T, LOSS_POLICY, LOSS_FORWARD, kOne>(a, bad, st);
+    launch<T, LOSS_POLICY, LOSS_FORWARD, kOne>(a, st);
   } else {
-    launch<T, LOSS_POLICY, LOSS_STEP, kOne>(a, bad, st);
+    launch<T, LOSS_POLICY, LOSS_STEP, kOne>(a, st);
   }
 }
 
@@ -1458,8 +1460,8 @@ static mtf_status after(const char* what) {
 }
 
 mtf_status launch_loss_rows(LossOp op, LossPass pass, const LossRows& a, void* stream) {
-  if (a.bf16) dispatch<__nv_bfloat16>(op, pass, a, bad_index_flag(), (cudaStream_t)stream);
-  else dispatch<float>(op, pass, a, bad_index_flag(), (cudaStream_t)stream);
+  if (a.bf16) dispatch<__nv_bfloat16>(op, pass, a, (cudaStream_t)stream);
+  else dispatch<float>(op, pass, a, (cudaStream_t)stream);
   return after("loss_rows_kernel");
 }
 
@@ -1469,6 +1471,14 @@ mtf_status read_loss_status(int* code) {
   if (e != cudaSuccess) return fail(MTF_ERR_CUDA, "cudaMemcpyFromSymbol: %s", cudaGetErrorString(e));
   if (v) { int z = 0; cudaMemcpyToSymbol(g_loss_status, &z, sizeof(int)); }
   *code = v;
+  return MTF_OK;
+}
+mtf_status read_loss_bad_id(int* seen) {
+  int v = 0;
+  cudaError_t e = cudaMemcpyFromSymbol(&v, g_bad_id, sizeof(int));
+  if (e != cudaSuccess) return fail(MTF_ERR_CUDA, "cudaMemcpyFromSymbol: %s", cudaGetErrorString(e));
+  if (v) { int z = 0; cudaMemcpyToSymbol(g_bad_id, &z, sizeof(int)); }
+  *seen = v;
   return MTF_OK;
 }
 

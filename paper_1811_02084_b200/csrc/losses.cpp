@@ -27,6 +27,7 @@ struct Checker {
   std::vector<Range> ranges;
 
   Checker(const char* w, const mtf_layout_t* L) : what(w), layout(L) {
+    ranges.reserve(16);
     if (!L) st = fail(MTF_ERR_INVALID_ARG, "%s: NULL layout", w);
   }
   bool ok() const { return st == MTF_OK; }
@@ -65,14 +66,26 @@ struct Checker {
       if (strcmp(t->dims[i].name, of->dims[first + i].name) || t->dims[i].size != of->dims[first + i].size)
         return wrong(MTF_ERR_SIZE_MISMATCH, "%s: dimension %d is not that of the logits ('%s', %lld)", name, i, of->dims[first + i].name, (long long)of->dims[first + i].size);
   }
+  // Whether it has exactly these dims of a tensor that is legal, and so is legal itself: nearly every tensor of a call that is in order, and
+  // the checks above then have nothing to find.
+  static bool alike(const mtf_tensor* t, const mtf_tensor* of, int first, int n) {
+    if (!t || !t->data || t->ndim != n || !t->dims) return false;
+    for (int i = 0; i < n; ++i) {
+      const mtf_dim &d = t->dims[i], &o = of->dims[first + i];
+      if (d.size != o.size || !d.name || (d.name != o.name && strcmp(d.name, o.name))) return false;
+    }
+    return true;
+  }
   void f32(const mtf_tensor* t, const char* name) {
     if (ok() && t->dtype != MTF_F32) wrong(MTF_ERR_UNSUPPORTED, "%s must be f32", name);
   }
   // f32 tensor of dims [first, first + n) of the logits
   const float* values(const mtf_tensor* t, const mtf_tensor* logits, int first, int n, const char* name, bool out) {
-    if (!there(t, name)) return nullptr;
+    if (!alike(t, logits, first, n)) {
+      if (!there(t, name)) return nullptr;
+      dims_like(t, logits, first, n, 0, name);
+    }
     f32(t, name);
-    dims_like(t, logits, first, n, 0, name);
     memory(t->data, ok() ? numel(*t) * 4 : 0, 4, out, name);
     return reinterpret_cast<const float*>(t->data);
   }
@@ -101,8 +114,10 @@ void take_logits(Checker& c, const mtf_tensor* logits, bool with_gradient, const
   a->rows = rows;
   a->bf16 = logits->dtype == MTF_BF16;
   if (with_gradient) {
-    if (!c.there(dlogits, "dlogits")) return;
-    c.dims_like(dlogits, logits, 0, logits->ndim, 0, "dlogits");
+    if (!Checker::alike(dlogits, logits, 0, logits->ndim)) {
+      if (!c.there(dlogits, "dlogits")) return;
+      c.dims_like(dlogits, logits, 0, logits->ndim, 0, "dlogits");
+    }
     if (dlogits->dtype != logits->dtype) c.wrong(MTF_ERR_INVALID_ARG, "dlogits must have the type of the logits");
     a->d = dlogits->data;
   }

@@ -280,7 +280,6 @@ mtf_status builtin_scratch_ptr(void** out);
 mtf_status launch_slice_gather(const void* src, void* dst, int elem_bytes, int ndim, const int64_t* sizes,
                                const int64_t* offs, const int64_t* gstrides, void* stream);
 void count_launch(int n = 1);
-int* bad_index_flag();      // device flag of ids outside [0, vocab), which mtf_device_status reports (vocab.cu)
 // stage tap (mtf_stage_tap_*): while a tap is open on this thread, `tap` copies the named intermediate
 // into the caller's buffer on the stream, right behind the launch that produced it
 mtf_status tap_begin(void* device_buffer, size_t bytes);

@@ -200,7 +200,7 @@ static mtf_status after(const char* what) {
   return MTF_OK;
 }
 
-int* bad_index_flag() {
+static int* bad_flag() {
   int* p = nullptr;
   cudaGetSymbolAddress(reinterpret_cast<void**>(&p), g_bad_index);
   return p;
@@ -212,7 +212,7 @@ mtf_status launch_embedding_gather(const int32_t* ids, const void* table, void* 
     return fail(MTF_ERR_UNSUPPORTED, "embedding: rows must be multiples of 16 bytes and 16-byte aligned");
   const int pieces = (int)(d * elem_bytes / 16);
   const long long blocks = std::min<long long>((n_tokens * pieces + 255) / 256, (long long)device_sm_count() * 16);
-  launch_chained(embedding_gather_kernel, (unsigned)blocks, 256, 0, (cudaStream_t)stream, ids, reinterpret_cast<const uint4*>(table), reinterpret_cast<uint4*>(x), n_tokens, pieces, (int)vocab, bad_index_flag());
+  launch_chained(embedding_gather_kernel, (unsigned)blocks, 256, 0, (cudaStream_t)stream, ids, reinterpret_cast<const uint4*>(table), reinterpret_cast<uint4*>(x), n_tokens, pieces, (int)vocab, bad_flag());
   return after("embedding_gather_kernel");
 }
 
@@ -234,7 +234,7 @@ mtf_status launch_xent_rows(const void* logits, const int32_t* targets, float* l
   if (n_rows <= 0) return MTF_OK;
   if (vocab % 8 || (reinterpret_cast<uintptr_t>(logits) & 15)) return fail(MTF_ERR_UNSUPPORTED, "cross-entropy: vocab must be a multiple of 8 and the logits 16-byte aligned");
   if (n_rows > 0x7fffffffLL) return fail(MTF_ERR_UNSUPPORTED, "cross-entropy: too many rows");
-  launch_chained(xent_rows_kernel, (unsigned)n_rows, 256, 0, (cudaStream_t)stream, reinterpret_cast<const __nv_bfloat16*>(logits), targets, lse, loss, (int)vocab, bad_index_flag());
+  launch_chained(xent_rows_kernel, (unsigned)n_rows, 256, 0, (cudaStream_t)stream, reinterpret_cast<const __nv_bfloat16*>(logits), targets, lse, loss, (int)vocab, bad_flag());
   return after("xent_rows_kernel");
 }
 
@@ -244,7 +244,7 @@ mtf_status launch_xent_combine(const void* partial, int parts, const void* logit
   if (parts <= 0 || n_rows > 0x7fffffffLL) return fail(MTF_ERR_UNSUPPORTED, "cross-entropy combine: bad sizes");
   launch_chained(xent_combine_kernel, (unsigned)((n_rows + 7) / 8), 256, 0, (cudaStream_t)stream, reinterpret_cast<const float2*>(partial), parts,
                                                                                    reinterpret_cast<const __nv_bfloat16*>(logits), targets, lse, loss, n_rows, (int)vocab,
-                                                                                   bad_index_flag());
+                                                                                   bad_flag());
   return after("xent_combine_kernel");
 }
 
