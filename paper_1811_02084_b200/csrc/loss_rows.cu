@@ -735,6 +735,11 @@ __device__ __forceinline__ uint32_t in_peer(const void* p, uint32_t rank) {
   return at;
 }
 
+// Bound: memory, for all but few rows; then a chain of latencies (the label, the row, its sums, its numbers in 64 bits).  Statistics are one pass with
+// a running reference, loads of four pieces ahead; a gradient reads its row again, from the L2 cache where the statistics have just left it.
+// 8192 x 32768 bf16: statistics 94 us (5.7 TB/s; the special-function unit is busy for 60), a gradient 157 (6.8); 16 rows in one call 6 us.
+// Registers are held to four blocks an SM (teacher's lists: three): with five 777 f32 rows of 50001 take 72 us in place of 66, with three 69.
+//
 // A row may be cut into `parts`, a block each.  Where sums are taken (few rows) the blocks are a cluster and read each other's sums.  A gradient on its own
 // needs nothing of the other parts: what a block reads of them it has no use for (they may be overwritten already).
 // A distillation's teacher is worked out by a warp of its own beside the walk.
@@ -886,6 +891,10 @@ __global__ void __launch_bounds__((kRowWarps + (OP == mtf::LOSS_DISTILL)) * 32, 
 // Sixteen warps walk over the chunks twice, for the statistics and, `lead` chunks later, for the gradient, taking a chunk of each walk in turn:
 // chunks are read, freed and written at one steady rate.  Three more warps work out the rows' numbers, a row each; a row's are wanted `lead`
 // chunks behind its first, that is some chunks behind its last.  Rows are numbered by those that are not skipped (o); row o has slot o mod 3.
+// Bound: memory, and close behind it the special-function unit: two exponentials an entry are 1020 cycles of the 1600 that a chunk takes.  Measured:
+// 8192 x 32768 bf16 184 us (5.85 TB/s, of measured 0.90), with a teacher's 64 words at temperature 1 190, at 2 210 (two powers an entry);
+// 4096 x 32768 f32 168 (6.4); 2048 x 131072 bf16 in pairs of blocks 226, which wait for each other's sums.  Four to six warps for the numbers take
+// issue slots from the walks: 220 in place of 210 with a teacher.
 constexpr int kWalkers = 16, kNumberWarps = 3, kStreamThreads = 32 * (1 + kNumberWarps + kWalkers);
 constexpr int kChunk = 16384, kChunkPieces = kChunk / 16, kMaxChunks = 13, kMaxParts = 8, kRowSlots = kNumberWarps;
 constexpr long long kWaitCycles = 4000000000LL;
@@ -1398,15 +1407,28 @@ void launch(const LossRows& b, cudaStream_t st) {
   const long long bytes = (long long)a.V * (a.bf16 ? 2 : 4), pieces = bytes / 16, sms = mtf::device_sm_count();
   int parts = 1, threads = 32;
   if (PASS == mtf::LOSS_BACKWARD) {
-    // independent blocks of 32 KB (a teacher's list is worked out by every block of its row, so there only with few rows)
+    // Independent blocks of 32 KB (777 f32 rows of 50001, both directions: 66 us, with whole rows 73, blocks of 12 KB 76; 8192 bf16 rows of 32768, half of them
+    // skipped: 121, with whole rows 126).  A teacher's list is worked out by every block of its row, so there only with few rows (822 rows of
+    // 128 KB with 100 slots: 37 us, in two blocks each 46).
     if (OP != mtf::LOSS_DISTILL) parts = (int)std::min<long long>(64, (bytes + 32767) / 32768);
     while (parts < 64 && a.rows * parts * 2 <= 4 * sms && bytes / parts > 2048) parts *= 2;
     while (threads < kRowWarps * 32 && threads * 8 < pieces / parts) threads *= 2;
   } else {
+    // Streamed or a block per row, us in one call: 8192 x 32768 bf16 184 or 217, 4096 x 32768 f32 168 or 248, 2048 x 131072 bf16 226 or 263,
+    // 1024 x 32768 bf16 30 or 33; but 512 x 32768 18 or 16, and 16384 x 16384 227 or 212: little that is read twice comes from memory twice, and
+    // short rows end too often.
     if constexpr (PASS == mtf::LOSS_STEP)
       if (bytes > 32768 && a.rows * bytes > (48LL << 20) && launch_stream<T, OP, NT>(a, list, cfg, at)) return;
-    while (parts < kMaxParts && a.rows * parts * 2 <= sms && bytes / parts > 4096) parts *= 2;
-    const int each = PASS == mtf::LOSS_STEP ? 16 : a.bf16 ? 32 : 256;      // pieces a thread, while there are rows enough
+    // Few rows are cut up, as far as the longer way to a row's sums leaves it worth: bf16 rows in one call, uncut / as here, 16 of 8192 4.7 / 4.7 us,
+    // 16 of 32768 7.4 / 6.0, 16 of 131072 19.8 / 8.2, 40 of 131072 19.9 / 11.5; their statistics alone 4.6 / 4.6 (32768), 8.4 / 5.8 and 8.4 / 7.5.
+    const long long least = PASS == mtf::LOSS_STEP ? 16384 : 32768;
+    if (PASS == mtf::LOSS_STEP || bytes > 131072)
+      while (parts < kMaxParts && bytes / parts > least &&
+             (a.rows * parts * 2 <= (PASS == mtf::LOSS_STEP ? sms : 2 * sms) || (PASS == mtf::LOSS_STEP && bytes / parts > 65536 && a.rows * parts * 2 <= 4 * sms)))
+        parts *= 2;
+    // pieces a thread, while there are rows enough (statistics of 4370 bf16 rows of 32768 among 8192: 62 us with 128 threads, 72 with 256; 528 f32
+    // rows of 50001: 36 with 128, 30 with 256)
+    const int each = PASS == mtf::LOSS_STEP ? 16 : a.bf16 ? 32 : 256;
     while (threads < kRowWarps * 32 && (threads * each < pieces / parts || a.rows * parts * threads * 2 <= (PASS == mtf::LOSS_STEP ? 1024 : 2048) * sms)) threads *= 2;
     if (parts > 1) {
       at[1].id = cudaLaunchAttributeClusterDimension;
