@@ -468,9 +468,13 @@ mtf_status mtf_xent_backward(const mtf_layout_t* layout, const mtf_tensor* h, co
  *   weight   f32 [*tokens], or NULL for ones: a factor of the token's loss.  A row of weight 0 (a prompt, padding) is not
  *            read, nor are its targets and other inputs: all its results are 0.
  *   f32 tensors "per token" have the dims of logits without the last one, in their order.  No output may overlap another
- *   tensor of the call.  Row statistics are f32 sums of f32 exponentials with the maximum subtracted, what a row works out
- *   from them is held in 64 bits, and each result is rounded once.  A logit of -infinity is a word of probability 0; a row
+ *   tensor of the call.  Row statistics are f32 sums of f32 exponentials relative to an entry of the row, what a row works
+ *   out from them is held in 64 bits, and each result is rounded once.  A logit of -infinity is a word of probability 0; a row
  *   with a NaN or +infinity, or with no finite logit, has NaN for its results.  Results repeat bit for bit.
+ *   lse and stats are f32, so a backward call's exponentials are off by 2^-24 of them; from 2^24 on (a row that is masked as a
+ *   whole by the type's lowest value, say) nothing is left of what lies behind the sign of a difference, and such a row's
+ *   probabilities come out as numbers from 0 to 1 and no more than that (weight 0 leaves it out).  A step has the row itself
+ *   and is exact to its tolerance there, too.
  *   Vocab split over processors is free (the logits are stored once); split across RANKS it is refused, MTF_ERR_UNSUPPORTED.
  * The forward calls leave what the backward calls read.  A step is both in one launch that reads the logits once: the gradient
  * is that of the SUM of the losses it returns (weights carry the normalisation).  dloss: NULL, or factors that

@@ -565,9 +565,11 @@ __device__ __forceinline__ void row_results(const LossRows& a, long long row, co
 template <int NT>
 __device__ __forceinline__ float gradient_of(float z, const RowGrad& g, const Factors& F) {
   const float y = fmaf(z, F.a0, g.nb0);
-  float v = g.k0 * ex2(soft_power(NT) * (g.huge ? (z - g.m0) * F.a0 : y));
-  if (NT == kTwo) v += g.k1 * ex2(g.huge ? (z - g.m1) * F.a1 : fmaf(z, F.a1, g.nb1));
-  if (is_powers(NT)) v += g.k1 * ex2(hard_power(NT) * (g.huge ? (z - g.m1) * F.a0 : y));
+  // (a stored log-sum-exp of that size is off by more than whole exponents: no probability above 1 comes of it; NaN stays)
+  auto below = [](float d) { return d > 0.f ? 0.f : d; };
+  float v = g.k0 * ex2(soft_power(NT) * (g.huge ? below((z - g.m0) * F.a0) : y));
+  if (NT == kTwo) v += g.k1 * ex2(g.huge ? below((z - g.m1) * F.a1) : fmaf(z, F.a1, g.nb1));
+  if (is_powers(NT)) v += g.k1 * ex2(hard_power(NT) * (g.huge ? below((z - g.m1) * F.a0) : y));
   return v;
 }
 

@@ -666,6 +666,151 @@ def test_distillation_rows_of_every_kind(mtf, dtype, T, V, mix, K):
     all_within(dz, want, torch.where(live[:, None], tol + (STEP[dtype] + 4 * U) * want.abs(), 0.0), "dlogits")
 
 
+def gradient_of_stored(z64, y, lse, coef, dtype):
+    """(gradient, tolerance) of coef * (onehot(y) - exp(z - lse)) from the f32 lse that a forward call stored"""
+    import torch
+    x = torch.where(z64.isfinite(), (z64.amax(-1, keepdim=True) - z64).abs(), 0.0)
+    part = coef[:, None] * (z64 - lse.double()[:, None]).exp()
+    want = -part
+    want.scatter_add_(-1, y[:, None], coef[:, None])
+    return want, part.abs() * ((3 * x + 8) * U + 2 * U * lse.double().abs()[:, None].clamp(max=1e6)) + (STEP[dtype] + 4 * U) * want.abs()
+
+
+@pytest.mark.parametrize("dtype,T,V", [("f32", 30, 5003), ("bf16", 40, 140001), ("bf16", 300, 2000), ("f32", 700, 20480)])
+def test_policy_directions_on_rows_of_every_kind(mtf, dtype, T, V):
+    import torch
+    g, z, kind, y, w = rows_of_every_kind(dtype, T, V, T + V, 0.2)
+    z64, d = z.double(), delta(V)
+    lse = torch.logsumexp(z64, -1)
+    logp = torch.log_softmax(z64, -1).gather(-1, y[:, None])[:, 0]
+    old = torch.where(logp.isnan(), 0.0, logp - 0.1).float()
+    adv = torch.randn(T, generator=g, device="cuda")
+    live = w != 0
+    bad = logp.isnan() & live
+    assert bool(bad.any()) and bool((~bad & live).any())
+    guard = Guarded()
+    N, lay = mtf.named, layout(mtf)
+    row, mat = lambda t: N(t.view(1, T), TOK), lambda t: N(t.view(1, T, V), TOK + ["vocab"])
+    out = {k: guard.empty([1, T], "f32") for k in ("lse", "logp", "dlogp", "loss")}
+    mtf.mtf_policy_forward(lay, mat(z), y.int().view(1, T), row(old), None, row(adv), row(w), 0.2, 0.25, 0.0, *[row(out[k]) for k in ("lse", "logp", "dlogp", "loss")])
+    zin, dz = in_guard(guard, z, dtype, T % 3 == 0)
+    mtf.mtf_policy_backward(lay, mat(zin), y.int().view(1, T), row(out["lse"]), row(out["dlogp"]), None, mat(dz))
+    mtf.mtf_device_status()
+    guard.check()
+    ratio = (logp - old.double()).exp()
+    slope = w * adv.abs() * ratio
+    for k, want, tol in (("lse", torch.where(bad, float("nan"), lse), d + U * lse.abs()), ("logp", logp, d + U * logp.abs()),
+                         ("dlogp", -w * adv * ratio, slope * d + 2 * U * slope), ("loss", -w * adv * ratio, slope * d + 2 * U * slope)):
+        got = out[k][0]
+        fine = live & ~bad
+        all_within(got, torch.where(live, torch.where(bad & got.isnan(), float("nan"), want), 0.0), torch.where(fine, tol, 0.0), k) if k != "lse" else \
+            all_within(got[fine], want[fine], tol[fine], k)
+    want, tol = gradient_of_stored(z64, y, out["lse"][0], out["dlogp"][0].double(), dtype)
+    off = out["dlogp"][0] == 0
+    want, tol = torch.where(off[:, None], 0.0, want), torch.where(off[:, None], 0.0, tol)
+    want = torch.where(bad[:, None], float("nan"), want)
+    all_within(dz, want, tol, "dlogits")
+
+
+@pytest.mark.parametrize("dtype,T,V", [("f32", 30, 5003), ("bf16", 40, 140001), ("bf16", 300, 2000), ("f32", 700, 20480)])
+@pytest.mark.parametrize("mix", [(1.0, 0.5, 0.5), (2.0, 0.75, 0.25), (1.5, 0.5, 0.5), (4.0, 0.5, 0.5), (0.75, 0.5, 0.5)], ids=str)
+def test_distillation_directions_on_rows_of_every_kind(mtf, dtype, T, V, mix):
+    import torch
+    tau, soft, hard = mix
+    K = 9
+    g, z, kind, y, w = rows_of_every_kind(dtype, T, V, T + V, 0.2)
+    ids = torch.stack([torch.randperm(V // 2, generator=g, device="cuda")[:K] for _ in range(T)])
+    teacher = torch.randn(T, K, generator=g, device="cuda")
+    z64, d = z.double(), delta(V)
+    live = w != 0
+    lses = torch.stack([torch.logsumexp(z64 / tau, -1), torch.logsumexp(z64, -1)], -1)
+    lp, lp2 = torch.log_softmax(z64, -1), torch.log_softmax(z64 / tau, -1)
+    bad = live & lp[:, 0].isnan()
+    q = torch.softmax(teacher.double() / tau, -1)
+    want_loss = w * (soft * tau ** 2 * (q * (q.log() - lp2.gather(-1, ids))).sum(-1) - hard * lp.gather(-1, y[:, None])[:, 0])
+    del lp, lp2
+    guard = Guarded()
+    N, lay = mtf.named, layout(mtf)
+    row, mat = lambda t: N(t.view(1, T), TOK), lambda t: N(t.view(1, T, -1), TOK + ["vocab"])
+    stats, loss = guard.empty([1, T, 2], "f32"), guard.empty([1, T], "f32")
+    args = (ids.int().view(1, T, K), N(teacher.view(1, T, K), TOK + ["slot"]), y.int().view(1, T), row(w), tau, soft, hard)
+    mtf.mtf_distill_forward(lay, mat(z), *args, N(stats, TOK + ["stat"]), row(loss))
+    zin, dz = in_guard(guard, z, dtype, T % 3 == 0)
+    mtf.mtf_distill_backward(lay, mat(zin), *args, N(stats, TOK + ["stat"]), None, mat(dz))
+    mtf.mtf_device_status()
+    guard.check()
+    fine = live & ~bad
+    all_within(loss[0], torch.where(live, want_loss, 0.0), w * (soft * tau * tau + hard) * d + 2 * U * want_loss.abs(), "loss")
+    in_f32 = lses.float().double()                                     # (all lowest, divided by a temperature below 1: infinity)
+    all_within(stats[0][fine], torch.where(in_f32.isinf(), in_f32, lses)[fine], (d + U * lses.abs())[fine], "stats")
+    if tau not in (1.0, 2.0, 4.0):
+        # An f32 log-sum-exp of 1e30 / tau is off by up to half a step, 2^-24 of it, 4e22: no digit is left of an exponential of the difference, and
+        # the formula on the stored number says nothing.  (Powers of two divide without a rounding.)
+        lost = live & ((kind == 3) | (kind == 8))
+        assert bool(dz[lost].isfinite().all()) and bool((dz[lost].double().abs() <= w[lost, None] * (2 * soft * tau + 2 * hard) * (1 + STEP[dtype])).all())
+        live = live & ~lost
+        dz = torch.where(lost[:, None], torch.zeros_like(dz), dz)
+    l0, l1 = stats[0].double().unbind(-1)
+    x = torch.where(z64.isfinite(), z64.amax(-1, keepdim=True) - z64, 0.0)
+    part0, part1 = soft * tau * (z64 / tau - l0[:, None]).exp(), hard * (z64 - l1[:, None]).exp()
+    want = part0 + part1
+    far = torch.minimum(torch.maximum(l0.abs() * tau, l1.abs()), torch.tensor(1e6, dtype=torch.float64, device="cuda"))[:, None]
+    tol = part0 * ((3 * x + 4 * far) / tau * U + 8 * U) + part1 * ((3 * x + 4 * far) * U + 8 * U)
+    want.scatter_add_(-1, ids, -soft * tau * q)
+    want.scatter_add_(-1, y[:, None], torch.full((T, 1), -hard, dtype=torch.float64, device="cuda"))
+    want, tol = w[:, None] * want, w[:, None] * tol
+    want = torch.where(live[:, None], torch.where(bad[:, None], float("nan"), want), 0.0)
+    all_within(dz, want, torch.where(live[:, None], tol + (STEP[dtype] + 4 * U) * want.abs(), 0.0), "dlogits")
+
+
+@pytest.mark.parametrize("dtype,B,L,V", [("f32", 16, 1, 5003), ("bf16", 24, 1, 2000), ("bf16", 8, 3, 140001), ("f32", 2, 1111, 800)])
+def test_preference_on_rows_of_every_kind(mtf, dtype, B, L, V):
+    """A pair with a row that is not finite is NaN, and no other; answers longer than a block has threads."""
+    import torch
+    T = 2 * B * L
+    g, z, kind, y, w = rows_of_every_kind(dtype, T, V, T + V, 0.2)
+    if L > 1000:                                                       # (one pair without rows that are not finite)
+        t = torch.arange(T, device="cuda") % (B * L)
+        w[(t < L) & ((kind == 4) | (kind == 5) | (kind == 6))] = 0.0
+    z64, d = z.double(), delta(V)
+    live = w != 0
+    logp = torch.where(live, torch.log_softmax(z64, -1).gather(-1, y[:, None])[:, 0], 0.0)
+    seq = (w * logp).view(2, B, L).sum(-1)
+    off = (w * (d + U * logp.abs())).view(2, B, L).sum(-1)
+    ref = torch.zeros(2, B, device="cuda")
+    beta = 0.25
+    margin = seq[0] - seq[1]
+    want_loss = torch.nn.functional.softplus(-beta * margin)
+    want_d = -beta * torch.sigmoid(-beta * margin)
+    moff = off[0] + off[1]
+    nan = margin.isnan()
+    assert bool(nan.any()) and bool((~nan).any())
+    guard = Guarded()
+    N, lay, tok = mtf.named, layout(mtf), ["branch", "batch", "length"]
+    row, mat = lambda t: N(t.view(2, B, L), tok), lambda t: N(t.view(2, B, L, V), tok + ["vocab"])
+    lse, got_logp = guard.empty([2, B, L], "f32"), guard.empty([2, B, L], "f32")
+    got_seq, dseq, loss = guard.empty([2, B], "f32"), guard.empty([2, B], "f32"), guard.empty([B], "f32")
+    pair = lambda t: N(t, ["branch", "batch"])
+    y32 = y.int().view(2, B, L)
+    mtf.mtf_preference_forward(lay, mat(z), y32, row(w), pair(ref), "sigmoid", beta, 0.0, row(lse), row(got_logp), pair(got_seq), pair(dseq), N(loss, ["batch"]))
+    zin, dz = in_guard(guard, z, dtype, True)
+    mtf.mtf_preference_backward(lay, mat(zin), y32, row(w), row(lse), pair(dseq), None, mat(dz))
+    mtf.mtf_device_status()
+    guard.check()
+    all_within(got_logp.view(-1), logp, d + U * logp.abs(), "logp")
+    all_within(got_seq, seq, off + U * seq.abs(), "seq_logp")
+    all_within(loss, want_loss, beta * moff + U * want_loss.abs(), "loss")
+    all_within(dseq, torch.stack([want_d, -want_d]), beta * beta / 4 * moff + U * want_d.abs(), "dseq")
+    fine = live & ~logp.isnan()
+    want_lse = torch.logsumexp(z64, -1)
+    all_within(lse.view(-1)[fine], want_lse[fine], (d + U * want_lse.abs())[fine], "lse")
+    coef = (w.view(2, B, L) * dseq[:, :, None]).double().view(-1)
+    want, tol = gradient_of_stored(z64, y, lse.view(-1), coef, dtype)
+    tol = tol + U * (want.abs() + coef.abs()[:, None] * (z64 - lse.view(-1).double()[:, None]).exp())
+    want = torch.where(live[:, None], torch.where((logp.isnan() | nan.repeat(2)[:, None].expand(2 * B, L).reshape(-1))[:, None], float("nan"), want), 0.0)
+    all_within(dz.view(T, V), want, torch.where(live[:, None], tol, 0.0), "dlogits")
+
+
 @pytest.mark.parametrize("op", ["policy", "distill"])
 @pytest.mark.parametrize("V", [20001, 150000])
 def test_streamed_rows_repeat_captured_and_side_by_side(mtf, op, V):
