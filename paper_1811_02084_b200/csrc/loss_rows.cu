@@ -1428,7 +1428,7 @@ void launch(const LossRows& b, cudaStream_t st) {
       while (parts < kMaxParts && bytes / parts > least &&
              (a.rows * parts * 2 <= (PASS == mtf::LOSS_STEP ? sms : 2 * sms) || (PASS == mtf::LOSS_STEP && bytes / parts > 65536 && a.rows * parts * 2 <= 4 * sms)))
         parts *= 2;
-    // pieces a thread, while there are rows enough (statistics of 4370 bf16 rows of 32768 among 8192: 62 us with 128 threads, 72 with 256; 528 f32
+    // pieces a thread, while there are rows enough (statistics of 4389 bf16 rows of 32768 among 8192: 62 us with 128 threads, 72 with 256; 529 f32
     // rows of 50001: 36 with 128, 30 with 256)
     const int each = PASS == mtf::LOSS_STEP ? 16 : a.bf16 ? 32 : 256;
     while (threads < kRowWarps * 32 && (threads * each < pieces / parts || a.rows * parts * threads * 2 <= (PASS == mtf::LOSS_STEP ? 1024 : 2048) * sms)) threads *= 2;
