@@ -573,39 +573,74 @@ __device__ __forceinline__ float gradient_of(float z, const RowGrad& g, const Fa
   return v;
 }
 
-// The entries of a distillation row's gradient that differ from the walk's, by one warp: their values take the place of sl.z, and slots that write
-// none get the id -1 (of slots with one id the first takes care of all).  True: a slot has the label's entry, too.
-template <int NT>
-__device__ __forceinline__ bool slot_values(const LossRows& a, const RowGrad& g, const RowNumbers& r, const Slots& sl, int label, int lane, const Factors& F) {
-  const int K = a.slots;
-  const int4* const ids = reinterpret_cast<const int4*>(sl.id);
-  bool has_label = false;
-  unsigned later = 0u;         // bit k / 32: not the first of its id
+// Slots with one id, by one warp: the first takes the others' share, and they get the id -1.  Up to 32 slots are compared at once.  For more, `seen`: two tables of kSeenBits bits, 0 before and
+// behind (slot_values clears them); an id whose bit comes up twice in the first has it set in the second, and only such ids are searched for.
+// (All pairs compared: 8192 rows of 32768 with 64 words 210 us in place of 196, with 256 592 in place of 334.)
+constexpr int kSeenBits = 8192, kSeenWords = 2 * kSeenBits / 32;
+__device__ __forceinline__ unsigned seen_bit(int id) { return ((unsigned)id ^ (unsigned)id >> 13) % kSeenBits; }
+__device__ __forceinline__ void join_slots(const Slots& sl, int K, unsigned* seen, int lane) {
+  if (K <= 32) {
+    const int id = lane < K ? sl.id[lane] : -1;
+    const unsigned same = __match_any_sync(0xffffffffu, id >= 0 ? id : -1 - lane);
+    const bool first = (same & ((1u << lane) - 1u)) == 0u;
+    __syncwarp();
+    if (lane < K && !first) sl.id[lane] = -1;
+    if (lane < K && first && (same & (same - 1u))) {
+      double q = sl.q[lane];
+      for (unsigned m = same & (same - 1u); m; m &= m - 1) q += sl.q[__ffs(m) - 1];
+      sl.q[lane] = q;
+    }
+    __syncwarp();
+    return;
+  }
+  bool twice = false;
 #pragma unroll 1
-  for (int k = lane, bit = 0; k < K; k += 32, ++bit) {
+  for (int k = lane; k < K; k += 32)
+    if (sl.id[k] >= 0) {
+      const unsigned bit = seen_bit(sl.id[k]), mask = 1u << (bit & 31);
+      if (atomicOr(seen + (bit >> 5), mask) & mask) {
+        atomicOr(seen + kSeenWords / 2 + (bit >> 5), mask);
+        twice = true;
+      }
+    }
+  if (!__any_sync(0xffffffffu, twice)) return;
+  __syncwarp();
+#pragma unroll 1
+  for (int base = 0; base < K; base += 32) {
+    const int k = base + lane, id = k < K ? sl.id[k] : -1;
+    const unsigned bit = seen_bit(id);
+    unsigned todo = __ballot_sync(0xffffffffu, id >= 0 && ((seen[kSeenWords / 2 + (bit >> 5)] >> (bit & 31)) & 1u));
+    for (; todo; todo &= todo - 1) {
+      const int first = base + __ffs(todo) - 1, wanted = sl.id[first];
+      if (wanted < 0) continue;                      // (joined to an earlier one by now)
+      double q = sl.q[first];
+      for (int from = base; from < K; from += 32) {
+        const int j = from + lane;
+        const bool same = j > first && j < K && sl.id[j] == wanted;
+        for (unsigned m = __ballot_sync(0xffffffffu, same); m; m &= m - 1) q += sl.q[from + __ffs(m) - 1];
+        if (same) sl.id[j] = -1;
+      }
+      if (lane == 0) sl.q[first] = q;
+      __syncwarp();
+    }
+  }
+}
+// The entries of a distillation row's gradient that differ from the walk's, by one warp: their values take the place of sl.z.  True: a slot has the
+// label's entry, too.
+template <int NT>
+__device__ __forceinline__ bool slot_values(const LossRows& a, const RowGrad& g, const RowNumbers& r, const Slots& sl, unsigned* seen, int label, int lane, const Factors& F) {
+  const int K = a.slots;
+  join_slots(sl, K, seen, lane);
+  bool has_label = false;
+#pragma unroll 1
+  for (int k = lane; k < K; k += 32) {
     const int id = sl.id[k];
     if (id < 0) continue;
-    int first = K, same = 0;
-#pragma unroll 2
-    for (int j = 0; 4 * j < K; ++j) {
-      const int4 v = ids[j];
-      if (v.w == id) { first = min(first, 4 * j + 3); ++same; }
-      if (v.z == id) { first = min(first, 4 * j + 2); ++same; }
-      if (v.y == id) { first = min(first, 4 * j + 1); ++same; }
-      if (v.x == id) { first = min(first, 4 * j); ++same; }
-    }
-    if (first != k) { later |= 1u << bit; continue; }
-    double q = sl.q[k];
-#pragma unroll 1
-    for (int j = k + 1; same > 1 && j < K; ++j)
-      if (sl.id[j] == id) { q += sl.q[j]; --same; }
+    if (K > 32) seen[seen_bit(id) >> 5] = seen[kSeenWords / 2 + (seen_bit(id) >> 5)] = 0u;
     const bool is_label = r.ch != 0.0 && id == label;
     has_label |= is_label;
-    sl.z[k] = (float)((double)gradient_of<NT>(sl.z[k], g, F) - r.cs * q - (is_label ? r.ch : 0.0));
+    sl.z[k] = (float)((double)gradient_of<NT>(sl.z[k], g, F) - r.cs * sl.q[k] - (is_label ? r.ch : 0.0));
   }
-  __syncwarp();
-  for (int k = lane, bit = 0; k < K; k += 32, ++bit)
-    if ((later >> bit) & 1u) sl.id[k] = -1;
   __syncwarp();
   return __any_sync(0xffffffffu, has_label);
 }
@@ -750,6 +785,7 @@ __global__ void __launch_bounds__((kRowWarps + (OP == mtf::LOSS_DISTILL)) * 32, 
   extern __shared__ __align__(128) unsigned char dyn[];
   Scratch& sc = *reinterpret_cast<Scratch*>(dyn);
   const Slots sl(dyn + sizeof(Scratch), a.slots);
+  unsigned* const seen = reinterpret_cast<unsigned*>(dyn + sizeof(Scratch) + Slots::bytes(a.slots));
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int n = OP == mtf::LOSS_DISTILL ? blockDim.x - 32 : blockDim.x, warps = n >> 5;      // of the walk
   const bool walks = tid < n, numbers = warp == (OP == mtf::LOSS_DISTILL ? warps : 0);
@@ -771,6 +807,8 @@ __global__ void __launch_bounds__((kRowWarps + (OP == mtf::LOSS_DISTILL)) * 32, 
   if (numbers) {
     Fetched f = {};
     if (OP == mtf::LOSS_DISTILL) fetch_slots(a, row, 0, lane, soft_on<OP>(a), f);
+    if (OP == mtf::LOSS_DISTILL && (PASS & mtf::LOSS_BACKWARD) && a.slots > 32)
+      for (int i = lane; i < kSeenWords; i += 32) seen[i] = 0u;
     x = row_inputs<T, OP>(a, row, part.zr, in.label, f, sl, lane, rank == 0);
     if (OP == mtf::LOSS_DISTILL && PASS != mtf::LOSS_BACKWARD) teacher(a, x, sl, lane);
   }
@@ -874,7 +912,7 @@ __global__ void __launch_bounds__((kRowWarps + (OP == mtf::LOSS_DISTILL)) * 32, 
       if (PASS & mtf::LOSS_FORWARD) row_results<OP, PASS, NT>(a, row, in, x, m, s0, s1, rank == 0 && lane == 0, F, r);
       if (OP == mtf::LOSS_DISTILL && PASS == mtf::LOSS_BACKWARD) teacher(a, x, sl, lane);
       fix = label_value<OP, NT>(sc.g, r, x.zy, F);
-      if (OP == mtf::LOSS_DISTILL) alone = !slot_values<NT>(a, sc.g, r, sl, in.label, lane, F) && hard_on<OP>(a);
+      if (OP == mtf::LOSS_DISTILL) alone = !slot_values<NT>(a, sc.g, r, sl, seen, in.label, lane, F) && hard_on<OP>(a);
     }
     __syncthreads();
     if (numbers && !zero) {
@@ -894,9 +932,9 @@ __global__ void __launch_bounds__((kRowWarps + (OP == mtf::LOSS_DISTILL)) * 32, 
 // chunks are read, freed and written at one steady rate.  Three more warps work out the rows' numbers, a row each; a row's are wanted `lead`
 // chunks behind its first, that is some chunks behind its last.  Rows are numbered by those that are not skipped (o); row o has slot o mod 3.
 // Bound: memory, and close behind it the special-function unit: two exponentials an entry are 1020 cycles of the 1600 that a chunk takes.  Measured:
-// 8192 x 32768 bf16 184 us (5.85 TB/s, of measured 0.90), with a teacher's 64 words at temperature 1 190, at 2 210 (two powers an entry);
+// 8192 x 32768 bf16 184 us (5.85 TB/s, of measured 0.90), with a teacher's 64 words at temperature 2 196 of 7592 rows that count (two powers an entry; with 256 words 334, the numbers);
 // 4096 x 32768 f32 168 (6.4); 2048 x 131072 bf16 in pairs of blocks 226, which wait for each other's sums.  Four to six warps for the numbers take
-// issue slots from the walks: 220 in place of 210 with a teacher.
+// issue slots from the walks (212 to 223 in place of 210 with a teacher, when its list was searched for equal words by comparing all pairs).
 constexpr int kWalkers = 16, kNumberWarps = 3, kStreamThreads = 32 * (1 + kNumberWarps + kWalkers);
 constexpr int kChunk = 16384, kChunkPieces = kChunk / 16, kMaxChunks = 13, kMaxParts = 8, kRowSlots = kNumberWarps;
 constexpr long long kWaitCycles = 4000000000LL;
@@ -1020,6 +1058,10 @@ __global__ void __launch_bounds__(kStreamThreads, 1) loss_stream_kernel(const Lo
     RowIn in = {}, in_next = {};
     RowInputs x = {};
     Fetched f = {};
+    unsigned* const seen = reinterpret_cast<unsigned*>(lists + 2 * kNumberWarps * list) + s * kSeenWords;
+    if (OP == mtf::LOSS_DISTILL)
+      for (int k = lane; k < kSeenWords; k += 32) seen[k] = 0u;
+    __syncwarp();
     auto list_of = [&](int use) { return Slots(lists + (2 * s + (use & 1)) * list, a.slots); };
     auto fetch = [&] {
       in_next.w = a.weight ? a.weight[row_of(i)] : 1.f;      // (a row that is not skipped: its label is good)
@@ -1071,7 +1113,7 @@ __global__ void __launch_bounds__(kStreamThreads, 1) loss_stream_kernel(const Lo
       if (rank == 0) row_results<OP, PASS, NT>(a, row, in, x, m, s0, s1, lane == 0, F, r);
       const int label = in.label;
       bool alone = true;
-      if (OP == mtf::LOSS_DISTILL) alone = !slot_values<NT>(a, g, r, sl, label, lane, F) && hard_on<OP>(a);
+      if (OP == mtf::LOSS_DISTILL) alone = !slot_values<NT>(a, g, r, sl, seen, label, lane, F) && hard_on<OP>(a);
       const float fix = label_value<OP, NT>(g, r, x.zy, F);
       const bool zero = g.zero;
       ++uses;
@@ -1368,7 +1410,7 @@ int resident_clusters(K kernel, const cudaLaunchConfig_t& cfg, int parts, std::a
 template <typename T, int OP, int NT>
 bool launch_stream(const LossRows& a, size_t list, cudaLaunchConfig_t cfg, cudaLaunchAttribute* at) {
   const long long pieces = (long long)a.V * (a.bf16 ? 2 : 4) / 16;
-  const size_t fixed = sizeof(Stream) + 2 * kNumberWarps * list;
+  const size_t fixed = sizeof(Stream) + kNumberWarps * (2 * list + (list ? kSeenWords * 4 : 0));
   const int chunks = std::min<int>(kMaxChunks, (int)((227 * 1024 - fixed) / kChunk));
   auto part_chunks = [&](int parts) { return (int)(((pieces + parts - 1) / parts + kChunkPieces - 1) / kChunkPieces); };
   // The ring holds the lead and three chunks on their way; the lead is more than a row's part, and two at most (their slots).
@@ -1439,7 +1481,7 @@ void launch(const LossRows& b, cudaStream_t st) {
     }
   }
   cfg.blockDim = dim3((unsigned)(threads + (OP == mtf::LOSS_DISTILL ? 32 : 0)), 1, 1);
-  cfg.dynamicSmemBytes = sizeof(Scratch) + list;
+  cfg.dynamicSmemBytes = sizeof(Scratch) + list + (list && PASS != mtf::LOSS_FORWARD ? kSeenWords * 4 : 0);
   cfg.gridDim = dim3((unsigned)(a.rows * parts), 1, 1);
   (void)cudaLaunchKernelEx(&cfg, loss_rows_kernel<T, OP, PASS, NT>, a, factors<NT>(a), parts, pieces_each<T>(a, parts));
 }
