@@ -7,6 +7,7 @@ taken from a contiguous torch tensor).  Planning-only calls accept descriptors w
 from __future__ import annotations
 
 import ctypes
+import math
 import os
 from ctypes import POINTER, Structure, byref, c_char_p, c_float, c_int, c_int32, c_int64, c_size_t, c_uint32, c_void_p
 
@@ -650,67 +651,78 @@ def mtf_xent_backward(layout, h: Named, wout: Named, targets, logits: Named, lse
 _int32 = None                                    # the type's object, once a call has come with it (its name takes longer to ask for)
 
 
-def _ids(t):
-    """The pointer of an int32 tensor of ids (None: no tensor)."""
+def _ids(t, of: Named, per_token: bool = True):
+    """The pointer of an int32 tensor of ids (None: no tensor), one per token of the logits `of`, or one per entry of `of`."""
     global _int32
     if t is None:
-        return c_void_p(0)
+        return None
     if (t.dtype is not _int32 and str(t.dtype) != "torch.int32") or not t.is_contiguous():
         raise MtfError(1, "ids and targets must be contiguous int32 tensors")
     _int32 = t.dtype
-    return c_void_p(t.data_ptr())
+    if of is not None:                           # (None: other logits than the call takes, which the library refuses)
+        try:
+            n = of.n_ids
+        except AttributeError:
+            n = of.n_ids = math.prod(s for _, s in (of.dims[:-1] if per_token else of.dims))
+        if t.numel() != n:
+            raise MtfError(STATUS_NAMES.index("MTF_ERR_SIZE_MISMATCH"), f"{t.numel()} ids or targets where the call has {n}")
+    return t.data_ptr()
 
 
 def mtf_distill_forward(layout, logits: Named, teacher_ids, teacher_logits: Named, targets, weight: Named | None, temperature: float, soft_weight: float,
                         hard_weight: float, stats: Named, loss: Named, stream=None) -> None:
     """teacher_ids [*tokens, slots] and targets [*tokens] (None when hard_weight is 0): contiguous int32 device tensors."""
     hp = mtf_distill_params(float(temperature), float(soft_weight), float(hard_weight))
-    _check(_lib.mtf_distill_forward(layout.handle, _p(logits), _ids(teacher_ids), _p(teacher_logits), _ids(targets), _p(weight), byref(hp), _p(stats), _p(loss),
+    _check(_lib.mtf_distill_forward(layout.handle, _p(logits), _ids(teacher_ids, teacher_logits, False), _p(teacher_logits), _ids(targets, logits), _p(weight), byref(hp), _p(stats), _p(loss),
                                     _stream(stream)))
 
 
 def mtf_distill_backward(layout, logits: Named, teacher_ids, teacher_logits: Named, targets, weight: Named | None, temperature: float, soft_weight: float,
                          hard_weight: float, stats: Named, dloss: Named | None, dlogits: Named, stream=None) -> None:
     hp = mtf_distill_params(float(temperature), float(soft_weight), float(hard_weight))
-    _check(_lib.mtf_distill_backward(layout.handle, _p(logits), _ids(teacher_ids), _p(teacher_logits), _ids(targets), _p(weight), byref(hp), _p(stats), _p(dloss),
+    _check(_lib.mtf_distill_backward(layout.handle, _p(logits), _ids(teacher_ids, teacher_logits, False), _p(teacher_logits), _ids(targets, logits), _p(weight), byref(hp), _p(stats), _p(dloss),
                                      _p(dlogits), _stream(stream)))
 
 
 def mtf_distill_step(layout, logits: Named, teacher_ids, teacher_logits: Named, targets, weight: Named | None, temperature: float, soft_weight: float,
                      hard_weight: float, loss: Named, dlogits: Named, stream=None) -> None:
     hp = mtf_distill_params(float(temperature), float(soft_weight), float(hard_weight))
-    _check(_lib.mtf_distill_step(layout.handle, _p(logits), _ids(teacher_ids), _p(teacher_logits), _ids(targets), _p(weight), byref(hp), _p(loss), _p(dlogits),
+    _check(_lib.mtf_distill_step(layout.handle, _p(logits), _ids(teacher_ids, teacher_logits, False), _p(teacher_logits), _ids(targets, logits), _p(weight), byref(hp), _p(loss), _p(dlogits),
                                  _stream(stream)))
 
 
 def mtf_policy_forward(layout, logits: Named, targets, old_logp: Named, ref_logp: Named | None, advantage: Named, weight: Named | None, clip_low: float,
                        clip_high: float, kl_weight: float, lse: Named, logp: Named, dlogp: Named, loss: Named, stream=None) -> None:
     hp = mtf_policy_params(float(clip_low), float(clip_high), float(kl_weight))
-    _check(_lib.mtf_policy_forward(layout.handle, _p(logits), _ids(targets), _p(old_logp), _p(ref_logp), _p(advantage), _p(weight), byref(hp), _p(lse), _p(logp),
+    _check(_lib.mtf_policy_forward(layout.handle, _p(logits), _ids(targets, logits), _p(old_logp), _p(ref_logp), _p(advantage), _p(weight), byref(hp), _p(lse), _p(logp),
                                    _p(dlogp), _p(loss), _stream(stream)))
 
 
 def mtf_policy_backward(layout, logits: Named, targets, lse: Named, dlogp: Named, dloss: Named | None, dlogits: Named, stream=None) -> None:
-    _check(_lib.mtf_policy_backward(layout.handle, _p(logits), _ids(targets), _p(lse), _p(dlogp), _p(dloss), _p(dlogits), _stream(stream)))
+    _check(_lib.mtf_policy_backward(layout.handle, _p(logits), _ids(targets, logits), _p(lse), _p(dlogp), _p(dloss), _p(dlogits), _stream(stream)))
 
 
 def mtf_policy_step(layout, logits: Named, targets, old_logp: Named, ref_logp: Named | None, advantage: Named, weight: Named | None, clip_low: float,
                     clip_high: float, kl_weight: float, logp: Named, loss: Named, dlogits: Named, stream=None) -> None:
     hp = mtf_policy_params(float(clip_low), float(clip_high), float(kl_weight))
-    _check(_lib.mtf_policy_step(layout.handle, _p(logits), _ids(targets), _p(old_logp), _p(ref_logp), _p(advantage), _p(weight), byref(hp), _p(logp), _p(loss),
+    _check(_lib.mtf_policy_step(layout.handle, _p(logits), _ids(targets, logits), _p(old_logp), _p(ref_logp), _p(advantage), _p(weight), byref(hp), _p(logp), _p(loss),
                                 _p(dlogits), _stream(stream)))
+
+
+def _pairs(logits):
+    return logits if logits is not None and len(logits.dims) > 2 and logits.dims[0][1] == 2 else None
 
 
 def mtf_preference_forward(layout, logits: Named, targets, weight: Named | None, ref_logp: Named, kind, beta: float, smoothing: float, lse: Named, logp: Named,
                            seq_logp: Named, dseq: Named, loss: Named, stream=None) -> None:
     """kind: "sigmoid", "hinge", "squared" or the constants of the same names."""
     hp = mtf_preference_params(_PREFERENCE_KINDS[kind] if kind in _PREFERENCE_KINDS else int(kind), float(beta), float(smoothing))
-    _check(_lib.mtf_preference_forward(layout.handle, _p(logits), _ids(targets), _p(weight), _p(ref_logp), byref(hp), _p(lse), _p(logp), _p(seq_logp), _p(dseq),
+    _check(_lib.mtf_preference_forward(layout.handle, _p(logits), _ids(targets, _pairs(logits)), _p(weight), _p(ref_logp), byref(hp), _p(lse), _p(logp), _p(seq_logp), _p(dseq),
                                        _p(loss), _stream(stream)))
 
 
 def mtf_preference_backward(layout, logits: Named, targets, weight: Named | None, lse: Named, dseq: Named, dloss: Named | None, dlogits: Named, stream=None) -> None:
-    _check(_lib.mtf_preference_backward(layout.handle, _p(logits), _ids(targets), _p(weight), _p(lse), _p(dseq), _p(dloss), _p(dlogits), _stream(stream)))
+    _check(_lib.mtf_preference_backward(layout.handle, _p(logits), _ids(targets, _pairs(logits)), _p(weight), _p(lse), _p(dseq), _p(dloss), _p(dlogits), _stream(stream)))
 
 
 def mtf_status_string(status: int) -> str:

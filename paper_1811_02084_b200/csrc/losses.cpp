@@ -19,14 +19,14 @@ int64_t numel(const mtf_tensor& t) {
 }
 
 // What the tensors of one call are checked against, one after the other; `st` keeps the first thing found wrong.
-struct Checker {
+struct Arguments {
   const char* what;
   const mtf_layout_t* layout;
   mtf_status st = MTF_OK;
   struct Range { uintptr_t lo, hi; bool out; };
   std::vector<Range> ranges;
 
-  Checker(const char* w, const mtf_layout_t* L) : what(w), layout(L) {
+  Arguments(const char* w, const mtf_layout_t* L) : what(w), layout(L) {
     ranges.reserve(16);
     if (!L) st = fail(MTF_ERR_INVALID_ARG, "%s: NULL layout", w);
   }
@@ -102,7 +102,7 @@ struct Checker {
 };
 
 // logits, and the gradient where the call has one
-void take_logits(Checker& c, const mtf_tensor* logits, bool with_gradient, const mtf_tensor* dlogits, LossRows* a) {
+void take_logits(Arguments& c, const mtf_tensor* logits, bool with_gradient, const mtf_tensor* dlogits, LossRows* a) {
   if (!c.there(logits, "logits")) return;
   if (logits->ndim < 2) return c.wrong(MTF_ERR_INVALID_ARG, "logits have the dims [*tokens, vocab]");
   if (logits->dtype != MTF_BF16 && logits->dtype != MTF_F32) return c.wrong(MTF_ERR_INVALID_ARG, "unknown type of the logits");
@@ -114,7 +114,7 @@ void take_logits(Checker& c, const mtf_tensor* logits, bool with_gradient, const
   a->rows = rows;
   a->bf16 = logits->dtype == MTF_BF16;
   if (with_gradient) {
-    if (!Checker::alike(dlogits, logits, 0, logits->ndim)) {
+    if (!Arguments::alike(dlogits, logits, 0, logits->ndim)) {
       if (!c.there(dlogits, "dlogits")) return;
       c.dims_like(dlogits, logits, 0, logits->ndim, 0, "dlogits");
     }
@@ -125,11 +125,11 @@ void take_logits(Checker& c, const mtf_tensor* logits, bool with_gradient, const
   if (with_gradient) c.memory(dlogits->data, bytes, 16, true, "dlogits");
 }
 
-void take_weight(Checker& c, const mtf_tensor* logits, const mtf_tensor* weight, LossRows* a) {
+void take_weight(Arguments& c, const mtf_tensor* logits, const mtf_tensor* weight, LossRows* a) {
   if (weight) a->weight = c.per_token(weight, logits, "weight");
 }
 
-void take_distill(Checker& c, const mtf_tensor* logits, const int32_t* teacher_ids, const mtf_tensor* teacher, const int32_t* targets, const mtf_tensor* weight,
+void take_distill(Arguments& c, const mtf_tensor* logits, const int32_t* teacher_ids, const mtf_tensor* teacher, const int32_t* targets, const mtf_tensor* weight,
                   const mtf_distill_params* hp, LossRows* a) {
   if (!c.ok()) return;
   if (!hp) return c.wrong(MTF_ERR_INVALID_ARG, "NULL params");
@@ -157,7 +157,7 @@ void take_distill(Checker& c, const mtf_tensor* logits, const int32_t* teacher_i
   take_weight(c, logits, weight, a);
 }
 
-float* take_stats(Checker& c, const mtf_tensor* logits, const mtf_tensor* stats, bool out) {
+float* take_stats(Arguments& c, const mtf_tensor* logits, const mtf_tensor* stats, bool out) {
   if (!c.there(stats, "stats")) return nullptr;
   c.f32(stats, "stats");
   c.dims_like(stats, logits, 0, logits->ndim - 1, 1, "stats");
@@ -168,7 +168,7 @@ float* take_stats(Checker& c, const mtf_tensor* logits, const mtf_tensor* stats,
   return reinterpret_cast<float*>(stats->data);
 }
 
-void take_policy(Checker& c, const mtf_tensor* logits, const int32_t* targets, const mtf_tensor* old_logp, const mtf_tensor* ref_logp, const mtf_tensor* advantage,
+void take_policy(Arguments& c, const mtf_tensor* logits, const int32_t* targets, const mtf_tensor* old_logp, const mtf_tensor* ref_logp, const mtf_tensor* advantage,
                  const mtf_tensor* weight, const mtf_policy_params* hp, LossRows* a) {
   if (!c.ok()) return;
   if (!hp) return c.wrong(MTF_ERR_INVALID_ARG, "NULL params");
@@ -186,11 +186,11 @@ void take_policy(Checker& c, const mtf_tensor* logits, const int32_t* targets, c
 }
 
 // one value per answer: [2, *pairs]
-float* per_sequence(Checker& c, const mtf_tensor* t, const mtf_tensor* logits, const char* name, bool out) {
+float* per_sequence(Arguments& c, const mtf_tensor* t, const mtf_tensor* logits, const char* name, bool out) {
   return c.ok() ? const_cast<float*>(c.values(t, logits, 0, logits->ndim - 2, name, out)) : nullptr;
 }
 // one value per pair: [*pairs]
-float* per_pair(Checker& c, const mtf_tensor* t, const mtf_tensor* logits, const char* name, bool out) {
+float* per_pair(Arguments& c, const mtf_tensor* t, const mtf_tensor* logits, const char* name, bool out) {
   if (!c.ok()) return nullptr;
   if (logits->ndim > 3) return const_cast<float*>(c.values(t, logits, 1, logits->ndim - 3, name, out));
   if (!c.there(t, name)) return nullptr;      // one pair, without dims of its own
@@ -200,7 +200,7 @@ float* per_pair(Checker& c, const mtf_tensor* t, const mtf_tensor* logits, const
   return reinterpret_cast<float*>(t->data);
 }
 
-void take_pairs(Checker& c, const mtf_tensor* logits, LossRows* a) {
+void take_pairs(Arguments& c, const mtf_tensor* logits, LossRows* a) {
   if (!c.ok()) return;
   if (logits->ndim < 3 || logits->dims[0].size != 2) return c.wrong(MTF_ERR_INVALID_ARG, "logits have the dims [2, *pairs, length, vocab]");
   a->length = logits->dims[logits->ndim - 2].size;
@@ -228,7 +228,7 @@ extern "C" {
 mtf_status mtf_distill_forward(const mtf_layout_t* layout, const mtf_tensor* logits, const int32_t* teacher_ids, const mtf_tensor* teacher_logits,
                                const int32_t* targets, const mtf_tensor* weight, const mtf_distill_params* params, mtf_tensor* stats, mtf_tensor* loss, void* stream) {
   return guarded("distill_forward", [&] {
-    Checker c("distill_forward", layout);
+    Arguments c("distill_forward", layout);
     LossRows a;
     take_logits(c, logits, false, nullptr, &a);
     take_distill(c, logits, teacher_ids, teacher_logits, targets, weight, params, &a);
@@ -242,7 +242,7 @@ mtf_status mtf_distill_backward(const mtf_layout_t* layout, const mtf_tensor* lo
                                 const int32_t* targets, const mtf_tensor* weight, const mtf_distill_params* params, const mtf_tensor* stats,
                                 const mtf_tensor* dloss, mtf_tensor* dlogits, void* stream) {
   return guarded("distill_backward", [&] {
-    Checker c("distill_backward", layout);
+    Arguments c("distill_backward", layout);
     LossRows a;
     take_logits(c, logits, true, dlogits, &a);
     take_distill(c, logits, teacher_ids, teacher_logits, targets, weight, params, &a);
@@ -255,7 +255,7 @@ mtf_status mtf_distill_backward(const mtf_layout_t* layout, const mtf_tensor* lo
 mtf_status mtf_distill_step(const mtf_layout_t* layout, const mtf_tensor* logits, const int32_t* teacher_ids, const mtf_tensor* teacher_logits, const int32_t* targets,
                             const mtf_tensor* weight, const mtf_distill_params* params, mtf_tensor* loss, mtf_tensor* dlogits, void* stream) {
   return guarded("distill_step", [&] {
-    Checker c("distill_step", layout);
+    Arguments c("distill_step", layout);
     LossRows a;
     take_logits(c, logits, true, dlogits, &a);
     take_distill(c, logits, teacher_ids, teacher_logits, targets, weight, params, &a);
@@ -268,7 +268,7 @@ mtf_status mtf_policy_forward(const mtf_layout_t* layout, const mtf_tensor* logi
                               const mtf_tensor* advantage, const mtf_tensor* weight, const mtf_policy_params* params, mtf_tensor* lse, mtf_tensor* logp,
                               mtf_tensor* dlogp, mtf_tensor* loss, void* stream) {
   return guarded("policy_forward", [&] {
-    Checker c("policy_forward", layout);
+    Arguments c("policy_forward", layout);
     LossRows a;
     take_logits(c, logits, false, nullptr, &a);
     take_policy(c, logits, targets, old_logp, ref_logp, advantage, weight, params, &a);
@@ -283,7 +283,7 @@ mtf_status mtf_policy_forward(const mtf_layout_t* layout, const mtf_tensor* logi
 mtf_status mtf_policy_backward(const mtf_layout_t* layout, const mtf_tensor* logits, const int32_t* targets, const mtf_tensor* lse, const mtf_tensor* dlogp,
                                const mtf_tensor* dloss, mtf_tensor* dlogits, void* stream) {
   return guarded("policy_backward", [&] {
-    Checker c("policy_backward", layout);
+    Arguments c("policy_backward", layout);
     LossRows a;
     take_logits(c, logits, true, dlogits, &a);
     if (c.ok()) a.targets = c.ids(targets, a.rows, "targets");
@@ -298,7 +298,7 @@ mtf_status mtf_policy_step(const mtf_layout_t* layout, const mtf_tensor* logits,
                            const mtf_tensor* advantage, const mtf_tensor* weight, const mtf_policy_params* params, mtf_tensor* logp, mtf_tensor* loss,
                            mtf_tensor* dlogits, void* stream) {
   return guarded("policy_step", [&] {
-    Checker c("policy_step", layout);
+    Arguments c("policy_step", layout);
     LossRows a;
     take_logits(c, logits, true, dlogits, &a);
     take_policy(c, logits, targets, old_logp, ref_logp, advantage, weight, params, &a);
@@ -312,7 +312,7 @@ mtf_status mtf_preference_forward(const mtf_layout_t* layout, const mtf_tensor* 
                                   const mtf_preference_params* params, mtf_tensor* lse, mtf_tensor* logp, mtf_tensor* seq_logp, mtf_tensor* dseq, mtf_tensor* loss,
                                   void* stream) {
   return guarded("preference_forward", [&] {
-    Checker c("preference_forward", layout);
+    Arguments c("preference_forward", layout);
     LossRows a;
     mtf::PreferencePairs p;
     take_logits(c, logits, false, nullptr, &a);
@@ -353,7 +353,7 @@ mtf_status mtf_preference_forward(const mtf_layout_t* layout, const mtf_tensor* 
 mtf_status mtf_preference_backward(const mtf_layout_t* layout, const mtf_tensor* logits, const int32_t* targets, const mtf_tensor* weight, const mtf_tensor* lse,
                                    const mtf_tensor* dseq, const mtf_tensor* dloss, mtf_tensor* dlogits, void* stream) {
   return guarded("preference_backward", [&] {
-    Checker c("preference_backward", layout);
+    Arguments c("preference_backward", layout);
     LossRows a;
     take_logits(c, logits, true, dlogits, &a);
     take_pairs(c, logits, &a);

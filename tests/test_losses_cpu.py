@@ -86,6 +86,15 @@ def test_missing_tensors_types_and_sizes(op, call):
 
 
 @pytest.mark.parametrize("op,call", ALL)
+def test_ids_of_another_number_or_type(op, call):
+    for name in ["targets"] + (["ids"] if op == "distill" else []):
+        refused(op, call, lambda n: {name: n[name][:1].contiguous()}, "MTF_ERR_SIZE_MISMATCH")
+        refused(op, call, lambda n: {name: torch.cat([n[name], n[name]])}, "MTF_ERR_SIZE_MISMATCH")
+        refused(op, call, lambda n: {name: n[name].long()})
+        refused(op, call, lambda n: {name: n[name].transpose(0, 1)})
+
+
+@pytest.mark.parametrize("op,call", ALL)
 def test_alignment_and_overlap(op, call):
     for name in READS[op][call]:
         t = tensors(op)[name]
