@@ -241,6 +241,7 @@ class Named:
         self.owner = owner            # keeps the torch tensor alive
         self._dims_arr, self._keep = _dims_array(self.dims)
         self.c = mtf_tensor(c_void_p(data_ptr) if data_ptr else None, self.dtype, len(self.dims), self._dims_arr)
+        self.ref = byref(self.c)
 
     @property
     def names(self):
@@ -261,13 +262,20 @@ def desc(dims, dtype) -> Named:
     return Named(dims, dtype)
 
 
+_torch = None                                    # the module, once a call has asked for its stream
+
+
 def _stream(stream):
+    global _torch
     if stream is not None:
         return c_void_p(int(stream))
     try:
-        import torch
+        if _torch is None:
+            import torch
+            _torch = torch
+        torch = _torch
         if torch.cuda.is_initialized():          # (asking the driver whether there is a device took half of a call's time)
-            return c_void_p(torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice()))
+            return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
         if torch.cuda.is_available():
             return c_void_p(torch.cuda.current_stream().cuda_stream)
     except Exception:
@@ -477,7 +485,7 @@ def mtf_plan_force(kernel_kind: int = -1, reduce_mode: int = -1) -> None:
 
 
 def _p(t: Named | None):
-    return byref(t.c) if t is not None else None
+    return t.ref if t is not None else None
 
 
 def mtf_ffn_forward(layout, x, w, bias, v, h_saved, y, workspace=None, stream=None) -> None:
