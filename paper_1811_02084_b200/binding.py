@@ -668,10 +668,14 @@ def _ids(t, of: Named, per_token: bool = True):
         raise MtfError(1, "ids and targets must be contiguous int32 tensors")
     _int32 = t.dtype
     if of is not None:                           # (None: other logits than the call takes, which the library refuses)
+        # (a descriptor may be the logits of one call and the teacher's of another: a number for each)
         try:
-            n = of.n_ids
+            n = of.n_tokens if per_token else of.n_entries
         except AttributeError:
-            n = of.n_ids = math.prod(s for _, s in (of.dims[:-1] if per_token else of.dims))
+            if per_token:
+                n = of.n_tokens = math.prod(s for _, s in of.dims[:-1])
+            else:
+                n = of.n_entries = math.prod(s for _, s in of.dims)
         if t.numel() != n:
             raise MtfError(STATUS_NAMES.index("MTF_ERR_SIZE_MISMATCH"), f"{t.numel()} ids or targets where the call has {n}")
     return t.data_ptr()
