@@ -938,6 +938,7 @@ __global__ void __launch_bounds__((kRowWarps + (OP == mtf::LOSS_DISTILL)) * 32, 
 constexpr int kWalkers = 16, kNumberWarps = 3, kStreamThreads = 32 * (1 + kNumberWarps + kWalkers);
 constexpr int kChunk = 16384, kChunkPieces = kChunk / 16, kMaxChunks = 13, kMaxParts = 8, kRowSlots = kNumberWarps;
 constexpr long long kWaitCycles = 4000000000LL;
+constexpr int kBlockSharedMemory = 227 * 1024;       // what a block may have
 
 struct Stream {
   uint64_t full[kMaxChunks], empty[kMaxChunks];      // a chunk has landed / every walking warp is through with it
@@ -1411,7 +1412,7 @@ template <typename T, int OP, int NT>
 bool launch_stream(const LossRows& a, size_t list, cudaLaunchConfig_t cfg, cudaLaunchAttribute* at) {
   const long long pieces = (long long)a.V * (a.bf16 ? 2 : 4) / 16;
   const size_t fixed = sizeof(Stream) + kNumberWarps * (2 * list + (list ? kSeenWords * 4 : 0));
-  const int chunks = std::min<int>(kMaxChunks, (int)((227 * 1024 - fixed) / kChunk));
+  const int chunks = std::min<int>(kMaxChunks, (int)((kBlockSharedMemory - fixed) / kChunk));
   auto part_chunks = [&](int parts) { return (int)(((pieces + parts - 1) / parts + kChunkPieces - 1) / kChunkPieces); };
   // The ring holds the lead and three chunks on their way; the lead is more than a row's part, and two at most (their slots).
   int parts = 1;
@@ -1420,7 +1421,8 @@ bool launch_stream(const LossRows& a, size_t list, cudaLaunchConfig_t cfg, cudaL
   if (lead < part_chunks(parts) + 1) return false;
   auto kernel = loss_stream_kernel<T, OP, NT>;
   cfg.dynamicSmemBytes = fixed + (size_t)chunks * kChunk;
-  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)cfg.dynamicSmemBytes) != cudaSuccess) return true;
+  // (the limit is one number for all host threads: always the same, or a call with a shorter list could lower it between another's setting and launch)
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kBlockSharedMemory) != cudaSuccess) return true;
   cfg.blockDim = dim3(kStreamThreads, 1, 1);
   long long at_once = mtf::device_sm_count();
   if (parts > 1) {
