@@ -528,6 +528,7 @@ __device__ __forceinline__ void row_results(const LossRows& a, long long row, co
     const double l1 = NT == kOne ? l0 : reference_off(m, NT == kTwo ? F.a1 : F.a0, hard_power(NT), F) + log64((double)s1);
     r.lse0 = (double)m * inv_tau + l0;
     r.lse1 = NT == kOne ? r.lse0 : (double)m + l1;      // (one sum: tau is 1, or only one of the two is used)
+    if (NT == kTwo && isnan(s1)) r.lse0 = r.lse1;       // (of two sums the softened one may have lost a NaN: see exponentials)
     logp = ((double)x.zy - (double)m) - l1;
     above = ((double)m - (double)x.zr) * inv_tau + l0;
   }

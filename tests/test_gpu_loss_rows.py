@@ -2,9 +2,11 @@
 import ctypes
 import threading
 
+import numpy as np
 import pytest
 
-from test_gpu_losses import TOK, bits, layout, mtf  # noqa: F401
+from helpers import Guarded
+from test_gpu_losses import TOK, bits, layout, mtf, t_dtype  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -60,3 +62,39 @@ def test_streamed_distillation_in_threads_with_lists_of_different_sizes(mtf):  #
     mtf.mtf_device_status()
     for (_, outs, _), w in zip(work, want):
         assert all(torch.equal(a, b) for a, b in zip(bits(outs), w))
+
+
+# ---- rows that are not finite -------------------------------------------------------------------------------------------------------------------
+
+def distill_forward(m, z, tau, soft=0.5, hard=0.5):
+    """(stats, loss, gradient of the step) of rows z with a list of three words and the label 0"""
+    import torch
+    T, V = z.shape
+    N, lay = m.named, layout(m)
+    ids = (torch.arange(3, device="cuda") % V).expand(1, T, 3).contiguous().int()
+    teacher, y = torch.zeros(1, T, 3, device="cuda"), torch.zeros(1, T, dtype=torch.int32, device="cuda")
+    guard = Guarded()
+    stats, loss, step_loss, dz = guard.empty([1, T, 2], "f32"), guard.empty([1, T], "f32"), guard.empty([1, T], "f32"), guard.empty([1, T, V], "bf16" if z.dtype == torch.bfloat16 else "f32")
+    args = (N(z.view(1, T, V), TOK + ["vocab"]), ids, N(teacher, TOK + ["slot"]), y, None, tau, soft, hard)
+    m.mtf_distill_forward(lay, *args, N(stats, TOK + ["stat"]), N(loss, TOK))
+    m.mtf_distill_step(lay, *args, N(step_loss, TOK), N(dz, TOK + ["vocab"]))
+    m.mtf_device_status()
+    guard.check()
+    return stats[0], loss[0], step_loss[0], dz[0]
+
+
+# (a row to a block, few long rows in clusters, and rows beside which a step streams)
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("V", [40, 4099, 150001])
+@pytest.mark.parametrize("tau", [1.0, 1.5, 2.0, 2.5, 0.7])
+def test_a_nan_anywhere_in_a_row_shows_in_all_its_results(mtf, V, dtype, tau):  # noqa: F811
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(V)
+    near = min(V, 40)
+    at = sorted({*range(near), *range(V - near, V), *np.random.RandomState(V).randint(0, V, 24).tolist()})
+    z = (2 * torch.randn(len(at) + 1, V, generator=g, device="cuda")).to(t_dtype(dtype))
+    z[torch.arange(len(at), device="cuda"), torch.tensor(at, device="cuda")] = float("nan")
+    stats, loss, step_loss, dz = distill_forward(mtf, z, tau)
+    assert bool(stats[:-1].isnan().all()), ("stats", [at[i] for i in (~stats[:-1].isnan()).any(-1).nonzero()[:8, 0].tolist()])
+    assert bool(loss[:-1].isnan().all()) and bool(step_loss[:-1].isnan().all()) and bool(dz[:-1].isnan().all())
+    assert bool(stats[-1].isfinite().all()) and bool(loss[-1].isfinite()) and bool(step_loss[-1].isfinite()) and bool(dz[-1].isfinite().all())
