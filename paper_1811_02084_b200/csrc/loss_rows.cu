@@ -529,6 +529,7 @@ __device__ __forceinline__ void row_results(const LossRows& a, long long row, co
     r.lse0 = (double)m * inv_tau + l0;
     r.lse1 = NT == kOne ? r.lse0 : (double)m + l1;      // (one sum: tau is 1, or only one of the two is used)
     if (NT == kTwo && isnan(s1)) r.lse0 = r.lse1;       // (of two sums the softened one may have lost a NaN: see exponentials)
+    if (s0 == 0.f) r.lse0 = r.lse1 = nan("");           // (no finite logit: the reference's own exponential is 1 in any other row's sums)
     logp = ((double)x.zy - (double)m) - l1;
     above = ((double)m - (double)x.zr) * inv_tau + l0;
   }

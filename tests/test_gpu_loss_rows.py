@@ -6,7 +6,7 @@ import numpy as np
 import pytest
 
 from helpers import Guarded
-from test_gpu_losses import TOK, bits, layout, mtf, t_dtype  # noqa: F401
+from test_gpu_losses import TOK, U, bits, layout, mtf, t_dtype  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -98,3 +98,38 @@ def test_a_nan_anywhere_in_a_row_shows_in_all_its_results(mtf, V, dtype, tau):  
     assert bool(stats[:-1].isnan().all()), ("stats", [at[i] for i in (~stats[:-1].isnan()).any(-1).nonzero()[:8, 0].tolist()])
     assert bool(loss[:-1].isnan().all()) and bool(step_loss[:-1].isnan().all()) and bool(dz[:-1].isnan().all())
     assert bool(stats[-1].isfinite().all()) and bool(loss[-1].isfinite()) and bool(step_loss[-1].isfinite()) and bool(dz[-1].isfinite().all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("V", [3, 40, 4099, 150001])
+def test_rows_without_a_finite_logit_have_nan_statistics(mtf, V, dtype):  # noqa: F811
+    import torch
+    T, inf = 4, float("inf")
+    z = torch.zeros(T, V, device="cuda").to(t_dtype(dtype))
+    z[0] = -inf                                                       # row 1 has one word left, row 2 a word of infinite weight, row 3 is ordinary
+    z[1], z[2, V - 1] = -inf, inf
+    z[1, V // 2] = -3.0
+    for tau in (1.0, 1.5, 2.0, 2.5, 0.7):
+        stats, loss, step_loss, _ = distill_forward(mtf, z, tau)
+        assert bool(stats[[0, 2]].isnan().all()) and bool(loss[[0, 2]].isnan().all()) and bool(step_loss[[0, 2]].isnan().all())
+        assert bool(stats[[1, 3]].isfinite().all())
+        # (the one exponential, of an argument of 0 or its rounding, is 1 but for 2^-22, and so are its powers up to the third but for three times that and their roundings)
+        t = float(np.float32(tau))
+        assert abs(float(stats[1, 0]) + 3.0 / t) <= (16 + 3.0 / t) * U and abs(float(stats[1, 1]) + 3.0) <= (16 + 3) * U
+    N, lay = mtf.named, layout(mtf)
+    guard = Guarded()
+    y = torch.full((1, T), V // 2, dtype=torch.int32, device="cuda")
+    zero, tok2 = torch.zeros(1, T, device="cuda"), ["branch", "batch", "length"]
+    room = [guard.empty([1, T], "f32") for _ in range(4)]
+    mtf.mtf_policy_forward(lay, N(z.view(1, T, V), TOK + ["vocab"]), y, N(zero, TOK), None, N(zero, TOK), None, 0.2, 0.2, 0.0, *[N(t, TOK) for t in room])
+    lse, logp = room[0][0], room[1][0]
+    assert bool(lse[[0, 2]].isnan().all()) and bool(logp[[0, 2]].isnan().all())
+    assert abs(float(lse[1]) + 3.0) <= (16 + 3) * U and abs(float(logp[1])) <= 16 * U and bool(lse[3].isfinite())
+    lse, logp, seq, dseq, loss = (guard.empty(s, "f32") for s in ([2, 2, 1], [2, 2, 1], [2, 2], [2, 2], [2]))
+    ref = torch.zeros(2, 2, device="cuda")
+    mtf.mtf_preference_forward(lay, N(z.view(2, 2, 1, V), tok2 + ["vocab"]), y.view(2, 2, 1), None, N(ref, tok2[:2]), "sigmoid", 0.1, 0.0, N(lse, tok2), N(logp, tok2), N(seq, tok2[:2]),
+                               N(dseq, tok2[:2]), N(loss, ["batch"]))
+    mtf.mtf_device_status()
+    guard.check()
+    lse = lse.view(-1)
+    assert bool(lse[[0, 2]].isnan().all()) and abs(float(lse[1]) + 3.0) <= (16 + 3) * U and bool(lse[3].isfinite())
