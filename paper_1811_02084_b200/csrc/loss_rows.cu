@@ -965,6 +965,8 @@ __device__ __forceinline__ bool bar_try(uint64_t* bar, uint32_t parity) {
   return ok != 0;
 }
 // Gives up after about two seconds: a code for mtf_device_status, and from then on no wait of the block waits (its rows' results are unspecified).
+// Warps that then go on only arrive at barriers whose phases end with the last of so many arrivals.  What counts bytes, or is another block's, needs the waits in
+// front of it: the copying warp and the numbers' warps leave (given_up behind each of their waits), and the other blocks' waits for this one run out in turn.
 __device__ __noinline__ void bar_wait_slow(uint64_t* bar, uint32_t parity, int code, volatile int* abort) {
   const long long t0 = clock64();
   while (!bar_try(bar, parity)) {
@@ -979,6 +981,9 @@ __device__ __noinline__ void bar_wait_slow(uint64_t* bar, uint32_t parity, int c
 __device__ __forceinline__ void bar_wait(uint64_t* bar, uint32_t parity, int code, int* abort) {
   if (!bar_try(bar, parity)) bar_wait_slow(bar, parity, code, abort);
 }
+// Whether a wait of the block has been given up, as any lane of the warp sees it (a lane that gave up itself does).
+__device__ __forceinline__ bool given_up(const Stream& st) { return __any_sync(0xffffffffu, *(const volatile int*)&st.abort); }
+constexpr long long kLandCycles = 200000000LL;       // 0.1 s, for copies in flight
 template <typename T, int OP, int NT>
 __global__ void __launch_bounds__(kStreamThreads, 1) loss_stream_kernel(const LossRows a, const Factors F, const int parts, const int each, const int chunks, const int lead) {
   constexpr int PASS = mtf::LOSS_STEP;
@@ -1037,7 +1042,16 @@ __global__ void __launch_bounds__(kStreamThreads, 1) loss_stream_kernel(const Lo
         }
       }
       __syncwarp();
+      if (given_up(st)) break;
     }
+    // The block does not end in front of its copies, which nobody else waits for once a wait was given up.  (Slots from `slot` on were last filled a turn of the ring
+    // before the others, or not yet: then the wait is for the phase before a barrier's first, which is over.)
+    if (lane == 0) {
+      const long long t0 = clock64();
+      for (int c = 0; c < chunks; ++c)
+        while (!bar_try(&st.full[c], c < slot ? phase ^ 1u : phase) && clock64() - t0 < kLandCycles) {}
+    }
+    __syncwarp();
   } else if (warp <= kNumberWarps) {
     // ------------------------------- the rows' numbers -------------------------------
     const int s = warp - 1;
@@ -1087,18 +1101,21 @@ __global__ void __launch_bounds__(kStreamThreads, 1) loss_stream_kernel(const Lo
       phase ^= 1u;
       float m = -F.huge, s0 = 0.f, s1 = 0.f;
       bar_wait(&st.sums[s], phase, 0xA02, &st.abort);
+      if (given_up(st)) break;
       if (lane < kWalkers) { const float4 v = st.sum[s][lane]; m = v.x; s0 = v.y; s1 = v.z; }
       warp_join<NT>(m, s0, s1, F);
       if (F.is_huge(m)) sums_of_differences<T, NT>(part, lane, F, m, s0, s1);
       if (parts > 1) {
         // to every block of the row, and from there
         if (uses) bar_wait(&st.heard[s], phase ^ 1u, 0xA03, &st.abort);
+        if (given_up(st)) break;
         if (lane == 0) bar_expect(&st.peers[s], (uint32_t)parts * 16u);
         __syncwarp();
         if (lane < parts)
           asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [%0], {%1, %2, %3, %4}, [%5];"
                        ::"r"(in_peer(&st.peer[s][rank], lane)), "f"(m), "f"(s0), "f"(s1), "f"(0.f), "r"(in_peer(&st.peers[s], lane)) : "memory");
         bar_wait(&st.peers[s], phase, 0xA04, &st.abort);
+        if (given_up(st)) break;
         m = kLowest;
         s0 = s1 = 0.f;
         if (lane < parts) { const float4 v = st.peer[s][lane]; m = v.x; s0 = v.y; s1 = v.z; }
@@ -1122,6 +1139,7 @@ __global__ void __launch_bounds__(kStreamThreads, 1) loss_stream_kernel(const Lo
       ++uses;
       if (more) read();
       bar_wait(&st.done[s], phase, 0xA05, &st.abort);
+      if (given_up(st)) break;
       if (!zero) {
         if (OP == mtf::LOSS_DISTILL) write_slots<T>(a, fix, sl, label, alone, part.dr, lane, 32, [&](int e) { return part.owned(e); });
         else if (lane == 0 && part.owned(label)) Piece<T>::set(part.dr, label, fix);
@@ -1297,8 +1315,8 @@ __global__ void __launch_bounds__(kStreamThreads, 1) loss_stream_kernel(const Lo
     }
   }
 
-  if (*(volatile int*)&st.abort)
-    for (int i = 0; i < 2000; ++i) __nanosleep(1000);      // copies in flight get time to land
+  if (parts > 1 && *(volatile int*)&st.abort)
+    for (int i = 0; i < 2000; ++i) __nanosleep(1000);      // sums on their way to and from other blocks get time to land
   if (parts > 1) {             // nobody leaves while another block may still write to its shared memory
     __syncwarp();
     cluster_arrive();
