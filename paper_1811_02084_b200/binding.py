@@ -784,9 +784,9 @@ def mtf_debug_pair_tiles(columns: int = 0, across: bool = False) -> tuple[int, b
     return bn.value, flat.value != 0
 
 
-def mtf_debug_wait_test(limit_cycles: int = 0, withhold_one_signal: bool = False) -> None:
+def mtf_debug_wait_test(limit_cycles: int = 0, withhold_one_signal: int = 0) -> None:
     """Testing hook: see mtf_debug_wait_test in include/mtf.h."""
-    _check(_lib.mtf_debug_wait_test(int(limit_cycles), 1 if withhold_one_signal else 0))
+    _check(_lib.mtf_debug_wait_test(int(limit_cycles), int(withhold_one_signal)))
 
 
 def mtf_launch_count() -> int:

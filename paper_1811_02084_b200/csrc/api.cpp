@@ -17,6 +17,7 @@ mtf_status read_device_status(int* code);
 mtf_status read_bad_index(int* seen);
 mtf_status read_row_status(int* code);
 mtf_status debug_wait_test(long long limit_cycles, int skip_first_commit);
+mtf_status debug_loss_wait_test(long long limit_cycles, int withhold);
 mtf_status debug_contraction(int bn, int split, int* ran_bn, int* ran_split);
 mtf_status debug_pair_tiles(int bn, int across, int* ran_bn, int* ran_across);
 mtf_status read_attention_status(int* code);
@@ -830,7 +831,10 @@ mtf_status mtf_debug_pair_tiles(int32_t columns, int32_t across, int32_t* ran_co
   return mtf::debug_pair_tiles(columns, across, ran_columns, ran_across);
 }
 
-mtf_status mtf_debug_wait_test(int64_t limit_cycles, int32_t withhold_one_signal) { return mtf::debug_wait_test(limit_cycles, withhold_one_signal); }
+mtf_status mtf_debug_wait_test(int64_t limit_cycles, int32_t withhold_one_signal) {
+  const mtf_status st = mtf::debug_wait_test(limit_cycles, withhold_one_signal != 0 && withhold_one_signal != 2);
+  return st == MTF_OK ? mtf::debug_loss_wait_test(limit_cycles, withhold_one_signal == 2 ? 2 : withhold_one_signal != 0) : st;
+}
 
 mtf_status mtf_stage_tap_begin(void* device_buffer, size_t bytes) { return mtf::tap_begin(device_buffer, bytes); }
 mtf_status mtf_stage_tap_end(int32_t* n_entries) { return mtf::tap_end(n_entries); }

@@ -19,6 +19,11 @@ using mtf::kMaxTeacher;
 
 __device__ int g_bad_id = 0;         // an id outside [0, V) was seen
 __device__ int g_loss_status = 0;    // a wait was given up
+// Testing hooks (mtf_debug_wait_test): how many cycles a wait may take, and a signal that is left out.
+constexpr long long kWaitCycles = 4000000000LL;
+__constant__ long long g_wait_limit = kWaitCycles;
+constexpr int kNoNumbers = 1, kNoSums = 2;
+__constant__ int g_withhold = 0;
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLowest = -3.402823466e38f;
@@ -939,7 +944,6 @@ __global__ void __launch_bounds__((kRowWarps + (OP == mtf::LOSS_DISTILL)) * 32, 
 // issue slots from the walks (212 to 223 in place of 210 with a teacher, when its list was searched for equal words by comparing all pairs).
 constexpr int kWalkers = 16, kNumberWarps = 3, kStreamThreads = 32 * (1 + kNumberWarps + kWalkers);
 constexpr int kChunk = 16384, kChunkPieces = kChunk / 16, kMaxChunks = 13, kMaxParts = 8, kRowSlots = kNumberWarps;
-constexpr long long kWaitCycles = 4000000000LL;
 constexpr int kBlockSharedMemory = 227 * 1024;       // what a block may have
 
 struct Stream {
@@ -968,10 +972,10 @@ __device__ __forceinline__ bool bar_try(uint64_t* bar, uint32_t parity) {
 // Warps that then go on only arrive at barriers whose phases end with the last of so many arrivals.  What counts bytes, or is another block's, needs the waits in
 // front of it: the copying warp and the numbers' warps leave (given_up behind each of their waits), and the other blocks' waits for this one run out in turn.
 __device__ __noinline__ void bar_wait_slow(uint64_t* bar, uint32_t parity, int code, volatile int* abort) {
-  const long long t0 = clock64();
+  const long long t0 = clock64(), limit = g_wait_limit;
   while (!bar_try(bar, parity)) {
     if (*abort) return;
-    if (clock64() - t0 > kWaitCycles) {
+    if (clock64() - t0 > limit) {
       atomicCAS(&g_loss_status, 0, code);
       *abort = 1;
       return;
@@ -1111,7 +1115,7 @@ __global__ void __launch_bounds__(kStreamThreads, 1) loss_stream_kernel(const Lo
         if (given_up(st)) break;
         if (lane == 0) bar_expect(&st.peers[s], (uint32_t)parts * 16u);
         __syncwarp();
-        if (lane < parts)
+        if (lane < parts && !(g_withhold == kNoSums && rank == 0 && s == 0 && uses == 0))
           asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [%0], {%1, %2, %3, %4}, [%5];"
                        ::"r"(in_peer(&st.peer[s][rank], lane)), "f"(m), "f"(s0), "f"(s1), "f"(0.f), "r"(in_peer(&st.peers[s], lane)) : "memory");
         bar_wait(&st.peers[s], phase, 0xA04, &st.abort);
@@ -1128,7 +1132,7 @@ __global__ void __launch_bounds__(kStreamThreads, 1) loss_stream_kernel(const Lo
       __syncwarp();            // (every lane has read the sums)
       if (lane == 0) {
         st.g[s] = g;
-        bar_arrive(&st.ready[s]);
+        if (!(g_withhold == kNoNumbers && s == 0 && uses == 0)) bar_arrive(&st.ready[s]);
       }
       if (rank == 0) row_results<OP, PASS, NT>(a, row, in, x, m, s0, s1, lane == 0, F, r);
       const int label = in.label;
@@ -1551,6 +1555,14 @@ mtf_status launch_loss_rows(LossOp op, LossPass pass, const LossRows& a, void* s
   if (a.bf16) dispatch<__nv_bfloat16>(op, pass, a, (cudaStream_t)stream);
   else dispatch<float>(op, pass, a, (cudaStream_t)stream);
   return after("loss_rows_kernel");
+}
+
+mtf_status debug_loss_wait_test(long long limit_cycles, int withhold) {
+  const long long limit = limit_cycles > 0 ? limit_cycles : kWaitCycles;
+  cudaError_t e = cudaMemcpyToSymbol(g_wait_limit, &limit, sizeof(limit));
+  if (e == cudaSuccess) e = cudaMemcpyToSymbol(g_withhold, &withhold, sizeof(int));
+  if (e != cudaSuccess) return fail(MTF_ERR_CUDA, "cudaMemcpyToSymbol: %s", cudaGetErrorString(e));
+  return MTF_OK;
 }
 
 mtf_status read_loss_status(int* code) {
