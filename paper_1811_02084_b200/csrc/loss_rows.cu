@@ -7,10 +7,10 @@
 #include <cuda_runtime.h>
 
 #include <algorithm>
-#include <atomic>
 
 #include "launch.cuh"
 #include "losses.h"
+#include "per_device.h"
 
 namespace {
 
@@ -1422,16 +1422,19 @@ template <typename T>
 int pieces_each(const LossRows& a, int parts) { return (a.V / Piece<T>::kN + parts - 1) / parts; }
 
 // Clusters of `parts` blocks of the stream kernel, one block to an SM, that the GPU holds at once (the SMs of a cluster lie in one group of
-// them, so this is less than SMs / parts); asked for once per process.
+// them, so this is less than SMs / parts); 0 where the driver does not say.
 template <typename K>
-int resident_clusters(K kernel, const cudaLaunchConfig_t& cfg, int parts, std::atomic<int>* known) {
-  int n = known[parts].load(std::memory_order_relaxed);
-  if (n > 0) return n;
-  if (cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess || n < 1) { (void)cudaGetLastError(); n = 1; }
-  known[parts].store(n, std::memory_order_relaxed);
-  return n;
+int resident_clusters(K kernel, const cudaLaunchConfig_t& cfg, mtf::KnownPerDevice& known) {
+  int device = -1;
+  if (cudaGetDevice(&device) != cudaSuccess) (void)cudaGetLastError();
+  return known.get(device, [&] {
+    int n = 0;
+    if (cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess) { (void)cudaGetLastError(); n = 0; }
+    return n;
+  });
 }
 
+// false: not a launch for this kernel (too long a list or row for the shared memory, no cluster of its size on the device)
 template <typename T, int OP, int NT>
 bool launch_stream(const LossRows& a, size_t list, cudaLaunchConfig_t cfg, cudaLaunchAttribute* at) {
   const long long pieces = (long long)a.V * (a.bf16 ? 2 : 4) / 16;
@@ -1450,12 +1453,13 @@ bool launch_stream(const LossRows& a, size_t list, cudaLaunchConfig_t cfg, cudaL
   cfg.blockDim = dim3(kStreamThreads, 1, 1);
   long long at_once = mtf::device_sm_count();
   if (parts > 1) {
-    static std::atomic<int> known[kMaxParts + 1];
+    static mtf::KnownPerDevice known[kMaxParts + 1];
     at[1].id = cudaLaunchAttributeClusterDimension;
     at[1].val.clusterDim.x = (unsigned)parts; at[1].val.clusterDim.y = 1; at[1].val.clusterDim.z = 1;
     cfg.numAttrs = 2;
     cfg.gridDim = dim3((unsigned)parts, 1, 1);
-    at_once = resident_clusters(kernel, cfg, parts, known);
+    at_once = resident_clusters(kernel, cfg, known[parts]);
+    if (at_once < 1) return false;
   }
   cfg.gridDim = dim3((unsigned)(std::min(a.rows, at_once) * parts), 1, 1);
   (void)cudaLaunchKernelEx(&cfg, kernel, a, factors<NT>(a), parts, pieces_each<T>(a, parts), chunks, lead);
