@@ -6,7 +6,7 @@ import numpy as np
 import pytest
 
 from helpers import Guarded
-from test_gpu_losses import TOK, U, bits, layout, mtf, t_dtype  # noqa: F401
+from test_gpu_losses import STEP, TOK, U, all_within, bits, layout, mtf, t_dtype  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -133,3 +133,97 @@ def test_rows_without_a_finite_logit_have_nan_statistics(mtf, V, dtype):  # noqa
     guard.check()
     lse = lse.view(-1)
     assert bool(lse[[0, 2]].isnan().all()) and abs(float(lse[1]) + 3.0) <= (16 + 3) * U and bool(lse[3].isfinite())
+
+
+# ---- rows whose weight lies in a few entries ----------------------------------------------------------------------------------------------------
+
+def delta(V):
+    """A sum's relative error, as in test_gpu_losses.py (additions, and the errors of the exponentials), but with the additions that a launch makes: rows of 40 000 entries
+    and more are walked by 128 threads at least, each with two partial sums, so that a chain has V / 256 of them at most; the joins of a warp's lanes, of warps and of a
+    row's parts are 5 + 4 + 3 more and as many rescalings, for which 32 stands.  At V = 270001 that is 6.8e-5, where an average entry
+    of those that hold a row's sum below is 1 / 1700 of it or more."""
+    return (V / 256 + 32 + 3 * (np.log(V) + 1) + 8) * U
+
+
+def rows_of_few_entries(dtype, T, V, seed):
+    """Logits near -13 but for a few near 0, which hold nearly all of a row's sum: its first entries (row t % 4 == 0), its last ones (1), those around the places at which a
+    row is cut into up to 8 parts (2), a few anywhere (3).  An entry left out or counted twice there moves the sum by far more than the bounds."""
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    z = 0.1 * torch.randn(T, V, generator=g, device="cuda") - 13.0
+    few = torch.randn(T, V, generator=g, device="cuda")
+    kind = torch.arange(T, device="cuda")[:, None] % 4
+    at = torch.arange(V, device="cuda")[None]
+    eighth = (at - at * 8 // V * V // 8).minimum((V - at * 8 % V) // 8)      # how far from a multiple of V / 8
+    some = torch.zeros(T, V, dtype=torch.bool, device="cuda")
+    some.scatter_(1, torch.randint(0, V, (T, 12), generator=g, device="cuda"), True)
+    chosen = torch.where(kind == 0, at < 15, torch.where(kind == 1, at >= V - 15, torch.where(kind == 2, (eighth < 72) & (at >= 72) & (at < V - 72), some)))
+    return g, torch.where(chosen, few, z).to(t_dtype(dtype))
+
+
+# few rows (blocks, clusters and independent parts of the rows' kernel) and rows that are streamed, by one block and by clusters
+@pytest.mark.parametrize("dtype,T,V", [("bf16", 5, 70001), ("f32", 8, 70001), ("bf16", 360, 70001), ("f32", 180, 70001), ("bf16", 9, 140001), ("bf16", 182, 140001), ("f32", 91, 140001),
+                                       ("bf16", 94, 270000), ("f32", 49, 270001), ("f32", 600, 40003), ("bf16", 700, 50007)])
+def test_no_entry_is_left_out_or_counted_twice(mtf, dtype, T, V):  # noqa: F811
+    import torch
+    g, z = rows_of_few_entries(dtype, T, V, T + V)
+    z64, d = z.double(), delta(V)
+    y = torch.randint(0, V, (T,), generator=g, device="cuda")
+    p1 = torch.log_softmax(z64, -1)
+    logp = p1.gather(-1, y[:, None])[:, 0]
+    lse = torch.logsumexp(z64, -1)
+    old, adv = (logp - 0.1).float(), torch.ones(T, device="cuda")
+    guard, N, lay = Guarded(), mtf.named, layout(mtf)
+    row, mat = lambda t: N(t.view(1, T), TOK), lambda t: N(t.view(1, T, V), TOK + ["vocab"])
+    y32 = y.int().view(1, T)
+    x = z64.amax(-1, keepdim=True) - z64
+    # policy: in one call, and its two directions
+    out = {k: guard.empty([1, T], "f32") for k in ("logp", "loss", "lse", "logp2", "dlogp", "loss2")}
+    dz, dz2 = guard.empty([1, T, V], dtype), guard.empty([1, T, V], dtype)
+    args = (mat(z), y32, row(old), None, row(adv), None, 0.2, 0.25, 0.0)
+    mtf.mtf_policy_step(lay, *args, row(out["logp"]), row(out["loss"]), mat(dz))
+    mtf.mtf_policy_forward(lay, *args, *[row(out[k]) for k in ("lse", "logp2", "dlogp", "loss2")])
+    mtf.mtf_policy_backward(lay, mat(z), y32, row(out["lse"]), row(out["dlogp"]), None, mat(dz2))
+    mtf.mtf_device_status()
+    guard.check()
+    ratio = (logp - old.double()).exp()
+    for k, want, tol in (("logp", logp, d + U * logp.abs()), ("logp2", logp, d + U * logp.abs()), ("lse", lse, d + U * lse.abs()), ("loss", -ratio, ratio * (d + 2 * U)),
+                         ("loss2", -ratio, ratio * (d + 2 * U)), ("dlogp", -ratio, ratio * (d + 2 * U))):
+        all_within(out[k][0], want, tol, k)
+    p = p1.exp()
+    # (the derivative's coefficient is off by d, too; the backward call's log-sum-exp, and so its exponentials, by a rounding to f32)
+    want = (ratio[:, None] * p).scatter_add_(1, y[:, None], -ratio[:, None])
+    tol = ratio[:, None] * p * (2 * d + (3 * x + 8) * U) + (d + STEP[dtype] + 4 * U) * want.abs()
+    all_within(dz[0], want, tol, "dlogits of the step")
+    all_within(dz2[0], want, tol + ratio[:, None] * p * 2 * U * lse.abs()[:, None], "dlogits")
+    del want, tol, dz, dz2
+    # distillation: powers of one exponential, two of them, one
+    K = 4
+    ids = torch.randint(0, V, (T, K), generator=g, device="cuda")
+    teacher = torch.randn(T, K, generator=g, device="cuda")
+    for tau in (2.0, 2.5, 1.0):
+        p2 = torch.log_softmax(z64 / tau, -1)
+        q = torch.softmax(teacher.double() / tau, -1)
+        want_loss = 0.5 * tau ** 2 * (q * (q.log() - p2.gather(-1, ids))).sum(-1) - 0.5 * logp
+        lses = torch.stack([torch.logsumexp(z64 / tau, -1), lse], -1)
+        want = 0.5 * tau * p2.exp() + 0.5 * p
+        tol = 0.5 * tau * p2.exp() * (d + (3 * x / tau + 8) * U) + 0.5 * p * (d + (3 * x + 8) * U)
+        off = 0.5 * tau * p2.exp() * 2 * U * lses[:, :1].abs() + 0.5 * p * 2 * U * lses[:, 1:].abs()
+        del p2
+        want.scatter_add_(-1, ids, -0.5 * tau * q)
+        want.scatter_add_(-1, y[:, None], torch.full((T, 1), -0.5, dtype=torch.float64, device="cuda"))
+        stats, loss, loss2 = guard.empty([1, T, 2], "f32"), guard.empty([1, T], "f32"), guard.empty([1, T], "f32")
+        dz, dz2 = guard.empty([1, T, V], dtype), guard.empty([1, T, V], dtype)
+        args = (ids.int().view(1, T, K), N(teacher.view(1, T, K), TOK + ["slot"]), y32, None, tau, 0.5, 0.5)
+        mtf.mtf_distill_step(lay, mat(z), *args, row(loss), mat(dz))
+        mtf.mtf_distill_forward(lay, mat(z), *args, N(stats, TOK + ["stat"]), row(loss2))
+        mtf.mtf_distill_backward(lay, mat(z), *args, N(stats, TOK + ["stat"]), None, mat(dz2))
+        mtf.mtf_device_status()
+        guard.check()
+        for got in (loss, loss2):
+            all_within(got[0], want_loss, (0.5 * tau * tau + 0.5) * d + 2 * U * want_loss.abs(), ("loss", tau))
+        all_within(stats[0], lses, d + U * lses.abs(), ("stats", tau))
+        tol += (STEP[dtype] + 4 * U) * want.abs()
+        all_within(dz[0], want, tol, ("dlogits of the step", tau))
+        all_within(dz2[0], want, tol + off, ("dlogits", tau))
+        del want, tol, off, dz, dz2
