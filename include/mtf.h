@@ -567,9 +567,9 @@ mtf_status mtf_device_status(int32_t* code);
  * streams rows of logits (mtf_policy_step and mtf_distill_step on more than 48 MB of rows above 32 KB); the other kernels' limits are
  * constants.  limit_cycles > 0 sets how many SM cycles a wait may take before it gives up (<= 0 restores the default of about two
  * seconds).  withhold_one_signal = 1 (or any other number but 0 and 2) makes every launch of the tensor-core kernel leave out the
- * "accumulator complete" signal of its first tile, and every block of the streaming kernel the "numbers complete" signal of its first row;
- * = 2 makes the first block of every cluster of the streaming kernel keep its sums of its first row from the cluster's blocks.  The wait
- * for it runs out: the kernel records a code, all its roles
+ * "accumulator complete" signal of its first tile, and every block of the streaming kernel wait for a second "numbers complete" signal of its
+ * first row; = 2 makes the blocks of the streaming kernel's clusters wait for a second signal with the sums of their first row.  Such a wait
+ * runs out: the kernel records a code, all its roles
  * leave through the common teardown (copies and MMAs in flight are given time to land, tensor memory
  * is freed), the launch ends normally, its output is unspecified, and the next mtf_device_status
  * returns MTF_ERR_TIMEOUT.  Nothing traps or faults and the context stays usable.  Affects the current

@@ -19,10 +19,10 @@ using mtf::kMaxTeacher;
 
 __device__ int g_bad_id = 0;         // an id outside [0, V) was seen
 __device__ int g_loss_status = 0;    // a wait was given up
-// Testing hooks (mtf_debug_wait_test): how many cycles a wait may take, and a signal that is left out.
+// Testing hooks (mtf_debug_wait_test): how many cycles a wait may take, and a barrier that waits for a signal more than is sent.
 constexpr long long kWaitCycles = 4000000000LL;
 __constant__ long long g_wait_limit = kWaitCycles;
-constexpr int kNoNumbers = 1, kNoSums = 2;
+constexpr int kNumbersHeld = 1, kSumsHeld = 2;
 __constant__ int g_withhold = 0;
 
 constexpr float kLog2e = 1.4426950408889634f;
@@ -969,8 +969,10 @@ __device__ __forceinline__ bool bar_try(uint64_t* bar, uint32_t parity) {
   return ok != 0;
 }
 // Gives up after about two seconds: a code for mtf_device_status, and from then on no wait of the block waits (its rows' results are unspecified).
-// Warps that then go on only arrive at barriers whose phases end with the last of so many arrivals.  What counts bytes, or is another block's, needs the waits in
-// front of it: the copying warp and the numbers' warps leave (given_up behind each of their waits), and the other blocks' waits for this one run out in turn.
+// Warps that then go on only write what is unspecified and arrive at barriers whose phases end with the last of so many arrivals.  What counts bytes, or is another
+// block's, needs the waits in front of it: there the copying warp and the numbers' warps leave (given_up), and the other blocks' waits for this one run out in turn.
+// (Checks behind the numbers' other waits and a signal left out by a comparison in each row took a step with 64 words at temperature 2 from 198 to 217 us: the rows'
+// numbers run at the rate at which their instructions come in.)
 __device__ __noinline__ void bar_wait_slow(uint64_t* bar, uint32_t parity, int code, volatile int* abort) {
   const long long t0 = clock64(), limit = g_wait_limit;
   while (!bar_try(bar, parity)) {
@@ -1005,9 +1007,9 @@ __global__ void __launch_bounds__(kStreamThreads, 1) loss_stream_kernel(const Lo
     for (int c = 0; c < chunks; ++c) { bar_init(&st.full[c], 1); bar_init(&st.empty[c], kWalkers); }
     for (int s = 0; s < kRowSlots; ++s) {
       bar_init(&st.sums[s], kWalkers);
-      bar_init(&st.ready[s], 1);
+      bar_init(&st.ready[s], s == 0 && g_withhold == kNumbersHeld ? 2 : 1);
       bar_init(&st.done[s], kWalkers);
-      bar_init(&st.peers[s], 1);
+      bar_init(&st.peers[s], s == 0 && g_withhold == kSumsHeld ? 2 : 1);
       bar_init(&st.heard[s], parts);
     }
     st.abort = 0;
@@ -1105,7 +1107,6 @@ __global__ void __launch_bounds__(kStreamThreads, 1) loss_stream_kernel(const Lo
       phase ^= 1u;
       float m = -F.huge, s0 = 0.f, s1 = 0.f;
       bar_wait(&st.sums[s], phase, 0xA02, &st.abort);
-      if (given_up(st)) break;
       if (lane < kWalkers) { const float4 v = st.sum[s][lane]; m = v.x; s0 = v.y; s1 = v.z; }
       warp_join<NT>(m, s0, s1, F);
       if (F.is_huge(m)) sums_of_differences<T, NT>(part, lane, F, m, s0, s1);
@@ -1115,7 +1116,7 @@ __global__ void __launch_bounds__(kStreamThreads, 1) loss_stream_kernel(const Lo
         if (given_up(st)) break;
         if (lane == 0) bar_expect(&st.peers[s], (uint32_t)parts * 16u);
         __syncwarp();
-        if (lane < parts && !(g_withhold == kNoSums && rank == 0 && s == 0 && uses == 0))
+        if (lane < parts)
           asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [%0], {%1, %2, %3, %4}, [%5];"
                        ::"r"(in_peer(&st.peer[s][rank], lane)), "f"(m), "f"(s0), "f"(s1), "f"(0.f), "r"(in_peer(&st.peers[s], lane)) : "memory");
         bar_wait(&st.peers[s], phase, 0xA04, &st.abort);
@@ -1132,7 +1133,7 @@ __global__ void __launch_bounds__(kStreamThreads, 1) loss_stream_kernel(const Lo
       __syncwarp();            // (every lane has read the sums)
       if (lane == 0) {
         st.g[s] = g;
-        if (!(g_withhold == kNoNumbers && s == 0 && uses == 0)) bar_arrive(&st.ready[s]);
+        bar_arrive(&st.ready[s]);
       }
       if (rank == 0) row_results<OP, PASS, NT>(a, row, in, x, m, s0, s1, lane == 0, F, r);
       const int label = in.label;
@@ -1143,7 +1144,6 @@ __global__ void __launch_bounds__(kStreamThreads, 1) loss_stream_kernel(const Lo
       ++uses;
       if (more) read();
       bar_wait(&st.done[s], phase, 0xA05, &st.abort);
-      if (given_up(st)) break;
       if (!zero) {
         if (OP == mtf::LOSS_DISTILL) write_slots<T>(a, fix, sl, label, alone, part.dr, lane, 32, [&](int e) { return part.owned(e); });
         else if (lane == 0 && part.owned(label)) Piece<T>::set(part.dr, label, fix);

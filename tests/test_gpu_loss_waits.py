@@ -1,5 +1,5 @@
-"""The failure path of the streamed losses' bounded waits, without faulting anything: the testing hook shortens the limit to about a millisecond and leaves one signal out, of a row's
-numbers within a block or of a block's sums within a cluster.  The call ends, the host reads MTF_ERR_TIMEOUT, nothing outside the outputs is written, and the next call is correct."""
+"""The failure path of the streamed losses' bounded waits, without faulting anything: the testing hook shortens the limit to about a millisecond and has a wait ask for a signal that
+does not come, of a row's numbers within a block or of the sums within a cluster.  The call ends, the host reads MTF_ERR_TIMEOUT, nothing outside the outputs is written, and the next call is correct."""
 import pytest
 
 from helpers import Guarded

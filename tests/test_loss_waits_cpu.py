@@ -17,18 +17,16 @@ def roles():
     return [kernel[a:b] for a, b in zip(at, at[1:] + [end])] + [kernel[end:]]
 
 
-def test_the_numbers_warps_leave_behind_every_wait():
+def test_the_numbers_warps_leave_before_they_announce_or_send():
     _, numbers, walks, _ = roles()
     lines = [line.strip() for line in numbers.splitlines()]
-    waits = [i for i, line in enumerate(lines) if "bar_wait(" in line]
-    assert [re.search(r"0xA0\d", lines[i]).group() for i in waits] == ["0xA02", "0xA03", "0xA04", "0xA05"]
-    assert all(lines[i + 1] == "if (given_up(st)) break;" for i in waits)
-    # what another block sees, and the announcement of bytes, lies behind such a wait; the walks have neither
-    first = numbers.index("if (given_up(st)) break;")
-    for what in ("bar_expect(", "st.async", "in_peer("):
-        assert what not in numbers[:first] and what in numbers[first:] and what not in walks
-    between = numbers[numbers.index("0xA03"):numbers.index("bar_expect(")], numbers[numbers.index("0xA04"):numbers.index("mbarrier.arrive.release.cluster")]
-    assert all("given_up(st)" in part for part in between)
+    waits = {re.search(r"0xA0\d", line).group(): i for i, line in enumerate(lines) if "bar_wait(" in line}
+    assert list(waits) == ["0xA02", "0xA03", "0xA04", "0xA05"]
+    assert all(lines[waits[w] + 1] == "if (given_up(st)) break;" for w in ("0xA03", "0xA04"))
+    # what another block sees, and the announcement of bytes, lies behind such a check, whichever wait was given up; the walks have neither
+    for what, behind in (("bar_expect(", "0xA03"), ("st.async", "0xA03"), ("mbarrier.arrive.release.cluster", "0xA04")):
+        assert numbers.count(what) == 1 and "given_up(st)" in numbers[numbers.index(behind):numbers.index(what)] and what not in walks
+    assert numbers.count("in_peer(") == 3 and "in_peer(" not in walks
 
 
 def test_the_copying_warp_leaves_and_waits_for_its_copies():
