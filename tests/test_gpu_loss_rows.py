@@ -227,3 +227,35 @@ def test_no_entry_is_left_out_or_counted_twice(mtf, dtype, T, V):  # noqa: F811
         all_within(dz[0], want, tol, ("dlogits of the step", tau))
         all_within(dz2[0], want, tol + off, ("dlogits", tau))
         del want, tol, off, dz, dz2
+
+
+# ---- one tensor in two parts of a call ----------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("V", [5, 33, 512])
+def test_logits_that_teach_themselves_and_each_other(mtf, V, dtype):  # noqa: F811
+    """All words are the list: against the logits themselves the softened term is 0, against another student's it is the divergence."""
+    import torch
+    T, tau = 40, 2.0
+    g = torch.Generator(device="cuda").manual_seed(V)
+    a, b = ((2 * torch.randn(1, T, V, generator=g, device="cuda")).to(t_dtype(dtype)) for _ in range(2))
+    N, lay, guard = mtf.named, layout(mtf), Guarded()
+    n = {"a": N(a, TOK + ["vocab"]), "b": N(b, TOK + ["vocab"])}
+    z = {"a": a[0].double(), "b": b[0].double()}
+    as_list = {k: N(t, TOK + ["slot"]) for k, t in (("a", a), ("b", b))}
+    ids = torch.stack([torch.randperm(V, generator=g, device="cuda") for _ in range(T)]).int().view(1, T, V)
+    in_order = torch.arange(V, device="cuda").expand(1, T, V).contiguous().int()
+    d = (V / 32 + 32 + 3 * (np.log(V) + 1) + 8) * U                    # (test_gpu_losses.py's)
+    for student, teacher, words in (("a", "a", in_order), ("a", "b", in_order), ("b", "a", ids), ("b", "b", in_order)):
+        for desc in (n, as_list):                                      # the very descriptor of the logits, or one of its own
+            loss, dz = guard.empty([1, T], "f32"), guard.empty([1, T, V], dtype)
+            mtf.mtf_distill_step(lay, n[student], words, desc[teacher], None, None, tau, 1.0, 0.0, N(loss, TOK), N(dz, TOK + ["vocab"]))
+            mtf.mtf_device_status()
+            guard.check()
+            p = torch.log_softmax(z[student] / tau, -1)
+            q = torch.zeros(T, V, dtype=torch.float64, device="cuda").scatter_(1, words[0].long(), torch.softmax(z[teacher] / tau, -1))
+            want_loss = tau ** 2 * (q * (q.log() - p)).sum(-1)
+            all_within(loss[0], want_loss, tau ** 2 * d + U * want_loss.abs(), "loss")
+            want = tau * (p.exp() - q)
+            x = z[student].amax(-1, keepdim=True) - z[student]
+            all_within(dz[0], want, tau * p.exp() * (d + (3 * x / tau + 8) * U) + (STEP[dtype] + 4 * U) * want.abs(), "dlogits")
