@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import math
+import operator
 import os
 from ctypes import POINTER, Structure, byref, c_char_p, c_float, c_int, c_int32, c_int64, c_size_t, c_uint32, c_void_p
 
@@ -728,7 +729,11 @@ def _pairs(logits):
 def mtf_preference_forward(layout, logits: Named, targets, weight: Named | None, ref_logp: Named, kind, beta: float, smoothing: float, lse: Named, logp: Named,
                            seq_logp: Named, dseq: Named, loss: Named, stream=None) -> None:
     """kind: "sigmoid", "hinge", "squared" or the constants of the same names."""
-    hp = mtf_preference_params(_PREFERENCE_KINDS[kind] if kind in _PREFERENCE_KINDS else int(kind), float(beta), float(smoothing))
+    try:
+        code = _PREFERENCE_KINDS[kind] if isinstance(kind, str) else operator.index(kind)
+    except (KeyError, TypeError):
+        raise MtfError(1, f"unknown kind {kind!r}") from None
+    hp = mtf_preference_params(code, float(beta), float(smoothing))
     _check(_lib.mtf_preference_forward(layout.handle, _p(logits), _ids(targets, _pairs(logits)), _p(weight), _p(ref_logp), byref(hp), _p(lse), _p(logp), _p(seq_logp), _p(dseq),
                                        _p(loss), _stream(stream)))
 

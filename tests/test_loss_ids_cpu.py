@@ -52,3 +52,13 @@ def test_a_descriptor_of_other_calls_as_teacher():
     assert code(distill(t, t["other"], z, t["per_word"], token)) == "MTF_ERR_INVALID_ARG"
     assert code(distill(t, t["other"], z, token, token)) == "MTF_ERR_SIZE_MISMATCH"
     assert code(policy) == "MTF_ERR_INVALID_ARG"
+
+
+@pytest.mark.parametrize("kind", ["other", "", None, 1.5, 3, -1, [0]], ids=str)
+def test_a_kind_that_is_none_is_refused_as_other_arguments_are(kind):
+    lay = tensors()["layout"]
+    tok = ["branch"] + TOK
+    z, value = mtf.named(torch.zeros(2, B, L, V), tok + ["vocab"]), [mtf.named(torch.zeros(2, B, L), tok) for _ in range(2)]
+    pair = [mtf.named(torch.zeros(2, B), tok[:2]) for _ in range(3)]
+    ids, loss = torch.zeros(2, B, L, dtype=torch.int32), mtf.named(torch.zeros(B), ["batch"])
+    assert code(lambda: mtf.mtf_preference_forward(lay, z, ids, None, pair[0], kind, 0.1, 0.0, *value, *pair[1:], loss)) == "MTF_ERR_INVALID_ARG"
