@@ -51,7 +51,8 @@ typedef enum {
   MTF_ERR_TIMEOUT = 10          /* a bounded device-side wait gave up (see mtf_device_status)           */
 } mtf_status;
 
-typedef enum { MTF_F32 = 0, MTF_BF16 = 1 } mtf_dtype;
+/* MTF_E4M3 (8 bits, values up to 448, no infinity) is the type of paged caches and of the states that mtf_beam_reorder copies; other calls refuse it. */
+typedef enum { MTF_F32 = 0, MTF_BF16 = 1, MTF_E4M3 = 2 } mtf_dtype;
 
 /* Opaque handles.  (The layout handle type carries a _t because mtf_layout is the call that makes one.) */
 typedef struct mtf_mesh_s mtf_mesh_t;
@@ -533,6 +534,72 @@ mtf_status mtf_preference_forward(const mtf_layout_t* layout, const mtf_tensor* 
 mtf_status mtf_preference_backward(const mtf_layout_t* layout, const mtf_tensor* logits, const int32_t* targets, const mtf_tensor* weight,
                                    const mtf_tensor* lse, const mtf_tensor* dseq, const mtf_tensor* dloss, mtf_tensor* dlogits, void* stream);
 
+/* ---- answering: a paged cache, attention of one new token, beam search --------------------------------------
+ * What a Transformer needs to answer with (the paper's models are judged on sentences found by beam search): the keys and values
+ * of the positions so far, which mtf_attention_forward leaves dense as kk and vv, are kept in pages, each new token attends to them, and a search
+ * over the vocabulary says which sentences go on.
+ *
+ * A cache: two pools of pages of `slot` positions, and for each sequence a list of its pages.  Position m of sequence s lies
+ * in page table[s][m / slots], slot m % slots.
+ *   k, v     : [page, slot, heads, d_k] or [page, heads, slot, d_k] (v: d_v), bf16 or e4m3, 16-byte aligned; d_k and d_v multiples of 8
+ *              (e4m3: 16), at most 256.  `slot` names the dimension of the slots (NULL: "slot"); the other one is the heads'.
+ *   scales   : f32 with k's first three dims, for e4m3 only: a row's values are its bytes' times its scale.  Scales are at least 0.
+ *   table    : device int32 [*sequences, table_pages]; only the entries of pages in use are read.
+ * Sequences may share pages (that they no longer write).  A page outside the pool, a position that the table has no page for, or a parent outside
+ * the beams is left out and reported by mtf_device_status, as an id outside the vocabulary is; nothing is read or written in its place.
+ * Layouts: nothing here sums over a split dimension, so any legal layout is free; page, slot, d_k, d_v, beam and vocab may not be split across RANKS
+ * (MTF_ERR_UNSUPPORTED; heads and sequences may).  No output may overlap another tensor of its call.  Results repeat bit for bit. */
+typedef struct {
+  const mtf_tensor *k, *v;
+  const mtf_tensor *k_scale, *v_scale;     /* NULL unless e4m3 */
+  const int32_t* table;
+  int64_t table_pages;                     /* pages of a sequence */
+  const char* slot;
+} mtf_cache;
+/* Rows into the cache: row i of sequence s of kk [*sequences, length, heads, d_k] and vv (d_v) (bf16 or f32, 16-byte aligned) becomes position
+ * starts[s] + i, for i < counts[s] (NULL: starts 0, all rows).  Everything else in the cache stays as it was.
+ * e4m3: scale = the smallest power of two (not below 2^-126) by which the row's largest finite value is at most 448, 1 for a row of zeros; each value is
+ * value / scale, rounded once to e4m3.  NaN and infinities become NaN.  Two rows of one call at one place: which of them stays is open. */
+mtf_status mtf_cache_write(const mtf_layout_t* layout, const mtf_tensor* kk, const mtf_tensor* vv, const int32_t* starts, const int32_t* counts,
+                           const mtf_cache* cache, void* stream);
+/* And back, rounded once to the type of kk and vv.  Rows from counts[s] on, and rows that the cache has no place for, are zeros. */
+mtf_status mtf_cache_read(const mtf_layout_t* layout, const mtf_cache* cache, const int32_t* starts, const int32_t* counts, mtf_tensor* kk, mtf_tensor* vv,
+                          void* stream);
+/* Attention of one new token a sequence over the first lengths[s] positions of its cache (the token's own key and value written before):
+ *     o[s, h, g, :] = sum_m p_m v[m, h, :],  p = softmax over m < lengths[s] of scale * sum_d q[s, h, g, d] k[m, h, d]
+ * q [*sequences, heads, group, d_k] or, for one head of queries to a head of the cache, [*sequences, heads, d_k]; o like q with d_v; both bf16, 16-byte
+ * aligned; `heads` and d_k named as in the cache; group up to 4096.  Where there is no position (length 0, all pages left out), or no weight (every logit -infinity), o is 0.  What
+ * lies in slots beyond the last position is not looked at.  Sums are f32; a weight is rounded to bf16 (e4m3: to f16, with the scale of its row of v) before
+ * it multiplies a row of v.  workspace: device, 16-byte aligned, at least what the query says (0: may be NULL), contents of no matter before and after; calls that may run at
+ * the same time need one each. */
+mtf_status mtf_attention_decode(const mtf_layout_t* layout, const mtf_tensor* q, const mtf_cache* cache, const int32_t* lengths, float scale, mtf_tensor* o,
+                                void* workspace, size_t workspace_bytes, void* stream);
+mtf_status mtf_attention_decode_workspace_bytes(const mtf_layout_t* layout, const mtf_tensor* q, const mtf_cache* cache, size_t* bytes);
+/* The best of a sentence's beams and words.  logits [*sentences, beam, vocab] (bf16 or f32, 16-byte aligned, any vocab), scores f32
+ * [*sentences, beam], finished int32 [*sentences, beam] or NULL (none is):
+ *     a beam that is not finished offers every word v with  score + logits[v] - log sum_w exp(logits[w]),
+ *     a finished one offers end_id with its score, and its logits are not read.
+ * The first slots of these in falling order, equal ones by the lower beam, then the lower word: parents (the beam), tokens, new_scores
+ * [*sentences, any name: slots], new_finished (may be NULL): 1 where the parent was finished or the token is end_id.  parents, tokens and new_finished are int32 of as many.
+ * Words with a logit of -infinity, beams whose score is not finite (a beam that is not yet one: -infinity), and those with a NaN, a +infinity or
+ * no finite logit offer nothing; slots without an offer have parent 0, token end_id, score -infinity, finished 1.
+ * beams and slots up to 64.  A beam's words are compared by their logits, offers of different beams in 64 bits, from f32 exponentials summed in f32 by threads and in 64 bits across them.
+ * workspace as above; it is always needed. */
+mtf_status mtf_beam_select(const mtf_layout_t* layout, const mtf_tensor* logits, const mtf_tensor* scores, const int32_t* finished, int32_t end_id,
+                           int32_t* parents, int32_t* tokens, mtf_tensor* new_scores, int32_t* new_finished, void* workspace, size_t workspace_bytes,
+                           void* stream);
+mtf_status mtf_beam_select_workspace_bytes(const mtf_layout_t* layout, const mtf_tensor* logits, int64_t slots, size_t* bytes);
+/* States after a selection: out[.., i, ..] = states[.., parents[.., i], ..] along the dimension `beam`, whose size in out may be another one.
+ * parents int32, one per index of the dimensions in front of `beam` and of out's `beam`.  f32, bf16 or e4m3, any dims and alignment of whole elements. */
+mtf_status mtf_beam_reorder(const mtf_layout_t* layout, const char* beam, const int32_t* parents, const mtf_tensor* states, mtf_tensor* out, void* stream);
+/* And a paged cache: sequence (sentence, i) of the new table goes on from sequence (sentence, parents[sentence, i]) of cache->table
+ * [sentences, beams, table_pages].  Whole pages are shared; the last one, if it is not full, is copied (its rows in use) to the page fresh[sentence, i], so that each may go on by itself.
+ * new_table int32 [sentences, slots, table_pages], new_lengths int32 [sentences, slots]; lengths int32 [sentences, beams]: positions so far.
+ * fresh int32 [sentences, slots]: pages that no table of the call has in use, different from each other; one that a full last page leaves no need for is not
+ * touched and may be given again. */
+mtf_status mtf_cache_reorder(const mtf_layout_t* layout, const mtf_cache* cache, int64_t sentences, int64_t beams, int64_t slots, const int32_t* parents,
+                             const int32_t* lengths, const int32_t* fresh, int32_t* new_table, int32_t* new_lengths, void* stream);
+
 /* ---- reductions (Section 6 "Reduction") --------------------------------------------------------- */
 /* out[out dims] = sum over the other dims of in (out dims a subset of in's).  Local reduction per
  * slice, then the group sum across the mesh dims of reduced-out split dims, in one launch. */
@@ -562,7 +629,8 @@ const char* mtf_last_error(void);
 /* Synchronises the current device and reads the sticky device status word: 0 = no kernel of this
  * library gave up on a bounded wait since the last call; non-zero = a code naming the wait.
  * Resets the word.  Returns MTF_ERR_TIMEOUT when it was non-zero, else MTF_ERR_INVALID_ARG when a
- * token id or target outside [0, vocab) was seen by the vocab and loss kernels since the last call. */
+ * token id or target outside [0, vocab) was seen by the vocab and loss kernels, or a page, position or parent outside its
+ * range by those of answering, since the last call. */
 mtf_status mtf_device_status(int32_t* code);
 /* Testing hook for the failure path of the bounded device-side waits of the persistent tensor-core kernel and of the kernel that
  * streams rows of logits (mtf_policy_step and mtf_distill_step on more than 48 MB of rows above 32 KB); the other kernels' limits are

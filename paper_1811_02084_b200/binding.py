@@ -42,7 +42,7 @@ def _choose_library() -> str:
 
 LIB_PATH = _choose_library()
 
-MTF_F32, MTF_BF16 = 0, 1
+MTF_F32, MTF_BF16, MTF_E4M3 = 0, 1, 2
 MTF_KERNEL_SIMT, MTF_KERNEL_TCGEN05 = 0, 1
 MTF_REDUCE_NONE, MTF_REDUCE_CHAINED, MTF_REDUCE_WORKSPACE = 0, 1, 2
 STATUS_NAMES = ["MTF_OK", "MTF_ERR_INVALID_ARG", "MTF_ERR_DUPLICATE_DIM", "MTF_ERR_UNKNOWN_DIM",
@@ -94,6 +94,11 @@ class mtf_policy_params(Structure):
 
 class mtf_preference_params(Structure):
     _fields_ = [("kind", c_int32), ("beta", c_float), ("smoothing", c_float)]
+
+
+class mtf_cache(Structure):
+    _fields_ = [("k", POINTER(mtf_tensor)), ("v", POINTER(mtf_tensor)), ("k_scale", POINTER(mtf_tensor)), ("v_scale", POINTER(mtf_tensor)), ("table", c_void_p),
+                ("table_pages", c_int64), ("slot", c_char_p)]
 
 
 MTF_PREFERENCE_SIGMOID, MTF_PREFERENCE_HINGE, MTF_PREFERENCE_SQUARED = 0, 1, 2
@@ -180,6 +185,14 @@ def _load():
         "mtf_policy_step": [vp, _T, vp, _T, _T, _T, _T, POINTER(mtf_policy_params), _T, _T, _T, vp],
         "mtf_preference_forward": [vp, _T, vp, _T, _T, POINTER(mtf_preference_params), _T, _T, _T, _T, _T, vp],
         "mtf_preference_backward": [vp, _T, vp, _T, _T, _T, _T, _T, vp],
+        "mtf_cache_write": [vp, _T, _T, vp, vp, POINTER(mtf_cache), vp],
+        "mtf_cache_read": [vp, POINTER(mtf_cache), vp, vp, _T, _T, vp],
+        "mtf_attention_decode": [vp, _T, POINTER(mtf_cache), vp, c_float, _T, vp, c_size_t, vp],
+        "mtf_attention_decode_workspace_bytes": [vp, _T, POINTER(mtf_cache), POINTER(c_size_t)],
+        "mtf_beam_select": [vp, _T, _T, vp, c_int32, vp, vp, _T, vp, vp, c_size_t, vp],
+        "mtf_beam_select_workspace_bytes": [vp, _T, c_int64, POINTER(c_size_t)],
+        "mtf_beam_reorder": [vp, c_char_p, vp, _T, _T, vp],
+        "mtf_cache_reorder": [vp, POINTER(mtf_cache), c_int64, c_int64, c_int64, vp, vp, vp, vp, vp, vp],
         "mtf_debug_wait_test": [c_int64, c_int32],
         "mtf_debug_contraction": [c_int32, c_int32, POINTER(c_int32), POINTER(c_int32)],
         "mtf_debug_pair_tiles": [c_int32, c_int32, POINTER(c_int32), POINTER(c_int32)],
@@ -224,9 +237,13 @@ def _dtype_code(dtype) -> int:
         return MTF_F32
     if dtype in (MTF_BF16, "bf16", "bfloat16"):
         return MTF_BF16
+    if dtype in (MTF_E4M3, "e4m3", "float8_e4m3fn"):
+        return MTF_E4M3
     name = str(dtype)
     if name == "torch.float32":
         return MTF_F32
+    if name == "torch.float8_e4m3fn":
+        return MTF_E4M3
     if name == "torch.bfloat16":
         return MTF_BF16
     raise MtfError(1, f"unsupported dtype {dtype!r}")
@@ -740,6 +757,119 @@ def mtf_preference_forward(layout, logits: Named, targets, weight: Named | None,
 
 def mtf_preference_backward(layout, logits: Named, targets, weight: Named | None, lse: Named, dseq: Named, dloss: Named | None, dlogits: Named, stream=None) -> None:
     _check(_lib.mtf_preference_backward(layout.handle, _p(logits), _ids(targets, _pairs(logits)), _p(weight), _p(lse), _p(dseq), _p(dloss), _p(dlogits), _stream(stream)))
+
+
+class Cache:
+    """A paged cache of keys and values (mtf_cache of include/mtf.h): pools ``k`` and ``v`` ([page, slot, heads, d] or [page, heads, slot, d]), for e4m3 a
+    scale a row, and ``table``, a contiguous int32 device tensor [*sequences, pages of a sequence]; ``slot`` names the dimension of a page's positions."""
+
+    def __init__(self, k: Named, v: Named, table, k_scale: Named | None = None, v_scale: Named | None = None, slot: str = "slot"):
+        if table is not None and (str(table.dtype) != "torch.int32" or not table.is_contiguous() or table.dim() < 1):
+            raise MtfError(1, "a cache's table must be a contiguous int32 tensor")
+        self.k, self.v, self.k_scale, self.v_scale, self.table = k, v, k_scale, v_scale, table
+        if k is not None and slot not in k.names[1:3]:
+            raise MtfError(STATUS_NAMES.index("MTF_ERR_UNKNOWN_DIM"), f"neither the second nor the third dimension of the cache's k is the slots' ({slot!r})")
+        self.heads = next((n for n in k.names[1:3] if n != slot), None) if k is not None else None
+        self.table_pages = int(table.shape[-1]) if table is not None else 0
+        self.sequences = math.prod(table.shape[:-1]) if table is not None else 0
+        self.c = mtf_cache(*(ctypes.pointer(t.c) if t is not None else None for t in (k, v, k_scale, v_scale)), table.data_ptr() if table is not None else None,
+                           self.table_pages, slot.encode())
+        self.ref = byref(self.c)
+
+
+def _places(t, n: int | None, what: str, none: bool = False):
+    """The pointer of an int32 tensor of n numbers."""
+    global _int32
+    if t is None and none:
+        return None
+    if t is None:
+        raise MtfError(1, f"{what} is None")
+    if (t.dtype is not _int32 and str(t.dtype) != "torch.int32") or not t.is_contiguous():
+        raise MtfError(1, f"{what} must be a contiguous int32 tensor")
+    _int32 = t.dtype
+    if n is not None and t.numel() != n:         # (None: another tensor of the call is missing, which the library refuses)
+        raise MtfError(STATUS_NAMES.index("MTF_ERR_SIZE_MISMATCH"), f"{what}: {t.numel()} numbers where the call has {n}")
+    return t.data_ptr()
+
+
+def _sequences(t: Named, inner: int, cache: Cache) -> int:
+    """Sequences of a tensor whose last `inner` dims are others, held against those of the cache's table."""
+    if t is None or cache is None or cache.k is None:
+        raise MtfError(1, "a tensor of the call, its cache or the cache's k is None")
+    n = math.prod(s for _, s in t.dims[:-inner])
+    if cache.table is not None and cache.sequences != n:
+        raise MtfError(STATUS_NAMES.index("MTF_ERR_SIZE_MISMATCH"), f"the cache's table is for {cache.sequences} sequences where the call has {n}")
+    return n
+
+
+def mtf_cache_write(layout, kk: Named, vv: Named, starts, counts, cache: Cache, stream=None) -> None:
+    """starts, counts: contiguous int32 device tensors [*sequences], or None (position 0, all rows)."""
+    n = _sequences(kk, 3, cache)
+    _check(_lib.mtf_cache_write(layout.handle, _p(kk), _p(vv), _places(starts, n, "starts", True), _places(counts, n, "counts", True), cache.ref, _stream(stream)))
+
+
+def mtf_cache_read(layout, cache: Cache, starts, counts, kk: Named, vv: Named, stream=None) -> None:
+    n = _sequences(kk, 3, cache)
+    _check(_lib.mtf_cache_read(layout.handle, cache.ref, _places(starts, n, "starts", True), _places(counts, n, "counts", True), _p(kk), _p(vv), _stream(stream)))
+
+
+def _query_sequences(q: Named, cache: Cache) -> int:
+    # (with a dimension for the heads of queries that share a head of the cache, or without)
+    return _sequences(q, 3 if q is not None and cache is not None and len(q.dims) > 3 and q.dims[-3][0] == cache.heads else 2, cache)
+
+
+def mtf_attention_decode(layout, q: Named, cache: Cache, lengths, scale: float, o: Named, workspace=None, stream=None) -> None:
+    """lengths: contiguous int32 device tensor [*sequences]: positions that each sequence attends to."""
+    wp, wb = _ws(workspace)
+    n = _query_sequences(q, cache)
+    _check(_lib.mtf_attention_decode(layout.handle, _p(q), cache.ref, _places(lengths, n, "lengths"), float(scale), _p(o), wp, wb, _stream(stream)))
+
+
+def mtf_attention_decode_workspace_bytes(layout, q: Named, cache: Cache) -> int:
+    b = c_size_t()
+    _query_sequences(q, cache)
+    _check(_lib.mtf_attention_decode_workspace_bytes(layout.handle, _p(q), cache.ref, byref(b)))
+    return b.value
+
+
+def mtf_beam_select(layout, logits: Named, scores: Named, finished, end_id: int, parents, tokens, new_scores: Named, new_finished=None, workspace=None, stream=None) -> None:
+    """finished [*sentences, beam] or None, parents, tokens and new_finished (or None) [*sentences, slots]: contiguous int32 device tensors."""
+    wp, wb = _ws(workspace)
+    out = math.prod(s for _, s in new_scores.dims) if new_scores is not None else None
+    _check(_lib.mtf_beam_select(layout.handle, _p(logits), _p(scores), _ids(finished, logits), operator.index(end_id), _places(parents, out, "parents"),
+                                _places(tokens, out, "tokens"), _p(new_scores), _places(new_finished, out, "new_finished", True), wp, wb, _stream(stream)))
+
+
+def mtf_beam_select_workspace_bytes(layout, logits: Named, slots: int) -> int:
+    b = c_size_t()
+    _check(_lib.mtf_beam_select_workspace_bytes(layout.handle, _p(logits), operator.index(slots), byref(b)))
+    return b.value
+
+
+def mtf_beam_reorder(layout, beam: str, parents, states: Named, out: Named, stream=None) -> None:
+    """parents: contiguous int32 device tensor, one number per index of out's dims up to and with `beam`."""
+    n = None
+    if out is not None:
+        names = out.names
+        if beam not in names:
+            raise MtfError(STATUS_NAMES.index("MTF_ERR_UNKNOWN_DIM"), f"out has no dimension {beam!r}")
+        n = math.prod(s for _, s in out.dims[:names.index(beam) + 1])
+    _check(_lib.mtf_beam_reorder(layout.handle, beam.encode(), _places(parents, n, "parents"), _p(states), _p(out), _stream(stream)))
+
+
+def mtf_cache_reorder(layout, cache: Cache, parents, lengths, fresh, new_table, new_lengths, stream=None) -> None:
+    """parents and fresh [*sentences, slots], lengths [*sentences, beams] of a cache whose table is [*sentences, beams, pages]; new_table [*sentences, slots, pages] and
+    new_lengths [*sentences, slots] are written.  All contiguous int32 device tensors."""
+    if cache is None or cache.table is None or cache.table.dim() < 2 or parents is None or parents.dim() != cache.table.dim() - 1 or parents.dim() < 1:
+        raise MtfError(1, "cache_reorder: a table [*sentences, beams, pages] and parents [*sentences, slots]")
+    beams, slots = int(cache.table.shape[-2]), int(parents.shape[-1])
+    sentences = math.prod(parents.shape[:-1])
+    if tuple(cache.table.shape[:-2]) != tuple(parents.shape[:-1]):
+        raise MtfError(STATUS_NAMES.index("MTF_ERR_SIZE_MISMATCH"), "cache_reorder: the table and the parents are for other sentences")
+    out = sentences * slots
+    _check(_lib.mtf_cache_reorder(layout.handle, cache.ref, sentences, beams, slots, _places(parents, out, "parents"), _places(lengths, sentences * beams, "lengths"),
+                                  _places(fresh, out, "fresh"), _places(new_table, out * cache.table_pages, "new_table"), _places(new_lengths, out, "new_lengths"),
+                                  _stream(stream)))
 
 
 def mtf_status_string(status: int) -> str:

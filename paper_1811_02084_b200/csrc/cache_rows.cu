@@ -1,0 +1,436 @@
+// A paged cache's rows: written from dense ones, read back as dense ones, and reordered behind a step of beam search; and the reordering of
+// dense states.
+//
+// An 8-bit cache holds a row of d values as e4m3 and one scale: the smallest power of two by which the row's largest finite value is at most 448,
+// e4m3's largest.  A power of two divides exactly, so a value is rounded once, to e4m3's 4 significant bits, and nothing about the result
+// depends on how a quotient is rounded; the finer scale amax / 448 would gain nothing, since a floating-point format's steps are relative.
+// NaN and infinities are stored as NaN.  A row of zeros has scale 1.
+//
+// All of it is copying (a row is read once and written once): HBM is the bound.
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+
+#include <algorithm>
+
+#include "answer.h"
+#include "launch.cuh"
+
+namespace {
+
+__device__ int g_bad_place = 0;                  // a position or page outside the cache, or a parent outside the beams, was seen
+
+// n / d for n < 2^31
+struct Divide {
+  uint32_t mul;
+  int shift, d;
+};
+Divide divide_by(int d) {
+  int n = 0;
+  while ((1LL << n) < d) ++n;
+  return {(uint32_t)(((1ULL << (31 + n)) + d - 1) / d), 31 + n, d};      // off by less than 2^n in 2^(31 + n)
+}
+__device__ __forceinline__ int over(int n, const Divide& d) { return (int)((unsigned long long)(uint32_t)n * d.mul >> d.shift); }
+
+struct RowsArgs {
+  uint8_t* pool[2];                              // K, V
+  float* scale[2];
+  uint8_t* dense[2];
+  int d[2];
+  const int32_t *table, *starts, *counts;
+  long long n_seq, length;
+  int heads, slots, pages, per_sequence, rows_page, row_slot, row_head;
+  long long rows;                                // n_seq * length * heads
+  Divide by_heads, by_length, by_slots;
+};
+
+__device__ __forceinline__ float lo16(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float hi16(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
+__device__ __forceinline__ uint32_t two_bf16(float x, float y) {
+  const __nv_bfloat162 v = __floats2bfloat162_rn(x, y);
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+// e4m3 of two values of magnitude up to 448 or NaN; x in the low byte
+__device__ __forceinline__ uint32_t two_e4m3(float x, float y) {
+  uint32_t v;
+  asm("{\n\t.reg .b16 t;\n\tcvt.rn.satfinite.e4m3x2.f32 t, %2, %1;\n\tcvt.u32.u16 %0, t;\n\t}" : "=r"(v) : "f"(x), "f"(y));
+  return v;
+}
+__device__ __forceinline__ float2 of_e4m3(uint32_t two) {
+  uint32_t h;
+  asm("{\n\t.reg .b16 t;\n\tcvt.u16.u32 t, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, t;\n\t}" : "=r"(h) : "r"(two));
+  return __half22float2(*reinterpret_cast<const __half2*>(&h));
+}
+
+// Row `i` of the dense rows (sequence, index, head): its place in the pool, -1 where the row is not meant, -2 where there is no place for it.
+__device__ __forceinline__ int place(const RowsArgs& a, long long i) {
+  // rows of up to 2^31 - 1 (sequence, index) pairs
+  long long si;
+  int head;
+  if (a.rows <= 0x7fffffffLL) {
+    const int q = over((int)i, a.by_heads);
+    si = q;
+    head = (int)i - q * a.heads;
+  } else {
+    si = i / a.heads;
+    head = (int)(i - si * a.heads);
+  }
+  const int s = over((int)si, a.by_length), at = (int)si - s * (int)a.length;
+  const int count = a.counts ? a.counts[s] : (int)a.length;
+  if (at >= count) return -1;
+  const long long m = (long long)(a.starts ? a.starts[s] : 0) + at;
+  if (m < 0 || m >= (long long)a.per_sequence * a.slots) return -2;
+  const int index = over((int)m, a.by_slots), page = a.table[(long long)s * a.per_sequence + index];
+  if (page < 0 || page >= a.pages) return -2;
+  return page * a.rows_page + ((int)m - index * a.slots) * a.row_slot + head * a.row_head;
+}
+
+// A row by kLanes lanes, 8 values each (d up to 8 kLanes); blockIdx.y: K or V.  Each group of lanes takes kEach rows at once, so that enough loads are under way.
+constexpr int kEach = 4;
+
+template <int kLanes, bool kBf16, bool kE4m3>
+__global__ void __launch_bounds__(256) cache_write_kernel(const RowsArgs a) {
+  mtf::chain_wait();
+  const int side = blockIdx.y, d = a.d[side], lane = threadIdx.x % kLanes;
+  const long long groups = (long long)gridDim.x * (256 / kLanes);
+  for (long long first = (long long)blockIdx.x * (256 / kLanes) + threadIdx.x / kLanes; first - threadIdx.x / kLanes < a.rows; first += groups * kEach) {
+    uint4 w[kEach][2];
+    int to[kEach];
+    bool in[kEach];
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) {
+      const long long i = first + e * groups;
+      to[e] = i < a.rows ? place(a, i) : -1;
+      if (to[e] == -2) atomicExch(&g_bad_place, 1);
+      in[e] = to[e] >= 0 && lane * 8 < d;
+      w[e][0] = w[e][1] = make_uint4(0u, 0u, 0u, 0u);
+      if (in[e]) {
+        const uint4* const p = reinterpret_cast<const uint4*>(a.dense[side] + (i * d + lane * 8) * (kBf16 ? 2 : 4));
+        w[e][0] = p[0];
+        if (!kBf16) w[e][1] = p[1];
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) {
+      const long long at = (long long)to[e] * d + lane * 8;
+      float x[8];
+      if (kBf16) {
+        const uint32_t u[4] = {w[e][0].x, w[e][0].y, w[e][0].z, w[e][0].w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) { x[2 * j] = lo16(u[j]); x[2 * j + 1] = hi16(u[j]); }
+      } else {
+        const uint32_t u[8] = {w[e][0].x, w[e][0].y, w[e][0].z, w[e][0].w, w[e][1].x, w[e][1].y, w[e][1].z, w[e][1].w};
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = __uint_as_float(u[j]);
+      }
+      if (!kE4m3) {
+        if (!in[e]) continue;
+        const uint4 v = kBf16 ? w[e][0] : make_uint4(two_bf16(x[0], x[1]), two_bf16(x[2], x[3]), two_bf16(x[4], x[5]), two_bf16(x[6], x[7]));
+        *reinterpret_cast<uint4*>(a.pool[side] + at * 2) = v;
+        continue;
+      }
+      uint32_t top = 0;                              // (as bits: magnitudes in rising order, and infinities and NaN above all)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const uint32_t m = __float_as_uint(x[j]) & 0x7fffffffu;
+        if (m < 0x7f800000u) top = max(top, m);
+      }
+#pragma unroll
+      for (int o = kLanes / 2; o > 0; o /= 2) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+      // 448 = 1.75 2^8: scale 2^(e - 8) for a largest value m 2^e with m up to 1.75, else 2^(e - 7); not below 2^-126, so that it is a normal number, too
+      int field = (int)(top >> 23) - 8 + ((top & 0x7fffffu) > 0x600000u ? 1 : 0);
+      field = max(field, 1);
+      if (top == 0) field = 127;
+      const float scale = __uint_as_float((uint32_t)field << 23);
+      if (!in[e]) continue;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const bool finite = (__float_as_uint(x[j]) & 0x7fffffffu) < 0x7f800000u;
+        x[j] = finite ? x[j] / scale : __uint_as_float(0x7fc00000u);
+      }
+      *reinterpret_cast<uint2*>(a.pool[side] + at) =
+          make_uint2(two_e4m3(x[0], x[1]) | two_e4m3(x[2], x[3]) << 16, two_e4m3(x[4], x[5]) | two_e4m3(x[6], x[7]) << 16);
+      if (lane == 0) a.scale[side][to[e]] = scale;
+    }
+  }
+}
+
+template <int kLanes, bool kBf16, bool kE4m3>
+__global__ void __launch_bounds__(256) cache_read_kernel(const RowsArgs a) {
+  mtf::chain_wait();
+  const int side = blockIdx.y, d = a.d[side], lane = threadIdx.x % kLanes;
+  const long long groups = (long long)gridDim.x * (256 / kLanes);
+  if (lane * 8 >= d) return;
+  for (long long first = (long long)blockIdx.x * (256 / kLanes) + threadIdx.x / kLanes; first < a.rows; first += groups * kEach) {
+    uint4 w[kEach];
+    float scale[kEach];
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) {
+      const long long i = first + e * groups;
+      const int from = i < a.rows ? place(a, i) : -1;
+      if (from == -2) atomicExch(&g_bad_place, 1);
+      w[e] = make_uint4(0u, 0u, 0u, 0u);             // (zeros in e4m3 as well)
+      scale[e] = 0.f;
+      if (from < 0) continue;
+      const long long at = (long long)from * d + lane * 8;
+      if (kE4m3) {
+        const uint2 v = *reinterpret_cast<const uint2*>(a.pool[side] + at);
+        w[e].x = v.x;
+        w[e].y = v.y;
+        scale[e] = a.scale[side][from];
+      } else {
+        w[e] = *reinterpret_cast<const uint4*>(a.pool[side] + at * 2);
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) {
+      const long long i = first + e * groups;
+      if (i >= a.rows) continue;
+      uint4* const p = reinterpret_cast<uint4*>(a.dense[side] + (i * d + lane * 8) * (kBf16 ? 2 : 4));
+      if (!kE4m3 && kBf16) { p[0] = w[e]; continue; }
+      float x[8];
+      if (kE4m3) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float2 v = of_e4m3((j < 2 ? w[e].x : w[e].y) >> (16 * (j & 1)));
+          x[2 * j] = v.x * scale[e];
+          x[2 * j + 1] = v.y * scale[e];
+        }
+      } else {
+        const uint32_t u[4] = {w[e].x, w[e].y, w[e].z, w[e].w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) { x[2 * j] = lo16(u[j]); x[2 * j + 1] = hi16(u[j]); }
+      }
+      if (kBf16) p[0] = make_uint4(two_bf16(x[0], x[1]), two_bf16(x[2], x[3]), two_bf16(x[4], x[5]), two_bf16(x[6], x[7]));
+      else {
+        p[0] = make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
+        p[1] = make_uint4(__float_as_uint(x[4]), __float_as_uint(x[5]), __float_as_uint(x[6]), __float_as_uint(x[7]));
+      }
+    }
+  }
+}
+
+struct ReorderArgs {
+  uint8_t* pool[2];
+  float* scale[2];
+  int row_bytes[2];
+  const int32_t *table, *parents, *lengths, *fresh;
+  int32_t *new_table, *new_lengths;
+  int beams, out, heads, slots, pages, per_sequence, rows_page, row_slot, row_head;
+};
+
+// Block (x, y): answer x = (group, i); the y-th share of what is copied for it.
+__global__ void __launch_bounds__(256) cache_reorder_kernel(const ReorderArgs a) {
+  mtf::chain_wait();
+  const int x = blockIdx.x, group = x / a.out, parent = a.parents[x];
+  const int tid = blockIdx.y * 256 + threadIdx.x, threads = gridDim.y * 256;
+  int32_t* const to = a.new_table + (long long)x * a.per_sequence;
+  if (parent < 0 || parent >= a.beams) {             // no such beam: an answer without positions
+    if (tid == 0) { atomicExch(&g_bad_place, 1); a.new_lengths[x] = 0; }
+    for (int i = tid; i < a.per_sequence; i += threads) to[i] = -1;
+    return;
+  }
+  const int from = group * a.beams + parent;
+  const int32_t* const of = a.table + (long long)from * a.per_sequence;
+  const int n = a.lengths[from], whole = max(n, 0) / a.slots, used = max(n, 0) - whole * a.slots;
+  const bool fits = n >= 0 && n <= (long long)a.per_sequence * a.slots;
+  const int page = used && fits ? of[whole] : 0, fresh = used && fits ? a.fresh[x] : 0;
+  const bool there = page >= 0 && page < a.pages && fresh >= 0 && fresh < a.pages;
+  if (tid == 0) {
+    a.new_lengths[x] = n;
+    if (!fits || !there) atomicExch(&g_bad_place, 1);
+  }
+  for (int i = tid; i < a.per_sequence; i += threads) to[i] = i == whole && used && fits ? fresh : of[i];
+  if (!used || !fits || !there) return;
+  // rows in use of the page that goes on: `used` slots of every head
+  for (int side = 0; side < 2; ++side) {
+    const int pieces = a.row_bytes[side] / 16, total = used * a.heads * pieces;
+    const uint4* const src = reinterpret_cast<const uint4*>(a.pool[side]) + (long long)page * a.rows_page * pieces;
+    uint4* const dst = reinterpret_cast<uint4*>(a.pool[side]) + (long long)fresh * a.rows_page * pieces;
+    // the inner one of slot and head is contiguous: slots of a head (used of them), or all heads of a slot
+    const int inner = (a.row_slot == 1 ? used : a.heads) * pieces, step = (a.row_slot == 1 ? a.row_head : a.row_slot) * pieces;
+    for (int i = tid; i < total; i += threads) {
+      const int run = i / inner, at = run * step + (i - run * inner);
+      dst[at] = src[at];
+    }
+    if (a.scale[side]) {
+      const int m = inner / pieces, gap = step / pieces;
+      for (int i = tid; i < used * a.heads; i += threads) {
+        const int run = i / m, at = run * gap + (i - run * m);
+        a.scale[side][(long long)fresh * a.rows_page + at] = a.scale[side][(long long)page * a.rows_page + at];
+      }
+    }
+  }
+}
+
+// out[x, :] = in[group(x), parents[x], :]; rows of `pieces` pieces of type T
+template <typename T>
+__global__ void __launch_bounds__(256) beam_reorder_kernel(const int32_t* __restrict__ parents, const T* __restrict__ in, T* __restrict__ out, int beams, int slots,
+                                                           long long pieces) {
+  mtf::chain_wait();
+  const long long x = blockIdx.x;
+  const int parent = parents[x];
+  const bool there = parent >= 0 && parent < beams;
+  if (!there && threadIdx.x == 0 && blockIdx.y == 0) atomicExch(&g_bad_place, 1);
+  const T* const src = in + (x / slots * beams + (there ? parent : 0)) * pieces;
+  T* const dst = out + x * pieces;
+  const long long step = (long long)gridDim.y * 256;
+  long long i = (long long)blockIdx.y * 256 + threadIdx.x;
+  for (; i + 3 * step < pieces; i += 4 * step) {
+    T v[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = there ? src[i + e * step] : T();
+#pragma unroll
+    for (int e = 0; e < 4; ++e) dst[i + e * step] = v[e];
+  }
+  for (; i < pieces; i += step) dst[i] = there ? src[i] : T();
+}
+
+RowsArgs rows_args(const mtf::CachePool& c, const mtf::CacheRows& r) {
+  RowsArgs a = {};
+  a.pool[0] = reinterpret_cast<uint8_t*>(c.k);
+  a.pool[1] = reinterpret_cast<uint8_t*>(c.v);
+  a.scale[0] = c.ks;
+  a.scale[1] = c.vs;
+  a.dense[0] = reinterpret_cast<uint8_t*>(r.k);
+  a.dense[1] = reinterpret_cast<uint8_t*>(r.v);
+  a.d[0] = c.dk;
+  a.d[1] = c.dv;
+  a.table = c.table;
+  a.starts = r.starts;
+  a.counts = r.counts;
+  a.n_seq = c.sequences;
+  a.length = r.length;
+  a.heads = c.heads;
+  a.slots = c.slots;
+  a.pages = c.pages;
+  a.per_sequence = c.per_sequence;
+  a.rows_page = c.rows_page;
+  a.row_slot = c.row_slot;
+  a.row_head = c.row_head;
+  a.rows = c.sequences * r.length * c.heads;
+  a.by_heads = divide_by(c.heads);
+  a.by_length = divide_by((int)r.length);
+  a.by_slots = divide_by(c.slots);
+  return a;
+}
+
+template <int kLanes, bool kBf16, bool kE4m3>
+void rows_launch(const RowsArgs& a, bool write, cudaStream_t st) {
+  const long long at_once = (256 / kLanes) * kEach, blocks = std::max(1LL, std::min<long long>((a.rows + at_once - 1) / at_once, (long long)mtf::device_sm_count() * 16));
+  cudaLaunchConfig_t cfg = {};
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.gridDim = dim3((unsigned)blocks, 2, 1);
+  cfg.blockDim = dim3(256, 1, 1);
+  cfg.stream = st;
+  cfg.attrs = at;
+  cfg.numAttrs = 1;
+  (void)cudaLaunchKernelEx(&cfg, write ? cache_write_kernel<kLanes, kBf16, kE4m3> : cache_read_kernel<kLanes, kBf16, kE4m3>, a);
+}
+template <bool kBf16, bool kE4m3>
+void rows_lanes(const RowsArgs& a, bool write, cudaStream_t st) {
+  const int d = std::max(a.d[0], a.d[1]);
+  if (d <= 64) rows_launch<8, kBf16, kE4m3>(a, write, st);
+  else if (d <= 128) rows_launch<16, kBf16, kE4m3>(a, write, st);
+  else rows_launch<32, kBf16, kE4m3>(a, write, st);
+}
+mtf_status after(const char* what) {
+  mtf::count_launch();
+  const cudaError_t e = cudaGetLastError();
+  if (e != cudaSuccess) return mtf::fail(MTF_ERR_CUDA, "%s: %s", what, cudaGetErrorString(e));
+  return MTF_OK;
+}
+mtf_status cache_rows(const mtf::CachePool& c, const mtf::CacheRows& r, bool write, void* stream) {
+  const RowsArgs a = rows_args(c, r);
+  cudaStream_t st = (cudaStream_t)stream;
+  if (r.bf16) c.e4m3 ? rows_lanes<true, true>(a, write, st) : rows_lanes<true, false>(a, write, st);
+  else c.e4m3 ? rows_lanes<false, true>(a, write, st) : rows_lanes<false, false>(a, write, st);
+  return after(write ? "cache_write_kernel" : "cache_read_kernel");
+}
+
+template <typename T>
+void reorder_launch(const int32_t* parents, const void* in, void* out, long long rows, int beams, int slots, long long bytes, cudaStream_t st) {
+  const long long pieces = bytes / (long long)sizeof(T);
+  const long long shares = std::max(1LL, std::min((pieces + 1023) / 1024, std::max(1LL, (long long)mtf::device_sm_count() * 16 / rows)));
+  cudaLaunchConfig_t cfg = {};
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.gridDim = dim3((unsigned)rows, (unsigned)std::min(shares, 65535LL), 1);
+  cfg.blockDim = dim3(256, 1, 1);
+  cfg.stream = st;
+  cfg.attrs = at;
+  cfg.numAttrs = 1;
+  (void)cudaLaunchKernelEx(&cfg, beam_reorder_kernel<T>, parents, reinterpret_cast<const T*>(in), reinterpret_cast<T*>(out), beams, slots, pieces);
+}
+
+}  // namespace
+
+namespace mtf {
+
+mtf_status launch_cache_write(const CachePool& c, const CacheRows& r, void* stream) { return cache_rows(c, r, true, stream); }
+mtf_status launch_cache_read(const CachePool& c, const CacheRows& r, void* stream) { return cache_rows(c, r, false, stream); }
+
+mtf_status launch_cache_reorder(const CachePool& c, const CacheReorder& r, void* stream) {
+  ReorderArgs a = {};
+  a.pool[0] = reinterpret_cast<uint8_t*>(c.k);
+  a.pool[1] = reinterpret_cast<uint8_t*>(c.v);
+  a.scale[0] = c.ks;
+  a.scale[1] = c.vs;
+  a.row_bytes[0] = c.dk * (c.e4m3 ? 1 : 2);
+  a.row_bytes[1] = c.dv * (c.e4m3 ? 1 : 2);
+  a.table = c.table;
+  a.parents = r.parents;
+  a.lengths = r.lengths;
+  a.fresh = r.fresh;
+  a.new_table = r.table;
+  a.new_lengths = r.new_lengths;
+  a.beams = r.beams;
+  a.out = r.out;
+  a.heads = c.heads;
+  a.slots = c.slots;
+  a.pages = c.pages;
+  a.per_sequence = c.per_sequence;
+  a.rows_page = c.rows_page;
+  a.row_slot = c.row_slot;
+  a.row_head = c.row_head;
+  const long long rows = r.groups * r.out, page_bytes = (long long)c.rows_page * (a.row_bytes[0] + a.row_bytes[1]);
+  // a share of a page's copy that is worth a block, as long as the GPU has room for more of them
+  const long long shares = std::max(1LL, std::min({(page_bytes + 32767) / 32768, (long long)device_sm_count() * 8 / rows + 1, 64LL}));
+  cudaLaunchConfig_t cfg = {};
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.gridDim = dim3((unsigned)rows, (unsigned)shares, 1);
+  cfg.blockDim = dim3(256, 1, 1);
+  cfg.stream = (cudaStream_t)stream;
+  cfg.attrs = at;
+  cfg.numAttrs = 1;
+  (void)cudaLaunchKernelEx(&cfg, cache_reorder_kernel, a);
+  return after("cache_reorder_kernel");
+}
+
+mtf_status launch_beam_reorder(const int32_t* parents, const void* in, void* out, long long groups, int beams, int slots, long long bytes, void* stream) {
+  const uintptr_t low = reinterpret_cast<uintptr_t>(in) | reinterpret_cast<uintptr_t>(out) | (uintptr_t)bytes;
+  const cudaStream_t st = (cudaStream_t)stream;
+  const long long rows = groups * slots;
+  if (low % 16 == 0) reorder_launch<uint4>(parents, in, out, rows, beams, slots, bytes, st);
+  else if (low % 4 == 0) reorder_launch<uint32_t>(parents, in, out, rows, beams, slots, bytes, st);
+  else if (low % 2 == 0) reorder_launch<uint16_t>(parents, in, out, rows, beams, slots, bytes, st);
+  else reorder_launch<uint8_t>(parents, in, out, rows, beams, slots, bytes, st);
+  return after("beam_reorder_kernel");
+}
+
+// 1 when a position, page or parent outside its range was met since the last call; resets the flag
+mtf_status read_cache_bad_place(int* seen) {
+  int v = 0;
+  cudaError_t e = cudaMemcpyFromSymbol(&v, g_bad_place, sizeof(int));
+  if (e != cudaSuccess) return fail(MTF_ERR_CUDA, "cudaMemcpyFromSymbol: %s", cudaGetErrorString(e));
+  if (v) { int z = 0; cudaMemcpyToSymbol(g_bad_place, &z, sizeof(int)); }
+  *seen = v;
+  return MTF_OK;
+}
+
+}  // namespace mtf

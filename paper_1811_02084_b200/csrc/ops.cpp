@@ -43,6 +43,8 @@ mtf_status legal(const mtf_layout_t* L, const mtf_tensor& t, const char* what) {
   return mtf::check_tensor(L, d);
 }
 
+bool f32_or_bf16(const mtf_tensor& t) { return t.dtype == MTF_F32 || t.dtype == MTF_BF16; }
+
 }  // namespace
 
 extern "C" {
@@ -105,6 +107,7 @@ mtf_status mtf_reshape_plan(const mtf_layout_t* layout, int32_t ndim, const mtf_
 mtf_status mtf_transpose(const mtf_layout_t* layout, const mtf_tensor* in, mtf_tensor* out, void* stream) {
   if (!layout || !in || !out || !in->data || !out->data) return fail(MTF_ERR_INVALID_ARG, "transpose: NULL argument");
   if (in->dtype != out->dtype || in->ndim != out->ndim) return fail(MTF_ERR_INVALID_ARG, "transpose: input and output must agree in type and number of dims");
+  if (!f32_or_bf16(*in)) return fail(MTF_ERR_INVALID_ARG, "transpose: f32 or bf16 tensors");
   mtf_status st = legal(layout, *in, "transpose input");
   if (st != MTF_OK || (st = legal(layout, *out, "transpose output")) != MTF_OK) return st;
   int64_t istr[mtf::kMaxTensorDims], ostr[mtf::kMaxTensorDims], sizes[mtf::kMaxTensorDims], sstr[mtf::kMaxTensorDims];
@@ -127,6 +130,7 @@ mtf_status mtf_transpose(const mtf_layout_t* layout, const mtf_tensor* in, mtf_t
 // one processor's dense slice written back into its box of the global tensor (the inverse of mtf_slice_gather)
 mtf_status mtf_slice_scatter(const mtf_layout_t* layout, const void* slice, int64_t processor, mtf_tensor* global, void* stream) {
   if (!layout || !slice || !global || !global->data) return fail(MTF_ERR_INVALID_ARG, "slice_scatter: NULL argument");
+  if (!f32_or_bf16(*global)) return fail(MTF_ERR_INVALID_ARG, "slice_scatter: f32 or bf16 tensors");
   std::vector<Dim> d;
   mtf_status st = mtf::read_dims(global->ndim, global->dims, &d, "tensor");
   if (st != MTF_OK) return st;
@@ -149,6 +153,7 @@ static mtf_status vocab_not_across_ranks(const mtf_layout_t* L, const char* voca
 mtf_status mtf_embedding_forward(const mtf_layout_t* layout, const int32_t* ids, const mtf_tensor* table, mtf_tensor* x, void* stream) {
   if (!layout || !ids || !table || !x || !table->data || !x->data) return fail(MTF_ERR_INVALID_ARG, "embedding_forward: NULL argument");
   if (table->ndim != 2 || x->ndim < 2 || table->dtype != x->dtype) return fail(MTF_ERR_INVALID_ARG, "embedding_forward: table [vocab, d], x [*tokens, d] of the same type");
+  if (!f32_or_bf16(*x)) return fail(MTF_ERR_INVALID_ARG, "embedding_forward: f32 or bf16 tensors");
   if (strcmp(table->dims[1].name, x->dims[x->ndim - 1].name) != 0 || table->dims[1].size != x->dims[x->ndim - 1].size)
     return fail(MTF_ERR_SIZE_MISMATCH, "embedding_forward: the table's second dim must be x's last dim");
   mtf_status st = legal(layout, *table, "embedding table");
@@ -160,6 +165,7 @@ mtf_status mtf_embedding_forward(const mtf_layout_t* layout, const int32_t* ids,
 
 mtf_status mtf_embedding_backward(const mtf_layout_t* layout, const int32_t* ids, const mtf_tensor* dx, mtf_tensor* dtable, void* stream) {
   if (!layout || !ids || !dx || !dtable || !dx->data || !dtable->data) return fail(MTF_ERR_INVALID_ARG, "embedding_backward: NULL argument");
+  if (!f32_or_bf16(*dx)) return fail(MTF_ERR_INVALID_ARG, "embedding_backward: dx in f32 or bf16");
   if (dtable->ndim != 2 || dx->ndim < 2 || dtable->dtype != MTF_F32) return fail(MTF_ERR_INVALID_ARG, "embedding_backward: dtable f32 [vocab, d], dx [*tokens, d]");
   if (strcmp(dtable->dims[1].name, dx->dims[dx->ndim - 1].name) != 0 || dtable->dims[1].size != dx->dims[dx->ndim - 1].size)
     return fail(MTF_ERR_SIZE_MISMATCH, "embedding_backward: dtable's second dim must be dx's last dim");
