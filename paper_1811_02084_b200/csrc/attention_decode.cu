@@ -3,21 +3,22 @@
 // where position m of sequence s lies in page table[s][m / slots], slot m % slots.
 //
 // Every row of the cache is read once and used for `group` heads of queries, 2 to 4 flops a byte and head: HBM is the bound, and the
-// products only have to keep out of its way.  So a warp is a stream of its own: it loads a chunk of 16 (or 32, 64) rows of K and of V straight into
-// the registers that matrix instructions want them in, and loads the next chunk of either as soon as the current one is used up; there is
-// no shared memory and no barrier in the loop, and each warp keeps its own running maximum and sums.  With the rows of the cache as the
-// instruction's 16 rows and the heads as its 8 columns, eight heads of queries cost no more than one and nothing is padded to 16:
+// products only have to keep out of its way.  So a warp is a stream of its own: it has chunks of 16 (or 32, 64) rows of K and of V, 8 KB, copied by TMA into a
+// ring of its own and waits for nobody but them; there is no block barrier in the loop, and each warp keeps its own running maximum and sums.  With the
+// rows of the cache as the instruction's 16 rows and the heads as its 8 columns, eight heads of queries cost no more than one and nothing is padded to 16:
 //     S^T [16 keys x 8 heads] = K [16 x d] q^T [d x 8],   O^T [d x 8 heads] += V^T [d x 16 keys] P^T [16 keys x 8]
-// The order of a sum's terms is free, so the lanes take d in the order in which 16-byte loads leave it (K), and the rows of O^T are the d that
-// a lane's load holds (V, whose pairs of keys are put together by byte permutes).
+// The order of a sum's terms is free, so a lane reads 16 bytes of a row at a time and what it has of d, and of the keys, is what it multiplies; V's pairs of keys are put together by
+// byte permutes.  (64 sequences of up to 4096 positions in bf16, 1.1 GB, whole call: loads into registers 252 us, copies by the lanes into shared memory 244, TMA 199.)
 //
 // The work is cut evenly: the keys of all (sequence, head) items are laid end to end in units of some rows a warp, and every block takes an equal
 // run of them, whatever the lengths.  Items that cross a block's edge are left as partial sums and joined behind the launch, in order.
+#include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
 
 #include <algorithm>
+#include <mutex>
 
 #include "answer.h"
 #include "launch.cuh"
@@ -26,7 +27,7 @@ namespace {
 
 constexpr int kWarps = 4;
 constexpr int kThreads = 32 * kWarps;
-constexpr int kPlanned = 2048;        // sequences whose units a block adds up by itself
+constexpr int kPlanned = 1024;        // sequences whose units a block adds up by itself
 constexpr int kLeastUnits = 2;        // a block's run
 constexpr float kLog2e = 1.4426950408889634f;
 // The running maximum is raised only where a logit lies 2^6 above it: otherwise every chunk would pay for a maximum across lanes.
@@ -36,7 +37,6 @@ constexpr float kLift = 9.f;
 
 struct Args {
   const __nv_bfloat16* q;
-  const uint8_t *k, *v;
   const float *ks, *vs;
   const int32_t *table, *lengths;
   __nv_bfloat16* o;
@@ -45,6 +45,7 @@ struct Args {
   uint32_t slots_mul;                            // m / slots = (m * slots_mul) >> slots_shift in 64 bits, for m below 2^31
   int slots_shift;
   float scale_log2;
+  int box_rows;                                  // keys of a copied box: a power of two up to 16 that divides a page's slots
   int balanced;
   float* part_o;                                 // [block][2][8 NT][DC]
   float* part_s;                                 // [block][2][8 NT][4]: reference of l, l, reference of o
@@ -59,34 +60,23 @@ __device__ __forceinline__ float ex2(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
-__device__ __forceinline__ uint4 load16(const uint8_t* p) {
-  uint4 v;
-  asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
-  return v;
+// four e4m3 values as f16 (exact), two and two
+__device__ __forceinline__ void halves(uint32_t four, uint32_t& lo, uint32_t& hi) {
+  asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, a;\n\tcvt.rn.f16x2.e4m3x2 %1, b;\n\t}" : "=r"(lo), "=r"(hi) : "r"(four));
 }
-__device__ __forceinline__ uint2 load8(const uint8_t* p) {
-  uint2 v;
-  asm volatile("ld.global.L1::no_allocate.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "l"(p));
-  return v;
-}
-// two e4m3 values as f16 (exact)
-__device__ __forceinline__ uint32_t halves(uint32_t two) {
-  uint32_t h;
-  asm("{\n\t.reg .b16 t;\n\tcvt.u16.u32 t, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, t;\n\t}" : "=r"(h) : "r"(two));
-  return h;
-}
+// (neither these nor the products touch memory, and no lane leaves the loop early: the compiler may move them)
 __device__ __forceinline__ uint32_t transposed(uint32_t x) {
   uint32_t y;
-  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
   return y;
 }
 template <bool kHalf>
 __device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
   if (kHalf)
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
   else
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 __device__ __forceinline__ uint32_t word(const uint4& v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
@@ -95,32 +85,89 @@ __device__ __forceinline__ uint32_t word(const uint2& v, int i) { return i == 0 
 template <bool kE4m3, int DC>
 struct Shape {
   static constexpr int kElt = kE4m3 ? 1 : 2;
-  static constexpr int kTiles = DC * kElt <= 64 ? 4 : DC * kElt <= 128 ? 2 : 1;     // 16-key tiles of a chunk: 4 to 8 KB of K and of V a warp (d = 256: 8)
+  static constexpr int kTiles = DC * kElt <= 64 ? 4 : DC * kElt <= 128 ? 2 : 1;     // 16-key tiles of a chunk: 4 KB of K and of V (bf16 rows of 256: 8)
   static constexpr int kKeys = 16 * kTiles;
+  static constexpr int kIndexes = (kKeys + 31) / 32;
   static constexpr int kTB = 16 / kElt;              // K: values of a lane's 16 bytes
   static constexpr int kKP = DC / (4 * kTB);         // ... pieces of a row
   static constexpr int kSteps = kTB / 4;             // ... products of a piece, 16 deep
   static constexpr int kVB = kE4m3 && DC == 64 ? 8 : kTB;   // V: values of a lane's piece (8 lanes a row)
   static constexpr int kVP = DC / (8 * kVB);
-  static constexpr int kIndexes = (kKeys + 31) / 32;
+  static constexpr int kRow = DC * kElt < 128 ? DC * kElt : 128;      // bytes of a box's rows
+  static constexpr int kBoxes = DC * kElt / kRow;    // ... beside each other for a whole row
+  static constexpr int kSide = kTiles * kBoxes * 16 * kRow;           // bytes of a chunk of K, and of V
+  static constexpr int kStage = 2 * kSide;
+  static constexpr int kStages = kStage > 8192 ? 3 : 2;
+  static constexpr int kRing = kWarps * kStages * kStage;
+  static constexpr int kBlocks = kStage > 8192 ? 1 : 3;               // an SM holds
 };
 template <int kBytes> struct Piece { using T = uint4; };
 template <> struct Piece<8> { using T = uint2; };
+
+// Which key of a tile is the i-th row of a product, and which 16 bytes of V's 128 are lane group r's: free choices, since the order of a sum's terms and of the
+// results' rows is, made so that the lanes that shared memory serves together find their pieces in different banks.  A copy puts piece j of row k at j ^ (k % 8)
+// (rows of 64 bytes: at j ^ (k / 2 % 4)).  K: lanes (r, t) of two neighbouring r read pieces t of rows key(r), which have to differ in bit 2 (64 bytes: in bit
+// 0); V: they read pieces piece(r) of the rows key(2t).
+template <int kRow>
+__device__ __forceinline__ int key_of_row(int i) {
+  return kRow == 128 ? (i & 8) | (i & 1) << 2 | (i >> 1 & 3) : (i & 8) | (((i >> 1 & 1) << 2 | (i >> 2 & 1)) ^ (i & 1 ? 3 : 0));
+}
+template <int kRow>
+__device__ __forceinline__ int swizzled(int key, int piece) { return kRow == 128 ? piece ^ (key & 7) : piece ^ (key >> 1 & 3); }
+
+__device__ __forceinline__ uint32_t smem_at(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ bool has_landed(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cta.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+  return ok != 0;
+}
+constexpr long long kWaitCycles = 4000000000LL;      // about two seconds
+constexpr long long kLandCycles = 200000000LL;       // 0.1 s, for copies in flight behind a wait that was given up
+__device__ int g_decode_status = 0;                  // a wait was given up
+__constant__ long long g_wait_limit = kWaitCycles;
+__constant__ int g_withhold = 0;                     // testing: each warp's first wait asks for a copy that nobody has sent
+__device__ __noinline__ bool landed_late(uint32_t bar, uint32_t parity, long long limit) {
+  const long long t0 = clock64();
+  while (!has_landed(bar, parity))
+    if (clock64() - t0 > limit) return false;
+  return true;
+}
+// (the same for all lanes)
+__device__ __forceinline__ bool landed(uint32_t bar, uint32_t parity) {
+  bool ok = has_landed(bar, parity);
+  if (!__all_sync(0xffffffffu, ok)) ok = __all_sync(0xffffffffu, landed_late(bar, parity, g_wait_limit));
+  else ok = true;
+  return ok;
+}
+__device__ __forceinline__ void copy_box(uint32_t to, const CUtensorMap* map, int d, int slot, int head, int page, uint32_t bar) {
+  asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(to), "l"(map), "r"(d), "r"(slot),
+               "r"(head), "r"(page), "r"(bar)
+               : "memory");
+}
 
 // first unit of block c, of `units` over `blocks`
 __device__ __forceinline__ long long first_unit(long long units, int blocks, int c) { return units * c / blocks; }
 
 template <bool kE4m3, int DC, int NT>
-__global__ void __launch_bounds__(kThreads, DC == 256 || (NT > 1 && DC == 128) ? 2 : 3) attention_decode_kernel(const Args a) {
+__global__ void __launch_bounds__(kThreads, Shape<kE4m3, DC>::kBlocks) attention_decode_kernel(const Args a, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v) {
   using S = Shape<kE4m3, DC>;
   using VT = typename Piece<S::kVB * S::kElt>::T;
   constexpr int kUnit = kWarps * S::kKeys, kHeads = 8 * NT, kMT = DC / 16;
-  __shared__ __align__(16) float so[kWarps][kHeads][DC + 4];      // (read and written two at a time)
+  extern __shared__ uint8_t room[];
+  uint8_t* const ring = room + (-smem_at(room) & 1023);      // each warp's stages; behind the loop, the warps' results
+  float(*const so)[kHeads][DC + 4] = reinterpret_cast<float(*)[kHeads][DC + 4]>(ring);
+  __shared__ float ring_scale[kE4m3 ? kWarps : 1][S::kStages][2][kE4m3 ? S::kKeys : 1];
+  __shared__ __align__(8) uint64_t bars[kWarps][S::kStages];
   __shared__ int cum[kPlanned + 1];
   __shared__ int warp_total[kWarps];
   __shared__ float ss[kWarps][kHeads][3];
-  mtf::chain_wait();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, r = lane >> 2, t = lane & 3;
+  if (lane == 0) {
+    for (int i = 0; i < S::kStages; ++i) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(smem_at(&bars[warp][i])) : "memory");
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  __syncwarp();
+  mtf::chain_wait();
   const int H = a.heads * a.chunks;
   const int capacity = (int)min((long long)a.per_sequence * a.slots, 0x7fffffffLL);
   auto length_of = [&](int s) {
@@ -171,6 +218,21 @@ __global__ void __launch_bounds__(kThreads, DC == 256 || (NT > 1 && DC == 128) ?
     u0 = 0;
     u1 = 1;
   }
+
+  // where this warp reads: its lanes' rows of K, its pieces of V's even and odd rows
+  const uint8_t* const mine = ring + warp * S::kStages * S::kStage;
+  const int key_r = key_of_row<S::kRow>(r);
+  const int at_k = key_r * S::kRow + swizzled<S::kRow>(key_r, t) * 16;
+  const int piece = S::kRow == 128 ? (r & 1) << 2 | r >> 1 : r;
+  int at_v[2];
+#pragma unroll
+  for (int e = 0; e < 2; ++e) {
+    const int key = key_of_row<S::kRow>(2 * t + e);
+    at_v[e] = key * S::kRow + (sizeof(VT) == 16 ? swizzled<S::kRow>(key, piece) * 16 : swizzled<S::kRow>(key, piece >> 1) * 16 + (piece & 1) * 8);
+  }
+  uint32_t into = 0, from = 0;                       // the stage that is filled next, and the one that is used next; bit 8: the parity of its barrier's phase
+  bool gone = false;                                 // a wait was given up: no keys from there on
+  auto onward = [](uint32_t x) { return (x & 255) + 1 == S::kStages ? (x & 256) ^ 256 : x + 1; };
 
   for (long long u = u0; u < u1;) {
     // ---- the item, and the part of it that is this block's
@@ -271,99 +333,131 @@ __global__ void __launch_bounds__(kThreads, DC == 256 || (NT > 1 && DC == 128) ?
     }
 
     const int32_t* const pages = a.table + (long long)seq * a.per_sequence;
-    // rows of a chunk's keys, key i with lane i % 32; -1: not there
-    auto rows_of = [&](int step, int (&row)[S::kIndexes]) {
+    auto page_of = [&](int m) { return (int)((unsigned long long)(uint32_t)m * a.slots_mul >> a.slots_shift); };
+    // The keys of a step's chunk, key i with lane i % 32: their pages' ids, asked for a step before they are needed.
+    auto ask_pages = [&](int step, int (&page)[S::kIndexes]) {
 #pragma unroll
       for (int i = 0; i < S::kIndexes; ++i) {
         const int m = (step * kWarps + warp) * S::kKeys + i * 32 + lane;
-        row[i] = -1;
-        if (step < j1 && m < n && (S::kKeys >= 32 || lane < S::kKeys)) {
-          const int index = (int)((unsigned long long)(uint32_t)m * a.slots_mul >> a.slots_shift);
-          const int page = pages[index];
-          if (page >= 0 && page < a.pages) row[i] = page * a.rows_page + (m - index * a.slots) * a.row_slot + head * a.row_head;
-          else atomicExch(&g_bad_page, 1);
-        }
+        page[i] = 0;
+        if (step < j1 && m < n && (S::kKeys >= 32 || lane < S::kKeys)) page[i] = pages[page_of(m)];
       }
     };
-    uint4 kr[S::kTiles][2][S::kKP];
-    VT vr[S::kTiles][4][S::kVP];
-    float ksr[S::kTiles][2], vsr[S::kTiles][2];
-    auto load_k = [&](const int (&row)[S::kIndexes]) {
+    // Chunks come as boxes of box_rows keys by kRow bytes, which no page's end cuts; lane i asks for boxes i, i + 32, ..  Keys without a place (behind the
+    // last, or of a page that is none) come as zeros, from a page behind the pool, and have no bit in the mask.
+    const int boxes = S::kKeys / a.box_rows * 2 * S::kBoxes;
+    auto fetch = [&](int step, const int (&asked)[S::kIndexes], uint32_t (&there)[S::kIndexes]) {
+      const uint32_t bar = smem_at(&bars[warp][into & 255]), to = smem_at(mine) + (into & 255) * S::kStage;
+      const int m0 = (step * kWarps + warp) * S::kKeys;
+      int page[S::kIndexes];
 #pragma unroll
-      for (int c = 0; c < S::kTiles; ++c)
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const int key = c * 16 + e * 8;
-          const int x = __shfl_sync(0xffffffffu, row[key / 32], key % 32 + r);
-          const uint8_t* const p = a.k + (long long)x * a.dk * S::kElt + t * 16;
-#pragma unroll
-          for (int i = 0; i < S::kKP; ++i) {
-            kr[c][e][i] = make_uint4(0u, 0u, 0u, 0u);
-            if (x >= 0 && (i * 4 + t) * S::kTB < a.dk) kr[c][e][i] = load16(p + i * 64);
-          }
-          if (kE4m3) ksr[c][e] = x >= 0 ? a.ks[x] : 0.f;
+      for (int i = 0; i < S::kIndexes; ++i) {
+        bool in = m0 + i * 32 + lane < n && (S::kKeys >= 32 || lane < S::kKeys);
+        if (in && (uint32_t)asked[i] >= (uint32_t)a.pages) {
+          atomicExch(&g_bad_page, 1);
+          in = false;
         }
-    };
-    auto load_v = [&](const int (&row)[S::kIndexes]) {
-#pragma unroll
-      for (int c = 0; c < S::kTiles; ++c)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int key = c * 16 + (e >> 1) * 8 + (e & 1);
-          const int x = __shfl_sync(0xffffffffu, row[key / 32], key % 32 + 2 * t);
-          const uint8_t* const p = a.v + ((long long)x * a.dv + r * S::kVB) * S::kElt;
-#pragma unroll
-          for (int i = 0; i < S::kVP; ++i) {
-            const bool in = x >= 0 && (i * 8 + r) * S::kVB < a.dv;
-            if constexpr (sizeof(VT) == 16) {
-              vr[c][e][i] = make_uint4(0u, 0u, 0u, 0u);
-              if (in) vr[c][e][i] = load16(p + i * 128);
-            } else {
-              vr[c][e][i] = make_uint2(0u, 0u);
-              if (in) vr[c][e][i] = load8(p + i * 64);
-            }
-          }
+        page[i] = in ? asked[i] : a.pages;
+        there[i] = __ballot_sync(0xffffffffu, in);
+      }
+      if (lane == 0) asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(S::kStage) : "memory");
+      __syncwarp();
+      for (int i0 = 0; i0 < boxes; i0 += 32) {
+        const int i = min(i0 + lane, boxes - 1), key = i / (2 * S::kBoxes) * a.box_rows, side = i / S::kBoxes & 1, box = i % S::kBoxes;
+        int pg = __shfl_sync(0xffffffffu, page[0], key & 31);
+        if (S::kIndexes > 1) {
+          const int pg1 = __shfl_sync(0xffffffffu, page[S::kIndexes - 1], key & 31);
+          pg = key >= 32 ? pg1 : pg;
         }
-      if (kE4m3)
+        const int m = m0 + key;
+        if (i0 + lane < boxes)
+          copy_box(to + side * S::kSide + (((key >> 4) * S::kBoxes + box) * 16 + (key & 15)) * S::kRow, side ? &map_v : &map_k, box * (S::kRow / S::kElt),
+                   m - page_of(m) * a.slots, head, pg, bar);
+      }
+      if (kE4m3) {
+        // scales, a key a lane
 #pragma unroll
-        for (int c = 0; c < S::kTiles; ++c)
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const int key = c * 16 + e * 8;
-            const int x = __shfl_sync(0xffffffffu, row[key / 32], key % 32 + r);
-            vsr[c][e] = x >= 0 ? a.vs[x] : 0.f;
+        for (int i = 0; i < S::kIndexes; ++i)
+          if (S::kKeys >= 32 || lane < S::kKeys) {
+            const int key = i * 32 + lane, m = m0 + key;
+            const bool in = there[i] >> lane & 1;
+            const int row = in ? page[i] * a.rows_page + (m - page_of(m) * a.slots) * a.row_slot + head * a.row_head : 0;
+            asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(smem_at(&ring_scale[warp][into & 255][0][key])), "l"(a.ks + row), "r"(in ? 4 : 0) : "memory");
+            asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(smem_at(&ring_scale[warp][into & 255][1][key])), "l"(a.vs + row), "r"(in ? 4 : 0) : "memory");
           }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+      }
+      into = onward(into);
     };
-
-    int row[S::kIndexes], next[S::kIndexes];
-    rows_of(j0, row);
-    load_k(row);
-    load_v(row);
-    rows_of(j0 + 1, next);
-    for (int step = j0; step < j1; ++step) {
-      // ---- logits
-      float s[S::kTiles][NT][4];
+    int page[S::kIndexes];
+    uint32_t there[S::kStages][S::kIndexes];         // of the stages, the oldest first
+    if (!gone) {
+      int first[S::kStages][S::kIndexes];
+#pragma unroll
+      for (int i = 0; i < S::kStages; ++i) ask_pages(j0 + i, first[i]);
+#pragma unroll
+      for (int i = 0; i < S::kStages; ++i)
+        if (j0 + i < j1) fetch(j0 + i, first[i], there[i]);
+        else if (kE4m3) asm volatile("cp.async.commit_group;" ::: "memory");
+      ask_pages(j0 + S::kStages, page);
+    }
+    for (int step = j0; step < j1 && !gone; ++step) {
+      const uint32_t bar = smem_at(&bars[warp][from & 255]), phase = from >> 8;
+      if (!landed(bar, phase) || (g_withhold && !landed(bar, phase ^ 1))) {
+        if (lane == 0) atomicCAS(&g_decode_status, 0, 0xB01);
+        gone = true;
+        for (uint32_t i = from; i != into; i = onward(i)) landed_late(smem_at(&bars[warp][i & 255]), i >> 8, kLandCycles);
+        break;
+      }
+      if (kE4m3) {
+        asm volatile("cp.async.wait_group %0;" ::"n"(S::kStages - 1) : "memory");
+        __syncwarp();
+      }
+      uint8_t* const stage = ring + warp * S::kStages * S::kStage + (from & 255) * S::kStage;
+      bool here_all = true;                          // no key is left out
+#pragma unroll
+      for (int i = 0; i < S::kIndexes; ++i) here_all &= there[0][i] == (S::kKeys < 32 ? (1u << (S::kKeys & 31)) - 1u : 0xffffffffu);
+      if (!here_all) {
+        // slots behind the last position may hold anything: zeros in their rows of V, which weights of 0 leave as they are
+        for (int i = lane; i < S::kSide / 16; i += 32) {
+          const int row = i / (S::kRow / 16), key = row / (16 * S::kBoxes) * 16 + row % 16;
+          if (!(there[0][S::kIndexes > 1 ? key / 32 : 0] >> (key & 31) & 1)) *reinterpret_cast<uint4*>(stage + S::kSide + i * 16) = make_uint4(0u, 0u, 0u, 0u);
+        }
+        __syncwarp();
+      }
+      // ---- logits; two sums where one would be a long chain
+      constexpr int kChains = S::kTiles * NT == 1 ? 2 : 1;
+      float s[S::kTiles][NT][4], s2[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int c = 0; c < S::kTiles; ++c) {
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) s[c][nt][0] = s[c][nt][1] = s[c][nt][2] = s[c][nt][3] = 0.f;
 #pragma unroll
-        for (int p = 0; p < S::kKP; ++p)
+        for (int p = 0; p < S::kKP; ++p) {
+          // piece 4p + t of the row: of box p / 2, its first or second half (rows of 64 bytes: all of it)
+          const int in_box = S::kRow == 128 ? p & 1 : 0, block = (c * S::kBoxes + (S::kRow == 128 ? p / 2 : 0)) * 16 * S::kRow;
+          const uint8_t* const from_k = stage + block + (at_k ^ (in_box * 64));
+          const uint4 k0 = *reinterpret_cast<const uint4*>(from_k);
+          const uint4 k1 = *reinterpret_cast<const uint4*>(from_k + 8 * S::kRow);
 #pragma unroll
           for (int j = 0; j < S::kSteps; ++j) {
             uint32_t a0, a1, a2, a3;
             if (kE4m3) {
-              const uint32_t x = word(kr[c][0][p], j), y = word(kr[c][1][p], j);
-              a0 = halves(x); a2 = halves(x >> 16);
-              a1 = halves(y); a3 = halves(y >> 16);
+              halves(word(k0, j), a0, a2);
+              halves(word(k1, j), a1, a3);
             } else {
-              a0 = word(kr[c][0][p], 2 * j); a2 = word(kr[c][0][p], 2 * j + 1);
-              a1 = word(kr[c][1][p], 2 * j); a3 = word(kr[c][1][p], 2 * j + 1);
+              a0 = word(k0, 2 * j); a2 = word(k0, 2 * j + 1);
+              a1 = word(k1, 2 * j); a3 = word(k1, 2 * j + 1);
             }
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) mma<kE4m3>(s[c][nt], a0, a1, a2, a3, qf[nt][p * S::kSteps + j][0], qf[nt][p * S::kSteps + j][1]);
+            for (int nt = 0; nt < NT; ++nt)
+              mma<kE4m3>(kChains == 2 && (p & 1) ? s2 : s[c][nt], a0, a1, a2, a3, qf[nt][p * S::kSteps + j][0], qf[nt][p * S::kSteps + j][1]);
           }
+        }
       }
+      if (kChains == 2)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[0][0][i] += s2[i];
       // in the scale of exp2; keys that are not there -infinity
       float tv[S::kTiles][2];                        // e4m3: log2 of the scale of V's row
       float xl[NT][2], xo[NT][2];
@@ -374,21 +468,25 @@ __global__ void __launch_bounds__(kThreads, DC == 256 || (NT > 1 && DC == 128) ?
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
           const int key = c * 16 + e * 8;
-          const bool in = __shfl_sync(0xffffffffu, row[key / 32], key % 32 + r) >= 0;
-          if (kE4m3) tv[c][e] = __log2f(vsr[c][e]);
+          float ks = 1.f;
+          if (kE4m3) {
+            ks = ring_scale[warp][from & 255][0][key + key_r];
+            tv[c][e] = __log2f(ring_scale[warp][from & 255][1][key + key_r]);
+          }
+          bool in = true;
+          if (!here_all) in = there[0][key / 32] >> (key % 32 + key_r) & 1;
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
               float x = s[c][nt][2 * e + h] * factor[nt][h];
-              if (kE4m3) x *= ksr[c][e];
+              if (kE4m3) x *= ks;
               if (!in) x = -INFINITY;
               s[c][nt][2 * e + h] = x;
               xl[nt][h] = fmaxf(xl[nt][h], x);
               if (kE4m3) xo[nt][h] = fmaxf(xo[nt][h], in ? x + tv[c][e] : -INFINITY);
             }
         }
-      load_k(next);                                  // K of this chunk is used up
       bool rise = false;
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
@@ -462,25 +560,45 @@ __global__ void __launch_bounds__(kThreads, DC == 256 || (NT > 1 && DC == 128) ?
 #pragma unroll
       for (int c = 0; c < S::kTiles; ++c)
 #pragma unroll
-        for (int p = 0; p < S::kVP; ++p)
+        for (int p = 0; p < S::kVP; ++p) {
+          VT v[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[e] = *reinterpret_cast<const VT*>(stage + S::kSide + (c * S::kBoxes + p) * 16 * S::kRow + at_v[e & 1] + (e >> 1) * 8 * S::kRow);
 #pragma unroll
           for (int w = 0; w < (int)sizeof(VT) / 4; ++w) {
-            const uint32_t x0 = word(vr[c][0][p], w), x1 = word(vr[c][1][p], w), x2 = word(vr[c][2][p], w), x3 = word(vr[c][3][p], w);
-#pragma unroll
+            const uint32_t x0 = word(v[0], w), x1 = word(v[1], w), x2 = word(v[2], w), x3 = word(v[3], w);
             for (int i = 0; i < (kE4m3 ? 2 : 1); ++i) {
-              uint32_t y0 = x0, y1 = x1, y2 = x2, y3 = x3;
-              if (kE4m3) { y0 = halves(x0 >> (16 * i)); y1 = halves(x1 >> (16 * i)); y2 = halves(x2 >> (16 * i)); y3 = halves(x3 >> (16 * i)); }
-              const uint32_t a0 = prmt(y0, y1, 0x5410), a1 = prmt(y0, y1, 0x7632), a2 = prmt(y2, y3, 0x5410), a3 = prmt(y2, y3, 0x7632);
+              // pairs of keys (2t, 2t + 1), (2t + 8, 2t + 9) of one column, two columns
+              uint32_t a0, a1, a2, a3;
+              if (kE4m3) {
+                halves(prmt(x0, x1, i ? 0x7362 : 0x5140), a0, a1);
+                halves(prmt(x2, x3, i ? 0x7362 : 0x5140), a2, a3);
+              } else {
+                a0 = prmt(x0, x1, 0x5410); a1 = prmt(x0, x1, 0x7632);
+                a2 = prmt(x2, x3, 0x5410); a3 = prmt(x2, x3, 0x7632);
+              }
               const int tile = p * (S::kVB / 2) + w * (kE4m3 ? 2 : 1) + i;
 #pragma unroll
               for (int nt = 0; nt < NT; ++nt) mma<kE4m3>(o[nt][tile], a0, a1, a2, a3, pb[c][nt][0], pb[c][nt][1]);
             }
           }
-      load_v(next);
+        }
+      // ---- the stage is used up: the chunk behind those under way
+      from = onward(from);
 #pragma unroll
-      for (int i = 0; i < S::kIndexes; ++i) row[i] = next[i];
-      rows_of(step + 2, next);
+      for (int i = 0; i + 1 < S::kStages; ++i)
+#pragma unroll
+        for (int j = 0; j < S::kIndexes; ++j) there[i][j] = there[i + 1][j];
+      if (step + S::kStages < j1) {
+        if (!here_all) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");      // (zeros were written there)
+        __syncwarp();                                // every lane has read it
+        fetch(step + S::kStages, page, there[S::kStages - 1]);
+        ask_pages(step + S::kStages + 1, page);
+      } else if (kE4m3) {
+        asm volatile("cp.async.commit_group;" ::: "memory");
+      }
     }
+    __syncthreads();                                 // (the results below lie over all warps' stages)
 
     // ---- the four warps' sums, in order
 #pragma unroll
@@ -499,7 +617,7 @@ __global__ void __launch_bounds__(kThreads, DC == 256 || (NT > 1 && DC == 128) ?
 #pragma unroll
         for (int i = 0; i < kMT; ++i) {
           constexpr int kHalfPiece = S::kVB / 2;
-          const int d = (i / kHalfPiece) * 8 * S::kVB + r * S::kVB + (i % kHalfPiece) * 2;
+          const int d = (i / kHalfPiece) * 8 * S::kVB + piece * S::kVB + (i % kHalfPiece) * 2;
           *reinterpret_cast<float2*>(&so[warp][g][d]) = make_float2(o[nt][i][h], o[nt][i][2 + h]);
         }
       }
@@ -532,46 +650,108 @@ __global__ void __launch_bounds__(kThreads, DC == 256 || (NT > 1 && DC == 128) ?
         if (d == 0) *reinterpret_cast<float4*>(a.part_s + ((long long)slot * kHeads + g) * 4) = make_float4(top_l, sum, top_o, 0.f);
       }
     }
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");     // (copies may come over the results from here on)
     __syncthreads();
   }
 }
 
-// Joins the parts of the item that starts last in block b and goes on behind it: one in b, and the first of every block up to the item's last.
+// Joins the parts of the item that starts last in block b and goes on behind it: one in b, and the first of every block up to the item's last.  Each part's
+// factor is worked out once; then a thread adds up four columns of a head, in the parts' order, with some loads under way at once.
+constexpr int kJoined = 64;                          // parts at a time
 template <int kHeads, int DC>
 __global__ void __launch_bounds__(256) attention_decode_join_kernel(const Args a) {
+  __shared__ float factor[kHeads][kJoined];
+  __shared__ float tops[kHeads][2], sums[kHeads], again[kHeads];
   mtf::chain_wait_only();
   const int4 piece = a.pieces[blockIdx.x];
   if (piece.x < 0) return;
-  const int head = piece.y / a.chunks, g0 = (piece.y - head * a.chunks) * kHeads;
-  const int here = min(kHeads, a.group - g0);
-  for (int i = threadIdx.x; i < here * (a.dv / 2); i += 256) {
-    const int g = i / (a.dv / 2), d = 2 * (i % (a.dv / 2));
-    float top_l = -INFINITY, top_o = -INFINITY, sum = 0.f, x = 0.f, y = 0.f;
-    for (int b = blockIdx.x; b <= piece.z; ++b) {
-      const long long at = (long long)(b == (int)blockIdx.x ? piece.w : 2 * b) * kHeads + g;
-      const float4 s = *reinterpret_cast<const float4*>(a.part_s + at * 4);
-      const float2 v = *reinterpret_cast<const float2*>(a.part_o + at * DC + d);
-      const float ml = fmaxf(top_l, s.x), mo = fmaxf(top_o, s.z);
-      const float f0 = top_l == ml ? 1.f : ex2(top_l - ml), f1 = s.x == ml ? 1.f : ex2(s.x - ml);
-      const float e0 = top_o == mo ? 1.f : ex2(top_o - mo), e1 = s.z == mo ? 1.f : ex2(s.z - mo);
-      sum = sum * f0 + s.y * f1;
-      x = x * e0 + v.x * e1;
-      y = y * e0 + v.y * e1;
-      top_l = ml;
-      top_o = mo;
+  const int head = piece.y / a.chunks, g0 = (piece.y - head * a.chunks) * kHeads, here = min(kHeads, a.group - g0);
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, parts = piece.z - (int)blockIdx.x + 1;
+  auto place = [&](int i) { return (long long)(i == 0 ? piece.w : 2 * ((int)blockIdx.x + i)) * kHeads; };
+  if (tid < kHeads) {
+    tops[tid][0] = tops[tid][1] = -INFINITY;
+    sums[tid] = 0.f;
+  }
+  constexpr int kFours = (kHeads * DC / 4 + 255) / 256;        // of a thread
+  float4 sum[kFours];
+#pragma unroll
+  for (int j = 0; j < kFours; ++j) sum[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int i0 = 0; i0 < parts; i0 += kJoined) {
+    const int some = min(kJoined, parts - i0);
+    __syncthreads();
+    for (int g = warp; g < here; g += 8) {           // a warp a head
+      float4 s[kJoined / 32];
+      float ml = tops[g][0], mo = tops[g][1];
+#pragma unroll
+      for (int j = 0; j < kJoined / 32; ++j) {
+        s[j] = make_float4(-INFINITY, 0.f, -INFINITY, 0.f);
+        if (j * 32 + lane < some) s[j] = *reinterpret_cast<const float4*>(a.part_s + (place(i0 + j * 32 + lane) + g) * 4);
+        ml = fmaxf(ml, s[j].x);
+        mo = fmaxf(mo, s[j].z);
+      }
+#pragma unroll
+      for (int w = 16; w > 0; w /= 2) {
+        ml = fmaxf(ml, __shfl_xor_sync(0xffffffffu, ml, w));
+        mo = fmaxf(mo, __shfl_xor_sync(0xffffffffu, mo, w));
+      }
+      float l = 0.f;
+#pragma unroll
+      for (int j = 0; j < kJoined / 32; ++j) {
+        l += s[j].y * (s[j].x == ml ? 1.f : ex2(s[j].x - ml));
+        factor[g][j * 32 + lane] = s[j].z == mo ? 1.f : ex2(s[j].z - mo);
+      }
+#pragma unroll
+      for (int w = 16; w > 0; w /= 2) l += __shfl_xor_sync(0xffffffffu, l, w);
+      if (lane == 0) {
+        again[g] = tops[g][1] == mo ? 1.f : ex2(tops[g][1] - mo);
+        sums[g] = sums[g] * (tops[g][0] == ml ? 1.f : ex2(tops[g][0] - ml)) + l;
+        tops[g][0] = ml;
+        tops[g][1] = mo;
+      }
     }
-    const float f = sum == 0.f ? 0.f : (top_o == top_l ? 1.f : ex2(top_o - top_l)) / sum;
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < kFours; ++j) {
+      const int at = (j * 256 + tid) * 4, g = at / DC, d = at % DC;
+      if (g >= here || d >= a.dv) continue;
+      const float f = again[g];
+      sum[j] = make_float4(sum[j].x * f, sum[j].y * f, sum[j].z * f, sum[j].w * f);
+      constexpr int kDeep = 8;
+      for (int i = 0; i < some; i += kDeep) {
+        float4 v[kDeep];
+#pragma unroll
+        for (int e = 0; e < kDeep; ++e) v[e] = *reinterpret_cast<const float4*>(a.part_o + (place(i0 + min(i + e, some - 1)) + g) * DC + d);
+#pragma unroll
+        for (int e = 0; e < kDeep; ++e)
+          if (i + e < some) {
+            const float w = factor[g][i + e];
+            sum[j].x += v[e].x * w;
+            sum[j].y += v[e].y * w;
+            sum[j].z += v[e].z * w;
+            sum[j].w += v[e].w * w;
+          }
+      }
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < kFours; ++j) {
+    const int at = (j * 256 + tid) * 4, g = at / DC, d = at % DC;
+    if (g >= here || d >= a.dv) continue;
+    const float l = sums[g], f = l == 0.f ? 0.f : (tops[g][1] == tops[g][0] ? 1.f : ex2(tops[g][1] - tops[g][0])) / l;
     __nv_bfloat162* const to = reinterpret_cast<__nv_bfloat162*>(a.o + ((((long long)piece.x * a.heads + head) * a.group + g0 + g) * a.dv + d));
-    *to = __floats2bfloat162_rn(sum == 0.f ? 0.f : x * f, sum == 0.f ? 0.f : y * f);
+    to[0] = __floats2bfloat162_rn(l == 0.f ? 0.f : sum[j].x * f, l == 0.f ? 0.f : sum[j].y * f);
+    to[1] = __floats2bfloat162_rn(l == 0.f ? 0.f : sum[j].z * f, l == 0.f ? 0.f : sum[j].w * f);
   }
 }
 
 int width_class(const mtf::CachePool& c) {
   const int d = std::max(c.dk, c.dv);
-  return d <= 64 ? 64 : d <= 128 ? 128 : 256;
+  // (rows of 64 bytes are copied two at least at a time, to where 128 bytes begin: a page of an odd number of slots has wider ones)
+  if (d <= 64) return c.e4m3 && c.slots % 2 ? 128 : 64;
+  return d <= 128 ? 128 : 256;
 }
 int tiles_of_heads(const mtf::CachePool& c, int group) { return group > 8 && width_class(c) < 256 ? 2 : 1; }
-int blocks_an_sm(int dc, int nt) { return dc == 256 || (nt > 1 && dc == 128) ? 2 : 3; }
+int blocks_an_sm(const mtf::CachePool& c) { return width_class(c) == 256 && !c.e4m3 ? Shape<false, 256>::kBlocks : Shape<false, 128>::kBlocks; }
 
 // Items of at most this many positions are not cut: a block takes one whole.
 constexpr long long kWholeItem = 256;
@@ -587,25 +767,59 @@ bool balanced(const mtf::CachePool& c) {
 }
 int grid_of(const mtf::CachePool& c, int group) {
   const int nt = tiles_of_heads(c, group), chunks = (group + 8 * nt - 1) / (8 * nt);
-  const long long most = (long long)mtf::device_sm_count() * blocks_an_sm(width_class(c), nt);
+  const long long most = (long long)mtf::device_sm_count() * blocks_an_sm(c);
   const long long units = c.sequences * c.heads * chunks * (((long long)c.per_sequence * c.slots + unit_keys(c) - 1) / unit_keys(c));
   return (int)std::max(1LL, std::min(most, units / kLeastUnits));
 }
 
+typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*, const cuuint32_t*,
+                                  CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+EncodeTiledFn encoder() {
+  static EncodeTiledFn fn = nullptr;
+  static std::once_flag once;
+  std::call_once(once, [] {
+    void* p = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) == cudaSuccess && q == cudaDriverEntryPointSuccess) fn = reinterpret_cast<EncodeTiledFn>(p);
+  });
+  return fn;
+}
+// a pool as [page][head][slot][d], whichever of slot and head lies inside; boxes of `rows` slots of a head, `row` bytes wide
+mtf_status pool_map(CUtensorMap* m, const void* pool, const mtf::CachePool& c, int width, int rows, int row) {
+  EncodeTiledFn enc = encoder();
+  if (!enc) return mtf::fail(MTF_ERR_CUDA, "cuTensorMapEncodeTiled is not available from the driver");
+  const cuuint64_t elt = c.e4m3 ? 1 : 2, bytes = width * elt;
+  const cuuint64_t d[4] = {(cuuint64_t)width, (cuuint64_t)c.slots, (cuuint64_t)c.heads, (cuuint64_t)c.pages};
+  const cuuint64_t s[3] = {bytes * c.row_slot, bytes * c.row_head, bytes * c.rows_page};
+  const cuuint32_t box[4] = {(cuuint32_t)(row / elt), (cuuint32_t)rows, 1, 1}, es[4] = {1, 1, 1, 1};
+  const CUresult r = mtf::in_context([&] { return enc(m, c.e4m3 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(pool), d, s, box, es,
+                                                      CU_TENSOR_MAP_INTERLEAVE_NONE, row == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+                                                      CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE); });
+  return r == CUDA_SUCCESS ? MTF_OK : mtf::fail(MTF_ERR_CUDA, "cuTensorMapEncodeTiled failed with %d", (int)r);
+}
+
 template <bool kE4m3, int DC, int NT>
-void launch(const Args& a, int grid, cudaStream_t st) {
-  mtf::launch_chained(attention_decode_kernel<kE4m3, DC, NT>, (unsigned)grid, kThreads, 0, st, a);
+mtf_status launch(const Args& a, const mtf::CachePool& c, int grid, cudaStream_t st) {
+  using S = Shape<kE4m3, DC>;
+  CUtensorMap map_k, map_v;
+  mtf_status ok = pool_map(&map_k, c.k, c, c.dk, a.box_rows, S::kRow);
+  if (ok != MTF_OK || (ok = pool_map(&map_v, c.v, c, c.dv, a.box_rows, S::kRow)) != MTF_OK) return ok;
+  constexpr int kResults = kWarps * 8 * NT * (DC + 4) * 4, kRoom = 1024 + (S::kRing > kResults ? S::kRing : kResults);
+  const cudaError_t e = cudaFuncSetAttribute(attention_decode_kernel<kE4m3, DC, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kRoom);
+  if (e != cudaSuccess) return mtf::fail(MTF_ERR_CUDA, "attention_decode_kernel: %s", cudaGetErrorString(e));
+  mtf::launch_chained(attention_decode_kernel<kE4m3, DC, NT>, (unsigned)grid, kThreads, kRoom, st, a, map_k, map_v);
   mtf::count_launch();
   if (a.balanced && grid > 1) {
     mtf::launch_chained(attention_decode_join_kernel<8 * NT, DC>, (unsigned)grid - 1, 256, 0, st, a);
     mtf::count_launch();
   }
+  return MTF_OK;
 }
 template <bool kE4m3>
-void dispatch(const Args& a, int dc, int nt, int grid, cudaStream_t st) {
-  if (dc == 256) launch<kE4m3, 256, 1>(a, grid, st);
-  else if (dc == 128) nt == 1 ? launch<kE4m3, 128, 1>(a, grid, st) : launch<kE4m3, 128, 2>(a, grid, st);
-  else nt == 1 ? launch<kE4m3, 64, 1>(a, grid, st) : launch<kE4m3, 64, 2>(a, grid, st);
+mtf_status dispatch(const Args& a, const mtf::CachePool& c, int dc, int nt, int grid, cudaStream_t st) {
+  if (dc == 256) return launch<kE4m3, 256, 1>(a, c, grid, st);
+  if (dc == 128) return nt == 1 ? launch<kE4m3, 128, 1>(a, c, grid, st) : launch<kE4m3, 128, 2>(a, c, grid, st);
+  return nt == 1 ? launch<kE4m3, 64, 1>(a, c, grid, st) : launch<kE4m3, 64, 2>(a, c, grid, st);
 }
 
 }  // namespace
@@ -622,8 +836,6 @@ mtf_status launch_attention_decode(const CachePool& c, const DecodeCall& d, void
   const int dc = width_class(c), nt = tiles_of_heads(c, d.group);
   Args a = {};
   a.q = reinterpret_cast<const __nv_bfloat16*>(d.q);
-  a.k = reinterpret_cast<const uint8_t*>(c.k);
-  a.v = reinterpret_cast<const uint8_t*>(c.v);
   a.ks = c.ks;
   a.vs = c.vs;
   a.table = c.table;
@@ -646,6 +858,8 @@ mtf_status launch_attention_decode(const CachePool& c, const DecodeCall& d, void
   while ((1LL << n) < c.slots) ++n;
   a.slots_mul = (uint32_t)(((1ULL << (31 + n)) + c.slots - 1) / c.slots);
   a.slots_shift = 31 + n;
+  a.box_rows = 16;
+  while (c.slots % a.box_rows) a.box_rows /= 2;
   a.scale_log2 = d.scale * kLog2e;
   a.balanced = balanced(c);
   long long grid = a.balanced ? grid_of(c, d.group) : c.sequences * c.heads * a.chunks;
@@ -656,8 +870,8 @@ mtf_status launch_attention_decode(const CachePool& c, const DecodeCall& d, void
     a.part_s = reinterpret_cast<float*>(a.pieces + grid);
     a.part_o = a.part_s + (size_t)grid * 2 * heads * 4;
   }
-  if (c.e4m3) dispatch<true>(a, dc, nt, (int)grid, (cudaStream_t)stream);
-  else dispatch<false>(a, dc, nt, (int)grid, (cudaStream_t)stream);
+  const mtf_status st = c.e4m3 ? dispatch<true>(a, c, dc, nt, (int)grid, (cudaStream_t)stream) : dispatch<false>(a, c, dc, nt, (int)grid, (cudaStream_t)stream);
+  if (st != MTF_OK) return st;
   const cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess) return fail(MTF_ERR_CUDA, "attention_decode_kernel: %s", cudaGetErrorString(e));
   return MTF_OK;
@@ -670,6 +884,22 @@ mtf_status read_decode_bad_page(int* seen) {
   if (e != cudaSuccess) return fail(MTF_ERR_CUDA, "cudaMemcpyFromSymbol: %s", cudaGetErrorString(e));
   if (v) { int z = 0; cudaMemcpyToSymbol(g_bad_page, &z, sizeof(int)); }
   *seen = v;
+  return MTF_OK;
+}
+
+mtf_status debug_decode_wait_test(long long limit_cycles, int withhold) {
+  const long long limit = limit_cycles > 0 ? limit_cycles : kWaitCycles;
+  cudaError_t e = cudaMemcpyToSymbol(g_wait_limit, &limit, sizeof(limit));
+  if (e == cudaSuccess) e = cudaMemcpyToSymbol(g_withhold, &withhold, sizeof(int));
+  if (e != cudaSuccess) return fail(MTF_ERR_CUDA, "cudaMemcpyToSymbol: %s", cudaGetErrorString(e));
+  return MTF_OK;
+}
+mtf_status read_decode_status(int* code) {
+  int v = 0;
+  cudaError_t e = cudaMemcpyFromSymbol(&v, g_decode_status, sizeof(int));
+  if (e != cudaSuccess) return fail(MTF_ERR_CUDA, "cudaMemcpyFromSymbol: %s", cudaGetErrorString(e));
+  if (v) { int z = 0; cudaMemcpyToSymbol(g_decode_status, &z, sizeof(int)); }
+  *code = v;
   return MTF_OK;
 }
 

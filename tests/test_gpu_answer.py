@@ -192,9 +192,9 @@ def test_attention(mtf, dtype, shape, slot_first):
 @pytest.mark.parametrize("dtype", ["bf16", "e4m3"])
 def test_attention_many_sequences(mtf, dtype):
     """More sequences than a block's plan, and just as many as it takes; few of them have positions."""
-    for n_seq in (2049, 2048):
+    for n_seq in (2049, 1025, 1024):
         lengths = [0] * n_seq
-        for i in (0, 7, 1000, 2047, n_seq - 1):
+        for i in (0, 7, 1000, 1020, n_seq - 1):
             lengths[i] = 1 + i % 400
         p = Paged(mtf, dtype, lengths, 1, 64, 64, 16, per=30, seed=5)
         q, o = decode(mtf, p, 2, 64, 64, 0.125)
