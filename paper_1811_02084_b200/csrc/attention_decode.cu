@@ -28,7 +28,10 @@ namespace {
 constexpr int kWarps = 4;
 constexpr int kThreads = 32 * kWarps;
 constexpr int kPlanned = 1024;        // sequences whose units a block adds up by itself
-constexpr int kLeastUnits = 2;        // a block's run
+constexpr int kSteps = 2, kMostSteps = 8;
+constexpr int kMostBlocks = 8;        // of a cluster
+constexpr int kOver = 3;              // units that an item costs beside its own: first loads, joining
+constexpr int kLeastCost = 5;         // a block's run
 constexpr float kLog2e = 1.4426950408889634f;
 // The running maximum is raised only where a logit lies 2^6 above it: otherwise every chunk would pay for a maximum across lanes.
 constexpr float kSlack = 6.f;
@@ -46,7 +49,8 @@ struct Args {
   int slots_shift;
   float scale_log2;
   int box_rows;                                  // keys of a copied box: a power of two up to 16 that divides a page's slots
-  int balanced;
+  int balanced;                                  // all blocks share all units evenly; else an item is one cluster's
+  int cluster;
   float* part_o;                                 // [block][2][8 NT][DC]
   float* part_s;                                 // [block][2][8 NT][4]: reference of l, l, reference of o
   int4* pieces;                                  // [block]: of the item that starts last in it and goes on: sequence, head and chunk, its last block, slot
@@ -139,6 +143,26 @@ __device__ __forceinline__ bool landed(uint32_t bar, uint32_t parity) {
   else ok = true;
   return ok;
 }
+// another block of the cluster's shared memory, and the barrier of all its threads
+__device__ __forceinline__ uint32_t in_block(uint32_t at, int rank) {
+  uint32_t x;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(x) : "r"(at), "r"(rank));
+  return x;
+}
+__device__ __forceinline__ float far(uint32_t at) {
+  float x;
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(x) : "r"(at) : "memory");
+  return x;
+}
+__device__ __forceinline__ float2 far2(uint32_t at) {
+  float2 x;
+  asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(x.x), "=f"(x.y) : "r"(at) : "memory");
+  return x;
+}
+__device__ __forceinline__ void cluster_barrier() {
+  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
 __device__ __forceinline__ void copy_box(uint32_t to, const CUtensorMap* map, int d, int slot, int head, int page, uint32_t bar) {
   asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(to), "l"(map), "r"(d), "r"(slot),
                "r"(head), "r"(page), "r"(bar)
@@ -160,7 +184,8 @@ __global__ void __launch_bounds__(kThreads, Shape<kE4m3, DC>::kBlocks) attention
   __shared__ __align__(8) uint64_t bars[kWarps][S::kStages];
   __shared__ int cum[kPlanned + 1];
   __shared__ int warp_total[kWarps];
-  __shared__ float ss[kWarps][kHeads][3];
+  __shared__ float ss[kWarps + 1][kHeads][3];        // (the last: the block's)
+  float(*const block_o)[DC + 4] = so[kWarps];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, r = lane >> 2, t = lane & 3;
   if (lane == 0) {
     for (int i = 0; i < S::kStages; ++i) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(smem_at(&bars[warp][i])) : "memory");
@@ -170,6 +195,7 @@ __global__ void __launch_bounds__(kThreads, Shape<kE4m3, DC>::kBlocks) attention
   mtf::chain_wait();
   const int H = a.heads * a.chunks;
   const int capacity = (int)min((long long)a.per_sequence * a.slots, 0x7fffffffLL);
+  auto cost_of = [&](int n) { return n ? (n + kUnit - 1) / kUnit + kOver : 0; };
   auto length_of = [&](int s) {
     const int n = a.lengths[s];
     if ((n < 0 || n > capacity)) atomicExch(&g_bad_page, 1);
@@ -183,7 +209,7 @@ __global__ void __launch_bounds__(kThreads, Shape<kE4m3, DC>::kBlocks) attention
     const int each = (a.n_seq + kThreads - 1) / kThreads, s0 = tid * each;
     int sum = 0;
     for (int i = 0; i < each; ++i)
-      if (s0 + i < a.n_seq) sum += (length_of(s0 + i) + kUnit - 1) / kUnit;
+      if (s0 + i < a.n_seq) sum += cost_of(length_of(s0 + i));
     int upto = sum;
 #pragma unroll
     for (int o = 1; o < 32; o *= 2) {
@@ -197,13 +223,13 @@ __global__ void __launch_bounds__(kThreads, Shape<kE4m3, DC>::kBlocks) attention
     for (int i = 0; i < each; ++i)
       if (s0 + i < a.n_seq) {
         cum[s0 + i] = before;
-        before += (length_of(s0 + i) + kUnit - 1) / kUnit;
+        before += cost_of(length_of(s0 + i));
         if (s0 + i == a.n_seq - 1) cum[a.n_seq] = before;
       }
     __syncthreads();
     units = (long long)cum[a.n_seq] * H;
     // (no block without a unit among those that share them: a join goes from block to block)
-    blocks = (int)min((long long)blocks, max(1LL, units / kLeastUnits));
+    blocks = (int)min((long long)blocks, max(1LL, units / kLeastCost));
     u0 = u1 = 0;
     if ((int)blockIdx.x < blocks) {
       u0 = first_unit(units, blocks, blockIdx.x);
@@ -250,25 +276,25 @@ __global__ void __launch_bounds__(kThreads, Shape<kE4m3, DC>::kBlocks) attention
       const int each = cum[seq + 1] - cum[seq];
       const long long in = u - (long long)cum[seq] * H;
       hc = (int)(in / each);
-      j0 = (int)(in - (long long)hc * each);
-      j1 = (int)min((long long)each, j0 + (u1 - u));
-      whole = j0 == 0 && j1 == each;
+      const int x0 = (int)(in - (long long)hc * each), x1 = (int)min((long long)each, x0 + (u1 - u));
+      j0 = max(0, x0 - kOver);
+      j1 = max(0, x1 - kOver);
+      whole = j0 == 0 && j1 == each - kOver;
       slot = 2 * blockIdx.x + (u == u0 ? 0 : 1);
-      if (tid == 0 && j0 == 0 && !whole) {
-        const long long end = u + each;              // behind the item's last unit
-        const int last = (int)((end * blocks - 1) / units);
-        a.pieces[blockIdx.x] = make_int4(seq, hc, last, slot);
-      }
+      const long long end = u - x0 + each;           // behind the item
+      u += x1 - x0;
+      if (j0 == j1) continue;
+      if (tid == 0 && j0 == 0 && !whole) a.pieces[blockIdx.x] = make_int4(seq, hc, (int)((end * blocks - 1) / units), slot);
       n = length_of(seq);
-      u += j1 - j0;
     } else {
-      const long long item = blockIdx.x;
-      seq = (int)(item / H);
-      hc = (int)(item - (long long)seq * H);
+      const int item = blockIdx.x / a.cluster, rank = blockIdx.x - item * a.cluster;
+      seq = item / H;
+      hc = item - seq * H;
       n = length_of(seq);
-      j0 = 0;
-      j1 = (n + kUnit - 1) / kUnit;
-      whole = true;
+      const long long each = (n + kUnit - 1) / kUnit;
+      j0 = (int)(each * rank / a.cluster);
+      j1 = (int)(each * (rank + 1) / a.cluster);
+      whole = a.cluster == 1;
       u = 1;
     }
     const int head = hc / a.chunks, g0 = (hc - head * a.chunks) * kHeads;
@@ -645,10 +671,48 @@ __global__ void __launch_bounds__(kThreads, Shape<kE4m3, DC>::kBlocks) attention
           __nv_bfloat162* const to = reinterpret_cast<__nv_bfloat162*>(a.o + ((((long long)seq * a.heads + head) * a.group + g0 + g) * a.dv + d));
           *to = __floats2bfloat162_rn(sum == 0.f ? 0.f : x * f, sum == 0.f ? 0.f : y * f);
         }
-      } else {
+      } else if (a.balanced) {
         *reinterpret_cast<float2*>(a.part_o + ((long long)slot * kHeads + g) * DC + d) = make_float2(x, y);
         if (d == 0) *reinterpret_cast<float4*>(a.part_s + ((long long)slot * kHeads + g) * 4) = make_float4(top_l, sum, top_o, 0.f);
+      } else {
+        *reinterpret_cast<float2*>(&block_o[g][d]) = make_float2(x, y);
+        if (d == 0) { ss[kWarps][g][0] = top_l; ss[kWarps][g][1] = sum; ss[kWarps][g][2] = top_o; }
       }
+    }
+    if (!whole && !a.balanced) {
+      // ---- the blocks' sums, in order, each block its share of the columns
+      cluster_barrier();
+      const int rank = blockIdx.x % a.cluster;
+      for (int i = rank * kThreads + tid; i < here * (DC / 2); i += a.cluster * kThreads) {
+        const int g = i / (DC / 2), d = 2 * (i % (DC / 2));
+        if (d >= a.dv) continue;
+        const uint32_t at_s = smem_at(&ss[kWarps][g][0]), at_o = smem_at(&block_o[g][d]);
+        float bl[kMostBlocks], bs[kMostBlocks], bo[kMostBlocks], top_l = -INFINITY, top_o = -INFINITY, sum = 0.f, x = 0.f, y = 0.f;
+        float2 v[kMostBlocks];
+#pragma unroll
+        for (int c = 0; c < kMostBlocks; ++c) {
+          const int of = min(c, a.cluster - 1);
+          const uint32_t p = in_block(at_s, of);
+          bl[c] = far(p);
+          bs[c] = far(p + 4);
+          bo[c] = far(p + 8);
+          v[c] = far2(in_block(at_o, of));
+          top_l = fmaxf(top_l, bl[c]);
+          top_o = fmaxf(top_o, bo[c]);
+        }
+#pragma unroll
+        for (int c = 0; c < kMostBlocks; ++c)
+          if (c < a.cluster) {
+            sum += bs[c] * (bl[c] == top_l ? 1.f : ex2(bl[c] - top_l));
+            const float f = bo[c] == top_o ? 1.f : ex2(bo[c] - top_o);
+            x += v[c].x * f;
+            y += v[c].y * f;
+          }
+        const float f = sum == 0.f ? 0.f : (top_o == top_l ? 1.f : ex2(top_o - top_l)) / sum;
+        __nv_bfloat162* const to = reinterpret_cast<__nv_bfloat162*>(a.o + ((((long long)seq * a.heads + head) * a.group + g0 + g) * a.dv + d));
+        *to = __floats2bfloat162_rn(sum == 0.f ? 0.f : x * f, sum == 0.f ? 0.f : y * f);
+      }
+      cluster_barrier();                             // (no block leaves while others read what it has)
     }
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");     // (copies may come over the results from here on)
     __syncthreads();
@@ -753,23 +817,27 @@ int width_class(const mtf::CachePool& c) {
 int tiles_of_heads(const mtf::CachePool& c, int group) { return group > 8 && width_class(c) < 256 ? 2 : 1; }
 int blocks_an_sm(const mtf::CachePool& c) { return width_class(c) == 256 && !c.e4m3 ? Shape<false, 256>::kBlocks : Shape<false, 128>::kBlocks; }
 
-// Items of at most this many positions are not cut: a block takes one whole.
-constexpr long long kWholeItem = 256;
-
 int unit_keys(const mtf::CachePool& c) {
   const int row = width_class(c) * (c.e4m3 ? 1 : 2);
   return kWarps * 16 * (row <= 64 ? 4 : row <= 128 ? 2 : 1);
 }
-// (the sum of all sequences' units is kept in 32 bits)
-bool balanced(const mtf::CachePool& c) {
-  const long long most = (long long)c.per_sequence * c.slots;
-  return c.sequences <= kPlanned && most > kWholeItem && c.sequences * (most / unit_keys(c) + 1) < (1LL << 31);
-}
-int grid_of(const mtf::CachePool& c, int group) {
+
+// How a call's items (a head, or as many heads of queries as a block takes, of a sequence) are shared out.
+struct Plan {
+  bool balanced;
+  int cluster;
+  long long grid;
+};
+Plan plan_of(const mtf::CachePool& c, int group) {
   const int nt = tiles_of_heads(c, group), chunks = (group + 8 * nt - 1) / (8 * nt);
+  const long long items = c.sequences * c.heads * chunks, units = ((long long)c.per_sequence * c.slots + unit_keys(c) - 1) / unit_keys(c);
   const long long most = (long long)mtf::device_sm_count() * blocks_an_sm(c);
-  const long long units = c.sequences * c.heads * chunks * (((long long)c.per_sequence * c.slots + unit_keys(c) - 1) / unit_keys(c));
-  return (int)std::max(1LL, std::min(most, units / kLeastUnits));
+  int cluster = 1;
+  while (cluster < kMostBlocks && units > kSteps * cluster && items * cluster * 2 <= most) cluster *= 2;
+  // (the sum of all sequences' units is kept in 32 bits)
+  const bool balanced = units > kMostSteps * cluster && c.sequences <= kPlanned && c.sequences * (units + kOver) < (1LL << 31);
+  if (balanced) return {true, 1, std::max(1LL, std::min(most, items * (units + kOver) / kLeastCost))};
+  return {false, cluster, items * cluster};
 }
 
 typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*, const cuuint32_t*,
@@ -804,10 +872,27 @@ mtf_status launch(const Args& a, const mtf::CachePool& c, int grid, cudaStream_t
   CUtensorMap map_k, map_v;
   mtf_status ok = pool_map(&map_k, c.k, c, c.dk, a.box_rows, S::kRow);
   if (ok != MTF_OK || (ok = pool_map(&map_v, c.v, c, c.dv, a.box_rows, S::kRow)) != MTF_OK) return ok;
-  constexpr int kResults = kWarps * 8 * NT * (DC + 4) * 4, kRoom = 1024 + (S::kRing > kResults ? S::kRing : kResults);
+  constexpr int kResults = (kWarps + 1) * 8 * NT * (DC + 4) * 4, kRoom = 1024 + (S::kRing > kResults ? S::kRing : kResults);
   const cudaError_t e = cudaFuncSetAttribute(attention_decode_kernel<kE4m3, DC, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kRoom);
   if (e != cudaSuccess) return mtf::fail(MTF_ERR_CUDA, "attention_decode_kernel: %s", cudaGetErrorString(e));
-  mtf::launch_chained(attention_decode_kernel<kE4m3, DC, NT>, (unsigned)grid, kThreads, kRoom, st, a, map_k, map_v);
+  if (a.cluster == 1) {
+    mtf::launch_chained(attention_decode_kernel<kE4m3, DC, NT>, (unsigned)grid, kThreads, kRoom, st, a, map_k, map_v);
+  } else {
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute at[2];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = a.cluster;
+    at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
+    cfg.gridDim = dim3((unsigned)grid, 1, 1);
+    cfg.blockDim = dim3(kThreads, 1, 1);
+    cfg.dynamicSmemBytes = kRoom;
+    cfg.stream = st;
+    cfg.attrs = at;
+    cfg.numAttrs = 2;
+    (void)cudaLaunchKernelEx(&cfg, attention_decode_kernel<kE4m3, DC, NT>, a, map_k, map_v);
+  }
   mtf::count_launch();
   if (a.balanced && grid > 1) {
     mtf::launch_chained(attention_decode_join_kernel<8 * NT, DC>, (unsigned)grid - 1, 256, 0, st, a);
@@ -827,9 +912,10 @@ mtf_status dispatch(const Args& a, const mtf::CachePool& c, int dc, int nt, int 
 namespace mtf {
 
 size_t attention_decode_workspace(const CachePool& c, int group) {
-  if (!balanced(c)) return 0;
-  const size_t grid = grid_of(c, group), heads = 8 * tiles_of_heads(c, group);
-  return grid * 2 * heads * (width_class(c) + 4) * sizeof(float) + grid * sizeof(int4);
+  const Plan p = plan_of(c, group);
+  if (!p.balanced) return 0;
+  const size_t heads = 8 * tiles_of_heads(c, group);
+  return p.grid * 2 * heads * (width_class(c) + 4) * sizeof(float) + p.grid * sizeof(int4);
 }
 
 mtf_status launch_attention_decode(const CachePool& c, const DecodeCall& d, void* stream) {
@@ -861,8 +947,10 @@ mtf_status launch_attention_decode(const CachePool& c, const DecodeCall& d, void
   a.box_rows = 16;
   while (c.slots % a.box_rows) a.box_rows /= 2;
   a.scale_log2 = d.scale * kLog2e;
-  a.balanced = balanced(c);
-  long long grid = a.balanced ? grid_of(c, d.group) : c.sequences * c.heads * a.chunks;
+  const Plan p = plan_of(c, d.group);
+  const long long grid = p.grid;
+  a.balanced = p.balanced;
+  a.cluster = p.cluster;
   if (grid > 0x7fffffffLL) return fail(MTF_ERR_UNSUPPORTED, "attention_decode: at most 2^31 heads of sequences");
   if (a.balanced) {
     const size_t heads = 8 * nt;

@@ -185,7 +185,7 @@ def test_attention():
     refused("decode", lambda n: {"o": mtf.Named(n["o"].dims, n["o"].dtype, n["v"].ptr, n["v"].owner)})
     # a workspace is asked for where an item may be cut
     n = things()
-    n["table"] = ints(B, 512)
+    n["table"] = ints(B, 1 << 14)
     cache = mtf.Cache(n["k"], n["v"], n["table"])
     need = mtf.mtf_attention_decode_workspace_bytes(n["layout"], n["q"], cache)
     assert need > 0
