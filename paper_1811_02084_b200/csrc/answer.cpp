@@ -263,9 +263,11 @@ mtf_status mtf_beam_select(const mtf_layout_t* layout, const mtf_tensor* logits,
     if (new_finished) b.new_finished = result(new_finished, "new_finished");
     if (!c.ok()) return c.st;
     const size_t need = mtf::beam_select_workspace(sentences, (int)beams, (int)slots, (int)V);
-    if (!workspace || workspace_bytes < need) return mtf::fail(MTF_ERR_WORKSPACE_TOO_SMALL, "beam_select: needs %zu workspace bytes, got %zu", need, workspace ? workspace_bytes : (size_t)0);
-    c.memory(workspace, (int64_t)need, 16, true, "workspace");
-    if (!c.ok()) return c.st;
+    if (need) {
+      if (!workspace || workspace_bytes < need) return mtf::fail(MTF_ERR_WORKSPACE_TOO_SMALL, "beam_select: needs %zu workspace bytes, got %zu", need, workspace ? workspace_bytes : (size_t)0);
+      c.memory(workspace, (int64_t)need, 16, true, "workspace");
+      if (!c.ok()) return c.st;
+    }
     b.logits = logits->data;
     b.bf16 = logits->dtype == MTF_BF16;
     b.vocab = (int)V;
