@@ -584,7 +584,7 @@ mtf_status mtf_attention_decode_workspace_bytes(const mtf_layout_t* layout, cons
  * Words with a logit of -infinity, beams whose score is not finite (a beam that is not yet one: -infinity), and those with a NaN, a +infinity or
  * no finite logit offer nothing; slots without an offer have parent 0, token end_id, score -infinity, finished 1.
  * beams and slots up to 64.  A beam's words are compared by their logits, offers of different beams in 64 bits, from f32 exponentials summed in f32 by threads and in 64 bits across them.
- * workspace as above. */
+ * workspace as above; it is always needed. */
 mtf_status mtf_beam_select(const mtf_layout_t* layout, const mtf_tensor* logits, const mtf_tensor* scores, const int32_t* finished, int32_t end_id,
                            int32_t* parents, int32_t* tokens, mtf_tensor* new_scores, int32_t* new_finished, void* workspace, size_t workspace_bytes,
                            void* stream);

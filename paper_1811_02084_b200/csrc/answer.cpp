@@ -262,12 +262,10 @@ mtf_status mtf_beam_select(const mtf_layout_t* layout, const mtf_tensor* logits,
     b.tokens = result(tokens, "tokens");
     if (new_finished) b.new_finished = result(new_finished, "new_finished");
     if (!c.ok()) return c.st;
-    const size_t need = mtf::beam_select_workspace(sentences, (int)beams, (int)slots, (int)V);
-    if (need) {
-      if (!workspace || workspace_bytes < need) return mtf::fail(MTF_ERR_WORKSPACE_TOO_SMALL, "beam_select: needs %zu workspace bytes, got %zu", need, workspace ? workspace_bytes : (size_t)0);
-      c.memory(workspace, (int64_t)need, 16, true, "workspace");
-      if (!c.ok()) return c.st;
-    }
+    const size_t need = mtf::beam_select_workspace(sentences, (int)beams, (int)V, logits->dtype == MTF_BF16);
+    if (!workspace || workspace_bytes < need) return mtf::fail(MTF_ERR_WORKSPACE_TOO_SMALL, "beam_select: needs %zu workspace bytes, got %zu", need, workspace ? workspace_bytes : (size_t)0);
+    c.memory(workspace, (int64_t)need, 16, true, "workspace");
+    if (!c.ok()) return c.st;
     b.logits = logits->data;
     b.bf16 = logits->dtype == MTF_BF16;
     b.vocab = (int)V;
@@ -295,7 +293,7 @@ mtf_status mtf_beam_select_workspace_bytes(const mtf_layout_t* layout, const mtf
     else if (slots < 1) c.wrong(MTF_ERR_INVALID_ARG, "at least one slot");
     if (!c.ok()) return c.st;
     const int64_t beams = logits->dims[last - 1].size, V = logits->dims[last].size;
-    *bytes = mtf::beam_select_workspace(numel(*logits) / V / beams, (int)beams, (int)slots, (int)V);
+    *bytes = mtf::beam_select_workspace(numel(*logits) / V / beams, (int)beams, (int)V, logits->dtype == MTF_BF16);
     return MTF_OK;
   });
 }

@@ -66,7 +66,7 @@ struct BeamSelect {
   float* new_scores = nullptr;
   void* workspace = nullptr;
 };
-size_t beam_select_workspace(long long sentences, int beams, int slots, int vocab);
+size_t beam_select_workspace(long long sentences, int beams, int vocab, int bf16);
 mtf_status launch_beam_select(const BeamSelect& b, void* stream);
 
 }  // namespace mtf

@@ -30,6 +30,8 @@ mtf_status read_loss_bad_id(int* seen);
 mtf_status read_decode_status(int* code);
 mtf_status read_decode_bad_page(int* seen);
 mtf_status debug_decode_wait_test(long long limit_cycles, int withhold);
+mtf_status read_beam_status(int* code);
+mtf_status debug_beam_wait_test(long long limit_cycles, int withhold);
 mtf_status read_cache_bad_place(int* seen);
 bool tap_is_open();
 bool ffn_small_pays(int64_t T, int64_t D, int64_t F, int64_t E, bool backward);
@@ -814,6 +816,7 @@ mtf_status mtf_device_status(int32_t* code) {
   if (!rc && (st = mtf::read_row_status(&rc)) != MTF_OK) return st;
   if (!rc && (st = mtf::read_loss_status(&rc)) != MTF_OK) return st;
   if (!rc && (st = mtf::read_decode_status(&rc)) != MTF_OK) return st;
+  if (!rc && (st = mtf::read_beam_status(&rc)) != MTF_OK) return st;
   if (rc) {
     if (code) *code = rc;
     return fail(MTF_ERR_TIMEOUT, "a bounded device-side wait gave up (code 0x%x)", rc);
@@ -841,6 +844,7 @@ mtf_status mtf_debug_pair_tiles(int32_t columns, int32_t across, int32_t* ran_co
 
 mtf_status mtf_debug_wait_test(int64_t limit_cycles, int32_t withhold_one_signal) {
   mtf_status st = mtf::debug_wait_test(limit_cycles, withhold_one_signal != 0 && withhold_one_signal != 2);
+  if (st == MTF_OK) st = mtf::debug_beam_wait_test(limit_cycles, withhold_one_signal != 0 && withhold_one_signal != 2);
   if (st == MTF_OK) st = mtf::debug_decode_wait_test(limit_cycles, withhold_one_signal != 0 && withhold_one_signal != 2);
   return st == MTF_OK ? mtf::debug_loss_wait_test(limit_cycles, withhold_one_signal == 2 ? 2 : withhold_one_signal != 0) : st;
 }

@@ -20,10 +20,22 @@
 #include <algorithm>
 #include <mutex>
 
+#include "answer.cuh"
 #include "answer.h"
 #include "launch.cuh"
 
 namespace {
+
+using mtf::cluster_barrier;
+using mtf::ex2;
+using mtf::far;
+using mtf::far2;
+using mtf::in_block;
+using mtf::kLandCycles;
+using mtf::kWaitCycles;
+using mtf::landed;
+using mtf::landed_late;
+using mtf::smem_at;
 
 constexpr int kWarps = 4;
 constexpr int kThreads = 32 * kWarps;
@@ -59,11 +71,6 @@ struct Args {
 __device__ int g_bad_page = 0;                   // a page id outside the pool, or a length beyond the table, was seen
 
 __device__ __forceinline__ uint32_t prmt(uint32_t a, uint32_t b, uint32_t s) { return __byte_perm(a, b, s); }
-__device__ __forceinline__ float ex2(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
 // four e4m3 values as f16 (exact), two and two
 __device__ __forceinline__ void halves(uint32_t four, uint32_t& lo, uint32_t& hi) {
   asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, a;\n\tcvt.rn.f16x2.e4m3x2 %1, b;\n\t}" : "=r"(lo), "=r"(hi) : "r"(four));
@@ -119,50 +126,9 @@ __device__ __forceinline__ int key_of_row(int i) {
 template <int kRow>
 __device__ __forceinline__ int swizzled(int key, int piece) { return kRow == 128 ? piece ^ (key & 7) : piece ^ (key >> 1 & 3); }
 
-__device__ __forceinline__ uint32_t smem_at(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
-__device__ __forceinline__ bool has_landed(uint32_t bar, uint32_t parity) {
-  uint32_t ok;
-  asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cta.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
-  return ok != 0;
-}
-constexpr long long kWaitCycles = 4000000000LL;      // about two seconds
-constexpr long long kLandCycles = 200000000LL;       // 0.1 s, for copies in flight behind a wait that was given up
 __device__ int g_decode_status = 0;                  // a wait was given up
 __constant__ long long g_wait_limit = kWaitCycles;
 __constant__ int g_withhold = 0;                     // testing: each warp's first wait asks for a copy that nobody has sent
-__device__ __noinline__ bool landed_late(uint32_t bar, uint32_t parity, long long limit) {
-  const long long t0 = clock64();
-  while (!has_landed(bar, parity))
-    if (clock64() - t0 > limit) return false;
-  return true;
-}
-// (the same for all lanes)
-__device__ __forceinline__ bool landed(uint32_t bar, uint32_t parity) {
-  bool ok = has_landed(bar, parity);
-  if (!__all_sync(0xffffffffu, ok)) ok = __all_sync(0xffffffffu, landed_late(bar, parity, g_wait_limit));
-  else ok = true;
-  return ok;
-}
-// another block of the cluster's shared memory, and the barrier of all its threads
-__device__ __forceinline__ uint32_t in_block(uint32_t at, int rank) {
-  uint32_t x;
-  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(x) : "r"(at), "r"(rank));
-  return x;
-}
-__device__ __forceinline__ float far(uint32_t at) {
-  float x;
-  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(x) : "r"(at) : "memory");
-  return x;
-}
-__device__ __forceinline__ float2 far2(uint32_t at) {
-  float2 x;
-  asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(x.x), "=f"(x.y) : "r"(at) : "memory");
-  return x;
-}
-__device__ __forceinline__ void cluster_barrier() {
-  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
 __device__ __forceinline__ void copy_box(uint32_t to, const CUtensorMap* map, int d, int slot, int head, int page, uint32_t bar) {
   asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(to), "l"(map), "r"(d), "r"(slot),
                "r"(head), "r"(page), "r"(bar)
@@ -188,8 +154,8 @@ __global__ void __launch_bounds__(kThreads, Shape<kE4m3, DC>::kBlocks) attention
   float(*const block_o)[DC + 4] = so[kWarps];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, r = lane >> 2, t = lane & 3;
   if (lane == 0) {
-    for (int i = 0; i < S::kStages; ++i) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(smem_at(&bars[warp][i])) : "memory");
-    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    for (int i = 0; i < S::kStages; ++i) mtf::landing_init(&bars[warp][i]);
+    mtf::landing_ready();
   }
   __syncwarp();
   mtf::chain_wait();
@@ -386,7 +352,7 @@ __global__ void __launch_bounds__(kThreads, Shape<kE4m3, DC>::kBlocks) attention
         page[i] = in ? asked[i] : a.pages;
         there[i] = __ballot_sync(0xffffffffu, in);
       }
-      if (lane == 0) asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(S::kStage) : "memory");
+      if (lane == 0) mtf::expect(bar, S::kStage);
       __syncwarp();
       for (int i0 = 0; i0 < boxes; i0 += 32) {
         const int i = min(i0 + lane, boxes - 1), key = i / (2 * S::kBoxes) * a.box_rows, side = i / S::kBoxes & 1, box = i % S::kBoxes;
@@ -429,7 +395,7 @@ __global__ void __launch_bounds__(kThreads, Shape<kE4m3, DC>::kBlocks) attention
     }
     for (int step = j0; step < j1 && !gone; ++step) {
       const uint32_t bar = smem_at(&bars[warp][from & 255]), phase = from >> 8;
-      if (!landed(bar, phase) || (g_withhold && !landed(bar, phase ^ 1))) {
+      if (!landed(bar, phase, g_wait_limit) || (g_withhold && !landed(bar, phase ^ 1, g_wait_limit))) {
         if (lane == 0) atomicCAS(&g_decode_status, 0, 0xB01);
         gone = true;
         for (uint32_t i = from; i != into; i = onward(i)) landed_late(smem_at(&bars[warp][i & 255]), i >> 8, kLandCycles);
@@ -875,24 +841,7 @@ mtf_status launch(const Args& a, const mtf::CachePool& c, int grid, cudaStream_t
   constexpr int kResults = (kWarps + 1) * 8 * NT * (DC + 4) * 4, kRoom = 1024 + (S::kRing > kResults ? S::kRing : kResults);
   const cudaError_t e = cudaFuncSetAttribute(attention_decode_kernel<kE4m3, DC, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kRoom);
   if (e != cudaSuccess) return mtf::fail(MTF_ERR_CUDA, "attention_decode_kernel: %s", cudaGetErrorString(e));
-  if (a.cluster == 1) {
-    mtf::launch_chained(attention_decode_kernel<kE4m3, DC, NT>, (unsigned)grid, kThreads, kRoom, st, a, map_k, map_v);
-  } else {
-    cudaLaunchConfig_t cfg = {};
-    cudaLaunchAttribute at[2];
-    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at[0].val.programmaticStreamSerializationAllowed = 1;
-    at[1].id = cudaLaunchAttributeClusterDimension;
-    at[1].val.clusterDim.x = a.cluster;
-    at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
-    cfg.gridDim = dim3((unsigned)grid, 1, 1);
-    cfg.blockDim = dim3(kThreads, 1, 1);
-    cfg.dynamicSmemBytes = kRoom;
-    cfg.stream = st;
-    cfg.attrs = at;
-    cfg.numAttrs = 2;
-    (void)cudaLaunchKernelEx(&cfg, attention_decode_kernel<kE4m3, DC, NT>, a, map_k, map_v);
-  }
+  mtf::launch_clusters(attention_decode_kernel<kE4m3, DC, NT>, dim3((unsigned)grid), kThreads, kRoom, a.cluster, st, a, map_k, map_v);
   mtf::count_launch();
   if (a.balanced && grid > 1) {
     mtf::launch_chained(attention_decode_join_kernel<8 * NT, DC>, (unsigned)grid - 1, 256, 0, st, a);

@@ -2,11 +2,11 @@
 //     score[i] + (logits[i, v] - log sum_w exp(logits[i, w])),
 // the better ones first, equal ones by the lower i, then the lower v.  A finished beam stands for itself (its end, its score) alone.
 //
-// A beam can only give its own `slots` best words, and which these are its logits say.  So one read of the logits (HBM is the bound) serves both
-// the sum of exponentials and the choice: while a block of threads walks over its part of a row, each thread keeps its sum and its own maximum.  The
-// slots-th largest of the threads' maxima is a value that at least `slots` words reach; only the threads whose maximum reaches it hold words that do, so
-// their pieces alone, about `slots` in 256 of them, are looked at again (they are in L2), by all threads.  A second launch joins a sentence's parts and
-// takes the best of the sorted lists.
+// One read of the logits (HBM is the bound, close behind it the exponentials' unit) gives the sums, and of every run of 128 16-byte pieces the largest word.  A sentence's best
+// words lie in runs whose largest words are among its best: the least of the maxima of `slots` groups of runs is a value that `slots` words at least
+// reach, and a second launch looks only into the runs that reach it, some tens of 1 or 2 KB.  So the first launch is a walk and nothing else: its warps are streams of their own, with bulk copies into
+// a ring each, and wait for nobody.  (64 x 8 rows of 131072 in bf16, whole call: lists of the best words kept for each part of a row, by blocks that stop to sort them, 47 us;
+// by a warp of their own, 82.)
 //
 // What decides between beams is held in 64 bits: sums of a thread are f32 sums of f32 exponentials relative to an entry of its own, so that
 // the entries that weigh are exact or nearly so; they are joined in 64 bits.  Which thread takes which word goes by the word's index alone, not by
@@ -16,31 +16,40 @@
 
 #include <algorithm>
 
+#include "answer.cuh"
 #include "answer.h"
 #include "launch.cuh"
 
 namespace {
 
-constexpr int kThreads = 256;
+using mtf::ex2;
+using mtf::kWaitCycles;
+using mtf::smem_at;
+
+constexpr int kThreads = 256, kWarps = kThreads / 32, kBlocks = 4;      // of the walk; blocks an SM holds
+constexpr int kRun = 128;             // 16-byte pieces that a warp takes at a time
+constexpr int kStages = 3;            // of a warp's ring, a run each: 50 KB a block
+constexpr int kStage = (kRun + 1) * 16, kRing = kWarps * kStages * kStage;
+constexpr int kChoosers = 512, kChooserWarps = kChoosers / 32;
 constexpr int kList = 1024;           // words that may be looked at again before the choice goes by counting
-constexpr int kMostBlocks = 8;        // of a cluster
+constexpr int kRuns = 1024;           // runs they may lie in
+constexpr int kParts = 2;             // of all rows together, a block's
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kSlack = 20.f;        // a thread's reference is raised where an entry lies e^20 above it
 
 struct Args {
   const void* z;
-  int vocab, beams, slots, parts, part;          // part: words of one, a multiple of 8
-  int cluster;                                   // a sentence's parts are one cluster's, which also joins them; else they are left in the workspace
+  int vocab, beams, slots, parts, part;          // part: words of one, whole runs
+  int runs;                                      // of a row
   long long rows;
   const float* scores;
   const int32_t* finished;
   int end_id;
   int32_t *parents, *tokens, *new_finished;
   float* new_scores;
-  float* tops;                                   // [row, part]: maximum
-  double* sums;                                  // ... and the sum of exponentials relative to it
-  float* best_z;                                 // [row, part, slots], sorted; index -1 behind the last
-  int* best_i;
+  float* run_max;                                // [row, run]
+  float* refs;                                   // [row, part, warp]: the reference of its sum of exponentials
+  double* sums;                                  // ... and the sum
 };
 
 // 16 bytes of words
@@ -126,8 +135,12 @@ template <> struct Words<float> {
   }
 };
 
-// One part of a row: words [0, n) from `first` on; pieces of kN words, piece p holding words p kN ..
 template <typename T>
+__device__ __noinline__ uint4 load_some(const T* p, int n) { return Words<T>::some(p, n); }
+
+// One part of a row: words [0, n) from `first` on; pieces of kN words, piece p holding words p kN ..  kAligned: rows begin on 16 bytes.  (What only row ends need is kept out of
+// line here and below: with it in the loops the warps, each at another place, waited for instructions more than for anything else.)
+template <typename T, bool kAligned>
 struct Part {
   static constexpr int kN = Words<T>::kN;
   const T* first;
@@ -138,16 +151,15 @@ struct Part {
   __device__ __forceinline__ Part(const T* z, long long at, int count, long long total) {
     first = z + at;
     n = count;
-    off = (int)(at % kN);
+    off = kAligned ? 0 : (int)(at % kN);
     base = reinterpret_cast<const uint4*>(z + (at - off));
-    const long long left = (total - (at - off)) / kN - (off ? 1 : 0);
-    whole = (int)min((long long)(n / kN), max(left, 0LL));
+    whole = n / kN;
+    if (!kAligned) whole = (int)min((long long)whole, max((total - (at - off)) / kN - (off ? 1 : 0), 0LL));
   }
   __device__ __forceinline__ int pieces() const { return (n + kN - 1) / kN; }
-  __device__ __forceinline__ uint4 load(int p) const {
-    if (p < whole) return off == 0 ? base[p] : Words<T>::shifted(base[p], base[p + 1], off);
-    return Words<T>::some(first + p * kN, n - p * kN);
-  }
+  // from the 16 bytes that piece p begins in, and those behind
+  __device__ __forceinline__ uint4 at(const uint4* p) const { return kAligned ? p[0] : Words<T>::shifted(p[0], p[1], off); }
+  __device__ __forceinline__ uint4 load(int p) const { return p < whole ? at(base + p) : load_some(first + p * kN, n - p * kN); }
 };
 
 // two f32 operations an instruction
@@ -163,20 +175,22 @@ __device__ __forceinline__ float2 times(float2 a, float2 b) {
       : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
   return r;
 }
-__device__ __forceinline__ float ex2(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
+__device__ int g_beam_status = 0;                    // a wait was given up
+__constant__ long long g_wait_limit = kWaitCycles;
+__constant__ int g_withhold = 0;                     // testing: each warp's first wait asks for a copy that nobody has sent
 
-// A thread's sum of exponentials relative to `ref`, an entry of the part (from differences, which are exact for the entries that weigh), and its largest entry.
+// e^(from - to), 1 for equal ones
+__device__ __noinline__ double far_apart(float from, float to) { return exp((double)from - (double)to); }
+__device__ __forceinline__ double rescale(float from, float to) { return from == to ? 1. : far_apart(from, to); }
+__device__ __noinline__ double log_of(double s) { return log(s); }
+
+// A thread's sum of exponentials relative to `ref`, a large entry (from differences, which are exact for the entries that weigh).
 struct Sum {
-  float ref, top = -INFINITY;
+  float ref = -INFINITY;
   float2 s = make_float2(0.f, 0.f);
+  // some more words, of which m is the largest
   template <typename T, int K>
-  __device__ __forceinline__ void add(const uint4 (&v)[K]) {
-    const float m = Words<T>::largest(v);
-    top = fmaxf(top, m);
+  __device__ __forceinline__ void add(const uint4 (&v)[K], float m) {
     if (m > ref + kSlack || (ref == -INFINITY && m > -INFINITY)) {
       const float f = ref == -INFINITY ? 0.f : exp2f((ref - m) * kLog2e);
       s = times(s, make_float2(f, f));               // (a sum of 0, or NaN, where there was no reference)
@@ -197,437 +211,462 @@ struct Sum {
 };
 
 __device__ __forceinline__ bool better(float z, int i, float y, int j) { return z > y || (z == y && i < j); }
-// 32 bits in the order of the values, -0 as 0; NaN does not come here
-__device__ __forceinline__ uint32_t key_of(float z) {
-  const uint32_t b = __float_as_uint(z + 0.f);
-  return b & 0x80000000u ? ~b : b | 0x80000000u;
+// 64 bits in the order of the values
+__device__ __forceinline__ unsigned long long order_of(double v) {
+  const unsigned long long b = (unsigned long long)__double_as_longlong(v);
+  return b >> 63 ? ~b : b | 0x8000000000000000ull;
 }
+// A warp's share of the copies: the runs w, w + 8, .. of a part, those whose pieces are whole by bulk copies into its ring, the last ones by loads.
+struct Ring {
+  uint8_t* base;                       // this warp's
+  uint64_t* bars;
+  int stage = 0;
+  uint32_t phase = 0;
+  bool gone = false;                   // a wait was given up
 
-// What a block knows, and what joins the lists of a sentence.
-struct Room {
-  float list_z[kList];
-  int list_i[kList];
-  float sorted_z[mtf::kMaxSlots];
-  int sorted_i[mtf::kMaxSlots];
-  double red_s[kThreads / 32];
-  float red_m[kThreads / 32], red_r[kThreads / 32];
-  int chosen[kThreads], counts[256];
-  int count, n_chosen, taken;
-  float top;
-  double sum;
-};
-
-// A list's first word.  The words of a beam go by their logits (a score far from 0 may leave nothing of those in the sum), equal ones by the lower word.
-struct Offer {
-  double value = -INFINITY;
-  float z = 0.f;
-  int beam = 0x7fffffff, word = 0, list = 0;
-  __device__ __forceinline__ bool before(const Offer& o) const {
-    return value > o.value || (value == o.value && (beam < o.beam || (beam == o.beam && better(z, word, o.z, o.word))));
+  template <typename P>
+  __device__ __forceinline__ void fetch(const P& w, int run, int into) const {      // (one lane)
+    const uint32_t bar = smem_at(&bars[into]), bytes = (kRun + (w.off ? 1 : 0)) * 16;
+    mtf::expect(bar, bytes);
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(smem_at(base) + into * kStage), "l"(w.base + (long long)run * kRun),
+                 "r"(bytes), "r"(bar)
+                 : "memory");
   }
-};
-
-// One warp: the best of a sentence's lists, one after the other.  All in shared memory: per list (beam, part) its maximum and sum, its words z, index (sorted; an index
-// below 0 behind the last); per beam two numbers, per list one, of this warp's own.
-__device__ __forceinline__ void merge_lists(const Args& a, long long sentence, const float* tops, const double* sums, const float* z, int* index, double* base, double* maxima, int* head) {
-  const int lane = threadIdx.x & 31, lists = a.beams * a.parts;
-  const long long row0 = sentence * a.beams;
-  for (int b = lane; b < a.beams; b += 32) {
-    const float score = a.scores[row0 + b];
-    const bool done = a.finished && a.finished[row0 + b];
-    bool live = fabsf(score) < INFINITY;
-    base[b] = score;
-    maxima[b] = 0.;
-    if (live && !done) {
-      float top = -INFINITY;
-      for (int p = 0; p < a.parts; ++p) top = fmaxf(top, tops[b * a.parts + p]);
-      double s = 0.;
-      for (int p = 0; p < a.parts; ++p) {
-        const float m = tops[b * a.parts + p];
-        const double x = sums[b * a.parts + p];
-        s += m == top ? x : x * exp((double)m - (double)top);      // (a part without a finite word: 0 times its sum, 0 or NaN)
-      }
-      live = s > 0. && s < INFINITY && fabsf(top) < INFINITY;
-      base[b] = (double)score - log(s);
-      maxima[b] = top;
-    }
-    if (!live) base[b] = -INFINITY;
-    // what a finished beam offers, and one that offers nothing
-    if (!live || done)
-      for (int p = 0; p < a.parts; ++p) index[(b * a.parts + p) * a.slots] = -1;
-    if (live && done) {
-      index[b * a.parts * a.slots] = a.end_id;
-      if (a.slots > 1) index[b * a.parts * a.slots + 1] = -1;
-    }
-  }
-  for (int l = lane; l < lists; l += 32) head[l] = 0;
-  __syncwarp();
-  for (int slot = 0; slot < a.slots; ++slot) {
-    Offer best;
-    for (int l = lane; l < lists; l += 32) {
-      const int i = l * a.slots + head[l];
-      if (head[l] >= a.slots || index[i] < 0) continue;
-      const int b = l / a.parts;
-      const bool done = a.finished && a.finished[row0 + b];
-      const float y = done ? 0.f : z[i];
-      const Offer o = {base[b] + ((double)y - maxima[b]), y, b, index[i], l};
-      if (o.before(best)) best = o;
-    }
-    // the largest value of the warp; where several lanes have it, the first of them by the other rules
-    double top = best.value;
+  // the first runs of a part, when nothing is under way
+  template <typename P>
+  __device__ __forceinline__ void begin(const P& w) const {
+    const int warp = threadIdx.x >> 5, whole = w.whole / kRun;
+    if ((threadIdx.x & 31) == 0 && !gone) {
+      int into = stage;
 #pragma unroll
-    for (int d = 16; d > 0; d >>= 1) top = fmax(top, __shfl_xor_sync(0xffffffffu, top, d));
-    uint32_t those = __ballot_sync(0xffffffffu, best.value == top && top > -INFINITY);
-    int from = those ? __ffs(those) - 1 : 0;
-    for (those &= those - 1; those; those &= those - 1) {
-      const int other = __ffs(those) - 1;
-      const int b0 = __shfl_sync(0xffffffffu, best.beam, from), b1 = __shfl_sync(0xffffffffu, best.beam, other);
-      const int w0 = __shfl_sync(0xffffffffu, best.word, from), w1 = __shfl_sync(0xffffffffu, best.word, other);
-      const float z0 = __shfl_sync(0xffffffffu, best.z, from), z1 = __shfl_sync(0xffffffffu, best.z, other);
-      if (b1 < b0 || (b1 == b0 && better(z1, w1, z0, w0))) from = other;
+      for (int i = 0; i < kStages; ++i) {
+        if (warp + i * kWarps < whole) fetch(w, warp + i * kWarps, into);
+        if (++into == kStages) into = 0;
+      }
     }
-    const bool any = top > -INFINITY;
-    if (lane == from) {
-      if (any) ++head[best.list];
-      const long long at = sentence * a.slots + slot;
-      const int parent = any ? best.beam : 0, token = any ? best.word : a.end_id;
-      a.parents[at] = parent;
-      a.tokens[at] = token;
-      a.new_scores[at] = any ? (float)top : -INFINITY;
-      if (a.new_finished) a.new_finished[at] = token == a.end_id || (any && a.finished && a.finished[row0 + parent]) ? 1 : 0;
-    }
-    __syncwarp();
   }
+  // a wait was given up: what is under way, the copy of this stage and those of the runs behind it
+  __device__ __noinline__ void give_up(int run, int whole) {
+    if ((threadIdx.x & 31) == 0) atomicCAS(&g_beam_status, 0, 0xB11);
+    gone = true;
+    for (int i = 0; i < kStages; ++i)
+      if (run + i * kWarps < whole) mtf::landed_late(smem_at(&bars[(stage + i) % kStages]), stage + i >= kStages ? phase ^ 1 : phase, mtf::kLandCycles);
+  }
+  // a run of whole pieces, from the ring
+  template <typename P, int K>
+  __device__ __forceinline__ void take(const P& w, int run, int whole, uint4 (&v)[K]) {
+    const int lane = threadIdx.x & 31;
+    const uint32_t bar = smem_at(&bars[stage]);
+    if (!gone && (!mtf::landed(bar, phase, g_wait_limit) || (g_withhold && !mtf::landed(bar, phase ^ 1, g_wait_limit)))) give_up(run, whole);
+    const uint4* const at = reinterpret_cast<const uint4*>(base + stage * kStage) + lane;
+#pragma unroll
+    for (int e = 0; e < K; ++e) v[e] = w.at(at + e * 32);
+    __syncwarp();
+    if (lane == 0 && !gone && run + kStages * kWarps < whole) fetch(w, run + kStages * kWarps, stage);
+    if (++stage == kStages) { stage = 0; phase ^= 1; }
+  }
+};
+
+__device__ __forceinline__ float warp_max(float m) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+  return m;
 }
 
-__device__ __forceinline__ uint32_t smem_at(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
-__device__ __forceinline__ uint32_t in_block(uint32_t at, int rank) {
-  uint32_t x;
-  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(x) : "r"(at), "r"(rank));
-  return x;
-}
-__device__ __forceinline__ uint32_t far(uint32_t at) {
-  uint32_t x;
-  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(x) : "r"(at) : "memory");
-  return x;
-}
-__device__ __forceinline__ double far_double(uint32_t at) {
-  double x;
-  asm volatile("ld.shared::cluster.f64 %0, [%1];" : "=d"(x) : "r"(at) : "memory");
-  return x;
-}
-__device__ __forceinline__ void cluster_barrier() {
-  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-
-// A part's maximum, sum and sorted best words, into room.
-template <typename T>
-__device__ __forceinline__ void part_of_row(const Args& a, long long row, int c0, int n, Room& m) {
-  constexpr int kN = Words<T>::kN, kDeep = 4, kWarps = kThreads / 32;
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const Part<T> w(reinterpret_cast<const T*>(a.z), row * a.vocab + c0, n, a.rows * a.vocab);
-  const int pieces = w.pieces();
-  const uint4 none = make_uint4(Words<T>::kNone, Words<T>::kNone, Words<T>::kNone, Words<T>::kNone);
-
-  // ---- one walk: sum and maximum.  All threads begin with the same reference, the largest of the first pieces, so that their sums can be added as they are.
+// A warp's share of a part, runs first + warp, first + warp + 8, .. of the row.  The copies for it are under way; behind it those for `next` (if there is one) are asked for.
+template <typename T, typename P>
+__device__ __forceinline__ void walk(const P& w, const P& next, bool more, Ring& ring, float* run_max, float* to_ref, double* to_sum) {
+  constexpr int kDeep = kRun / 32;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int pieces = w.pieces(), runs = (pieces + kRun - 1) / kRun, whole = w.whole / kRun;
   Sum sum;
   uint4 v[kDeep];
-  int p = tid;
-  auto load = [&](int first, uint4 (&to)[kDeep]) {
-    if (first + (kDeep - 1) * kThreads < w.whole && w.off == 0) {
-#pragma unroll
-      for (int e = 0; e < kDeep; ++e) to[e] = w.base[first + e * kThreads];
-    } else {
-#pragma unroll
-      for (int e = 0; e < kDeep; ++e) to[e] = first + e * kThreads < pieces ? w.load(first + e * kThreads) : none;
+  int run = warp;
+  for (; run < whole; run += kWarps) {
+    ring.take(w, run, whole, v);
+    const float m = Words<T>::largest(v), all = warp_max(m);
+    if (run == warp) sum.ref = all;                  // (all lanes begin with the same, so that their sums can be added as they are)
+    sum.add<T>(v, m);
+    if (lane == 0) run_max[run] = all;
+  }
+  for (; run < runs; run += kWarps) {
+    float all = -INFINITY;
+#pragma unroll 1
+    for (int e = 0; e < kDeep; ++e) {
+      const int q = run * kRun + e * 32 + lane;
+      const uint4 u[1] = {q < pieces ? w.load(q) : make_uint4(Words<T>::kNone, Words<T>::kNone, Words<T>::kNone, Words<T>::kNone)};
+      const float m = Words<T>::largest(u);
+      all = fmaxf(all, m);
+      sum.add<T>(u, m);
     }
-  };
-  load(p, v);
-  float top = Words<T>::largest(v);
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-  if (lane == 0) m.red_m[warp] = top;
-  if (tid == 0) { m.count = 0; m.n_chosen = 0; }
-  __syncthreads();
-  top = m.red_m[0];
-#pragma unroll
-  for (int i = 1; i < kWarps; ++i) top = fmaxf(top, m.red_m[i]);
-  sum.ref = top;
-  for (; p < pieces; p += kDeep * kThreads) {
-    uint4 next[kDeep];
-    if (p + kDeep * kThreads < pieces) load(p + kDeep * kThreads, next);
-    sum.add<T>(v);
-#pragma unroll
-    for (int e = 0; e < kDeep; ++e) v[e] = next[e];
+    all = warp_max(all);
+    if (lane == 0) run_max[run] = all;
   }
-
-  // ---- the largest, and a value that `slots` words at least reach: the least of the maxima of as many groups of threads (the next power of two)
-  float group = sum.top, ref = sum.ref;
-  int groups = 1;
-  while (groups < a.slots) groups *= 2;
-  const int width = kThreads / groups;                       // threads of a group
-  for (int o = 1; o < min(width, 32); o *= 2) group = fmaxf(group, __shfl_xor_sync(0xffffffffu, group, o));
-  float low = group;
-  top = group;
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
-    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-    low = fminf(low, __shfl_xor_sync(0xffffffffu, low, o));
-    ref = fmaxf(ref, __shfl_xor_sync(0xffffffffu, ref, o));
-  }
-  __syncthreads();
-  if (lane == 0) {
-    m.red_m[warp] = top;
-    m.red_r[warp] = ref;
-    m.chosen[warp] = __float_as_int(low);
-  }
-  __syncthreads();
-  top = m.red_m[0];
-  ref = m.red_r[0];
-  float thr = INFINITY;
-#pragma unroll
-  for (int i = 0; i < kWarps; ++i) {
-    top = fmaxf(top, m.red_m[i]);
-    ref = fmaxf(ref, m.red_r[i]);
-    thr = fminf(thr, __int_as_float(m.chosen[i]));
-  }
-  if (width > 32) {                                          // groups of whole warps
-    thr = INFINITY;
-    const int warps = width / 32;
-    for (int g = 0; g < kWarps; g += warps) {
-      float x = m.red_m[g];
-      for (int i = 1; i < warps; ++i) x = fmaxf(x, m.red_m[g + i]);
-      thr = fminf(thr, x);
-    }
-  }
-  // ---- the threads' sums, joined in 64 bits in a fixed order
+  if (more) ring.begin(next);
+  // the warp's sum, in 64 bits in a fixed order
+  const float ref = warp_max(sum.ref);
   double s = (double)sum.s.x + (double)sum.s.y;
-  if (sum.ref != ref && sum.ref != -INFINITY) s *= exp((double)sum.ref - (double)ref);
+  if (sum.ref != -INFINITY) s *= rescale(sum.ref, ref);
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-  if (lane == 0) m.red_s[warp] = s;
-  __syncthreads();                                           // (the maxima have been read, too)
-  if (tid == 0) {
-    double all = m.red_s[0];
-#pragma unroll
-    for (int i = 1; i < kWarps; ++i) all += m.red_s[i];
-    m.top = top;
-    m.sum = top == ref || top == -INFINITY ? all : all * exp((double)ref - (double)top);
+  if (lane == 0) {
+    *to_ref = ref;
+    *to_sum = s;
   }
-  if (sum.top >= thr && sum.top > -INFINITY) m.chosen[atomicAdd(&m.n_chosen, 1)] = tid;
-  __syncthreads();
+}
 
-  // ---- the words that reach it, from the pieces of the threads that have some
-  const int per = (pieces + kThreads - 1) / kThreads, again = m.n_chosen * per;
-  for (int i = tid; i < again; i += kThreads) {
-    const int which = i / per, q = m.chosen[which] + (i - which * per) * kThreads;
-    if (q >= pieces) continue;
-    float x[kN];
-    Words<T>::values(w.load(q), x);
-#pragma unroll
-    for (int j = 0; j < kN; ++j)
-      if (x[j] >= thr && x[j] > -INFINITY) {
-        const int at = atomicAdd(&m.count, 1);
-        if (at < kList) { m.list_z[at] = x[j]; m.list_i[at] = c0 + q * kN + j; }
-      }
+// Blocks go from part to part; the first copies of the next one are asked for as soon as a warp is through with its share.
+template <typename T, bool kAligned>
+__global__ void __launch_bounds__(kThreads, kBlocks) beam_rows_kernel(const Args a) {
+  __shared__ uint64_t bars[kWarps][kStages];
+  extern __shared__ __align__(16) uint8_t dyn[];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  Ring ring;
+  ring.base = dyn + warp * kStages * kStage;
+  ring.bars = bars[warp];
+  if (lane == 0) {
+    for (int i = 0; i < kStages; ++i) mtf::landing_init(&ring.bars[i]);
+    mtf::landing_ready();
+  }
+  __syncwarp();
+  mtf::chain_wait();
+  auto part_at = [&](int row, int part) {
+    return Part<T, kAligned>(reinterpret_cast<const T*>(a.z), (long long)row * a.vocab + (long long)part * a.part, min(a.part, a.vocab - part * a.part), a.rows * a.vocab);
+  };
+  const int units = (int)a.rows * a.parts;           // (below 2^31 less the grid's blocks)
+  // unit u, or the first one behind it of this block's that is to be read (a beam that is finished, or none, is not); -1: none
+  auto from = [&](int u) {
+    for (; u < units; u += gridDim.x) {
+      const int row = u / a.parts, done = a.finished ? a.finished[row] : 0;
+      const float score = a.scores[row];
+      if (fabsf(score) < INFINITY && !done) return u;
+    }
+    return -1;
+  };
+  int u = from(blockIdx.x);
+  if (u < 0) return;
+  int row = u / a.parts, part = u - row * a.parts;
+  Part<T, kAligned> w = part_at(row, part);
+  ring.begin(w);
+  while (u >= 0) {
+    const int next = from(u + gridDim.x), next_row = next >= 0 ? next / a.parts : row, next_part = next >= 0 ? next - next_row * a.parts : part;
+    const Part<T, kAligned> behind = part_at(next_row, next_part);
+    const long long list = ((long long)row * a.parts + part) * kWarps + warp;
+    walk<T>(w, behind, next >= 0, ring, a.run_max + (long long)row * a.runs + part * (a.part / (kRun * Words<T>::kN)), a.refs + list, a.sums + list);
+    u = next;
+    row = next_row;
+    part = next_part;
+    w = behind;
+  }
+}
+
+// What a sentence's choice is made from.
+struct Room {
+  unsigned long long key[kList];       // words that may be among the best: their values in order, beams, logits and numbers (and counters, before)
+  float z[kList];
+  int word[kList], beam[kList];
+  int runs[kRuns];
+  unsigned long long group[kChooserWarps][32];
+  double base[mtf::kMaxBeams];         // a word's value is base + (logit - ref)
+  float ref[mtf::kMaxBeams], low[mtf::kMaxBeams];
+  signed char state[mtf::kMaxBeams];   // 0: offers nothing, 1: its words, 2: its end
+  int count, n_runs, below[kChooserWarps];
+};
+
+__device__ __forceinline__ unsigned long long value_key(const Room& m, int b, float z) { return order_of(m.base[b] + ((double)z - (double)m.ref[b]) + 0.); }
+// a logit that no word of value v or more lies below: a little under v - base + ref, which is rounded
+__device__ __forceinline__ float lowest(double v, double base, float ref) {
+  const double at = v - base + (double)ref;
+  return v > -INFINITY ? (float)(at - (fabs(at) * 1e-6 + (fabs(v) + fabs(base)) * 1e-15)) : -INFINITY;
+}
+__device__ __forceinline__ double value_of(unsigned long long key) { return __longlong_as_double((long long)(key >> 63 ? key & 0x7fffffffffffffffull : ~key)); }
+
+// A beam's row, whole (words by the same pieces as the walk's)
+template <typename T, bool kAligned>
+__device__ __forceinline__ Part<T, kAligned> row_at(const Args& a, long long row) {
+  return Part<T, kAligned>(reinterpret_cast<const T*>(a.z), row * a.vocab, a.vocab, a.rows * a.vocab);
+}
+
+// The words whose value is at least thr (strict: above it), into the list, from the runs whose largest word's is; and the ends of finished beams.  All threads.  Returns how many
+// there are: over kList where that is more than the list holds, or where they lie in too many runs.
+template <typename T, bool kAligned>
+__device__ __noinline__ int gather(const Args& a, long long row0, Room& m, unsigned long long thr, bool strict) {
+  constexpr int kN = Words<T>::kN, kDeep = kRun / 32;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  auto reaches = [&](unsigned long long k) { return strict ? k > thr : k >= thr; };
+  __syncthreads();
+  if (tid == 0) m.count = m.n_runs = 0;
+  if (tid < a.beams) m.low[tid] = thr ? lowest(value_of(thr), m.base[tid], m.ref[tid]) : -INFINITY;
+  __syncthreads();
+  for (int i = tid; i < a.beams * a.runs; i += kChoosers) {
+    const int b = i / a.runs;
+    if (m.state[b] != 1) continue;
+    const float top = a.run_max[row0 * a.runs + i];
+    if (top > -INFINITY && reaches(value_key(m, b, top))) {
+      const int at = atomicAdd(&m.n_runs, 1);
+      if (at < kRuns) m.runs[at] = i;
+    }
+  }
+  if (tid < a.beams && m.state[tid] == 2 && reaches(order_of(m.base[tid] + 0.))) {
+    const int at = atomicAdd(&m.count, 1);
+    m.key[at] = order_of(m.base[tid] + 0.);
+    m.z[at] = 0.f;
+    m.word[at] = a.end_id;
+    m.beam[at] = tid;
   }
   __syncthreads();
-  int found = m.count;
-  if (found > kList) {
-    // Too many to be sorted (a row of equal words, or masked by a finite value): the slots-th largest value by counting its bytes from the highest on,
-    // then all words above it, fewer than `slots`, and of those equal to it the first.
-    uint32_t prefix = 0;
+  const int n = m.n_runs;
+  if (n > kRuns) return kList + 1;
+  for (int i = warp; i < n; i += kChooserWarps) {
+    const int b = m.runs[i] / a.runs, run = m.runs[i] - b * a.runs;
+    const Part<T, kAligned> w = row_at<T, kAligned>(a, row0 + b);
+    const float low = m.low[b];
+    uint4 v[kDeep];
+#pragma unroll
+    for (int e = 0; e < kDeep; ++e) {
+      const int q = run * kRun + e * 32 + lane;
+      v[e] = q < w.pieces() ? w.load(q) : make_uint4(Words<T>::kNone, Words<T>::kNone, Words<T>::kNone, Words<T>::kNone);
+    }
+#pragma unroll 1
+    for (int e = 0; e < kDeep; ++e) {
+      const uint4 u[1] = {e == 0 ? v[0] : e == 1 ? v[1] : e == 2 ? v[2] : v[3]};
+      if (!(Words<T>::largest(u) >= low)) continue;
+      float x[kN];
+      Words<T>::values(u[0], x);
+#pragma unroll
+      for (int j = 0; j < kN; ++j)
+        if (x[j] >= low && x[j] > -INFINITY) {
+          const unsigned long long k = value_key(m, b, x[j]);
+          if (reaches(k)) {
+            const int at = atomicAdd(&m.count, 1);
+            if (at < kList) {
+              m.key[at] = k;
+              m.z[at] = x[j];
+              m.word[at] = (run * kRun + e * 32 + lane) * kN + j;
+              m.beam[at] = b;
+            }
+          }
+        }
+    }
+  }
+  __syncthreads();
+  return m.count;
+}
+
+// Where too many words reach thr to be sorted (rows of equal words, or masked by a finite value): those above it, and the first of those equal to it.  Where those above are
+// too many, too, thr becomes the slots-th largest value, by counting its bytes from the highest on.  Returns how many the list holds.  All threads.
+template <typename T, bool kAligned>
+__device__ __noinline__ int narrowed(const Args& a, long long row0, Room& m, unsigned long long thr) {
+  constexpr int kN = Words<T>::kN;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  int above = gather<T, kAligned>(a, row0, m, thr, true);
+  if (above > kList) {
+    int* const counts = reinterpret_cast<int*>(m.key);
+    unsigned long long prefix = 0;
     int want = a.slots;                            // of those that share the prefix
-    for (int byte = 3; byte >= 0; --byte) {
+    for (int byte = 7; byte >= 0; --byte) {
       __syncthreads();
-      m.counts[tid] = 0;
+      if (tid < 256) counts[tid] = 0;
       __syncthreads();
-      for (int q = tid; q < pieces; q += kThreads) {
+      auto note = [&](unsigned long long k) {
+        if (byte == 7 || k >> (8 * byte + 8) == prefix) atomicAdd(&counts[k >> (8 * byte) & 255], 1);
+      };
+      for (int b = 0; b < a.beams; ++b) {
+        if (m.state[b] == 2 && tid == 0) note(order_of(m.base[b] + 0.));
+        if (m.state[b] != 1) continue;
+        const Part<T, kAligned> w = row_at<T, kAligned>(a, row0 + b);
+        for (int q = tid; q < w.pieces(); q += kChoosers) {
+          float x[kN];
+          Words<T>::values(w.load(q), x);
+#pragma unroll 1
+          for (int j = 0; j < kN; ++j)
+            if (x[j] > -INFINITY) note(value_key(m, b, x[j]));
+        }
+      }
+      __syncthreads();
+      int over = 0, d = 255;
+      while (d > 0 && over + counts[d] < want) over += counts[d--];
+      want -= over;
+      prefix = prefix << 8 | (unsigned)d;
+    }
+    thr = prefix;
+    above = gather<T, kAligned>(a, row0, m, thr, true);              // fewer than `slots`, in runs of which there are no more
+  }
+  // equal ones: by the lower beam, of a beam's the larger logits (the sums may have lost what tells them apart), of these the lower words; as long as there is need of them
+  int at = above;
+  for (int b = 0; b < a.beams && at < a.slots; ++b) {
+    if (m.state[b] == 2 && order_of(m.base[b] + 0.) == thr) {
+      __syncthreads();
+      if (tid == 0) { m.key[at] = thr; m.z[at] = 0.f; m.word[at] = a.end_id; m.beam[at] = b; }
+      ++at;
+    }
+    if (m.state[b] != 1) continue;
+    const Part<T, kAligned> w = row_at<T, kAligned>(a, row0 + b);
+    for (float below = INFINITY; at < a.slots;) {
+      // the largest logit under `below` whose value is thr
+      float z = -INFINITY;
+      for (int q = tid; q < w.pieces(); q += kChoosers) {
         float x[kN];
         Words<T>::values(w.load(q), x);
 #pragma unroll
-        for (int j = 0; j < kN; ++j) {
-          const uint32_t k = key_of(x[j]);
-          if (x[j] > -INFINITY && (byte == 3 || (k >> (8 * byte + 8)) == prefix)) atomicAdd(&m.counts[k >> (8 * byte) & 255], 1);
-        }
+        for (int j = 0; j < kN; ++j)
+          if (x[j] < below && x[j] > z && value_key(m, b, x[j]) == thr) z = x[j];
       }
+      z = warp_max(z);
       __syncthreads();
-      int above = 0, b = 255;
-      while (b > 0 && above + m.counts[b] < want) above += m.counts[b--];
-      want -= above;
-      prefix = prefix << 8 | (uint32_t)b;
-    }
-    __syncthreads();
-    if (tid == 0) { m.count = 0; m.taken = 0; }
-    __syncthreads();
-    for (int q0 = 0; q0 < pieces; q0 += kThreads) {
-      const int q = q0 + tid;
-      float x[kN];
-      int same = 0;
-      if (q < pieces) {
-        Words<T>::values(w.load(q), x);
+      if (lane == 0) m.low[warp] = z;
+      __syncthreads();
+      for (int i = 0; i < kChooserWarps; ++i) z = fmaxf(z, m.low[i]);
+      if (z == -INFINITY) break;
+      below = z;
+      for (int q0 = 0; q0 < w.pieces() && at < a.slots; q0 += kChoosers) {
+        const int q = q0 + tid;
+        float x[kN];
+        int same = 0;
+        if (q < w.pieces()) {
+          Words<T>::values(w.load(q), x);
 #pragma unroll
-        for (int j = 0; j < kN; ++j) {
-          const uint32_t k = key_of(x[j]);
-          if (x[j] > -INFINITY && k > prefix) {
-            const int at = atomicAdd(&m.count, 1);
-            m.list_z[at] = x[j];
-            m.list_i[at] = c0 + q * kN + j;
-          }
-          same += x[j] > -INFINITY && k == prefix;
+          for (int j = 0; j < kN; ++j) same += x[j] == z;
         }
-      }
-      // equal ones in the order of their index, as long as there is need of them
-      if (m.taken < want) {                        // (the same for all threads: it is written between barriers)
         int upto = same;
 #pragma unroll
-        for (int o = 1; o < 32; o *= 2) {
-          const int y = __shfl_up_sync(0xffffffffu, upto, o);
-          if (lane >= o) upto += y;
+        for (int d = 1; d < 32; d *= 2) {
+          const int y = __shfl_up_sync(0xffffffffu, upto, d);
+          if (lane >= d) upto += y;
         }
-        if (lane == 31) m.counts[warp] = upto;
         __syncthreads();
-        int at = m.taken + upto - same, all = m.taken;
-        for (int i = 0; i < kWarps; ++i) {
-          if (i < warp) at += m.counts[i];
-          all += m.counts[i];
+        if (lane == 31) m.below[warp] = upto;
+        __syncthreads();
+        int to = at + upto - same, all = 0;
+        for (int i = 0; i < kChooserWarps; ++i) {
+          if (i < warp) to += m.below[i];
+          all += m.below[i];
         }
-        if (q < pieces)
+        if (q < w.pieces())
 #pragma unroll
           for (int j = 0; j < kN; ++j)
-            if (x[j] > -INFINITY && key_of(x[j]) == prefix) {
-              if (at < want) {
-                const int to = kList - 1 - at;     // from the other end
-                m.list_z[to] = x[j];
-                m.list_i[to] = c0 + q * kN + j;
-              }
-              ++at;
+            if (x[j] == z) {
+              if (to < a.slots) { m.key[to] = thr; m.z[to] = z; m.word[to] = q * kN + j; m.beam[to] = b; }
+              ++to;
             }
-        __syncthreads();
-        if (tid == 0) m.taken = min(all, want);
-        __syncthreads();
+        at = min(a.slots, at + all);
       }
     }
-    __syncthreads();
-    const int over = m.count, equal = m.taken;
-    if (tid < equal) { m.list_z[over + tid] = m.list_z[kList - 1 - tid]; m.list_i[over + tid] = m.list_i[kList - 1 - tid]; }
-    found = over + equal;
-    __syncthreads();
   }
-
-  // ---- in order
-  for (int i = tid; i < found; i += kThreads) {
-    const float z = m.list_z[i];
-    const int at = m.list_i[i];
-    int place = 0;
-    for (int j = 0; j < found; ++j) place += better(m.list_z[j], m.list_i[j], z, at);
-    if (place < a.slots) { m.sorted_z[place] = z; m.sorted_i[place] = at; }
-  }
-  for (int i = found + tid; i < a.slots; i += kThreads) m.sorted_i[i] = -1;
   __syncthreads();
+  return max(above, at);
 }
 
-template <typename T>
-__global__ void __launch_bounds__(kThreads) beam_rows_kernel(const Args a) {
-  __shared__ __align__(16) Room m;
-  mtf::chain_wait();
-  const int tid = threadIdx.x;
-  const long long row = blockIdx.x / a.parts;
-  const int part = (int)(blockIdx.x - row * a.parts);
-  const float score = a.scores[row];
-  // (a beam that is finished, or none, is not looked at behind this either)
-  const bool live = fabsf(score) < INFINITY && !(a.finished && a.finished[row]);
-  if (live) part_of_row<T>(a, row, part * a.part, max(0, min(a.part, a.vocab - part * a.part)), m);
-  if (!a.cluster) {
-    if (!live) return;
-    if (tid == 0) {
-      a.tops[blockIdx.x] = m.top;
-      a.sums[blockIdx.x] = m.sum;
-    }
-    if (tid < a.slots) {
-      a.best_z[(long long)blockIdx.x * a.slots + tid] = m.sorted_z[tid];
-      a.best_i[(long long)blockIdx.x * a.slots + tid] = m.sorted_i[tid];
-    }
-    return;
-  }
-  // a sentence's parts are this cluster's blocks: the first takes what the others have
-  cluster_barrier();
-  const int lists = a.cluster, rank = blockIdx.x % lists;
-  __shared__ float tops[kMostBlocks];
-  __shared__ double sums[kMostBlocks], base[kMostBlocks], maxima[kMostBlocks];
-  __shared__ int head[kMostBlocks];
-  if (rank == 0) {
-    for (int i = tid; i < lists * a.slots; i += kThreads) {
-      const int l = i / a.slots, j = i - l * a.slots;
-      m.list_z[i] = __uint_as_float(far(in_block(smem_at(&m.sorted_z[j]), l)));
-      m.list_i[i] = (int)far(in_block(smem_at(&m.sorted_i[j]), l));
-    }
-    if (tid < lists) {
-      tops[tid] = __uint_as_float(far(in_block(smem_at(&m.top), tid)));
-      sums[tid] = far_double(in_block(smem_at(&m.sum), tid));
-    }
-  }
-  cluster_barrier();                               // (from here on a block may leave)
-  if (rank == 0 && tid < 32) merge_lists(a, blockIdx.x / lists, tops, sums, m.list_z, m.list_i, base, maxima, head);
-}
-
-// A sentence's parts from the workspace.
-__global__ void __launch_bounds__(128) beam_merge_kernel(const Args a) {
-  extern __shared__ __align__(16) uint8_t room[];
+// A block a sentence.
+template <typename T, bool kAligned>
+__global__ void __launch_bounds__(kChoosers, 1) beam_choose_kernel(const Args a) {
+  __shared__ Room m;
   mtf::chain_wait_only();
-  const int tid = threadIdx.x, lists = a.beams * a.parts, n = lists * a.slots;
-  double* const sums = reinterpret_cast<double*>(room);
-  double* const base = sums + lists;
-  double* const maxima = base + a.beams;
-  float* const z = reinterpret_cast<float*>(maxima + a.beams);
-  int* const index = reinterpret_cast<int*>(z + n);
-  float* const tops = reinterpret_cast<float*>(index + n);
-  int* const head = reinterpret_cast<int*>(tops + lists);
-  // (the lists of beams that were not looked at hold anything, and are not used)
-  const long long list0 = (long long)blockIdx.x * lists;
-  for (int i = tid; i < n; i += 128) {
-    index[i] = a.best_i[list0 * a.slots + i];
-    z[i] = a.best_z[list0 * a.slots + i];
-  }
-  for (int i = tid; i < lists; i += 128) {
-    tops[i] = a.tops[list0 + i];
-    sums[i] = a.sums[list0 + i];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const long long sentence = blockIdx.x, row0 = sentence * a.beams;
+  // ---- a warp a beam: its sum
+  for (int b = warp; b < a.beams; b += kChooserWarps) {
+    const long long row = row0 + b;
+    const float score = a.scores[row];
+    const int done = a.finished ? a.finished[row] : 0, n = a.parts * kWarps;
+    int state = fabsf(score) < INFINITY ? done ? 2 : 1 : 0;
+    float top = 0.f;
+    double at = score;
+    if (state == 1) {
+      top = -INFINITY;
+      for (int i = lane; i < n; i += 32) top = fmaxf(top, a.refs[row * n + i]);
+      top = warp_max(top);
+      double s = 0.;
+      for (int i = lane; i < n; i += 32) {
+        const float ref = a.refs[row * n + i];
+        s += a.sums[row * n + i] * (ref == -INFINITY ? 1. : rescale(ref, top));      // (no word: 0, or NaN)
+      }
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+      if (!(s > 0. && s < INFINITY && fabsf(top) < INFINITY)) state = 0;
+      at -= log_of(s);
+    }
+    if (lane == 0) {
+      m.state[b] = (signed char)state;
+      m.base[b] = at;
+      m.ref[b] = top;
+    }
   }
   __syncthreads();
-  if (tid < 32) merge_lists(a, blockIdx.x, tops, sums, z, index, base, maxima, head);
+  // ---- the largest words of as many groups of runs as there are slots (the next power of two): the least of them is a value that `slots` words at least reach.  A group
+  // is the lanes that are alike modulo their number (more slots than lanes: those of the even warps and those of the odd ones)
+  unsigned long long best = 0;
+  for (int i = tid; i < a.beams * a.runs; i += kChoosers) {
+    const int b = i / a.runs;
+    if (m.state[b] != 1) continue;
+    const float top = a.run_max[row0 * a.runs + i];
+    if (top > -INFINITY) best = max(best, value_key(m, b, top));
+  }
+  if (tid < a.beams && m.state[tid] == 2) best = max(best, order_of(m.base[tid] + 0.));
+  int groups = 1;
+  while (groups < min(a.slots, 32)) groups *= 2;
+  for (int o = groups; o < 32; o *= 2) best = max(best, __shfl_xor_sync(0xffffffffu, best, o));
+  m.group[warp][lane] = best;
+  __syncthreads();
+  unsigned long long even = m.group[0][lane], odd = m.group[1][lane];
+#pragma unroll
+  for (int i = 2; i < kChooserWarps; i += 2) {
+    even = max(even, m.group[i][lane]);
+    odd = max(odd, m.group[i + 1][lane]);
+  }
+  unsigned long long thr = a.slots > 32 ? min(even, odd) : max(even, odd);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) thr = min(thr, __shfl_xor_sync(0xffffffffu, thr, o));
+  // ---- the words that reach it, and their places among each other: a warp a word
+  int n = gather<T, kAligned>(a, row0, m, thr, false);
+  if (n > kList) n = narrowed<T, kAligned>(a, row0, m, thr);
+  for (int i = warp; i < n; i += kChooserWarps) {
+    const unsigned long long k = m.key[i];
+    const int b = m.beam[i], word = m.word[i];
+    const float z = m.z[i];
+    int place = 0;
+    for (int j = lane; j < n; j += 32)
+      place += m.key[j] > k || (m.key[j] == k && (m.beam[j] < b || (m.beam[j] == b && better(m.z[j], m.word[j], z, word))));
+    place = __reduce_add_sync(0xffffffffu, place);
+    if (lane == 0 && place < a.slots) {
+      const long long at = sentence * a.slots + place;
+      a.parents[at] = b;
+      a.tokens[at] = word;
+      a.new_scores[at] = (float)value_of(k);
+      if (a.new_finished) a.new_finished[at] = word == a.end_id || m.state[b] == 2 ? 1 : 0;
+    }
+  }
+  // slots without an offer
+  for (int i = n + tid; i < a.slots; i += kChoosers) {
+    const long long at = sentence * a.slots + i;
+    a.parents[at] = 0;
+    a.tokens[at] = a.end_id;
+    a.new_scores[at] = -INFINITY;
+    if (a.new_finished) a.new_finished[at] = 1;
+  }
 }
 
-// How a row is cut, and whether a sentence's parts are a cluster that joins them itself.
-struct Cut {
-  int parts, cluster;
-};
-Cut cut_of(long long sentences, int beams, int slots, int vocab) {
-  const long long rows = sentences * beams, sms = mtf::device_sm_count();
-  if (beams <= kMostBlocks && rows <= sms * 2) {
-    int parts = 1;
-    while (beams * parts * 2 <= kMostBlocks && rows * parts * 2 <= sms * 2 && vocab / (parts * 2) >= 4096) parts *= 2;
-    return {parts, beams * parts};
-  }
-  // parts of at least 4096 words, so many that every SM has some blocks, and so few that a sentence's lists fit shared memory
-  const long long wanted = std::max(1LL, (sms * 8 + rows - 1) / rows);
-  const long long most = std::max(1LL, std::min<long long>(vocab / 4096, 4096 / ((long long)beams * slots)));
-  return {(int)std::min(wanted, most), 0};
-}
-size_t merge_room(int beams, int slots, int parts) {
-  return (size_t)beams * (2 + parts) * sizeof(double) + (size_t)beams * parts * slots * 8 + (size_t)beams * parts * 8;
-}
 size_t up16(size_t n) { return (n + 15) / 16 * 16; }
+// How a row is cut: parts of whole runs, so many that every block has some, of at least two runs a warp.
+struct Cut {
+  int parts, part, runs;
+};
+Cut cut_of(long long rows, int vocab, bool bf16) {
+  const long long words = kRun * (bf16 ? 8 : 4), runs = (vocab + words - 1) / words;
+  const long long wanted = std::max(1LL, ((long long)mtf::device_sm_count() * kBlocks * kParts + rows - 1) / rows), most = std::max(1LL, runs / (2 * kWarps));
+  const long long each = (runs + std::min(wanted, most) - 1) / std::min(wanted, most);
+  return {(int)((runs + each - 1) / each), (int)(each * words), (int)runs};
+}
 
 }  // namespace
 
 namespace mtf {
 
-size_t beam_select_workspace(long long sentences, int beams, int slots, int vocab) {
-  const Cut c = cut_of(sentences, beams, slots, vocab);
-  if (c.cluster) return 0;
-  const size_t lists = (size_t)sentences * beams * c.parts;
-  return up16(lists * sizeof(double)) + up16(lists * sizeof(float)) + up16(lists * slots * 4) + lists * slots * 4;
+size_t beam_select_workspace(long long sentences, int beams, int vocab, int bf16) {
+  const long long rows = sentences * beams;
+  const Cut c = cut_of(rows, vocab, bf16);
+  const size_t sums = (size_t)rows * c.parts * kWarps;
+  return up16(sums * sizeof(double)) + up16(sums * sizeof(float)) + (size_t)rows * c.runs * sizeof(float);
 }
 
 mtf_status launch_beam_select(const BeamSelect& b, void* stream) {
@@ -637,10 +676,10 @@ mtf_status launch_beam_select(const BeamSelect& b, void* stream) {
   a.beams = b.beams;
   a.slots = b.slots;
   a.rows = b.sentences * b.beams;
-  const Cut c = cut_of(b.sentences, b.beams, b.slots, b.vocab);
+  const Cut c = cut_of(a.rows, b.vocab, b.bf16);
   a.parts = c.parts;
-  a.cluster = c.cluster;
-  a.part = ((b.vocab + a.parts - 1) / a.parts + 7) / 8 * 8;
+  a.part = c.part;
+  a.runs = c.runs;
   a.scores = b.scores;
   a.finished = b.finished;
   a.end_id = b.end_id;
@@ -648,41 +687,44 @@ mtf_status launch_beam_select(const BeamSelect& b, void* stream) {
   a.tokens = b.tokens;
   a.new_finished = b.new_finished;
   a.new_scores = b.new_scores;
-  const size_t lists = (size_t)a.rows * a.parts;
+  const size_t sums = (size_t)a.rows * a.parts * kWarps;
   uint8_t* w = reinterpret_cast<uint8_t*>(b.workspace);
   a.sums = reinterpret_cast<double*>(w);
-  w += up16(lists * sizeof(double));
-  a.tops = reinterpret_cast<float*>(w);
-  w += up16(lists * sizeof(float));
-  a.best_z = reinterpret_cast<float*>(w);
-  w += up16(lists * a.slots * 4);
-  a.best_i = reinterpret_cast<int*>(w);
+  w += up16(sums * sizeof(double));
+  a.refs = reinterpret_cast<float*>(w);
+  w += up16(sums * sizeof(float));
+  a.run_max = reinterpret_cast<float*>(w);
+  if (a.rows * a.parts > 0x7fff0000LL || (long long)a.beams * a.runs > 0x7fff0000LL) return fail(MTF_ERR_UNSUPPORTED, "beam_select: at most 2^31 parts of rows");
   cudaStream_t st = (cudaStream_t)stream;
-  if (a.rows * a.parts > 0x7fffffffLL) return fail(MTF_ERR_UNSUPPORTED, "beam_select: at most 2^31 parts of rows");
-  if (a.cluster) {
-    cudaLaunchConfig_t cfg = {};
-    cudaLaunchAttribute at[2];
-    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at[0].val.programmaticStreamSerializationAllowed = 1;
-    at[1].id = cudaLaunchAttributeClusterDimension;
-    at[1].val.clusterDim.x = a.cluster;
-    at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
-    cfg.gridDim = dim3((unsigned)(a.rows * a.parts), 1, 1);
-    cfg.blockDim = dim3(kThreads, 1, 1);
-    cfg.stream = st;
-    cfg.attrs = at;
-    cfg.numAttrs = 2;
-    (void)cudaLaunchKernelEx(&cfg, b.bf16 ? beam_rows_kernel<__nv_bfloat16> : beam_rows_kernel<float>, a);
-    count_launch();
-  } else {
-    if (b.bf16) launch_chained(beam_rows_kernel<__nv_bfloat16>, (unsigned)(a.rows * a.parts), kThreads, 0, st, a);
-    else launch_chained(beam_rows_kernel<float>, (unsigned)(a.rows * a.parts), kThreads, 0, st, a);
-    count_launch();
-    launch_chained(beam_merge_kernel, (unsigned)b.sentences, 128, merge_room(a.beams, a.slots, a.parts), st, a);
-    count_launch();
-  }
+  const bool aligned = (long long)b.vocab * (b.bf16 ? 2 : 4) % 16 == 0;
+  const auto rows = b.bf16 ? (aligned ? beam_rows_kernel<__nv_bfloat16, true> : beam_rows_kernel<__nv_bfloat16, false>)
+                           : (aligned ? beam_rows_kernel<float, true> : beam_rows_kernel<float, false>);
+  const auto choose = b.bf16 ? (aligned ? beam_choose_kernel<__nv_bfloat16, true> : beam_choose_kernel<__nv_bfloat16, false>)
+                             : (aligned ? beam_choose_kernel<float, true> : beam_choose_kernel<float, false>);
+  const cudaError_t set = cudaFuncSetAttribute(rows, cudaFuncAttributeMaxDynamicSharedMemorySize, kRing);
+  if (set != cudaSuccess) return fail(MTF_ERR_CUDA, "beam_rows_kernel: %s", cudaGetErrorString(set));
+  launch_chained(rows, (unsigned)std::min<long long>(a.rows * a.parts, (long long)device_sm_count() * kBlocks), kThreads, kRing, st, a);
+  count_launch();
+  launch_chained(choose, (unsigned)b.sentences, kChoosers, 0, st, a);
+  count_launch();
   const cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess) return fail(MTF_ERR_CUDA, "beam_select kernels: %s", cudaGetErrorString(e));
+  return MTF_OK;
+}
+
+mtf_status debug_beam_wait_test(long long limit_cycles, int withhold) {
+  const long long limit = limit_cycles > 0 ? limit_cycles : kWaitCycles;
+  cudaError_t e = cudaMemcpyToSymbol(g_wait_limit, &limit, sizeof(limit));
+  if (e == cudaSuccess) e = cudaMemcpyToSymbol(g_withhold, &withhold, sizeof(int));
+  if (e != cudaSuccess) return fail(MTF_ERR_CUDA, "cudaMemcpyToSymbol: %s", cudaGetErrorString(e));
+  return MTF_OK;
+}
+mtf_status read_beam_status(int* code) {
+  int v = 0;
+  cudaError_t e = cudaMemcpyFromSymbol(&v, g_beam_status, sizeof(int));
+  if (e != cudaSuccess) return fail(MTF_ERR_CUDA, "cudaMemcpyFromSymbol: %s", cudaGetErrorString(e));
+  if (v) { int z = 0; cudaMemcpyToSymbol(g_beam_status, &z, sizeof(int)); }
+  *code = v;
   return MTF_OK;
 }
 

@@ -13,6 +13,7 @@
 
 #include <algorithm>
 
+#include "answer.cuh"
 #include "answer.h"
 #include "launch.cuh"
 
@@ -318,16 +319,7 @@ RowsArgs rows_args(const mtf::CachePool& c, const mtf::CacheRows& r) {
 template <int kLanes, bool kBf16, bool kE4m3>
 void rows_launch(const RowsArgs& a, bool write, cudaStream_t st) {
   const long long at_once = (256 / kLanes) * kEach, blocks = std::max(1LL, std::min<long long>((a.rows + at_once - 1) / at_once, (long long)mtf::device_sm_count() * 16));
-  cudaLaunchConfig_t cfg = {};
-  cudaLaunchAttribute at[1];
-  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  at[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.gridDim = dim3((unsigned)blocks, 2, 1);
-  cfg.blockDim = dim3(256, 1, 1);
-  cfg.stream = st;
-  cfg.attrs = at;
-  cfg.numAttrs = 1;
-  (void)cudaLaunchKernelEx(&cfg, write ? cache_write_kernel<kLanes, kBf16, kE4m3> : cache_read_kernel<kLanes, kBf16, kE4m3>, a);
+  mtf::launch_clusters(write ? cache_write_kernel<kLanes, kBf16, kE4m3> : cache_read_kernel<kLanes, kBf16, kE4m3>, dim3((unsigned)blocks, 2, 1), 256, 0, 1, st, a);
 }
 template <bool kBf16, bool kE4m3>
 void rows_lanes(const RowsArgs& a, bool write, cudaStream_t st) {
@@ -354,16 +346,7 @@ template <typename T>
 void reorder_launch(const int32_t* parents, const void* in, void* out, long long rows, int beams, int slots, long long bytes, cudaStream_t st) {
   const long long pieces = bytes / (long long)sizeof(T);
   const long long shares = std::max(1LL, std::min((pieces + 1023) / 1024, std::max(1LL, (long long)mtf::device_sm_count() * 16 / rows)));
-  cudaLaunchConfig_t cfg = {};
-  cudaLaunchAttribute at[1];
-  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  at[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.gridDim = dim3((unsigned)rows, (unsigned)std::min(shares, 65535LL), 1);
-  cfg.blockDim = dim3(256, 1, 1);
-  cfg.stream = st;
-  cfg.attrs = at;
-  cfg.numAttrs = 1;
-  (void)cudaLaunchKernelEx(&cfg, beam_reorder_kernel<T>, parents, reinterpret_cast<const T*>(in), reinterpret_cast<T*>(out), beams, slots, pieces);
+  mtf::launch_clusters(beam_reorder_kernel<T>, dim3((unsigned)rows, (unsigned)std::min(shares, 65535LL), 1), 256, 0, 1, st, parents, reinterpret_cast<const T*>(in), reinterpret_cast<T*>(out), beams, slots, pieces);
 }
 
 }  // namespace
@@ -399,16 +382,7 @@ mtf_status launch_cache_reorder(const CachePool& c, const CacheReorder& r, void*
   const long long rows = r.groups * r.out, page_bytes = (long long)c.rows_page * (a.row_bytes[0] + a.row_bytes[1]);
   // a share of a page's copy that is worth a block, as long as the GPU has room for more of them
   const long long shares = std::max(1LL, std::min({(page_bytes + 32767) / 32768, (long long)device_sm_count() * 8 / rows + 1, 64LL}));
-  cudaLaunchConfig_t cfg = {};
-  cudaLaunchAttribute at[1];
-  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  at[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.gridDim = dim3((unsigned)rows, (unsigned)shares, 1);
-  cfg.blockDim = dim3(256, 1, 1);
-  cfg.stream = (cudaStream_t)stream;
-  cfg.attrs = at;
-  cfg.numAttrs = 1;
-  (void)cudaLaunchKernelEx(&cfg, cache_reorder_kernel, a);
+  mtf::launch_clusters(cache_reorder_kernel, dim3((unsigned)rows, (unsigned)shares, 1), 256, 0, 1, (cudaStream_t)stream, a);
   return after("cache_reorder_kernel");
 }
 
