@@ -29,17 +29,16 @@ using mtf::smem_at;
 constexpr int kThreads = 256, kWarps = kThreads / 32, kBlocks = 4;      // of the walk; blocks an SM holds
 constexpr int kRun = 128;             // 16-byte pieces that a warp takes at a time
 constexpr int kStages = 3;            // of a warp's ring, a run each: 50 KB a block
-constexpr int kStage = (kRun + 1) * 16, kRing = kWarps * kStages * kStage;
+constexpr int kStage = (kRun + 8) * 16, kRing = kWarps * kStages * kStage;
 constexpr int kChoosers = 512, kChooserWarps = kChoosers / 32;
 constexpr int kList = 1024;           // words that may be looked at again before the choice goes by counting
 constexpr int kRuns = 1024;           // runs they may lie in
-constexpr int kParts = 2;             // of all rows together, a block's
+constexpr int kFirst = 4;             // a sentence's runs that a thread of the choice keeps the largest words of
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kSlack = 20.f;        // a thread's reference is raised where an entry lies e^20 above it
 
 struct Args {
   const void* z;
-  int vocab, beams, slots, parts, part;          // part: words of one, whole runs
+  int vocab, beams, slots;
   int runs;                                      // of a row
   long long rows;
   const float* scores;
@@ -47,9 +46,7 @@ struct Args {
   int end_id;
   int32_t *parents, *tokens, *new_finished;
   float* new_scores;
-  float* run_max;                                // [row, run]
-  float* refs;                                   // [row, part, warp]: the reference of its sum of exponentials
-  double* sums;                                  // ... and the sum
+  float2* of_run;                                // [row, run]: the largest word, and the sum of exponentials relative to it
 };
 
 // 16 bytes of words
@@ -184,31 +181,23 @@ __device__ __noinline__ double far_apart(float from, float to) { return exp((dou
 __device__ __forceinline__ double rescale(float from, float to) { return from == to ? 1. : far_apart(from, to); }
 __device__ __noinline__ double log_of(double s) { return log(s); }
 
-// A thread's sum of exponentials relative to `ref`, a large entry (from differences, which are exact for the entries that weigh).
-struct Sum {
-  float ref = -INFINITY;
+// the sum of exponentials of some words relative to ref (from differences, which are exact for the words that weigh)
+template <typename T, int K>
+__device__ __forceinline__ float2 exponentials(const uint4 (&v)[K], float ref) {
   float2 s = make_float2(0.f, 0.f);
-  // some more words, of which m is the largest
-  template <typename T, int K>
-  __device__ __forceinline__ void add(const uint4 (&v)[K], float m) {
-    if (m > ref + kSlack || (ref == -INFINITY && m > -INFINITY)) {
-      const float f = ref == -INFINITY ? 0.f : exp2f((ref - m) * kLog2e);
-      s = times(s, make_float2(f, f));               // (a sum of 0, or NaN, where there was no reference)
-      ref = m;
-    }
-    const float r = ref == -INFINITY ? 0.f : -ref;
+  const float r = ref == -INFINITY ? 0.f : -ref;
 #pragma unroll
-    for (int e = 0; e < K; ++e) {
-      float x[Words<T>::kN];
-      Words<T>::values(v[e], x);
+  for (int e = 0; e < K; ++e) {
+    float x[Words<T>::kN];
+    Words<T>::values(v[e], x);
 #pragma unroll
-      for (int j = 0; j < Words<T>::kN; j += 2) {
-        const float2 d = times(plus(make_float2(x[j], x[j + 1]), make_float2(r, r)), make_float2(kLog2e, kLog2e));
-        s = plus(s, make_float2(ex2(d.x), ex2(d.y)));
-      }
+    for (int j = 0; j < Words<T>::kN; j += 2) {
+      const float2 d = times(plus(make_float2(x[j], x[j + 1]), make_float2(r, r)), make_float2(kLog2e, kLog2e));
+      s = plus(s, make_float2(ex2(d.x), ex2(d.y)));
     }
   }
-};
+  return s;
+}
 
 __device__ __forceinline__ bool better(float z, int i, float y, int j) { return z > y || (z == y && i < j); }
 // 64 bits in the order of the values
@@ -216,147 +205,135 @@ __device__ __forceinline__ unsigned long long order_of(double v) {
   const unsigned long long b = (unsigned long long)__double_as_longlong(v);
   return b >> 63 ? ~b : b | 0x8000000000000000ull;
 }
-// A warp's share of the copies: the runs w, w + 8, .. of a part, those whose pieces are whole by bulk copies into its ring, the last ones by loads.
-struct Ring {
-  uint8_t* base;                       // this warp's
-  uint64_t* bars;
-  int stage = 0;
-  uint32_t phase = 0;
-  bool gone = false;                   // a wait was given up
-
-  template <typename P>
-  __device__ __forceinline__ void fetch(const P& w, int run, int into) const {      // (one lane)
-    const uint32_t bar = smem_at(&bars[into]), bytes = (kRun + (w.off ? 1 : 0)) * 16;
-    mtf::expect(bar, bytes);
-    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(smem_at(base) + into * kStage), "l"(w.base + (long long)run * kRun),
-                 "r"(bytes), "r"(bar)
-                 : "memory");
-  }
-  // the first runs of a part, when nothing is under way
-  template <typename P>
-  __device__ __forceinline__ void begin(const P& w) const {
-    const int warp = threadIdx.x >> 5, whole = w.whole / kRun;
-    if ((threadIdx.x & 31) == 0 && !gone) {
-      int into = stage;
-#pragma unroll
-      for (int i = 0; i < kStages; ++i) {
-        if (warp + i * kWarps < whole) fetch(w, warp + i * kWarps, into);
-        if (++into == kStages) into = 0;
-      }
-    }
-  }
-  // a wait was given up: what is under way, the copy of this stage and those of the runs behind it
-  __device__ __noinline__ void give_up(int run, int whole) {
-    if ((threadIdx.x & 31) == 0) atomicCAS(&g_beam_status, 0, 0xB11);
-    gone = true;
-    for (int i = 0; i < kStages; ++i)
-      if (run + i * kWarps < whole) mtf::landed_late(smem_at(&bars[(stage + i) % kStages]), stage + i >= kStages ? phase ^ 1 : phase, mtf::kLandCycles);
-  }
-  // a run of whole pieces, from the ring
-  template <typename P, int K>
-  __device__ __forceinline__ void take(const P& w, int run, int whole, uint4 (&v)[K]) {
-    const int lane = threadIdx.x & 31;
-    const uint32_t bar = smem_at(&bars[stage]);
-    if (!gone && (!mtf::landed(bar, phase, g_wait_limit) || (g_withhold && !mtf::landed(bar, phase ^ 1, g_wait_limit)))) give_up(run, whole);
-    const uint4* const at = reinterpret_cast<const uint4*>(base + stage * kStage) + lane;
-#pragma unroll
-    for (int e = 0; e < K; ++e) v[e] = w.at(at + e * 32);
-    __syncwarp();
-    if (lane == 0 && !gone && run + kStages * kWarps < whole) fetch(w, run + kStages * kWarps, stage);
-    if (++stage == kStages) { stage = 0; phase ^= 1; }
-  }
-};
-
 __device__ __forceinline__ float warp_max(float m) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
   return m;
 }
 
-// A warp's share of a part, runs first + warp, first + warp + 8, .. of the row.  The copies for it are under way; behind it those for `next` (if there is one) are asked for.
-template <typename T, typename P>
-__device__ __forceinline__ void walk(const P& w, const P& next, bool more, Ring& ring, float* run_max, float* to_ref, double* to_sum) {
-  constexpr int kDeep = kRun / 32;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int pieces = w.pieces(), runs = (pieces + kRun - 1) / kRun, whole = w.whole / kRun;
-  Sum sum;
-  uint4 v[kDeep];
-  int run = warp;
-  for (; run < whole; run += kWarps) {
-    ring.take(w, run, whole, v);
-    const float m = Words<T>::largest(v), all = warp_max(m);
-    if (run == warp) sum.ref = all;                  // (all lanes begin with the same, so that their sums can be added as they are)
-    sum.add<T>(v, m);
-    if (lane == 0) run_max[run] = all;
-  }
-  for (; run < runs; run += kWarps) {
-    float all = -INFINITY;
-#pragma unroll 1
-    for (int e = 0; e < kDeep; ++e) {
-      const int q = run * kRun + e * 32 + lane;
-      const uint4 u[1] = {q < pieces ? w.load(q) : make_uint4(Words<T>::kNone, Words<T>::kNone, Words<T>::kNone, Words<T>::kNone)};
-      const float m = Words<T>::largest(u);
-      all = fmaxf(all, m);
-      sum.add<T>(u, m);
-    }
-    all = warp_max(all);
-    if (lane == 0) run_max[run] = all;
-  }
-  if (more) ring.begin(next);
-  // the warp's sum, in 64 bits in a fixed order
-  const float ref = warp_max(sum.ref);
-  double s = (double)sum.s.x + (double)sum.s.y;
-  if (sum.ref != -INFINITY) s *= rescale(sum.ref, ref);
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-  if (lane == 0) {
-    *to_ref = ref;
-    *to_sum = s;
-  }
+// A beam's row, whole
+template <typename T, bool kAligned>
+__device__ __forceinline__ Part<T, kAligned> row_at(const Args& a, long long row) {
+  return Part<T, kAligned>(reinterpret_cast<const T*>(a.z), row * a.vocab, a.vocab, a.rows * a.vocab);
 }
 
-// Blocks go from part to part; the first copies of the next one are asked for as soon as a warp is through with its share.
+// The runs of all rows one behind another, every warp of the grid the next one: all of them have as many, wherever beams lie that are not to be read.
 template <typename T, bool kAligned>
 __global__ void __launch_bounds__(kThreads, kBlocks) beam_rows_kernel(const Args a) {
+  constexpr int kDeep = kRun / 32;
   __shared__ uint64_t bars[kWarps][kStages];
-  extern __shared__ __align__(16) uint8_t dyn[];
+  extern __shared__ __align__(128) uint8_t dyn[];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  Ring ring;
-  ring.base = dyn + warp * kStages * kStage;
-  ring.bars = bars[warp];
+  const uint8_t* const ring = dyn + warp * kStages * kStage;
   if (lane == 0) {
-    for (int i = 0; i < kStages; ++i) mtf::landing_init(&ring.bars[i]);
+    for (int i = 0; i < kStages; ++i) mtf::landing_init(&bars[warp][i]);
     mtf::landing_ready();
   }
   __syncwarp();
   mtf::chain_wait();
-  auto part_at = [&](int row, int part) {
-    return Part<T, kAligned>(reinterpret_cast<const T*>(a.z), (long long)row * a.vocab + (long long)part * a.part, min(a.part, a.vocab - part * a.part), a.rows * a.vocab);
+  const int all = gridDim.x * kWarps, rows = (int)a.rows, some_rows = all / a.runs, some_runs = all - some_rows * a.runs;
+  struct Place {
+    int row, run;
   };
-  const int units = (int)a.rows * a.parts;           // (below 2^31 less the grid's blocks)
-  // unit u, or the first one behind it of this block's that is to be read (a beam that is finished, or none, is not); -1: none
-  auto from = [&](int u) {
-    for (; u < units; u += gridDim.x) {
-      const int row = u / a.parts, done = a.finished ? a.finished[row] : 0;
-      const float score = a.scores[row];
-      if (fabsf(score) < INFINITY && !done) return u;
+  auto onward = [&](Place& p) {
+    p.row += some_rows;
+    p.run += some_runs;
+    if (p.run >= a.runs) {
+      p.run -= a.runs;
+      ++p.row;
     }
-    return -1;
   };
-  int u = from(blockIdx.x);
-  if (u < 0) return;
-  int row = u / a.parts, part = u - row * a.parts;
-  Part<T, kAligned> w = part_at(row, part);
-  ring.begin(w);
-  while (u >= 0) {
-    const int next = from(u + gridDim.x), next_row = next >= 0 ? next / a.parts : row, next_part = next >= 0 ? next - next_row * a.parts : part;
-    const Part<T, kAligned> behind = part_at(next_row, next_part);
-    const long long list = ((long long)row * a.parts + part) * kWarps + warp;
-    walk<T>(w, behind, next >= 0, ring, a.run_max + (long long)row * a.runs + part * (a.part / (kRun * Words<T>::kN)), a.refs + list, a.sums + list);
-    u = next;
-    row = next_row;
-    part = next_part;
-    w = behind;
+  // whether a row is to be read (a beam that is finished, or none, is not): asked for a step before it is needed
+  struct Asked {
+    float score;
+    int done;
+  };
+  auto ask = [&](const Place& p) {
+    const bool in = p.row < rows;
+    Asked q;
+    q.score = in ? a.scores[p.row] : INFINITY;
+    q.done = in && a.finished ? a.finished[p.row] : 0;
+    return q;
+  };
+  const int first = blockIdx.x * kWarps + warp;
+  Place now = {first / a.runs, first % a.runs}, ahead = now;
+  uint32_t read = 0, flying = 0;                     // of the stages: the run is to be read, and is being copied
+  auto fetch = [&](int stage, const Place& p, const Asked& q) {
+    const bool live = fabsf(q.score) < INFINITY && !q.done;
+    read = (read & ~(1u << stage)) | (live ? 1u : 0u) << stage;
+    flying &= ~(1u << stage);
+    if (!live) return;
+    const Part<T, kAligned> w = row_at<T, kAligned>(a, p.row);
+    if ((p.run + 1) * kRun > w.whole) return;        // (a row's last words: by loads)
+    flying |= 1u << stage;
+    if (lane == 0) {
+      const uint32_t bar = smem_at(&bars[warp][stage]), bytes = (kRun + (w.off ? 1 : 0)) * 16;
+      mtf::expect(bar, bytes);
+      asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(smem_at(ring) + stage * kStage), "l"(w.base + (long long)p.run * kRun),
+                   "r"(bytes), "r"(bar)
+                   : "memory");
+    }
+  };
+  {
+    Place p = now;
+    Asked q[kStages];
+#pragma unroll
+    for (int i = 0; i < kStages; ++i) {
+      q[i] = ask(p);
+      onward(p);
+    }
+#pragma unroll
+    for (int i = 0; i < kStages; ++i) {
+      fetch(i, ahead, q[i]);
+      onward(ahead);
+    }
+  }
+  Asked next = ask(ahead);
+  uint32_t phases = 0;                               // of the stages' barriers
+  for (int stage = 0; now.row < rows; stage = stage + 1 == kStages ? 0 : stage + 1) {
+    if (read >> stage & 1) {
+      const Part<T, kAligned> w = row_at<T, kAligned>(a, now.row);
+      uint4 v[kDeep];
+      if (flying >> stage & 1) {
+        const uint32_t bar = smem_at(&bars[warp][stage]), phase = phases >> stage & 1;
+        if (!mtf::landed(bar, phase, g_wait_limit) || (g_withhold && !mtf::landed(bar, phase ^ 1, g_wait_limit))) {
+          if (lane == 0) atomicCAS(&g_beam_status, 0, 0xB11);
+          // given up: what is under way gets a little more time
+          for (int i = 0; i < kStages; ++i)
+            if (flying >> i & 1) mtf::landed_late(smem_at(&bars[warp][i]), phases >> i & 1, mtf::kLandCycles);
+          return;
+        }
+        phases ^= 1u << stage;
+        const uint4* const at = reinterpret_cast<const uint4*>(ring + stage * kStage) + lane;
+#pragma unroll
+        for (int e = 0; e < kDeep; ++e) v[e] = w.at(at + e * 32);
+      } else {
+#pragma unroll 1
+        for (int e = 0; e < kDeep; ++e) {
+          const int q = now.run * kRun + e * 32 + lane;
+          const uint4 u = q < w.pieces() ? w.load(q) : make_uint4(Words<T>::kNone, Words<T>::kNone, Words<T>::kNone, Words<T>::kNone);
+          if (e == 0) v[0] = u;
+          else if (e == 1) v[1] = u;
+          else if (e == 2) v[2] = u;
+          else v[3] = u;
+        }
+      }
+      const float top = warp_max(Words<T>::largest(v));
+      __syncwarp();                                  // (every lane has its words)
+      fetch(stage, ahead, next);
+      onward(ahead);
+      next = ask(ahead);
+      const float2 s2 = exponentials<T>(v, top);
+      float s = s2.x + s2.y;
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+      if (lane == 0) a.of_run[(long long)now.row * a.runs + now.run] = make_float2(top, s);
+    } else {
+      fetch(stage, ahead, next);
+      onward(ahead);
+      next = ask(ahead);
+    }
+    onward(now);
   }
 }
 
@@ -381,16 +358,10 @@ __device__ __forceinline__ float lowest(double v, double base, float ref) {
 }
 __device__ __forceinline__ double value_of(unsigned long long key) { return __longlong_as_double((long long)(key >> 63 ? key & 0x7fffffffffffffffull : ~key)); }
 
-// A beam's row, whole (words by the same pieces as the walk's)
-template <typename T, bool kAligned>
-__device__ __forceinline__ Part<T, kAligned> row_at(const Args& a, long long row) {
-  return Part<T, kAligned>(reinterpret_cast<const T*>(a.z), row * a.vocab, a.vocab, a.rows * a.vocab);
-}
-
 // The words whose value is at least thr (strict: above it), into the list, from the runs whose largest word's is; and the ends of finished beams.  All threads.  Returns how many
 // there are: over kList where that is more than the list holds, or where they lie in too many runs.
 template <typename T, bool kAligned>
-__device__ __noinline__ int gather(const Args& a, long long row0, Room& m, unsigned long long thr, bool strict) {
+__device__ __forceinline__ int gather(const Args& a, long long row0, Room& m, unsigned long long thr, bool strict, const float (&first)[kFirst]) {
   constexpr int kN = Words<T>::kN, kDeep = kRun / 32;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   auto reaches = [&](unsigned long long k) { return strict ? k > thr : k >= thr; };
@@ -398,15 +369,16 @@ __device__ __noinline__ int gather(const Args& a, long long row0, Room& m, unsig
   if (tid == 0) m.count = m.n_runs = 0;
   if (tid < a.beams) m.low[tid] = thr ? lowest(value_of(thr), m.base[tid], m.ref[tid]) : -INFINITY;
   __syncthreads();
-  for (int i = tid; i < a.beams * a.runs; i += kChoosers) {
+  auto note = [&](int i, float top) {
     const int b = i / a.runs;
-    if (m.state[b] != 1) continue;
-    const float top = a.run_max[row0 * a.runs + i];
-    if (top > -INFINITY && reaches(value_key(m, b, top))) {
-      const int at = atomicAdd(&m.n_runs, 1);
-      if (at < kRuns) m.runs[at] = i;
-    }
-  }
+    if (m.state[b] != 1 || !(top > -INFINITY) || !reaches(value_key(m, b, top))) return;
+    const int at = atomicAdd(&m.n_runs, 1);
+    if (at < kRuns) m.runs[at] = i;
+  };
+#pragma unroll
+  for (int e = 0; e < kFirst; ++e)
+    if (tid + e * kChoosers < a.beams * a.runs) note(tid + e * kChoosers, first[e]);
+  for (int i = tid + kFirst * kChoosers; i < a.beams * a.runs; i += kChoosers) note(i, a.of_run[row0 * a.runs + i].x);
   if (tid < a.beams && m.state[tid] == 2 && reaches(order_of(m.base[tid] + 0.))) {
     const int at = atomicAdd(&m.count, 1);
     m.key[at] = order_of(m.base[tid] + 0.);
@@ -421,16 +393,17 @@ __device__ __noinline__ int gather(const Args& a, long long row0, Room& m, unsig
     const int b = m.runs[i] / a.runs, run = m.runs[i] - b * a.runs;
     const Part<T, kAligned> w = row_at<T, kAligned>(a, row0 + b);
     const float low = m.low[b];
-    uint4 v[kDeep];
+    // (the loads of a run under way at once; the few pieces that have some are loaded again)
+    uint32_t have = 0;
 #pragma unroll
     for (int e = 0; e < kDeep; ++e) {
       const int q = run * kRun + e * 32 + lane;
-      v[e] = q < w.pieces() ? w.load(q) : make_uint4(Words<T>::kNone, Words<T>::kNone, Words<T>::kNone, Words<T>::kNone);
+      const uint4 u[1] = {q < w.pieces() ? w.load(q) : make_uint4(Words<T>::kNone, Words<T>::kNone, Words<T>::kNone, Words<T>::kNone)};
+      have |= (Words<T>::largest(u) >= low ? 1u : 0u) << e;
     }
-#pragma unroll 1
-    for (int e = 0; e < kDeep; ++e) {
-      const uint4 u[1] = {e == 0 ? v[0] : e == 1 ? v[1] : e == 2 ? v[2] : v[3]};
-      if (!(Words<T>::largest(u) >= low)) continue;
+    for (; have; have &= have - 1) {
+      const int e = __ffs(have) - 1;
+      const uint4 u[1] = {w.load(run * kRun + e * 32 + lane)};
       float x[kN];
       Words<T>::values(u[0], x);
 #pragma unroll
@@ -456,10 +429,10 @@ __device__ __noinline__ int gather(const Args& a, long long row0, Room& m, unsig
 // Where too many words reach thr to be sorted (rows of equal words, or masked by a finite value): those above it, and the first of those equal to it.  Where those above are
 // too many, too, thr becomes the slots-th largest value, by counting its bytes from the highest on.  Returns how many the list holds.  All threads.
 template <typename T, bool kAligned>
-__device__ __noinline__ int narrowed(const Args& a, long long row0, Room& m, unsigned long long thr) {
+__device__ __noinline__ int narrowed(const Args& a, long long row0, Room& m, unsigned long long thr, const float (&first)[kFirst]) {
   constexpr int kN = Words<T>::kN;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  int above = gather<T, kAligned>(a, row0, m, thr, true);
+  int above = gather<T, kAligned>(a, row0, m, thr, true, first);
   if (above > kList) {
     int* const counts = reinterpret_cast<int*>(m.key);
     unsigned long long prefix = 0;
@@ -490,7 +463,7 @@ __device__ __noinline__ int narrowed(const Args& a, long long row0, Room& m, uns
       prefix = prefix << 8 | (unsigned)d;
     }
     thr = prefix;
-    above = gather<T, kAligned>(a, row0, m, thr, true);              // fewer than `slots`, in runs of which there are no more
+    above = gather<T, kAligned>(a, row0, m, thr, true, first);              // fewer than `slots`, in runs of which there are no more
   }
   // equal ones: by the lower beam, of a beam's the larger logits (the sums may have lost what tells them apart), of these the lower words; as long as there is need of them
   int at = above;
@@ -564,23 +537,36 @@ __global__ void __launch_bounds__(kChoosers, 1) beam_choose_kernel(const Args a)
   mtf::chain_wait_only();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const long long sentence = blockIdx.x, row0 = sentence * a.beams;
-  // ---- a warp a beam: its sum
+  float first[kFirst];
+#pragma unroll
+  for (int e = 0; e < kFirst; ++e) first[e] = tid + e * kChoosers < a.beams * a.runs ? a.of_run[row0 * a.runs + tid + e * kChoosers].x : -INFINITY;
+  // ---- a warp a beam: its sum, joined in 64 bits in a fixed order
   for (int b = warp; b < a.beams; b += kChooserWarps) {
     const long long row = row0 + b;
+    const float2* const runs = a.of_run + row * a.runs;
+    constexpr int kMine = 4;                         // that a lane keeps
+    float2 r[kMine];                                 // (of a beam that was not looked at anything)
+#pragma unroll
+    for (int e = 0; e < kMine; ++e) r[e] = lane + e * 32 < a.runs ? runs[lane + e * 32] : make_float2(-INFINITY, 0.f);
     const float score = a.scores[row];
-    const int done = a.finished ? a.finished[row] : 0, n = a.parts * kWarps;
+    const int done = a.finished ? a.finished[row] : 0;
     int state = fabsf(score) < INFINITY ? done ? 2 : 1 : 0;
     float top = 0.f;
     double at = score;
     if (state == 1) {
       top = -INFINITY;
-      for (int i = lane; i < n; i += 32) top = fmaxf(top, a.refs[row * n + i]);
+#pragma unroll
+      for (int e = 0; e < kMine; ++e) top = fmaxf(top, r[e].x);
+      for (int i = lane + kMine * 32; i < a.runs; i += 32) top = fmaxf(top, runs[i].x);
       top = warp_max(top);
+      // (a run without a finite word: 0 times its sum, 0 or NaN)
       double s = 0.;
-      for (int i = lane; i < n; i += 32) {
-        const float ref = a.refs[row * n + i];
-        s += a.sums[row * n + i] * (ref == -INFINITY ? 1. : rescale(ref, top));      // (no word: 0, or NaN)
+#pragma unroll 1
+      for (int e = 0; e < kMine; ++e) {
+        const float2 x = e == 0 ? r[0] : e == 1 ? r[1] : e == 2 ? r[2] : r[3];
+        if (lane + e * 32 < a.runs) s += x.y * rescale(x.x, top);
       }
+      for (int i = lane + kMine * 32; i < a.runs; i += 32) s += runs[i].y * rescale(runs[i].x, top);
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
       if (!(s > 0. && s < INFINITY && fabsf(top) < INFINITY)) state = 0;
@@ -596,12 +582,14 @@ __global__ void __launch_bounds__(kChoosers, 1) beam_choose_kernel(const Args a)
   // ---- the largest words of as many groups of runs as there are slots (the next power of two): the least of them is a value that `slots` words at least reach.  A group
   // is the lanes that are alike modulo their number (more slots than lanes: those of the even warps and those of the odd ones)
   unsigned long long best = 0;
-  for (int i = tid; i < a.beams * a.runs; i += kChoosers) {
+  auto better_of = [&](int i, float top) {
     const int b = i / a.runs;
-    if (m.state[b] != 1) continue;
-    const float top = a.run_max[row0 * a.runs + i];
-    if (top > -INFINITY) best = max(best, value_key(m, b, top));
-  }
+    if (m.state[b] == 1 && top > -INFINITY) best = max(best, value_key(m, b, top));
+  };
+#pragma unroll
+  for (int e = 0; e < kFirst; ++e)
+    if (tid + e * kChoosers < a.beams * a.runs) better_of(tid + e * kChoosers, first[e]);
+  for (int i = tid + kFirst * kChoosers; i < a.beams * a.runs; i += kChoosers) better_of(i, a.of_run[row0 * a.runs + i].x);
   if (tid < a.beams && m.state[tid] == 2) best = max(best, order_of(m.base[tid] + 0.));
   int groups = 1;
   while (groups < min(a.slots, 32)) groups *= 2;
@@ -618,8 +606,8 @@ __global__ void __launch_bounds__(kChoosers, 1) beam_choose_kernel(const Args a)
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) thr = min(thr, __shfl_xor_sync(0xffffffffu, thr, o));
   // ---- the words that reach it, and their places among each other: a warp a word
-  int n = gather<T, kAligned>(a, row0, m, thr, false);
-  if (n > kList) n = narrowed<T, kAligned>(a, row0, m, thr);
+  int n = gather<T, kAligned>(a, row0, m, thr, false, first);
+  if (n > kList) n = narrowed<T, kAligned>(a, row0, m, thr, first);
   for (int i = warp; i < n; i += kChooserWarps) {
     const unsigned long long k = m.key[i];
     const int b = m.beam[i], word = m.word[i];
@@ -646,28 +634,16 @@ __global__ void __launch_bounds__(kChoosers, 1) beam_choose_kernel(const Args a)
   }
 }
 
-size_t up16(size_t n) { return (n + 15) / 16 * 16; }
-// How a row is cut: parts of whole runs, so many that every block has some, of at least two runs a warp.
-struct Cut {
-  int parts, part, runs;
-};
-Cut cut_of(long long rows, int vocab, bool bf16) {
-  const long long words = kRun * (bf16 ? 8 : 4), runs = (vocab + words - 1) / words;
-  const long long wanted = std::max(1LL, ((long long)mtf::device_sm_count() * kBlocks * kParts + rows - 1) / rows), most = std::max(1LL, runs / (2 * kWarps));
-  const long long each = (runs + std::min(wanted, most) - 1) / std::min(wanted, most);
-  return {(int)((runs + each - 1) / each), (int)(each * words), (int)runs};
+int runs_of(int vocab, bool bf16) {
+  const int words = kRun * (bf16 ? 8 : 4);
+  return (vocab + words - 1) / words;
 }
 
 }  // namespace
 
 namespace mtf {
 
-size_t beam_select_workspace(long long sentences, int beams, int vocab, int bf16) {
-  const long long rows = sentences * beams;
-  const Cut c = cut_of(rows, vocab, bf16);
-  const size_t sums = (size_t)rows * c.parts * kWarps;
-  return up16(sums * sizeof(double)) + up16(sums * sizeof(float)) + (size_t)rows * c.runs * sizeof(float);
-}
+size_t beam_select_workspace(long long sentences, int beams, int vocab, int bf16) { return (size_t)sentences * beams * runs_of(vocab, bf16) * sizeof(float2); }
 
 mtf_status launch_beam_select(const BeamSelect& b, void* stream) {
   Args a = {};
@@ -676,10 +652,7 @@ mtf_status launch_beam_select(const BeamSelect& b, void* stream) {
   a.beams = b.beams;
   a.slots = b.slots;
   a.rows = b.sentences * b.beams;
-  const Cut c = cut_of(a.rows, b.vocab, b.bf16);
-  a.parts = c.parts;
-  a.part = c.part;
-  a.runs = c.runs;
+  a.runs = runs_of(b.vocab, b.bf16);
   a.scores = b.scores;
   a.finished = b.finished;
   a.end_id = b.end_id;
@@ -687,14 +660,9 @@ mtf_status launch_beam_select(const BeamSelect& b, void* stream) {
   a.tokens = b.tokens;
   a.new_finished = b.new_finished;
   a.new_scores = b.new_scores;
-  const size_t sums = (size_t)a.rows * a.parts * kWarps;
-  uint8_t* w = reinterpret_cast<uint8_t*>(b.workspace);
-  a.sums = reinterpret_cast<double*>(w);
-  w += up16(sums * sizeof(double));
-  a.refs = reinterpret_cast<float*>(w);
-  w += up16(sums * sizeof(float));
-  a.run_max = reinterpret_cast<float*>(w);
-  if (a.rows * a.parts > 0x7fff0000LL || (long long)a.beams * a.runs > 0x7fff0000LL) return fail(MTF_ERR_UNSUPPORTED, "beam_select: at most 2^31 parts of rows");
+  a.of_run = reinterpret_cast<float2*>(b.workspace);
+  // (places are counted in 32 bits, with one step of the grid beyond the last)
+  if (a.rows > 0x7ff00000LL || (long long)a.beams * a.runs > 0x7fff0000LL) return fail(MTF_ERR_UNSUPPORTED, "beam_select: at most 2^31 rows, and runs of a sentence");
   cudaStream_t st = (cudaStream_t)stream;
   const bool aligned = (long long)b.vocab * (b.bf16 ? 2 : 4) % 16 == 0;
   const auto rows = b.bf16 ? (aligned ? beam_rows_kernel<__nv_bfloat16, true> : beam_rows_kernel<__nv_bfloat16, false>)
@@ -703,7 +671,8 @@ mtf_status launch_beam_select(const BeamSelect& b, void* stream) {
                              : (aligned ? beam_choose_kernel<float, true> : beam_choose_kernel<float, false>);
   const cudaError_t set = cudaFuncSetAttribute(rows, cudaFuncAttributeMaxDynamicSharedMemorySize, kRing);
   if (set != cudaSuccess) return fail(MTF_ERR_CUDA, "beam_rows_kernel: %s", cudaGetErrorString(set));
-  launch_chained(rows, (unsigned)std::min<long long>(a.rows * a.parts, (long long)device_sm_count() * kBlocks), kThreads, kRing, st, a);
+  const long long blocks = (a.rows * a.runs + kWarps - 1) / kWarps;
+  launch_chained(rows, (unsigned)std::min<long long>(blocks, (long long)device_sm_count() * kBlocks), kThreads, kRing, st, a);
   count_launch();
   launch_chained(choose, (unsigned)b.sentences, kChoosers, 0, st, a);
   count_launch();
