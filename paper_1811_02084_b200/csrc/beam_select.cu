@@ -176,9 +176,8 @@ __device__ int g_beam_status = 0;                    // a wait was given up
 __constant__ long long g_wait_limit = kWaitCycles;
 __constant__ int g_withhold = 0;                     // testing: each warp's first wait asks for a copy that nobody has sent
 
-// e^(from - to), 1 for equal ones
-__device__ __noinline__ double far_apart(float from, float to) { return exp((double)from - (double)to); }
-__device__ __forceinline__ double rescale(float from, float to) { return from == to ? 1. : far_apart(from, to); }
+// e^(from - to), 1 for equal ones (in f32: a run's share of a row's sum is off by 2^-22 at most, and the runs' by less together)
+__device__ __forceinline__ double rescale(float from, float to) { return from == to ? 1. : (double)expf(from - to); }
 __device__ __noinline__ double log_of(double s) { return log(s); }
 
 // the sum of exponentials of some words relative to ref (from differences, which are exact for the words that weigh)
@@ -393,17 +392,21 @@ __device__ __forceinline__ int gather(const Args& a, long long row0, Room& m, un
     const int b = m.runs[i] / a.runs, run = m.runs[i] - b * a.runs;
     const Part<T, kAligned> w = row_at<T, kAligned>(a, row0 + b);
     const float low = m.low[b];
-    // (the loads of a run under way at once; the few pieces that have some are loaded again)
-    uint32_t have = 0;
+    uint4 v[kDeep];
 #pragma unroll
     for (int e = 0; e < kDeep; ++e) {
       const int q = run * kRun + e * 32 + lane;
-      const uint4 u[1] = {q < w.pieces() ? w.load(q) : make_uint4(Words<T>::kNone, Words<T>::kNone, Words<T>::kNone, Words<T>::kNone)};
+      v[e] = q < w.pieces() ? w.load(q) : make_uint4(Words<T>::kNone, Words<T>::kNone, Words<T>::kNone, Words<T>::kNone);
+    }
+    uint32_t have = 0;
+#pragma unroll
+    for (int e = 0; e < kDeep; ++e) {
+      const uint4 u[1] = {v[e]};
       have |= (Words<T>::largest(u) >= low ? 1u : 0u) << e;
     }
     for (; have; have &= have - 1) {
       const int e = __ffs(have) - 1;
-      const uint4 u[1] = {w.load(run * kRun + e * 32 + lane)};
+      const uint4 u[1] = {e == 0 ? v[0] : e == 1 ? v[1] : e == 2 ? v[2] : v[3]};
       float x[kN];
       Words<T>::values(u[0], x);
 #pragma unroll
@@ -561,11 +564,9 @@ __global__ void __launch_bounds__(kChoosers, 1) beam_choose_kernel(const Args a)
       top = warp_max(top);
       // (a run without a finite word: 0 times its sum, 0 or NaN)
       double s = 0.;
-#pragma unroll 1
-      for (int e = 0; e < kMine; ++e) {
-        const float2 x = e == 0 ? r[0] : e == 1 ? r[1] : e == 2 ? r[2] : r[3];
-        if (lane + e * 32 < a.runs) s += x.y * rescale(x.x, top);
-      }
+#pragma unroll
+      for (int e = 0; e < kMine; ++e)
+        if (lane + e * 32 < a.runs) s += r[e].y * rescale(r[e].x, top);
       for (int i = lane + kMine * 32; i < a.runs; i += 32) s += runs[i].y * rescale(runs[i].x, top);
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
