@@ -39,10 +39,10 @@ struct RowsArgs {
   uint8_t* dense[2];
   int d[2];
   const int32_t *table, *starts, *counts;
-  long long n_seq, length;
+  long long length;
+  int units;                                     // sequences * length
   int heads, slots, pages, per_sequence, rows_page, row_slot, row_head;
-  long long rows;                                // n_seq * length * heads
-  Divide by_heads, by_length, by_slots;
+  Divide by_length, by_slots;
 };
 
 __device__ __forceinline__ float lo16(uint32_t w) { return __uint_as_float(w << 16); }
@@ -63,95 +63,95 @@ __device__ __forceinline__ float2 of_e4m3(uint32_t two) {
   return __half22float2(*reinterpret_cast<const __half2*>(&h));
 }
 
-// Row `i` of the dense rows (sequence, index, head): its place in the pool, -1 where the row is not meant, -2 where there is no place for it.
-__device__ __forceinline__ int place(const RowsArgs& a, long long i) {
-  // rows of up to 2^31 - 1 (sequence, index) pairs
-  long long si;
-  int head;
-  if (a.rows <= 0x7fffffffLL) {
-    const int q = over((int)i, a.by_heads);
-    si = q;
-    head = (int)i - q * a.heads;
-  } else {
-    si = i / a.heads;
-    head = (int)(i - si * a.heads);
-  }
-  const int s = over((int)si, a.by_length), at = (int)si - s * (int)a.length;
+// Position `unit` = (sequence, index) of the dense rows: its first row in the pool (head 0), -1 where the rows are not meant, -2 where there is no place for them.
+__device__ __forceinline__ int place(const RowsArgs& a, int unit) {
+  const int s = over(unit, a.by_length), at = unit - s * (int)a.length;
   const int count = a.counts ? a.counts[s] : (int)a.length;
-  if (at >= count) return -1;
   const long long m = (long long)(a.starts ? a.starts[s] : 0) + at;
+  if (at >= count) return -1;
   if (m < 0 || m >= (long long)a.per_sequence * a.slots) return -2;
   const int index = over((int)m, a.by_slots), page = a.table[(long long)s * a.per_sequence + index];
   if (page < 0 || page >= a.pages) return -2;
-  return page * a.rows_page + ((int)m - index * a.slots) * a.row_slot + head * a.row_head;
+  return page * a.rows_page + ((int)m - index * a.slots) * a.row_slot;
 }
 
-// A row by kLanes lanes, 8 values each (d up to 8 kLanes); blockIdx.y: K or V.  Each group of lanes takes kEach rows at once, so that enough loads are under way.
-constexpr int kEach = 4;
+// A position's rows of all heads are together in the dense tensor, and their place is one look at the table: a warp takes a position after another, kLanes lanes a head, 8 values
+// each (d up to 8 kLanes), some heads at once; the next position's place is looked up while this one's rows are under way.  blockIdx.y: K or V.  (A group of lanes a row with a look
+// at the table each: 32 x 512 prompts of 16 heads of 64 written and read back 63 us, 8 x 16384 positions of 8 heads of 128 read back 138.)
+constexpr int kRowBlocks = 4;          // of K, and of V, an SM
+constexpr int kEach = 4;               // heads of a group of lanes whose loads are under way at once
 
 template <int kLanes, bool kBf16, bool kE4m3>
 __global__ void __launch_bounds__(256) cache_write_kernel(const RowsArgs a) {
   mtf::chain_wait();
-  const int side = blockIdx.y, d = a.d[side], lane = threadIdx.x % kLanes;
-  const long long groups = (long long)gridDim.x * (256 / kLanes);
-  for (long long first = (long long)blockIdx.x * (256 / kLanes) + threadIdx.x / kLanes; first - threadIdx.x / kLanes < a.rows; first += groups * kEach) {
-    uint4 w[kEach][2];
-    int to[kEach];
-    bool in[kEach];
-#pragma unroll
-    for (int e = 0; e < kEach; ++e) {
-      const long long i = first + e * groups;
-      to[e] = i < a.rows ? place(a, i) : -1;
-      if (to[e] == -2) atomicExch(&g_bad_place, 1);
-      in[e] = to[e] >= 0 && lane * 8 < d;
-      w[e][0] = w[e][1] = make_uint4(0u, 0u, 0u, 0u);
-      if (in[e]) {
-        const uint4* const p = reinterpret_cast<const uint4*>(a.dense[side] + (i * d + lane * 8) * (kBf16 ? 2 : 4));
-        w[e][0] = p[0];
-        if (!kBf16) w[e][1] = p[1];
-      }
+  const int side = blockIdx.y, d = a.d[side], lane = threadIdx.x & 31, col = lane % kLanes * 8, group = lane / kLanes;
+  constexpr int kHeads = 32 / kLanes;
+  const int warps = gridDim.x * 8;
+  int unit = blockIdx.x * 8 + (threadIdx.x >> 5);
+  int to = unit < a.units ? place(a, unit) : -1;
+  while (unit < a.units) {
+    const int here = to, now = unit;
+    unit = warps < a.units - unit ? unit + warps : a.units;
+    if (here < 0) {
+      if (here == -2 && lane == 0) atomicExch(&g_bad_place, 1);
+      to = unit < a.units ? place(a, unit) : -1;
+      continue;
     }
+    for (int h0 = 0; h0 < a.heads; h0 += kEach * kHeads) {
+      uint4 w[kEach][2];
 #pragma unroll
-    for (int e = 0; e < kEach; ++e) {
-      const long long at = (long long)to[e] * d + lane * 8;
-      float x[8];
-      if (kBf16) {
-        const uint32_t u[4] = {w[e][0].x, w[e][0].y, w[e][0].z, w[e][0].w};
-#pragma unroll
-        for (int j = 0; j < 4; ++j) { x[2 * j] = lo16(u[j]); x[2 * j + 1] = hi16(u[j]); }
-      } else {
-        const uint32_t u[8] = {w[e][0].x, w[e][0].y, w[e][0].z, w[e][0].w, w[e][1].x, w[e][1].y, w[e][1].z, w[e][1].w};
-#pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] = __uint_as_float(u[j]);
+      for (int e = 0; e < kEach; ++e) {
+        const int head = h0 + e * kHeads + group;
+        w[e][0] = w[e][1] = make_uint4(0u, 0u, 0u, 0u);
+        if (head < a.heads && col < d) {
+          const uint4* const p = reinterpret_cast<const uint4*>(a.dense[side] + (((long long)now * a.heads + head) * d + col) * (kBf16 ? 2 : 4));
+          w[e][0] = p[0];
+          if (!kBf16) w[e][1] = p[1];
+        }
       }
-      if (!kE4m3) {
-        if (!in[e]) continue;
-        const uint4 v = kBf16 ? w[e][0] : make_uint4(two_bf16(x[0], x[1]), two_bf16(x[2], x[3]), two_bf16(x[4], x[5]), two_bf16(x[6], x[7]));
-        *reinterpret_cast<uint4*>(a.pool[side] + at * 2) = v;
-        continue;
-      }
-      uint32_t top = 0;                              // (as bits: magnitudes in rising order, and infinities and NaN above all)
+      if (h0 == 0) to = unit < a.units ? place(a, unit) : -1;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const uint32_t m = __float_as_uint(x[j]) & 0x7fffffffu;
-        if (m < 0x7f800000u) top = max(top, m);
-      }
+      for (int e = 0; e < kEach; ++e) {
+        const int head = h0 + e * kHeads + group, row = here + head * a.row_head;
+        const bool in = head < a.heads && col < d;
+        const long long at = (long long)row * d + col;
+        float x[8];
+        if (kBf16) {
+          const uint32_t u[4] = {w[e][0].x, w[e][0].y, w[e][0].z, w[e][0].w};
 #pragma unroll
-      for (int o = kLanes / 2; o > 0; o /= 2) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
-      // 448 = 1.75 2^8: scale 2^(e - 8) for a largest value m 2^e with m up to 1.75, else 2^(e - 7); not below 2^-126, so that it is a normal number, too
-      int field = (int)(top >> 23) - 8 + ((top & 0x7fffffu) > 0x600000u ? 1 : 0);
-      field = max(field, 1);
-      if (top == 0) field = 127;
-      const float scale = __uint_as_float((uint32_t)field << 23);
-      if (!in[e]) continue;
+          for (int j = 0; j < 4; ++j) { x[2 * j] = lo16(u[j]); x[2 * j + 1] = hi16(u[j]); }
+        } else {
+          const uint32_t u[8] = {w[e][0].x, w[e][0].y, w[e][0].z, w[e][0].w, w[e][1].x, w[e][1].y, w[e][1].z, w[e][1].w};
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const bool finite = (__float_as_uint(x[j]) & 0x7fffffffu) < 0x7f800000u;
-        x[j] = finite ? x[j] / scale : __uint_as_float(0x7fc00000u);
+          for (int j = 0; j < 8; ++j) x[j] = __uint_as_float(u[j]);
+        }
+        if (!kE4m3) {
+          if (in) *reinterpret_cast<uint4*>(a.pool[side] + at * 2) = kBf16 ? w[e][0] : make_uint4(two_bf16(x[0], x[1]), two_bf16(x[2], x[3]), two_bf16(x[4], x[5]), two_bf16(x[6], x[7]));
+          continue;
+        }
+        uint32_t top = 0;                            // (as bits: magnitudes in rising order, and infinities and NaN above all)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const uint32_t m = __float_as_uint(x[j]) & 0x7fffffffu;
+          if (m < 0x7f800000u) top = max(top, m);
+        }
+#pragma unroll
+        for (int o = kLanes / 2; o > 0; o /= 2) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+        // 448 = 1.75 2^8: scale 2^(e - 8) for a largest value m 2^e with m up to 1.75, else 2^(e - 7); not below 2^-126, so that it is a normal number, too, and so is its inverse
+        int field = (int)(top >> 23) - 8 + ((top & 0x7fffffu) > 0x600000u ? 1 : 0);
+        field = max(field, 1);
+        if (top == 0) field = 127;
+        const float up = __uint_as_float((uint32_t)(254 - field) << 23);
+        if (!in) continue;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const bool finite = (__float_as_uint(x[j]) & 0x7fffffffu) < 0x7f800000u;
+          x[j] = finite ? x[j] * up : __uint_as_float(0x7fc00000u);
+        }
+        *reinterpret_cast<uint2*>(a.pool[side] + at) =
+            make_uint2(two_e4m3(x[0], x[1]) | two_e4m3(x[2], x[3]) << 16, two_e4m3(x[4], x[5]) | two_e4m3(x[6], x[7]) << 16);
+        if (col == 0) a.scale[side][row] = __uint_as_float((uint32_t)field << 23);
       }
-      *reinterpret_cast<uint2*>(a.pool[side] + at) =
-          make_uint2(two_e4m3(x[0], x[1]) | two_e4m3(x[2], x[3]) << 16, two_e4m3(x[4], x[5]) | two_e4m3(x[6], x[7]) << 16);
-      if (lane == 0) a.scale[side][to[e]] = scale;
     }
   }
 }
@@ -159,53 +159,59 @@ __global__ void __launch_bounds__(256) cache_write_kernel(const RowsArgs a) {
 template <int kLanes, bool kBf16, bool kE4m3>
 __global__ void __launch_bounds__(256) cache_read_kernel(const RowsArgs a) {
   mtf::chain_wait();
-  const int side = blockIdx.y, d = a.d[side], lane = threadIdx.x % kLanes;
-  const long long groups = (long long)gridDim.x * (256 / kLanes);
-  if (lane * 8 >= d) return;
-  for (long long first = (long long)blockIdx.x * (256 / kLanes) + threadIdx.x / kLanes; first < a.rows; first += groups * kEach) {
-    uint4 w[kEach];
-    float scale[kEach];
+  const int side = blockIdx.y, d = a.d[side], lane = threadIdx.x & 31, col = lane % kLanes * 8, group = lane / kLanes;
+  constexpr int kHeads = 32 / kLanes;
+  const int warps = gridDim.x * 8;
+  int unit = blockIdx.x * 8 + (threadIdx.x >> 5);
+  int from = unit < a.units ? place(a, unit) : -1;
+  while (unit < a.units) {
+    const int here = from, now = unit;
+    unit = warps < a.units - unit ? unit + warps : a.units;
+    if (here == -2 && lane == 0) atomicExch(&g_bad_place, 1);
+    for (int h0 = 0; h0 < a.heads; h0 += kEach * kHeads) {
+      uint4 w[kEach];
+      float scale[kEach];
 #pragma unroll
-    for (int e = 0; e < kEach; ++e) {
-      const long long i = first + e * groups;
-      const int from = i < a.rows ? place(a, i) : -1;
-      if (from == -2) atomicExch(&g_bad_place, 1);
-      w[e] = make_uint4(0u, 0u, 0u, 0u);             // (zeros in e4m3 as well)
-      scale[e] = 0.f;
-      if (from < 0) continue;
-      const long long at = (long long)from * d + lane * 8;
-      if (kE4m3) {
-        const uint2 v = *reinterpret_cast<const uint2*>(a.pool[side] + at);
-        w[e].x = v.x;
-        w[e].y = v.y;
-        scale[e] = a.scale[side][from];
-      } else {
-        w[e] = *reinterpret_cast<const uint4*>(a.pool[side] + at * 2);
-      }
-    }
-#pragma unroll
-    for (int e = 0; e < kEach; ++e) {
-      const long long i = first + e * groups;
-      if (i >= a.rows) continue;
-      uint4* const p = reinterpret_cast<uint4*>(a.dense[side] + (i * d + lane * 8) * (kBf16 ? 2 : 4));
-      if (!kE4m3 && kBf16) { p[0] = w[e]; continue; }
-      float x[8];
-      if (kE4m3) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const float2 v = of_e4m3((j < 2 ? w[e].x : w[e].y) >> (16 * (j & 1)));
-          x[2 * j] = v.x * scale[e];
-          x[2 * j + 1] = v.y * scale[e];
+      for (int e = 0; e < kEach; ++e) {
+        const int head = h0 + e * kHeads + group, row = here + head * a.row_head;
+        w[e] = make_uint4(0u, 0u, 0u, 0u);           // (zeros in e4m3 as well)
+        scale[e] = 0.f;
+        if (here < 0 || head >= a.heads || col >= d) continue;
+        const long long at = (long long)row * d + col;
+        if (kE4m3) {
+          const uint2 v = *reinterpret_cast<const uint2*>(a.pool[side] + at);
+          w[e].x = v.x;
+          w[e].y = v.y;
+          scale[e] = a.scale[side][row];
+        } else {
+          w[e] = *reinterpret_cast<const uint4*>(a.pool[side] + at * 2);
         }
-      } else {
-        const uint32_t u[4] = {w[e].x, w[e].y, w[e].z, w[e].w};
-#pragma unroll
-        for (int j = 0; j < 4; ++j) { x[2 * j] = lo16(u[j]); x[2 * j + 1] = hi16(u[j]); }
       }
-      if (kBf16) p[0] = make_uint4(two_bf16(x[0], x[1]), two_bf16(x[2], x[3]), two_bf16(x[4], x[5]), two_bf16(x[6], x[7]));
-      else {
-        p[0] = make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
-        p[1] = make_uint4(__float_as_uint(x[4]), __float_as_uint(x[5]), __float_as_uint(x[6]), __float_as_uint(x[7]));
+      if (h0 == 0) from = unit < a.units ? place(a, unit) : -1;
+#pragma unroll
+      for (int e = 0; e < kEach; ++e) {
+        const int head = h0 + e * kHeads + group;
+        if (head >= a.heads || col >= d) continue;
+        uint4* const p = reinterpret_cast<uint4*>(a.dense[side] + (((long long)now * a.heads + head) * d + col) * (kBf16 ? 2 : 4));
+        if (!kE4m3 && kBf16) { p[0] = w[e]; continue; }
+        float x[8];
+        if (kE4m3) {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const float2 v = of_e4m3((j < 2 ? w[e].x : w[e].y) >> (16 * (j & 1)));
+            x[2 * j] = v.x * scale[e];
+            x[2 * j + 1] = v.y * scale[e];
+          }
+        } else {
+          const uint32_t u[4] = {w[e].x, w[e].y, w[e].z, w[e].w};
+#pragma unroll
+          for (int j = 0; j < 4; ++j) { x[2 * j] = lo16(u[j]); x[2 * j + 1] = hi16(u[j]); }
+        }
+        if (kBf16) p[0] = make_uint4(two_bf16(x[0], x[1]), two_bf16(x[2], x[3]), two_bf16(x[4], x[5]), two_bf16(x[6], x[7]));
+        else {
+          p[0] = make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
+          p[1] = make_uint4(__float_as_uint(x[4]), __float_as_uint(x[5]), __float_as_uint(x[6]), __float_as_uint(x[7]));
+        }
       }
     }
   }
@@ -300,7 +306,6 @@ RowsArgs rows_args(const mtf::CachePool& c, const mtf::CacheRows& r) {
   a.table = c.table;
   a.starts = r.starts;
   a.counts = r.counts;
-  a.n_seq = c.sequences;
   a.length = r.length;
   a.heads = c.heads;
   a.slots = c.slots;
@@ -309,8 +314,7 @@ RowsArgs rows_args(const mtf::CachePool& c, const mtf::CacheRows& r) {
   a.rows_page = c.rows_page;
   a.row_slot = c.row_slot;
   a.row_head = c.row_head;
-  a.rows = c.sequences * r.length * c.heads;
-  a.by_heads = divide_by(c.heads);
+  a.units = (int)(c.sequences * r.length);
   a.by_length = divide_by((int)r.length);
   a.by_slots = divide_by(c.slots);
   return a;
@@ -318,7 +322,7 @@ RowsArgs rows_args(const mtf::CachePool& c, const mtf::CacheRows& r) {
 
 template <int kLanes, bool kBf16, bool kE4m3>
 void rows_launch(const RowsArgs& a, bool write, cudaStream_t st) {
-  const long long at_once = (256 / kLanes) * kEach, blocks = std::max(1LL, std::min<long long>((a.rows + at_once - 1) / at_once, (long long)mtf::device_sm_count() * 16));
+  const long long blocks = std::min<long long>(((long long)a.units + 7) / 8, (long long)mtf::device_sm_count() * kRowBlocks);
   mtf::launch_clusters(write ? cache_write_kernel<kLanes, kBf16, kE4m3> : cache_read_kernel<kLanes, kBf16, kE4m3>, dim3((unsigned)blocks, 2, 1), 256, 0, 1, st, a);
 }
 template <bool kBf16, bool kE4m3>
