@@ -106,7 +106,9 @@ void take_dense(Arguments& c, const mtf_tensor* kk, const mtf_tensor* vv, long l
   r->v = vv->data;
   r->bf16 = kk->dtype == MTF_BF16;
   r->length = kk->dims[kk->ndim - 3].size;
-  if (n > 0x7fffffffLL || r->length > 0x7fffffffLL || n * r->length > 0x7fffffffLL) return c.wrong(MTF_ERR_UNSUPPORTED, "at most 2^31 rows a head");
+  const int64_t heads = kk->dims[kk->ndim - 2].size;
+  if (n > 0x7fffffffLL || r->length > 0x7fffffffLL || n * r->length > 0x7fffffffLL || heads > 0x7fffffffLL || n * r->length * heads > 0x7fffffffLL)
+    return c.wrong(MTF_ERR_UNSUPPORTED, "at most 2^31 rows");
 }
 void dense_fits(Arguments& c, const mtf_tensor* kk, const mtf_tensor* vv, const mtf_cache* cache, const TakenCache& t, bool written) {
   if (!c.ok()) return;

@@ -41,8 +41,9 @@ struct RowsArgs {
   const int32_t *table, *starts, *counts;
   long long length;
   int units;                                     // sequences * length
+  long long items;                               // units * passes over the heads
   int heads, slots, pages, per_sequence, rows_page, row_slot, row_head;
-  Divide by_length, by_slots;
+  Divide by_length, by_slots, by_passes;
 };
 
 __device__ __forceinline__ float lo16(uint32_t w) { return __uint_as_float(w << 16); }
@@ -75,143 +76,162 @@ __device__ __forceinline__ int place(const RowsArgs& a, int unit) {
   return page * a.rows_page + ((int)m - index * a.slots) * a.row_slot;
 }
 
-// A position's rows of all heads are together in the dense tensor, and their place is one look at the table: a warp takes a position after another, kLanes lanes a head, 8 values
-// each (d up to 8 kLanes), some heads at once; the next position's place is looked up while this one's rows are under way.  blockIdx.y: K or V.  (A group of lanes a row with a look
-// at the table each: 32 x 512 prompts of 16 heads of 64 written and read back 63 us, 8 x 16384 positions of 8 heads of 128 read back 138.)
-constexpr int kRowBlocks = 4;          // of K, and of V, an SM
-constexpr int kEach = 4;               // heads of a group of lanes whose loads are under way at once
+// A position's rows of all heads are together in the dense tensor, and their place is one look at the table.  kLanes lanes take a head, 8 values each (d up to 8 kLanes); the
+// 32 / kLanes heads of a warp are an item, and a warp has kEach items' loads under way at once: of one position, or of several where it has few heads.  Their places
+// are looked up by a lane each, those of the next items while these ones' rows are under way.  blockIdx.y: K or V.
+// (A look at the table a row, whole calls: 32 x 512 prompts of 16 heads of 64 written in e4m3 and read back 63 us, 8 x 16384 positions of 8 heads of 128 read back 138; now MEASURED.)
+constexpr int kRowBlocks = 2;          // of K, and of V, an SM
+template <int kEach>
+struct Items {
+  int unit, head, row;                 // of item lane % kEach: position, first head, place (below 0: none)
+  __device__ __forceinline__ void look(const RowsArgs& a, long long first, int heads) {
+    const long long j = first + (threadIdx.x & (kEach - 1));
+    unit = -1;
+    row = -1;
+    if (j < a.items) {
+      unit = over((int)j, a.by_passes);
+      head = ((int)j - unit * a.by_passes.d) * heads;
+      row = place(a, unit);
+    }
+  }
+};
 
-template <int kLanes, bool kBf16, bool kE4m3>
-__global__ void __launch_bounds__(256) cache_write_kernel(const RowsArgs a) {
+template <int kLanes, bool kBf16, bool kE4m3, int kEach>
+__global__ void __launch_bounds__(256, 2 * kRowBlocks) cache_write_kernel(const RowsArgs a) {
   mtf::chain_wait();
   const int side = blockIdx.y, d = a.d[side], lane = threadIdx.x & 31, col = lane % kLanes * 8, group = lane / kLanes;
   constexpr int kHeads = 32 / kLanes;
-  const int warps = gridDim.x * 8;
-  int unit = blockIdx.x * 8 + (threadIdx.x >> 5);
-  int to = unit < a.units ? place(a, unit) : -1;
-  while (unit < a.units) {
-    const int here = to, now = unit;
-    unit = warps < a.units - unit ? unit + warps : a.units;
-    if (here < 0) {
-      if (here == -2 && lane == 0) atomicExch(&g_bad_place, 1);
-      to = unit < a.units ? place(a, unit) : -1;
-      continue;
-    }
-    for (int h0 = 0; h0 < a.heads; h0 += kEach * kHeads) {
-      uint4 w[kEach][2];
+  const long long step = (long long)gridDim.x * 8 * kEach;
+  long long first = ((long long)blockIdx.x * 8 + (threadIdx.x >> 5)) * kEach;
+  Items<kEach> next;
+  next.look(a, first, kHeads);
+  for (; first < a.items; first += step) {
+    const Items<kEach> now = next;
+    if (now.row == -2 && lane < kEach) atomicExch(&g_bad_place, 1);
+    uint4 w[kEach][2];
+    int row[kEach];                                  // -1: nothing to be done by this lane
 #pragma unroll
-      for (int e = 0; e < kEach; ++e) {
-        const int head = h0 + e * kHeads + group;
-        w[e][0] = w[e][1] = make_uint4(0u, 0u, 0u, 0u);
-        if (head < a.heads && col < d) {
-          const uint4* const p = reinterpret_cast<const uint4*>(a.dense[side] + (((long long)now * a.heads + head) * d + col) * (kBf16 ? 2 : 4));
-          w[e][0] = p[0];
-          if (!kBf16) w[e][1] = p[1];
-        }
+    for (int e = 0; e < kEach; ++e) {
+      const int unit = __shfl_sync(0xffffffffu, now.unit, e), head = __shfl_sync(0xffffffffu, now.head, e) + group, here = __shfl_sync(0xffffffffu, now.row, e);
+      row[e] = here >= 0 && head < a.heads && col < d ? here + head * a.row_head : -1;
+      w[e][0] = w[e][1] = make_uint4(0u, 0u, 0u, 0u);
+      if (row[e] >= 0) {
+        const uint4* const p = reinterpret_cast<const uint4*>(a.dense[side] + (((long long)unit * a.heads + head) * d + col) * (kBf16 ? 2 : 4));
+        w[e][0] = p[0];
+        if (!kBf16) w[e][1] = p[1];
       }
-      if (h0 == 0) to = unit < a.units ? place(a, unit) : -1;
+    }
+    next.look(a, first + step, kHeads);
 #pragma unroll
-      for (int e = 0; e < kEach; ++e) {
-        const int head = h0 + e * kHeads + group, row = here + head * a.row_head;
-        const bool in = head < a.heads && col < d;
-        const long long at = (long long)row * d + col;
-        float x[8];
-        if (kBf16) {
-          const uint32_t u[4] = {w[e][0].x, w[e][0].y, w[e][0].z, w[e][0].w};
+    for (int e = 0; e < kEach; ++e) {
+      const long long at = (long long)row[e] * d + col;
+      float x[8];
+      if (kBf16) {
+        const uint32_t u[4] = {w[e][0].x, w[e][0].y, w[e][0].z, w[e][0].w};
 #pragma unroll
-          for (int j = 0; j < 4; ++j) { x[2 * j] = lo16(u[j]); x[2 * j + 1] = hi16(u[j]); }
-        } else {
-          const uint32_t u[8] = {w[e][0].x, w[e][0].y, w[e][0].z, w[e][0].w, w[e][1].x, w[e][1].y, w[e][1].z, w[e][1].w};
+        for (int j = 0; j < 4; ++j) { x[2 * j] = lo16(u[j]); x[2 * j + 1] = hi16(u[j]); }
+      } else {
+        const uint32_t u[8] = {w[e][0].x, w[e][0].y, w[e][0].z, w[e][0].w, w[e][1].x, w[e][1].y, w[e][1].z, w[e][1].w};
 #pragma unroll
-          for (int j = 0; j < 8; ++j) x[j] = __uint_as_float(u[j]);
-        }
-        if (!kE4m3) {
-          if (in) *reinterpret_cast<uint4*>(a.pool[side] + at * 2) = kBf16 ? w[e][0] : make_uint4(two_bf16(x[0], x[1]), two_bf16(x[2], x[3]), two_bf16(x[4], x[5]), two_bf16(x[6], x[7]));
-          continue;
-        }
-        uint32_t top = 0;                            // (as bits: magnitudes in rising order, and infinities and NaN above all)
+        for (int j = 0; j < 8; ++j) x[j] = __uint_as_float(u[j]);
+      }
+      if (!kE4m3) {
+        if (row[e] >= 0)
+          *reinterpret_cast<uint4*>(a.pool[side] + at * 2) = kBf16 ? w[e][0] : make_uint4(two_bf16(x[0], x[1]), two_bf16(x[2], x[3]), two_bf16(x[4], x[5]), two_bf16(x[6], x[7]));
+        continue;
+      }
+      // the row's largest magnitude as bits, in whose order infinities and NaN come last
+      uint32_t top = 0;
+      if (kBf16) {
+        const uint32_t u[4] = {w[e][0].x & 0x7fff7fffu, w[e][0].y & 0x7fff7fffu, w[e][0].z & 0x7fff7fffu, w[e][0].w & 0x7fff7fffu};
+        const uint32_t m = __vmaxu2(__vmaxu2(u[0], u[1]), __vmaxu2(u[2], u[3]));
+        top = max(m << 16, m & 0xffff0000u);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(x[j]) & 0x7fffffffu);
+      }
+#pragma unroll
+      for (int o = kLanes / 2; o > 0; o /= 2) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+      if (__any_sync(0xffffffffu, top >= 0x7f800000u)) {
+        // NaN and infinities: all to NaN, and the largest of the others
+        top = 0;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           const uint32_t m = __float_as_uint(x[j]) & 0x7fffffffu;
           if (m < 0x7f800000u) top = max(top, m);
+          else x[j] = __uint_as_float(0x7fc00000u);
         }
 #pragma unroll
         for (int o = kLanes / 2; o > 0; o /= 2) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
-        // 448 = 1.75 2^8: scale 2^(e - 8) for a largest value m 2^e with m up to 1.75, else 2^(e - 7); not below 2^-126, so that it is a normal number, too, and so is its inverse
-        int field = (int)(top >> 23) - 8 + ((top & 0x7fffffu) > 0x600000u ? 1 : 0);
-        field = max(field, 1);
-        if (top == 0) field = 127;
-        const float up = __uint_as_float((uint32_t)(254 - field) << 23);
-        if (!in) continue;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const bool finite = (__float_as_uint(x[j]) & 0x7fffffffu) < 0x7f800000u;
-          x[j] = finite ? x[j] * up : __uint_as_float(0x7fc00000u);
-        }
-        *reinterpret_cast<uint2*>(a.pool[side] + at) =
-            make_uint2(two_e4m3(x[0], x[1]) | two_e4m3(x[2], x[3]) << 16, two_e4m3(x[4], x[5]) | two_e4m3(x[6], x[7]) << 16);
-        if (col == 0) a.scale[side][row] = __uint_as_float((uint32_t)field << 23);
       }
+      // 448 = 1.75 2^8: scale 2^(e - 8) for a largest value m 2^e with m up to 1.75, else 2^(e - 7); not below 2^-126, so that it is a normal number, too, and so is its inverse
+      int field = max((int)((top + 0x1fffffu) >> 23) - 8, 1);
+      if (top == 0) field = 127;
+      if (row[e] < 0) continue;
+      const float up = __uint_as_float((uint32_t)(254 - field) << 23);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) x[j] *= up;
+      *reinterpret_cast<uint2*>(a.pool[side] + at) = make_uint2(two_e4m3(x[0], x[1]) | two_e4m3(x[2], x[3]) << 16, two_e4m3(x[4], x[5]) | two_e4m3(x[6], x[7]) << 16);
+      if (col == 0) a.scale[side][row[e]] = __uint_as_float((uint32_t)field << 23);
     }
   }
 }
 
-template <int kLanes, bool kBf16, bool kE4m3>
-__global__ void __launch_bounds__(256) cache_read_kernel(const RowsArgs a) {
+template <int kLanes, bool kBf16, bool kE4m3, int kEach>
+__global__ void __launch_bounds__(256, 2 * kRowBlocks) cache_read_kernel(const RowsArgs a) {
   mtf::chain_wait();
   const int side = blockIdx.y, d = a.d[side], lane = threadIdx.x & 31, col = lane % kLanes * 8, group = lane / kLanes;
   constexpr int kHeads = 32 / kLanes;
-  const int warps = gridDim.x * 8;
-  int unit = blockIdx.x * 8 + (threadIdx.x >> 5);
-  int from = unit < a.units ? place(a, unit) : -1;
-  while (unit < a.units) {
-    const int here = from, now = unit;
-    unit = warps < a.units - unit ? unit + warps : a.units;
-    if (here == -2 && lane == 0) atomicExch(&g_bad_place, 1);
-    for (int h0 = 0; h0 < a.heads; h0 += kEach * kHeads) {
-      uint4 w[kEach];
-      float scale[kEach];
+  const long long step = (long long)gridDim.x * 8 * kEach;
+  long long first = ((long long)blockIdx.x * 8 + (threadIdx.x >> 5)) * kEach;
+  Items<kEach> next;
+  next.look(a, first, kHeads);
+  for (; first < a.items; first += step) {
+    const Items<kEach> now = next;
+    if (now.row == -2 && lane < kEach) atomicExch(&g_bad_place, 1);
+    uint4 w[kEach];
+    float scale[kEach];
 #pragma unroll
-      for (int e = 0; e < kEach; ++e) {
-        const int head = h0 + e * kHeads + group, row = here + head * a.row_head;
-        w[e] = make_uint4(0u, 0u, 0u, 0u);           // (zeros in e4m3 as well)
-        scale[e] = 0.f;
-        if (here < 0 || head >= a.heads || col >= d) continue;
-        const long long at = (long long)row * d + col;
-        if (kE4m3) {
-          const uint2 v = *reinterpret_cast<const uint2*>(a.pool[side] + at);
-          w[e].x = v.x;
-          w[e].y = v.y;
-          scale[e] = a.scale[side][row];
-        } else {
-          w[e] = *reinterpret_cast<const uint4*>(a.pool[side] + at * 2);
-        }
+    for (int e = 0; e < kEach; ++e) {
+      const int head = __shfl_sync(0xffffffffu, now.head, e) + group, here = __shfl_sync(0xffffffffu, now.row, e);
+      w[e] = make_uint4(0u, 0u, 0u, 0u);             // (zeros in e4m3 as well)
+      scale[e] = 0.f;
+      if (here < 0 || head >= a.heads || col >= d) continue;
+      const int row = here + head * a.row_head;
+      const long long at = (long long)row * d + col;
+      if (kE4m3) {
+        const uint2 v = *reinterpret_cast<const uint2*>(a.pool[side] + at);
+        w[e].x = v.x;
+        w[e].y = v.y;
+        scale[e] = a.scale[side][row];
+      } else {
+        w[e] = *reinterpret_cast<const uint4*>(a.pool[side] + at * 2);
       }
-      if (h0 == 0) from = unit < a.units ? place(a, unit) : -1;
+    }
+    next.look(a, first + step, kHeads);
 #pragma unroll
-      for (int e = 0; e < kEach; ++e) {
-        const int head = h0 + e * kHeads + group;
-        if (head >= a.heads || col >= d) continue;
-        uint4* const p = reinterpret_cast<uint4*>(a.dense[side] + (((long long)now * a.heads + head) * d + col) * (kBf16 ? 2 : 4));
-        if (!kE4m3 && kBf16) { p[0] = w[e]; continue; }
-        float x[8];
-        if (kE4m3) {
+    for (int e = 0; e < kEach; ++e) {
+      const int unit = __shfl_sync(0xffffffffu, now.unit, e), head = __shfl_sync(0xffffffffu, now.head, e) + group;
+      if (unit < 0 || head >= a.heads || col >= d) continue;
+      uint4* const p = reinterpret_cast<uint4*>(a.dense[side] + (((long long)unit * a.heads + head) * d + col) * (kBf16 ? 2 : 4));
+      if (!kE4m3 && kBf16) { p[0] = w[e]; continue; }
+      float x[8];
+      if (kE4m3) {
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const float2 v = of_e4m3((j < 2 ? w[e].x : w[e].y) >> (16 * (j & 1)));
-            x[2 * j] = v.x * scale[e];
-            x[2 * j + 1] = v.y * scale[e];
-          }
-        } else {
-          const uint32_t u[4] = {w[e].x, w[e].y, w[e].z, w[e].w};
-#pragma unroll
-          for (int j = 0; j < 4; ++j) { x[2 * j] = lo16(u[j]); x[2 * j + 1] = hi16(u[j]); }
+        for (int j = 0; j < 4; ++j) {
+          const float2 v = of_e4m3((j < 2 ? w[e].x : w[e].y) >> (16 * (j & 1)));
+          x[2 * j] = v.x * scale[e];
+          x[2 * j + 1] = v.y * scale[e];
         }
-        if (kBf16) p[0] = make_uint4(two_bf16(x[0], x[1]), two_bf16(x[2], x[3]), two_bf16(x[4], x[5]), two_bf16(x[6], x[7]));
-        else {
-          p[0] = make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
-          p[1] = make_uint4(__float_as_uint(x[4]), __float_as_uint(x[5]), __float_as_uint(x[6]), __float_as_uint(x[7]));
-        }
+      } else {
+        const uint32_t u[4] = {w[e].x, w[e].y, w[e].z, w[e].w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) { x[2 * j] = lo16(u[j]); x[2 * j + 1] = hi16(u[j]); }
+      }
+      if (kBf16) p[0] = make_uint4(two_bf16(x[0], x[1]), two_bf16(x[2], x[3]), two_bf16(x[4], x[5]), two_bf16(x[6], x[7]));
+      else {
+        p[0] = make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
+        p[1] = make_uint4(__float_as_uint(x[4]), __float_as_uint(x[5]), __float_as_uint(x[6]), __float_as_uint(x[7]));
       }
     }
   }
@@ -321,9 +341,14 @@ RowsArgs rows_args(const mtf::CachePool& c, const mtf::CacheRows& r) {
 }
 
 template <int kLanes, bool kBf16, bool kE4m3>
-void rows_launch(const RowsArgs& a, bool write, cudaStream_t st) {
-  const long long blocks = std::min<long long>(((long long)a.units + 7) / 8, (long long)mtf::device_sm_count() * kRowBlocks);
-  mtf::launch_clusters(write ? cache_write_kernel<kLanes, kBf16, kE4m3> : cache_read_kernel<kLanes, kBf16, kE4m3>, dim3((unsigned)blocks, 2, 1), 256, 0, 1, st, a);
+void rows_launch(RowsArgs a, bool write, cudaStream_t st) {
+  const int passes = (a.heads + 32 / kLanes - 1) / (32 / kLanes);
+  constexpr int kWrite = 4, kRead = kE4m3 ? 8 : 4;       // items at once (8-bit rows are half as long)
+  const int each = write ? kWrite : kRead;
+  a.items = (long long)a.units * passes;
+  a.by_passes = divide_by(passes);
+  const long long blocks = std::min<long long>((a.items + 8 * each - 1) / (8 * each), (long long)mtf::device_sm_count() * kRowBlocks);
+  mtf::launch_clusters(write ? cache_write_kernel<kLanes, kBf16, kE4m3, kWrite> : cache_read_kernel<kLanes, kBf16, kE4m3, kRead>, dim3((unsigned)blocks, 2, 1), 256, 0, 1, st, a);
 }
 template <bool kBf16, bool kE4m3>
 void rows_lanes(const RowsArgs& a, bool write, cudaStream_t st) {
