@@ -796,7 +796,13 @@ def _sequences(t: Named, inner: int, cache: Cache) -> int:
     """Sequences of a tensor whose last `inner` dims are others, held against those of the cache's table."""
     if t is None or cache is None or cache.k is None:
         raise MtfError(1, "a tensor of the call, its cache or the cache's k is None")
-    n = math.prod(s for _, s in t.dims[:-inner])
+    try:
+        n = t.sequences[inner]
+    except AttributeError:
+        t.sequences = {}
+        n = t.sequences[inner] = math.prod(s for _, s in t.dims[:-inner])
+    except KeyError:
+        n = t.sequences[inner] = math.prod(s for _, s in t.dims[:-inner])
     if cache.table is not None and cache.sequences != n:
         raise MtfError(STATUS_NAMES.index("MTF_ERR_SIZE_MISMATCH"), f"the cache's table is for {cache.sequences} sequences where the call has {n}")
     return n

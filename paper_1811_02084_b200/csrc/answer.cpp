@@ -79,7 +79,7 @@ void take_cache(Arguments& c, const mtf_cache* cache, long long sequences, bool 
 
 // The layout has to keep apart all dimensions that an operation walks over, those of several tensors together.
 void together(Arguments& c, std::initializer_list<std::pair<const mtf_tensor*, int>> of) {
-  if (!c.ok()) return;
+  if (!c.ok() || c.layout->rules.empty()) return;
   std::vector<Dim> all;
   for (const auto& t : of)
     for (int i = t.second; i < t.first->ndim; ++i) {
@@ -141,9 +141,7 @@ mtf_status cache_rows(const char* what, const mtf_layout_t* layout, const mtf_te
 // q [*sequences, heads, d_k] or [*sequences, heads, group, d_k]
 void take_queries(Arguments& c, const mtf_tensor* q, const mtf_cache* cache, TakenCache* t, int* group, bool data) {
   if (!c.ok()) return;
-  if (!q || (data && !q->data)) return c.wrong(MTF_ERR_INVALID_ARG, "q is NULL or has no data");
-  std::vector<Dim> d;
-  if ((c.st = mtf::read_dims(q->ndim, q->dims, &d, "q")) != MTF_OK || (c.st = mtf::check_tensor(c.layout, d)) != MTF_OK) return;
+  if (!c.there(q, "q", data)) return;
   if (q->ndim < 3) return c.wrong(MTF_ERR_INVALID_ARG, "q has the dims [*sequences, heads, d_k] or [*sequences, heads, group, d_k]");
   // the heads' place is known from the cache, whose checks want the number of sequences: by name first
   if (!cache || !cache->k || !cache->k->dims || cache->k->ndim != 4) return c.wrong(MTF_ERR_INVALID_ARG, "the cache's k is NULL or has other dims than [page, slot, heads, d] or [page, heads, slot, d]");

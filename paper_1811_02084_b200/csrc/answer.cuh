@@ -5,6 +5,8 @@
 
 #include <cstdint>
 
+#include "per_device.h"
+
 namespace mtf {
 
 __device__ __forceinline__ uint32_t smem_at(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
@@ -66,6 +68,19 @@ __device__ __forceinline__ float ex2(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
+}
+
+// The shared memory that a kernel may have, always the same number: set once a device, as `known` has it.
+template <typename K>
+cudaError_t shared_memory_limit(KnownPerDevice& known, K* kernel, int bytes) {
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  known.get(dev, [&] {
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    return e == cudaSuccess ? 1 : 0;
+  });
+  return e;
 }
 
 // A launch that may be set up while the one before it drains, as clusters of so many blocks.

@@ -49,10 +49,22 @@ struct Arguments {
       if ((out || o.out) && r.lo < o.hi && o.lo < r.hi) return wrong(MTF_ERR_INVALID_ARG, "%s overlaps another tensor of the call", name);
     ranges.push_back(r);
   }
-  // a tensor whose own dims are legal under the layout; not NULL, with data
-  bool there(const mtf_tensor* t, const char* name) {
+  // Whether dims are in order under a layout without rules: nearly every call's, and the checks below, which copy the names, then have nothing to find.
+  bool in_order(const mtf_tensor* t) const {
+    if (!layout->rules.empty() || t->ndim < 0 || t->ndim > kMaxTensorDims || (t->ndim > 0 && !t->dims)) return false;
+    for (int i = 0; i < t->ndim; ++i) {
+      const mtf_dim& d = t->dims[i];
+      if (!d.name || !d.name[0] || d.size <= 0) return false;
+      for (int j = 0; j < i; ++j)
+        if (!strcmp(t->dims[j].name, d.name)) return false;
+    }
+    return true;
+  }
+  // a tensor whose own dims are legal under the layout; not NULL, with data (unless it is a description alone)
+  bool there(const mtf_tensor* t, const char* name, bool data = true) {
     if (!ok()) return false;
-    if (!t || !t->data) { wrong(MTF_ERR_INVALID_ARG, "%s is NULL or has no data", name); return false; }
+    if (!t || (data && !t->data)) { wrong(MTF_ERR_INVALID_ARG, "%s is NULL or has no data", name); return false; }
+    if (in_order(t)) return true;
     std::vector<Dim> d;
     if ((st = mtf::read_dims(t->ndim, t->dims, &d, name)) != MTF_OK) return false;
     return (st = mtf::check_tensor(layout, d)) == MTF_OK;

@@ -839,7 +839,8 @@ mtf_status launch(const Args& a, const mtf::CachePool& c, int grid, cudaStream_t
   mtf_status ok = pool_map(&map_k, c.k, c, c.dk, a.box_rows, S::kRow);
   if (ok != MTF_OK || (ok = pool_map(&map_v, c.v, c, c.dv, a.box_rows, S::kRow)) != MTF_OK) return ok;
   constexpr int kResults = (kWarps + 1) * 8 * NT * (DC + 4) * 4, kRoom = 1024 + (S::kRing > kResults ? S::kRing : kResults);
-  const cudaError_t e = cudaFuncSetAttribute(attention_decode_kernel<kE4m3, DC, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kRoom);
+  static mtf::KnownPerDevice limit;
+  const cudaError_t e = mtf::shared_memory_limit(limit, attention_decode_kernel<kE4m3, DC, NT>, kRoom);
   if (e != cudaSuccess) return mtf::fail(MTF_ERR_CUDA, "attention_decode_kernel: %s", cudaGetErrorString(e));
   mtf::launch_clusters(attention_decode_kernel<kE4m3, DC, NT>, dim3((unsigned)grid), kThreads, kRoom, a.cluster, st, a, map_k, map_v);
   mtf::count_launch();

@@ -670,7 +670,8 @@ mtf_status launch_beam_select(const BeamSelect& b, void* stream) {
                            : (aligned ? beam_rows_kernel<float, true> : beam_rows_kernel<float, false>);
   const auto choose = b.bf16 ? (aligned ? beam_choose_kernel<__nv_bfloat16, true> : beam_choose_kernel<__nv_bfloat16, false>)
                              : (aligned ? beam_choose_kernel<float, true> : beam_choose_kernel<float, false>);
-  const cudaError_t set = cudaFuncSetAttribute(rows, cudaFuncAttributeMaxDynamicSharedMemorySize, kRing);
+  static mtf::KnownPerDevice limit[4];
+  const cudaError_t set = shared_memory_limit(limit[(b.bf16 ? 2 : 0) + (aligned ? 1 : 0)], rows, kRing);
   if (set != cudaSuccess) return fail(MTF_ERR_CUDA, "beam_rows_kernel: %s", cudaGetErrorString(set));
   const long long blocks = (a.rows * a.runs + kWarps - 1) / kWarps;
   launch_chained(rows, (unsigned)std::min<long long>(blocks, (long long)device_sm_count() * kBlocks), kThreads, kRing, st, a);

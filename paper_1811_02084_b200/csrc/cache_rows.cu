@@ -80,7 +80,7 @@ __device__ __forceinline__ int place(const RowsArgs& a, int unit) {
 // 32 / kLanes heads of a warp are an item, and a warp has kEach items' loads under way at once: of one position, or of several where it has few heads.  Their places
 // are looked up by a lane each, those of the next items while these ones' rows are under way.  blockIdx.y: K or V.
 // (A look at the table a row, whole calls: 32 x 512 prompts of 16 heads of 64 written in e4m3 and read back 63 us, 8 x 16384 positions of 8 heads of 128 read back 138; now MEASURED.)
-constexpr int kRowBlocks = 2;          // of K, and of V, an SM
+constexpr int kRowBlocks = 4;          // an SM holds; K's come first
 template <int kEach>
 struct Items {
   int unit, head, row;                 // of item lane % kEach: position, first head, place (below 0: none)
@@ -97,7 +97,7 @@ struct Items {
 };
 
 template <int kLanes, bool kBf16, bool kE4m3, int kEach>
-__global__ void __launch_bounds__(256, 2 * kRowBlocks) cache_write_kernel(const RowsArgs a) {
+__global__ void __launch_bounds__(256, kRowBlocks) cache_write_kernel(const RowsArgs a) {
   mtf::chain_wait();
   const int side = blockIdx.y, d = a.d[side], lane = threadIdx.x & 31, col = lane % kLanes * 8, group = lane / kLanes;
   constexpr int kHeads = 32 / kLanes;
@@ -178,7 +178,7 @@ __global__ void __launch_bounds__(256, 2 * kRowBlocks) cache_write_kernel(const 
 }
 
 template <int kLanes, bool kBf16, bool kE4m3, int kEach>
-__global__ void __launch_bounds__(256, 2 * kRowBlocks) cache_read_kernel(const RowsArgs a) {
+__global__ void __launch_bounds__(256, kRowBlocks) cache_read_kernel(const RowsArgs a) {
   mtf::chain_wait();
   const int side = blockIdx.y, d = a.d[side], lane = threadIdx.x & 31, col = lane % kLanes * 8, group = lane / kLanes;
   constexpr int kHeads = 32 / kLanes;
