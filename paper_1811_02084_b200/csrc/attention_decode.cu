@@ -746,7 +746,7 @@ __global__ void __launch_bounds__(256) attention_decode_join_kernel(const Args a
       if (g >= here || d >= a.dv) continue;
       const float f = again[g];
       sum[j] = make_float4(sum[j].x * f, sum[j].y * f, sum[j].z * f, sum[j].w * f);
-      constexpr int kDeep = 8;
+      constexpr int kDeep = 16;                      // under way at once
       for (int i = 0; i < some; i += kDeep) {
         float4 v[kDeep];
 #pragma unroll

@@ -269,25 +269,36 @@ __global__ void __launch_bounds__(256) cache_reorder_kernel(const ReorderArgs a)
   }
   for (int i = tid; i < a.per_sequence; i += threads) to[i] = i == whole && used && fits ? fresh : of[i];
   if (!used || !fits || !there) return;
-  // rows in use of the page that goes on: `used` slots of every head
-  for (int side = 0; side < 2; ++side) {
-    const int pieces = a.row_bytes[side] / 16, total = used * a.heads * pieces;
-    const uint4* const src = reinterpret_cast<const uint4*>(a.pool[side]) + (long long)page * a.rows_page * pieces;
-    uint4* const dst = reinterpret_cast<uint4*>(a.pool[side]) + (long long)fresh * a.rows_page * pieces;
-    // the inner one of slot and head is contiguous: slots of a head (used of them), or all heads of a slot
-    const int inner = (a.row_slot == 1 ? used : a.heads) * pieces, step = (a.row_slot == 1 ? a.row_head : a.row_slot) * pieces;
-    for (int i = tid; i < total; i += threads) {
-      const int run = i / inner, at = run * step + (i - run * inner);
-      dst[at] = src[at];
+  // Rows in use of the page that goes on, `used` slots of every head, K's and V's as one range of 16-byte pieces, four under way a thread.  The inner one of slot and head is
+  // contiguous: slots of a head (used of them), or all heads of a slot.
+  const int rows = used * a.heads, run = a.row_slot == 1 ? used : a.heads, gap = a.row_slot == 1 ? a.row_head : a.row_slot;
+  const int pieces_k = a.row_bytes[0] / 16, pieces_v = a.row_bytes[1] / 16, total_k = rows * pieces_k, total = total_k + rows * pieces_v;
+  const long long src = (long long)page * a.rows_page, dst = (long long)fresh * a.rows_page;
+  constexpr int kDeep = 4;
+  for (int i0 = tid; i0 < total; i0 += kDeep * threads) {
+    uint4 v[kDeep];
+    uint4* to[kDeep];
+#pragma unroll
+    for (int e = 0; e < kDeep; ++e) {
+      const int i = i0 + e * threads;
+      to[e] = nullptr;
+      if (i >= total) continue;
+      const int side = i >= total_k, j = side ? i - total_k : i, pieces = side ? pieces_v : pieces_k;
+      const int inner = run * pieces, n = j / inner, at = n * gap * pieces + (j - n * inner);
+      uint4* const pool = reinterpret_cast<uint4*>(a.pool[side]);
+      to[e] = pool + dst * pieces + at;
+      v[e] = pool[src * pieces + at];
     }
-    if (a.scale[side]) {
-      const int m = inner / pieces, gap = step / pieces;
-      for (int i = tid; i < used * a.heads; i += threads) {
-        const int run = i / m, at = run * gap + (i - run * m);
-        a.scale[side][(long long)fresh * a.rows_page + at] = a.scale[side][(long long)page * a.rows_page + at];
-      }
-    }
+#pragma unroll
+    for (int e = 0; e < kDeep; ++e)
+      if (to[e]) *to[e] = v[e];
   }
+  if (a.scale[0])
+    for (int i = tid; i < 2 * rows; i += threads) {
+      float* const scale = a.scale[i >= rows];
+      const int j = i >= rows ? i - rows : i, n = j / run, at = n * gap + (j - n * run);
+      scale[dst + at] = scale[src + at];
+    }
 }
 
 // out[x, :] = in[group(x), parents[x], :]; rows of `pieces` pieces of type T
