@@ -545,6 +545,7 @@ mtf_status mtf_preference_backward(const mtf_layout_t* layout, const mtf_tensor*
  *              (e4m3: 16), at most 256.  `slot` names the dimension of the slots (NULL: "slot"); the other one is the heads'.
  *   scales   : f32 with k's first three dims, for e4m3 only: a row's values are its bytes' times its scale.  Scales are at least 0.
  *   table    : device int32 [*sequences, table_pages]; only the entries of pages in use are read.
+ * At most 2^31 rows in a pool, 2^24 in a page, 2^30 positions a sequence (MTF_ERR_UNSUPPORTED).
  * Sequences may share pages (that they no longer write).  A page outside the pool, a position that the table has no page for, or a parent outside
  * the beams is left out and reported by mtf_device_status, as an id outside the vocabulary is; nothing is read or written in its place.
  * Layouts: nothing here sums over a split dimension, so any legal layout is free; page, slot, d_k, d_v, beam and vocab may not be split across RANKS
@@ -583,7 +584,7 @@ mtf_status mtf_attention_decode_workspace_bytes(const mtf_layout_t* layout, cons
  * [*sentences, any name: slots], new_finished (may be NULL): 1 where the parent was finished or the token is end_id.  parents, tokens and new_finished are int32 of as many.
  * Words with a logit of -infinity, beams whose score is not finite (a beam that is not yet one: -infinity), and those with a NaN, a +infinity or
  * no finite logit offer nothing; slots without an offer have parent 0, token end_id, score -infinity, finished 1.
- * beams and slots up to 64.  A beam's words are compared by their logits, offers of different beams in 64 bits, from f32 exponentials summed in f32 by threads and in 64 bits across them.
+ * beams and slots up to 64, below 2^31 words in a sentence's beams.  A beam's words are compared by their logits, offers of different beams in 64 bits, from f32 exponentials summed in f32 by threads and in 64 bits across them.
  * workspace as above; it is always needed. */
 mtf_status mtf_beam_select(const mtf_layout_t* layout, const mtf_tensor* logits, const mtf_tensor* scores, const int32_t* finished, int32_t end_id,
                            int32_t* parents, int32_t* tokens, mtf_tensor* new_scores, int32_t* new_finished, void* workspace, size_t workspace_bytes,
@@ -632,12 +633,13 @@ const char* mtf_last_error(void);
  * token id or target outside [0, vocab) was seen by the vocab and loss kernels, or a page, position or parent outside its
  * range by those of answering, since the last call. */
 mtf_status mtf_device_status(int32_t* code);
-/* Testing hook for the failure path of the bounded device-side waits of the persistent tensor-core kernel and of the kernel that
- * streams rows of logits (mtf_policy_step and mtf_distill_step on more than 48 MB of rows above 32 KB); the other kernels' limits are
- * constants.  limit_cycles > 0 sets how many SM cycles a wait may take before it gives up (<= 0 restores the default of about two
+/* Testing hook for the failure path of the bounded device-side waits of the persistent tensor-core kernel, of the kernel that
+ * streams rows of logits (mtf_policy_step and mtf_distill_step on more than 48 MB of rows above 32 KB), of mtf_attention_decode and of mtf_beam_select; the
+ * other kernels' limits are constants.  limit_cycles > 0 sets how many SM cycles a wait may take before it gives up (<= 0 restores the default of about two
  * seconds).  withhold_one_signal = 1 (or any other number but 0 and 2) makes every launch of the tensor-core kernel leave out the
- * "accumulator complete" signal of its first tile, and every block of the streaming kernel wait for a second "numbers complete" signal of its
- * first row; = 2 makes the blocks of the streaming kernel's clusters wait for a second signal with the sums of their first row.  Such a wait
+ * "accumulator complete" signal of its first tile, every block of the streaming kernel wait for a second "numbers complete" signal of its
+ * first row, and every warp of the attention and of the selection's walk over the logits wait for a second signal of its first copy; = 2 makes the blocks of the streaming
+ * kernel's clusters wait for a second signal with the sums of their first row.  Such a wait
  * runs out: the kernel records a code, all its roles
  * leave through the common teardown (copies and MMAs in flight are given time to land, tensor memory
  * is freed), the launch ends normally, its output is unspecified, and the next mtf_device_status

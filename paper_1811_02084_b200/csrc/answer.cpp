@@ -13,6 +13,16 @@ using mtf::numel;
 
 namespace {
 
+// (sizes whose product no memory holds would wrap around in what follows)
+void holds(Arguments& c, const mtf_tensor* t, const char* name) {
+  if (!c.ok()) return;
+  int64_t n = 1;
+  for (int i = 0; i < t->ndim; ++i) {
+    if (t->dims[i].size > (1LL << 46) / n) return c.wrong(MTF_ERR_UNSUPPORTED, "%s has more than 2^46 values", name);
+    n *= t->dims[i].size;
+  }
+}
+
 bool same(const mtf_dim& a, const mtf_dim& b) { return a.size == b.size && (a.name == b.name || !strcmp(a.name, b.name)); }
 
 // The pools of a cache and their places in memory; `heads`: the name of the heads' dimension (NULL: whichever is not the slots').
@@ -26,6 +36,9 @@ void take_cache(Arguments& c, const mtf_cache* cache, long long sequences, bool 
   if (!cache) return c.wrong(MTF_ERR_INVALID_ARG, "NULL cache");
   const mtf_tensor *k = cache->k, *v = cache->v;
   if (!c.there(k, "the cache's k") || !c.there(v, "the cache's v")) return;
+  holds(c, k, "the cache's k");
+  holds(c, v, "the cache's v");
+  if (!c.ok()) return;
   if (k->ndim != 4 || v->ndim != 4) return c.wrong(MTF_ERR_INVALID_ARG, "the cache's k and v have the dims [page, slot, heads, d] or [page, heads, slot, d]");
   if (k->dtype != MTF_BF16 && k->dtype != MTF_E4M3) return c.wrong(MTF_ERR_UNSUPPORTED, "the cache must be bf16 or e4m3");
   if (v->dtype != k->dtype) return c.wrong(MTF_ERR_INVALID_ARG, "the cache's k and v must be of one type");
@@ -42,8 +55,8 @@ void take_cache(Arguments& c, const mtf_cache* cache, long long sequences, bool 
   const int step = p.e4m3 ? 16 : 8;
   if (dk % step || dv % step || dk > mtf::kMaxCacheWidth || dv > mtf::kMaxCacheWidth)
     return c.wrong(MTF_ERR_UNSUPPORTED, "rows of the cache have a multiple of %d values, at most %d; these have %lld and %lld", step, mtf::kMaxCacheWidth, (long long)dk, (long long)dv);
-  if (pages > 0x7fffffffLL || slots > 0x7fffffffLL || heads > 0x7fffffffLL || slots * heads > (1LL << 26) || pages * slots * heads > 0x7fffffffLL)
-    return c.wrong(MTF_ERR_UNSUPPORTED, "at most 2^31 rows in a cache, and 2^26 in a page");
+  if (pages > 0x7fffffffLL || slots > 0x7fffffffLL || heads > 0x7fffffffLL || slots * heads > (1LL << 24) || pages * slots * heads > 0x7fffffffLL)
+    return c.wrong(MTF_ERR_UNSUPPORTED, "at most 2^31 rows in a cache, and 2^24 in a page");
   if (cache->table_pages < 1) return c.wrong(MTF_ERR_INVALID_ARG, "table_pages must be at least 1");
   if (cache->table_pages > (1LL << 30) || cache->table_pages * slots > (1LL << 30) || sequences > 0x7fffffffLL) return c.wrong(MTF_ERR_UNSUPPORTED, "at most 2^30 positions a sequence, 2^31 sequences");
   c.not_across_ranks(k->dims[0].name);
@@ -94,6 +107,8 @@ void together(Arguments& c, std::initializer_list<std::pair<const mtf_tensor*, i
 void take_dense(Arguments& c, const mtf_tensor* kk, const mtf_tensor* vv, long long* sequences, mtf::CacheRows* r) {
   if (!c.there(kk, "kk") || !c.there(vv, "vv")) return;
   if (kk->ndim < 4) return c.wrong(MTF_ERR_INVALID_ARG, "kk and vv have the dims [*sequences, length, heads, d]");
+  holds(c, kk, "kk");
+  holds(c, vv, "vv");
   c.of_name = "kk";
   c.dims_like(vv, kk, 0, kk->ndim - 1, 1, "vv");
   if (!c.ok()) return;
@@ -142,6 +157,8 @@ mtf_status cache_rows(const char* what, const mtf_layout_t* layout, const mtf_te
 void take_queries(Arguments& c, const mtf_tensor* q, const mtf_cache* cache, TakenCache* t, int* group, bool data) {
   if (!c.ok()) return;
   if (!c.there(q, "q", data)) return;
+  holds(c, q, "q");
+  if (!c.ok()) return;
   if (q->ndim < 3) return c.wrong(MTF_ERR_INVALID_ARG, "q has the dims [*sequences, heads, d_k] or [*sequences, heads, group, d_k]");
   // the heads' place is known from the cache, whose checks want the number of sequences: by name first
   if (!cache || !cache->k || !cache->k->dims || cache->k->ndim != 4) return c.wrong(MTF_ERR_INVALID_ARG, "the cache's k is NULL or has other dims than [page, slot, heads, d] or [page, heads, slot, d]");
@@ -189,6 +206,7 @@ mtf_status mtf_attention_decode(const mtf_layout_t* layout, const mtf_tensor* q,
     mtf::DecodeCall d;
     take_queries(c, q, cache, &t, &d.group, true);
     if (!c.there(o, "o")) return c.st;
+    holds(c, o, "o");
     c.of_name = "q";
     c.dims_like(o, q, 0, q->ndim - 1, 1, "o");
     if (c.ok() && !same(o->dims[o->ndim - 1], cache->v->dims[3])) c.wrong(MTF_ERR_SIZE_MISMATCH, "o's last dimension is not that of the cache's v");
@@ -232,12 +250,13 @@ mtf_status mtf_beam_select(const mtf_layout_t* layout, const mtf_tensor* logits,
     Arguments c("beam_select", layout);
     mtf::BeamSelect b;
     if (!c.there(logits, "logits")) return c.st;
+    holds(c, logits, "logits");
     const int last = logits->ndim - 1;
     if (last < 1) c.wrong(MTF_ERR_INVALID_ARG, "logits have the dims [*sentences, beam, vocab]");
     if (c.ok() && logits->dtype != MTF_BF16 && logits->dtype != MTF_F32) c.wrong(MTF_ERR_UNSUPPORTED, "logits must be bf16 or f32");
     if (!c.ok()) return c.st;
     const int64_t V = logits->dims[last].size, beams = logits->dims[last - 1].size, rows = numel(*logits) / V, sentences = rows / beams;
-    if (V > 0x7fffff00LL || rows > 0x7fffffffLL) c.wrong(MTF_ERR_UNSUPPORTED, "at most 2^31 beams and words");
+    if (rows > 0x7ff00000LL || beams * V > 0x7fffff00LL) c.wrong(MTF_ERR_UNSUPPORTED, "at most 2^31 beams, and 2^31 words of a sentence's beams");
     if (c.ok() && beams > mtf::kMaxBeams) c.wrong(MTF_ERR_UNSUPPORTED, "at most %d beams, got %lld", mtf::kMaxBeams, (long long)beams);
     c.not_across_ranks(logits->dims[last].name);
     c.not_across_ranks(logits->dims[last - 1].name);
@@ -286,9 +305,11 @@ mtf_status mtf_beam_select_workspace_bytes(const mtf_layout_t* layout, const mtf
     if (!c.ok()) return c.st;
     std::vector<Dim> d;
     if ((c.st = mtf::read_dims(logits->ndim, logits->dims, &d, "logits")) != MTF_OK || (c.st = mtf::check_tensor(layout, d)) != MTF_OK) return c.st;
+    holds(c, logits, "logits");
     const int last = logits->ndim - 1;
     if (last < 1) c.wrong(MTF_ERR_INVALID_ARG, "logits have the dims [*sentences, beam, vocab]");
-    else if (logits->dims[last].size > 0x7fffff00LL || numel(*logits) / logits->dims[last].size > 0x7fffffffLL) c.wrong(MTF_ERR_UNSUPPORTED, "at most 2^31 beams and words");
+    else if (logits->dims[last - 1].size * logits->dims[last].size > 0x7fffff00LL || numel(*logits) / logits->dims[last].size > 0x7ff00000LL)
+      c.wrong(MTF_ERR_UNSUPPORTED, "at most 2^31 beams, and 2^31 words of a sentence's beams");
     else if (logits->dims[last - 1].size > mtf::kMaxBeams || slots > mtf::kMaxSlots) c.wrong(MTF_ERR_UNSUPPORTED, "at most %d beams and %d slots", mtf::kMaxBeams, mtf::kMaxSlots);
     else if (slots < 1) c.wrong(MTF_ERR_INVALID_ARG, "at least one slot");
     if (!c.ok()) return c.st;
@@ -303,6 +324,9 @@ mtf_status mtf_beam_reorder(const mtf_layout_t* layout, const char* beam, const 
     Arguments c("beam_reorder", layout);
     if (c.ok() && !beam) c.wrong(MTF_ERR_INVALID_ARG, "NULL name of the beams' dimension");
     if (!c.there(states, "states") || !c.there(out, "out")) return c.st;
+    holds(c, states, "states");
+    holds(c, out, "out");
+    if (!c.ok()) return c.st;
     int at = -1;
     for (int i = 0; i < states->ndim; ++i)
       if (!strcmp(states->dims[i].name, beam)) at = i;

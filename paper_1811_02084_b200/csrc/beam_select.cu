@@ -662,8 +662,7 @@ mtf_status launch_beam_select(const BeamSelect& b, void* stream) {
   a.new_finished = b.new_finished;
   a.new_scores = b.new_scores;
   a.of_run = reinterpret_cast<float2*>(b.workspace);
-  // (places are counted in 32 bits, with one step of the grid beyond the last)
-  if (a.rows > 0x7ff00000LL || (long long)a.beams * a.runs > 0x7fff0000LL) return fail(MTF_ERR_UNSUPPORTED, "beam_select: at most 2^31 rows, and runs of a sentence");
+  // (rows, with a step of the grid beyond the last, and a sentence's words are counted in 32 bits: the entry's checks keep them below 2^31)
   cudaStream_t st = (cudaStream_t)stream;
   const bool aligned = (long long)b.vocab * (b.bf16 ? 2 : 4) % 16 == 0;
   const auto rows = b.bf16 ? (aligned ? beam_rows_kernel<__nv_bfloat16, true> : beam_rows_kernel<__nv_bfloat16, false>)

@@ -243,6 +243,34 @@ def test_reorderings():
     refused("cache_reorder", {"parents": ints(SENT + 1, OUT)}, "MTF_ERR_SIZE_MISMATCH")
 
 
+def sized(t, **sizes):
+    """The same memory with other sizes of some dims: refused before anything looks at it."""
+    return mtf.Named([(n, sizes.get(n, s)) for n, s in t.dims], {0: "f32", 1: "bf16", 2: "e4m3"}[t.dtype], t.ptr, t.owner)
+
+
+@pytest.mark.parametrize("op", PAGED)
+def test_caches_beyond_the_kernels_numbers(op):
+    # rows of a page, rows of a pool, and products that wrap around 64 bits
+    for sizes in (dict(slot=(1 << 23) + 1), dict(page=1 << 28), dict(page=1 << 40, slot=1 << 30), dict(page=1 << 62)):
+        refused(op, lambda n: {name: sized(n[name], **sizes) for name in ("k", "v")}, "MTF_ERR_UNSUPPORTED")
+    for sizes in (dict(length=1 << 31), dict(length=1 << 62)):
+        if op in ("write", "read"):
+            refused(op, lambda n: {name: sized(n[name], **sizes) for name in ("kk", "vv")}, "MTF_ERR_UNSUPPORTED")
+    if op == "decode":
+        for group in (4097, 1 << 61):
+            refused(op, lambda n: {name: sized(n[name], group=group) for name in ("q", "o")}, "MTF_ERR_UNSUPPORTED")
+
+
+def test_selections_and_states_beyond_the_kernels_numbers():
+    for vocab in (1 << 30, 1 << 62):                           # (of three beams)
+        refused("select", lambda n: {"logits": sized(n["logits"], vocab=vocab)}, "MTF_ERR_UNSUPPORTED")
+        n = things()
+        with pytest.raises(mtf.MtfError) as e:
+            mtf.mtf_beam_select_workspace_bytes(n["layout"], sized(n["logits"], vocab=vocab), 4)
+        assert e.value.code == "MTF_ERR_UNSUPPORTED"
+    refused("reorder", lambda n: {name: sized(n[name], x=1 << 62) for name in ("states", "out")}, "MTF_ERR_UNSUPPORTED")
+
+
 def test_other_calls_refuse_8_bits():
     """A type that only caches and their reordering have: what took f32 and bf16 does not take it for one of them."""
     x = mtf.named(tensor((4, 16), torch.float8_e4m3fn), ["a", "b"])
