@@ -3,10 +3,11 @@
 // the better ones first, equal ones by the lower i, then the lower v.  A finished beam stands for itself (its end, its score) alone.
 //
 // One read of the logits (HBM is the bound, close behind it the exponentials' unit) gives the sums, and of every run of 128 16-byte pieces the largest word.  A sentence's best
-// words lie in runs whose largest words are among its best: the least of the maxima of `slots` groups of runs is a value that `slots` words at least
-// reach, and a second launch looks only into the runs that reach it, some tens of 1 or 2 KB.  So the first launch is a walk and nothing else: its warps are streams of their own, with bulk copies into
-// a ring each, and wait for nobody.  (64 x 8 rows of 131072 in bf16, whole call: lists of the best words kept for each part of a row, by blocks that stop to sort them, 47 us;
-// by a warp of their own, 82.)
+// words lie in runs whose largest words are among its best: the slots-th largest of the maxima of 64 groups of runs is a value that `slots` words at least
+// reach, and a second launch looks only into the runs that reach it, hardly more than `slots` of 1 or 2 KB.  So the first launch is a walk and nothing else: its warps are streams of
+// their own, with bulk copies into a ring each, and wait for nobody.  (64 x 8 rows of 131072 in bf16, a tenth of them finished, whole call: lists of the best words kept for each part of a row,
+// by blocks that stop to sort them, 47 us; by a warp of their own, 82; the walk with as many groups as slots, in 64 bits, 35.2; as it is 28.9, of which the walk is 24.  It
+// would take 18.8 without its exponentials; 1 x 4 rows of 32768 take 6.5 us, 2.3 of them the walk, and the rest is the choice's chain of some ten dependent steps.)
 //
 // What decides between beams is held in 64 bits: sums of a thread are f32 sums of f32 exponentials relative to an entry of its own, so that
 // the entries that weigh are exact or nearly so; they are joined in 64 bits.  Which thread takes which word goes by the word's index alone, not by
@@ -35,11 +36,14 @@ constexpr int kList = 1024;           // words that may be looked at again befor
 constexpr int kRuns = 1024;           // runs they may lie in
 constexpr int kFirst = 4;             // a sentence's runs that a thread of the choice keeps the largest words of
 constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kSlack = 0x1p-20f;    // of values in f32, which are off by some 2^-24
 
 struct Args {
   const void* z;
   int vocab, beams, slots;
   int runs;                                      // of a row
+  uint32_t runs_mul;                             // i / runs = (i * runs_mul) >> runs_shift in 64 bits, for i below 2^31
+  int runs_shift;
   long long rows;
   const float* scores;
   const int32_t* finished;
@@ -48,6 +52,20 @@ struct Args {
   float* new_scores;
   float2* of_run;                                // [row, run]: the largest word, and the sum of exponentials relative to it
 };
+
+// two f32 operations an instruction
+__device__ __forceinline__ float2 plus(float2 a, float2 b) {
+  float2 r;
+  asm("{\n\t.reg .b64 x, y;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tadd.rn.f32x2 x, x, y;\n\tmov.b64 {%0, %1}, x;\n\t}"
+      : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return r;
+}
+__device__ __forceinline__ float2 times(float2 a, float2 b) {
+  float2 r;
+  asm("{\n\t.reg .b64 x, y;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmul.rn.f32x2 x, x, y;\n\tmov.b64 {%0, %1}, x;\n\t}"
+      : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return r;
+}
 
 // 16 bytes of words
 template <typename T> struct Words;
@@ -86,6 +104,13 @@ template <> struct Words<__nv_bfloat16> {
       x[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
     }
   }
+  // words 2j and 2j + 1, and r to each, in f32
+  static __device__ __forceinline__ float2 plus_two(const uint4& v, int j, float r) {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    float2 s;
+    asm("{\n\t.reg .b16 x, y;\n\tmov.b32 {x, y}, %2;\n\tadd.rn.f32.bf16 %0, x, %3;\n\tadd.rn.f32.bf16 %1, y, %3;\n\t}" : "=f"(s.x), "=f"(s.y) : "r"(w[j]), "f"(r));
+    return s;
+  }
   static __device__ __forceinline__ __nv_bfloat162 two(uint32_t w) { return *reinterpret_cast<const __nv_bfloat162*>(&w); }
   template <int K>
   static __device__ __forceinline__ float largest(const uint4 (&v)[K]) {          // (NaN are passed over)
@@ -118,6 +143,9 @@ template <> struct Words<float> {
   }
   static __device__ __forceinline__ void values(const uint4& v, float (&x)[4]) {
     x[0] = __uint_as_float(v.x); x[1] = __uint_as_float(v.y); x[2] = __uint_as_float(v.z); x[3] = __uint_as_float(v.w);
+  }
+  static __device__ __forceinline__ float2 plus_two(const uint4& v, int j, float r) {
+    return plus(j ? make_float2(__uint_as_float(v.z), __uint_as_float(v.w)) : make_float2(__uint_as_float(v.x), __uint_as_float(v.y)), make_float2(r, r));
   }
   template <int K>
   static __device__ __forceinline__ float largest(const uint4 (&v)[K]) {
@@ -159,19 +187,6 @@ struct Part {
   __device__ __forceinline__ uint4 load(int p) const { return p < whole ? at(base + p) : load_some(first + p * kN, n - p * kN); }
 };
 
-// two f32 operations an instruction
-__device__ __forceinline__ float2 plus(float2 a, float2 b) {
-  float2 r;
-  asm("{\n\t.reg .b64 x, y;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tadd.rn.f32x2 x, x, y;\n\tmov.b64 {%0, %1}, x;\n\t}"
-      : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
-  return r;
-}
-__device__ __forceinline__ float2 times(float2 a, float2 b) {
-  float2 r;
-  asm("{\n\t.reg .b64 x, y;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmul.rn.f32x2 x, x, y;\n\tmov.b64 {%0, %1}, x;\n\t}"
-      : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
-  return r;
-}
 __device__ int g_beam_status = 0;                    // a wait was given up
 __constant__ long long g_wait_limit = kWaitCycles;
 __constant__ int g_withhold = 0;                     // testing: each warp's first wait asks for a copy that nobody has sent
@@ -187,11 +202,9 @@ __device__ __forceinline__ float2 exponentials(const uint4 (&v)[K], float ref) {
   const float r = ref == -INFINITY ? 0.f : -ref;
 #pragma unroll
   for (int e = 0; e < K; ++e) {
-    float x[Words<T>::kN];
-    Words<T>::values(v[e], x);
 #pragma unroll
-    for (int j = 0; j < Words<T>::kN; j += 2) {
-      const float2 d = times(plus(make_float2(x[j], x[j + 1]), make_float2(r, r)), make_float2(kLog2e, kLog2e));
+    for (int j = 0; j < Words<T>::kN / 2; ++j) {
+      const float2 d = times(Words<T>::plus_two(v[e], j, r), make_float2(kLog2e, kLog2e));
       s = plus(s, make_float2(ex2(d.x), ex2(d.y)));
     }
   }
@@ -204,10 +217,10 @@ __device__ __forceinline__ unsigned long long order_of(double v) {
   const unsigned long long b = (unsigned long long)__double_as_longlong(v);
   return b >> 63 ? ~b : b | 0x8000000000000000ull;
 }
-__device__ __forceinline__ float warp_max(float m) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-  return m;
+__device__ __forceinline__ float warp_max(float m) {                  // (NaN are passed over)
+  float top;
+  asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(top) : "f"(m));
+  return top;
 }
 
 // A beam's row, whole
@@ -343,10 +356,12 @@ struct Room {
   int word[kList], beam[kList];
   int runs[kRuns];
   unsigned long long group[kChooserWarps][32];
+  float near_group[kChooserWarps][32], near_bar;
   double base[mtf::kMaxBeams];         // a word's value is base + (logit - ref)
   float ref[mtf::kMaxBeams], low[mtf::kMaxBeams];
+  float off[mtf::kMaxBeams], slack[mtf::kMaxBeams];    // in f32: a word's value is logit + off, give or take slack / 2
   signed char state[mtf::kMaxBeams];   // 0: offers nothing, 1: its words, 2: its end
-  int count, n_runs, below[kChooserWarps];
+  int count, n_runs, far, below[kChooserWarps];       // far: off is none in f32
 };
 
 __device__ __forceinline__ unsigned long long value_key(const Room& m, int b, float z) { return order_of(m.base[b] + ((double)z - (double)m.ref[b]) + 0.); }
@@ -357,20 +372,15 @@ __device__ __forceinline__ float lowest(double v, double base, float ref) {
 }
 __device__ __forceinline__ double value_of(unsigned long long key) { return __longlong_as_double((long long)(key >> 63 ? key & 0x7fffffffffffffffull : ~key)); }
 
-// The words whose value is at least thr (strict: above it), into the list, from the runs whose largest word's is; and the ends of finished beams.  All threads.  Returns how many
-// there are: over kList where that is more than the list holds, or where they lie in too many runs.
-template <typename T, bool kAligned>
-__device__ __forceinline__ int gather(const Args& a, long long row0, Room& m, unsigned long long thr, bool strict, const float (&first)[kFirst]) {
-  constexpr int kN = Words<T>::kN, kDeep = kRun / 32;
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  auto reaches = [&](unsigned long long k) { return strict ? k > thr : k >= thr; };
-  __syncthreads();
-  if (tid == 0) m.count = m.n_runs = 0;
-  if (tid < a.beams) m.low[tid] = thr ? lowest(value_of(thr), m.base[tid], m.ref[tid]) : -INFINITY;
-  __syncthreads();
+__device__ __forceinline__ int beam_of(const Args& a, int i) { return (int)((unsigned long long)(uint32_t)i * a.runs_mul >> a.runs_shift); }
+
+// The runs (of all beams of the sentence, one behind another) that `noted` has, into the room's list; `first`: the largest words of the thread's first.  Behind it, a barrier.
+template <typename N>
+__device__ __forceinline__ void note_runs(const Args& a, long long row0, Room& m, const float (&first)[kFirst], N noted) {
+  const int tid = threadIdx.x;
   auto note = [&](int i, float top) {
-    const int b = i / a.runs;
-    if (m.state[b] != 1 || !(top > -INFINITY) || !reaches(value_key(m, b, top))) return;
+    const int b = beam_of(a, i);
+    if (m.state[b] != 1 || !(top > -INFINITY) || !noted(b, top)) return;
     const int at = atomicAdd(&m.n_runs, 1);
     if (at < kRuns) m.runs[at] = i;
   };
@@ -378,20 +388,17 @@ __device__ __forceinline__ int gather(const Args& a, long long row0, Room& m, un
   for (int e = 0; e < kFirst; ++e)
     if (tid + e * kChoosers < a.beams * a.runs) note(tid + e * kChoosers, first[e]);
   for (int i = tid + kFirst * kChoosers; i < a.beams * a.runs; i += kChoosers) note(i, a.of_run[row0 * a.runs + i].x);
-  if (tid < a.beams && m.state[tid] == 2 && reaches(order_of(m.base[tid] + 0.))) {
-    const int at = atomicAdd(&m.count, 1);
-    m.key[at] = order_of(m.base[tid] + 0.);
-    m.z[at] = 0.f;
-    m.word[at] = a.end_id;
-    m.beam[at] = tid;
-  }
   __syncthreads();
-  const int n = m.n_runs;
-  if (n > kRuns) return kList + 1;
-  for (int i = warp; i < n; i += kChooserWarps) {
-    const int b = m.runs[i] / a.runs, run = m.runs[i] - b * a.runs;
+}
+// The words of these runs that are low(b) at least, and whose values `wanted` has, into the list of words: a warp a run.  Behind it, a barrier.
+template <typename T, bool kAligned, typename L, typename W>
+__device__ __forceinline__ void list_words(const Args& a, long long row0, Room& m, L low_of, W wanted) {
+  constexpr int kN = Words<T>::kN, kDeep = kRun / 32;
+  const int lane = threadIdx.x & 31, n = m.n_runs;
+  for (int i = threadIdx.x >> 5; i < n; i += kChooserWarps) {
+    const int at_run = m.runs[i], b = beam_of(a, at_run), run = at_run - b * a.runs;
     const Part<T, kAligned> w = row_at<T, kAligned>(a, row0 + b);
-    const float low = m.low[b];
+    const float low = low_of(b);
     uint4 v[kDeep];
 #pragma unroll
     for (int e = 0; e < kDeep; ++e) {
@@ -406,36 +413,93 @@ __device__ __forceinline__ int gather(const Args& a, long long row0, Room& m, un
     }
     for (; have; have &= have - 1) {
       const int e = __ffs(have) - 1;
-      const uint4 u[1] = {e == 0 ? v[0] : e == 1 ? v[1] : e == 2 ? v[2] : v[3]};
+      const uint4 u = e == 0 ? v[0] : e == 1 ? v[1] : e == 2 ? v[2] : v[3];
       float x[kN];
-      Words<T>::values(u[0], x);
+      Words<T>::values(u, x);
+      uint32_t those = 0;
 #pragma unroll
-      for (int j = 0; j < kN; ++j)
-        if (x[j] >= low && x[j] > -INFINITY) {
-          const unsigned long long k = value_key(m, b, x[j]);
-          if (reaches(k)) {
-            const int at = atomicAdd(&m.count, 1);
-            if (at < kList) {
-              m.key[at] = k;
-              m.z[at] = x[j];
-              m.word[at] = (run * kRun + e * 32 + lane) * kN + j;
-              m.beam[at] = b;
-            }
-          }
+      for (int j = 0; j < kN; ++j) those |= (x[j] >= low && x[j] > -INFINITY ? 1u : 0u) << j;
+      for (; those; those &= those - 1) {
+        const int j = __ffs(those) - 1;
+        float z = x[0];
+#pragma unroll
+        for (int k = 1; k < kN; ++k) z = j == k ? x[k] : z;
+        const unsigned long long k = value_key(m, b, z);
+        if (!wanted(k)) continue;
+        const int at = atomicAdd(&m.count, 1);
+        if (at < kList) {
+          m.key[at] = k;
+          m.z[at] = z;
+          m.word[at] = (run * kRun + e * 32 + lane) * kN + j;
+          m.beam[at] = b;
         }
+      }
     }
   }
   __syncthreads();
+}
+// The ends of finished beams, into the list (which has room for them: they come first).
+template <typename W>
+__device__ __forceinline__ void list_ends(const Args& a, Room& m, W wanted) {
+  const int b = threadIdx.x;
+  if (b >= a.beams || m.state[b] != 2) return;
+  const unsigned long long k = order_of(m.base[b] + 0.);
+  if (!wanted(k)) return;
+  const int at = atomicAdd(&m.count, 1);
+  m.key[at] = k;
+  m.z[at] = 0.f;
+  m.word[at] = a.end_id;
+  m.beam[at] = b;
+}
+
+// The words whose value is above thr, and such ends.  All threads.  Returns how many there are: over kList where that is more than the list holds, or where they lie in too many runs.
+template <typename T, bool kAligned>
+__device__ __noinline__ int gather_above(const Args& a, long long row0, Room& m, unsigned long long thr, const float (&first)[kFirst]) {
+  const int tid = threadIdx.x;
+  auto above = [&](unsigned long long k) { return k > thr; };
+  __syncthreads();
+  if (tid == 0) m.count = m.n_runs = 0;
+  if (tid < a.beams) m.low[tid] = thr ? lowest(value_of(thr), m.base[tid], m.ref[tid]) : -INFINITY;
+  __syncthreads();
+  list_ends(a, m, above);
+  note_runs(a, row0, m, first, [&](int b, float top) { return above(value_key(m, b, top)); });
+  if (m.n_runs > kRuns) return kList + 1;
+  list_words<T, kAligned>(a, row0, m, [&](int b) { return m.low[b]; }, above);
   return m.count;
 }
 
-// Where too many words reach thr to be sorted (rows of equal words, or masked by a finite value): those above it, and the first of those equal to it.  Where those above are
+// Where too many words reach the bar to be sorted (rows of equal words, or masked by a finite value).  In 64 bits: thr = the least of the largest words of as many groups of runs as
+// there are slots (the next power of two), which `slots` words at least reach; those above it, and the first of those equal to it.  Where those above are
 // too many, too, thr becomes the slots-th largest value, by counting its bytes from the highest on.  Returns how many the list holds.  All threads.
 template <typename T, bool kAligned>
-__device__ __noinline__ int narrowed(const Args& a, long long row0, Room& m, unsigned long long thr, const float (&first)[kFirst]) {
+__device__ __noinline__ int narrowed(const Args& a, long long row0, Room& m, const float (&first)[kFirst]) {
   constexpr int kN = Words<T>::kN;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  int above = gather<T, kAligned>(a, row0, m, thr, true, first);
+  unsigned long long best = 0;
+  auto better_of = [&](int i, float top) {
+    const int b = beam_of(a, i);
+    if (m.state[b] == 1 && top > -INFINITY) best = max(best, value_key(m, b, top));
+  };
+#pragma unroll
+  for (int e = 0; e < kFirst; ++e)
+    if (tid + e * kChoosers < a.beams * a.runs) better_of(tid + e * kChoosers, first[e]);
+  for (int i = tid + kFirst * kChoosers; i < a.beams * a.runs; i += kChoosers) better_of(i, a.of_run[row0 * a.runs + i].x);
+  if (tid < a.beams && m.state[tid] == 2) best = max(best, order_of(m.base[tid] + 0.));
+  int groups = 1;
+  while (groups < min(a.slots, 32)) groups *= 2;
+  for (int o = groups; o < 32; o *= 2) best = max(best, __shfl_xor_sync(0xffffffffu, best, o));
+  m.group[warp][lane] = best;
+  __syncthreads();
+  unsigned long long even = m.group[0][lane], odd = m.group[1][lane];
+#pragma unroll
+  for (int i = 2; i < kChooserWarps; i += 2) {
+    even = max(even, m.group[i][lane]);
+    odd = max(odd, m.group[i + 1][lane]);
+  }
+  unsigned long long thr = a.slots > 32 ? min(even, odd) : max(even, odd);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) thr = min(thr, __shfl_xor_sync(0xffffffffu, thr, o));
+  int above = gather_above<T, kAligned>(a, row0, m, thr, first);
   if (above > kList) {
     int* const counts = reinterpret_cast<int*>(m.key);
     unsigned long long prefix = 0;
@@ -466,7 +530,7 @@ __device__ __noinline__ int narrowed(const Args& a, long long row0, Room& m, uns
       prefix = prefix << 8 | (unsigned)d;
     }
     thr = prefix;
-    above = gather<T, kAligned>(a, row0, m, thr, true, first);              // fewer than `slots`, in runs of which there are no more
+    above = gather_above<T, kAligned>(a, row0, m, thr, first);              // fewer than `slots`, in runs of which there are no more
   }
   // equal ones: by the lower beam, of a beam's the larger logits (the sums may have lost what tells them apart), of these the lower words; as long as there is need of them
   int at = above;
@@ -537,6 +601,8 @@ __device__ __noinline__ int narrowed(const Args& a, long long row0, Room& m, uns
 template <typename T, bool kAligned>
 __global__ void __launch_bounds__(kChoosers, 1) beam_choose_kernel(const Args a) {
   __shared__ Room m;
+  if (threadIdx.x == 0) m.count = m.n_runs = m.far = 0;
+  __syncthreads();
   mtf::chain_wait_only();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const long long sentence = blockIdx.x, row0 = sentence * a.beams;
@@ -577,38 +643,54 @@ __global__ void __launch_bounds__(kChoosers, 1) beam_choose_kernel(const Args a)
       m.state[b] = (signed char)state;
       m.base[b] = at;
       m.ref[b] = top;
+      const double off = at - top;
+      const float slack = (float)(fabs(off) * kSlack + (fabs(at) + fabsf(top)) * 1e-14);
+      const bool near = fabs(off) < 1e38 && slack < 1e38f;
+      m.off[b] = near ? (float)off : 0.f;
+      m.slack[b] = near ? slack : 0.f;
+      if (state && !near) m.far = 1;
     }
   }
   __syncthreads();
-  // ---- the largest words of as many groups of runs as there are slots (the next power of two): the least of them is a value that `slots` words at least reach.  A group
-  // is the lanes that are alike modulo their number (more slots than lanes: those of the even warps and those of the odd ones)
-  unsigned long long best = 0;
+  // ---- the largest words of 64 groups of runs, in f32 and a little too low: the slots-th largest of them is a bar that `slots` words at least reach, and hardly more runs than
+  // those have to be looked into.  A group is the lanes that are alike modulo their number, of the even warps or of the odd ones.
+  float best = -INFINITY;
   auto better_of = [&](int i, float top) {
-    const int b = i / a.runs;
-    if (m.state[b] == 1 && top > -INFINITY) best = max(best, value_key(m, b, top));
+    const int b = beam_of(a, i);
+    const float v = top + m.off[b];
+    if (m.state[b] == 1 && top > -INFINITY) best = fmaxf(best, v - (m.slack[b] + fabsf(v) * kSlack));
   };
 #pragma unroll
   for (int e = 0; e < kFirst; ++e)
     if (tid + e * kChoosers < a.beams * a.runs) better_of(tid + e * kChoosers, first[e]);
   for (int i = tid + kFirst * kChoosers; i < a.beams * a.runs; i += kChoosers) better_of(i, a.of_run[row0 * a.runs + i].x);
-  if (tid < a.beams && m.state[tid] == 2) best = max(best, order_of(m.base[tid] + 0.));
-  int groups = 1;
-  while (groups < min(a.slots, 32)) groups *= 2;
-  for (int o = groups; o < 32; o *= 2) best = max(best, __shfl_xor_sync(0xffffffffu, best, o));
-  m.group[warp][lane] = best;
+  if (tid < a.beams && m.state[tid] == 2) best = fmaxf(best, m.off[tid] - m.slack[tid]);
+  m.near_group[warp][lane] = best;
   __syncthreads();
-  unsigned long long even = m.group[0][lane], odd = m.group[1][lane];
+  float even = m.near_group[0][lane], odd = m.near_group[1][lane];
 #pragma unroll
   for (int i = 2; i < kChooserWarps; i += 2) {
-    even = max(even, m.group[i][lane]);
-    odd = max(odd, m.group[i + 1][lane]);
+    even = fmaxf(even, m.near_group[i][lane]);
+    odd = fmaxf(odd, m.near_group[i + 1][lane]);
   }
-  unsigned long long thr = a.slots > 32 ? min(even, odd) : max(even, odd);
+  constexpr int kPlaces = 64 / kChooserWarps;      // groups whose place among all a warp finds
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) thr = min(thr, __shfl_xor_sync(0xffffffffu, thr, o));
-  // ---- the words that reach it, and their places among each other: a warp a word
-  int n = gather<T, kAligned>(a, row0, m, thr, false, first);
-  if (n > kList) n = narrowed<T, kAligned>(a, row0, m, thr, first);
+  for (int e = 0; e < kPlaces; ++e) {
+    const int c = warp * kPlaces + e;
+    const float v = __shfl_sync(0xffffffffu, c < 32 ? even : odd, c & 31);
+    const int place = __popc(__ballot_sync(0xffffffffu, even > v || (even == v && lane < c))) + __popc(__ballot_sync(0xffffffffu, odd > v || (odd == v && lane + 32 < c)));
+    if (lane == 0 && place == a.slots - 1) m.near_bar = m.far ? -INFINITY : v;
+  }
+  __syncthreads();
+  // ---- the words that may reach it (all that do, and some a little below), and their places among each other: a warp a word
+  const float bar = m.near_bar;
+  auto low_of = [&](int b) { return bar - m.off[b] - (m.slack[b] + (fabsf(bar) + fabsf(m.off[b])) * kSlack); };
+  auto any = [](unsigned long long) { return true; };
+  list_ends(a, m, any);
+  note_runs(a, row0, m, first, [&](int b, float top) { return top >= low_of(b); });
+  if (m.n_runs <= kRuns) list_words<T, kAligned>(a, row0, m, low_of, any);
+  int n = m.n_runs <= kRuns ? m.count : kList + 1;
+  if (n > kList) n = narrowed<T, kAligned>(a, row0, m, first);
   for (int i = warp; i < n; i += kChooserWarps) {
     const unsigned long long k = m.key[i];
     const int b = m.beam[i], word = m.word[i];
@@ -654,6 +736,11 @@ mtf_status launch_beam_select(const BeamSelect& b, void* stream) {
   a.slots = b.slots;
   a.rows = b.sentences * b.beams;
   a.runs = runs_of(b.vocab, b.bf16);
+  // with 2^n >= runs > 2^(n - 1) the factor ceil(2^(31 + n) / runs) is below 2^32 and off by less than 2^n in 2^(31 + n): exact for i < 2^31
+  int log2_runs = 0;
+  while ((1LL << log2_runs) < a.runs) ++log2_runs;
+  a.runs_mul = (uint32_t)(((1ULL << (31 + log2_runs)) + a.runs - 1) / a.runs);
+  a.runs_shift = 31 + log2_runs;
   a.scores = b.scores;
   a.finished = b.finished;
   a.end_id = b.end_id;
