@@ -8,10 +8,13 @@
 // rows of the cache as the instruction's 16 rows and the heads as its 8 columns, eight heads of queries cost no more than one and nothing is padded to 16:
 //     S^T [16 keys x 8 heads] = K [16 x d] q^T [d x 8],   O^T [d x 8 heads] += V^T [d x 16 keys] P^T [16 keys x 8]
 // The order of a sum's terms is free, so a lane reads 16 bytes of a row at a time and what it has of d, and of the keys, is what it multiplies; V's pairs of keys are put together by
-// byte permutes.  (64 sequences of up to 4096 positions in bf16, 1.1 GB, whole call: loads into registers 252 us, copies by the lanes into shared memory 244, TMA 199.)
+// byte permutes.  (64 sequences of up to 4096 positions in bf16, 1.1 GB, whole call: loads into registers 252 us, copies by the lanes into shared memory 244, TMA 199,
+// of warps that look the pages up a step ahead and join in fours 180: 6.2 TB/s.  4 sequences of up to 65536 in e4m3, 0.4 GB: 74 to 77, half of the issue slots used, two thirds of them to
+// make f16 of e4m3, and 5 for joining.)
 //
-// The work is cut evenly: the keys of all (sequence, head) items are laid end to end in units of some rows a warp, and every block takes an equal
-// run of them, whatever the lengths.  Items that cross a block's edge are left as partial sums and joined behind the launch, in order.
+// What is shared out are units, 64 to 256 keys of an item (a sequence's head) that the block's warps take a chunk each: a block or a cluster of blocks an item, or, where sequences may be
+// long, the units of all items end to end and an equal run of them for every block, whatever the lengths (plan_of has the rule and what was measured).  Items that cross a block's edge are left
+// as partial sums then, and joined behind the launch, in order.
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -39,8 +42,8 @@ using mtf::smem_at;
 
 constexpr int kWarps = 4;
 constexpr int kThreads = 32 * kWarps;
-constexpr int kPlanned = 1024;        // sequences whose units a block adds up by itself
-constexpr int kSteps = 2, kMostSteps = 8;
+constexpr int kPlanned = 1024;        // sequences whose units a block adds up by itself, eight a thread; more of them have items enough for a block each
+constexpr int kFewSteps = 8, kLoneSteps = 11;      // units a block of a cluster, and one by itself: plan_of
 constexpr int kMostBlocks = 8;        // of a cluster
 constexpr int kOver = 3;              // units that an item costs beside its own: first loads, joining
 constexpr int kLeastCost = 5;         // a block's run
@@ -232,7 +235,7 @@ __global__ void __launch_bounds__(kThreads, Shape<kE4m3, DC>::kBlocks) attention
     bool whole;
     int slot = 0;
     if (a.balanced) {
-      const int x = (int)(u / H);                   // (units of a sequence's heads lie one behind another)
+      const int x = (int)(u / H);                   // (units of a sequence's heads lie one behind another: 182 us; of a head's sequences: 184)
       int lo = 0, hi = a.n_seq;                     // the last sequence with cum <= x
       while (hi - lo > 1) {
         const int m = (lo + hi) / 2;
@@ -689,7 +692,7 @@ __global__ void __launch_bounds__(kThreads, Shape<kE4m3, DC>::kBlocks) attention
 // factor is worked out once; then a thread adds up four columns of a head, in the parts' order, with some loads under way at once.
 constexpr int kJoined = 64;                          // parts at a time
 template <int kHeads, int DC>
-__global__ void __launch_bounds__(256) attention_decode_join_kernel(const Args a) {
+__global__ void __launch_bounds__(256, 4) attention_decode_join_kernel(const Args a) {
   __shared__ float factor[kHeads][kJoined];
   __shared__ float tops[kHeads][2], sums[kHeads], again[kHeads];
   mtf::chain_wait_only();
@@ -746,7 +749,7 @@ __global__ void __launch_bounds__(256) attention_decode_join_kernel(const Args a
       if (g >= here || d >= a.dv) continue;
       const float f = again[g];
       sum[j] = make_float4(sum[j].x * f, sum[j].y * f, sum[j].z * f, sum[j].w * f);
-      constexpr int kDeep = 16;                      // under way at once
+      constexpr int kDeep = 8;                       // under way at once
       for (int i = 0; i < some; i += kDeep) {
         float4 v[kDeep];
 #pragma unroll
@@ -788,7 +791,20 @@ int unit_keys(const mtf::CachePool& c) {
   return kWarps * 16 * (row <= 64 ? 4 : row <= 128 ? 2 : 1);
 }
 
-// How a call's items (a head, or as many heads of queries as a block takes, of a sequence) are shared out.
+// How a call's items (a head, or as many heads of queries as a block takes, of a sequence) are shared out: to a block each, to a cluster of blocks each, which join their sums
+// through their shared memory, or, cut into units, evenly to all blocks of the GPU, which leave parts for a second launch.  The host knows how many positions a sequence may have, not how
+// many it has.  A unit takes a block 0.7 us; the cluster's joining 1.2, and its blocks start the later the more there are beyond one an SM; the even cut pays 5 to 6 for its sums over the
+// lengths and its second launch, and is the only one of the three whose time does not go by the longest sequence.  Hence
+//   - clusters as long as they are no more blocks than SMs, and cut something off: not for 2 units;
+//   - beyond that, up to what the SMs hold at once, where a block has more than 8 units left;
+//   - the even cut where it still has (a block by itself: more than 11).
+// Measured (bf16, d 128 unless said; us for a block an item / clusters of 2 / 4 / 8 / the even cut):
+//   1 x 16 heads, 512 positions of d 64 (4 units)  6.8  6.1  5.6  5.6  10.3;  256 positions (2 units)  4.9  5.6  5.3  5.7  6.8
+//   4 x 8, 512 (8 units)                          10.8  8.9  7.6  8.2  12.6;  26 x 8, 300 (5)          9.2 11.1 18.7 33.4  14.5
+//   40 x 5, up to 777 (13)                        15.5 13.0 18.0 33.1  14.8;  80 x 5, 700 (11)        28.5 35.4 47.7 73.4  33.2
+//   16 x 8, up to 1500 (24)                       24.4 17.6 19.2 23.9  14.8;  all of 1500             25.9 20.8 26.6 29.8  20.1
+//   64 x 16, up to 4096 (64)                       179  169  182  257   176;  all of 4096              322  310  319  383   335
+// (In the last line clusters of two are ahead, but where one sequence in 64 has 4096 positions and the others few they take three times as long as the even cut.)
 struct Plan {
   bool balanced;
   int cluster;
@@ -797,11 +813,11 @@ struct Plan {
 Plan plan_of(const mtf::CachePool& c, int group) {
   const int nt = tiles_of_heads(c, group), chunks = (group + 8 * nt - 1) / (8 * nt);
   const long long items = c.sequences * c.heads * chunks, units = ((long long)c.per_sequence * c.slots + unit_keys(c) - 1) / unit_keys(c);
-  const long long most = (long long)mtf::device_sm_count() * blocks_an_sm(c);
+  const long long sms = mtf::device_sm_count(), most = sms * blocks_an_sm(c);
   int cluster = 1;
-  while (cluster < kMostBlocks && units > kSteps * cluster && items * cluster * 2 <= most) cluster *= 2;
+  while (cluster < kMostBlocks && ((units > std::max(2, cluster) && items * cluster * 2 <= sms) || (units > kFewSteps * cluster && items * cluster * 2 <= most))) cluster *= 2;
   // (the sum of all sequences' units is kept in 32 bits)
-  const bool balanced = units > kMostSteps * cluster && c.sequences <= kPlanned && c.sequences * (units + kOver) < (1LL << 31);
+  const bool balanced = units > (cluster > 1 ? kFewSteps * cluster : kLoneSteps) && c.sequences <= kPlanned && c.sequences * (units + kOver) < (1LL << 31);
   if (balanced) return {true, 1, std::max(1LL, std::min(most, items * (units + kOver) / kLeastCost))};
   return {false, cluster, items * cluster};
 }
