@@ -5,9 +5,9 @@
 // One read of the logits (HBM is the bound, close behind it the exponentials' unit) gives the sums, and of every run of 128 16-byte pieces the largest word.  A sentence's best
 // words lie in runs whose largest words are among its best: the slots-th largest of the maxima of 64 groups of runs is a value that `slots` words at least
 // reach, and a second launch looks only into the runs that reach it, hardly more than `slots` of 1 or 2 KB.  So the first launch is a walk and nothing else: its warps are streams of
-// their own, with bulk copies into a ring each, and wait for nobody.  (64 x 8 rows of 131072 in bf16, a tenth of them finished, whole call: lists of the best words kept for each part of a row,
+// their own, with bulk copies into a ring each, and wait for nobody.  (64 x 8 rows of 131072 in bf16, a tenth of them finished, calls in a graph: lists of the best words kept for each part of a row,
 // by blocks that stop to sort them, 47 us; by a warp of their own, 82; the walk with as many groups as slots, in 64 bits, 35.2; as it is 28.9, of which the walk is 24.  It
-// would take 18.8 without its exponentials; 1 x 4 rows of 32768 take 6.5 us, 2.3 of them the walk, and the rest is the choice's chain of some ten dependent steps.)
+// would take 18.8 without its exponentials; 1 x 4 rows of 32768 take 6.8 us in one launch, 2.3 of them the walk, and the rest is the choice's chain of some ten dependent steps.)
 //
 // What decides between beams is held in 64 bits: sums of a thread are f32 sums of f32 exponentials relative to an entry of its own, so that
 // the entries that weigh are exact or nearly so; they are joined in 64 bits.  Which thread takes which word goes by the word's index alone, not by
@@ -30,8 +30,9 @@ using mtf::smem_at;
 constexpr int kThreads = 256, kWarps = kThreads / 32, kBlocks = 4;      // of the walk; blocks an SM holds
 constexpr int kRun = 128;             // 16-byte pieces that a warp takes at a time
 constexpr int kStages = 3;            // of a warp's ring, a run each: 50 KB a block
-constexpr int kStage = (kRun + 8) * 16, kRing = kWarps * kStages * kStage;
+constexpr int kStage = (kRun + 8) * 16, kRing = kWarps * kStages * kStage, kFewRing = 2 * kRing;
 constexpr int kChoosers = 512, kChooserWarps = kChoosers / 32;
+constexpr int kCluster = 8;           // blocks a sentence, where there are few
 constexpr int kList = 1024;           // words that may be looked at again before the choice goes by counting
 constexpr int kRuns = 1024;           // runs they may lie in
 constexpr int kFirst = 4;             // a sentence's runs that a thread of the choice keeps the largest words of
@@ -229,21 +230,19 @@ __device__ __forceinline__ Part<T, kAligned> row_at(const Args& a, long long row
   return Part<T, kAligned>(reinterpret_cast<const T*>(a.z), row * a.vocab, a.vocab, a.rows * a.vocab);
 }
 
-// The runs of all rows one behind another, every warp of the grid the next one: all of them have as many, wherever beams lie that are not to be read.
-template <typename T, bool kAligned>
-__global__ void __launch_bounds__(kThreads, kBlocks) beam_rows_kernel(const Args a) {
-  constexpr int kDeep = kRun / 32;
-  __shared__ uint64_t bars[kWarps][kStages];
-  extern __shared__ __align__(128) uint8_t dyn[];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const uint8_t* const ring = dyn + warp * kStages * kStage;
-  if (lane == 0) {
-    for (int i = 0; i < kStages; ++i) mtf::landing_init(&bars[warp][i]);
+__device__ __forceinline__ void ready(uint64_t (&bars)[kStages]) {
+  if ((threadIdx.x & 31) == 0) {
+    for (int i = 0; i < kStages; ++i) mtf::landing_init(&bars[i]);
     mtf::landing_ready();
   }
   __syncwarp();
-  mtf::chain_wait();
-  const int all = gridDim.x * kWarps, rows = (int)a.rows, some_rows = all / a.runs, some_runs = all - some_rows * a.runs;
+}
+
+// One of `all` warps' walk over the runs of rows [begin, rows), one behind another, every warp the next one: all of them have as many, wherever beams lie that are not to be read.
+template <typename T, bool kAligned>
+__device__ __forceinline__ void walk(const Args& a, const uint8_t* ring, uint64_t (&bars)[kStages], int first, int all, int begin, int rows) {
+  constexpr int kDeep = kRun / 32;
+  const int lane = threadIdx.x & 31, some_rows = all / a.runs, some_runs = all - some_rows * a.runs;
   struct Place {
     int row, run;
   };
@@ -267,8 +266,7 @@ __global__ void __launch_bounds__(kThreads, kBlocks) beam_rows_kernel(const Args
     q.done = in && a.finished ? a.finished[p.row] : 0;
     return q;
   };
-  const int first = blockIdx.x * kWarps + warp;
-  Place now = {first / a.runs, first % a.runs}, ahead = now;
+  Place now = {begin + first / a.runs, first % a.runs}, ahead = now;
   uint32_t read = 0, flying = 0;                     // of the stages: the run is to be read, and is being copied
   auto fetch = [&](int stage, const Place& p, const Asked& q) {
     const bool live = fabsf(q.score) < INFINITY && !q.done;
@@ -279,7 +277,7 @@ __global__ void __launch_bounds__(kThreads, kBlocks) beam_rows_kernel(const Args
     if ((p.run + 1) * kRun > w.whole) return;        // (a row's last words: by loads)
     flying |= 1u << stage;
     if (lane == 0) {
-      const uint32_t bar = smem_at(&bars[warp][stage]), bytes = (kRun + (w.off ? 1 : 0)) * 16;
+      const uint32_t bar = smem_at(&bars[stage]), bytes = (kRun + (w.off ? 1 : 0)) * 16;
       mtf::expect(bar, bytes);
       asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(smem_at(ring) + stage * kStage), "l"(w.base + (long long)p.run * kRun),
                    "r"(bytes), "r"(bar)
@@ -307,12 +305,12 @@ __global__ void __launch_bounds__(kThreads, kBlocks) beam_rows_kernel(const Args
       const Part<T, kAligned> w = row_at<T, kAligned>(a, now.row);
       uint4 v[kDeep];
       if (flying >> stage & 1) {
-        const uint32_t bar = smem_at(&bars[warp][stage]), phase = phases >> stage & 1;
+        const uint32_t bar = smem_at(&bars[stage]), phase = phases >> stage & 1;
         if (!mtf::landed(bar, phase, g_wait_limit) || (g_withhold && !mtf::landed(bar, phase ^ 1, g_wait_limit))) {
           if (lane == 0) atomicCAS(&g_beam_status, 0, 0xB11);
           // given up: what is under way gets a little more time
           for (int i = 0; i < kStages; ++i)
-            if (flying >> i & 1) mtf::landed_late(smem_at(&bars[warp][i]), phases >> i & 1, mtf::kLandCycles);
+            if (flying >> i & 1) mtf::landed_late(smem_at(&bars[i]), phases >> i & 1, mtf::kLandCycles);
           return;
         }
         phases ^= 1u << stage;
@@ -347,6 +345,16 @@ __global__ void __launch_bounds__(kThreads, kBlocks) beam_rows_kernel(const Args
     }
     onward(now);
   }
+}
+
+template <typename T, bool kAligned>
+__global__ void __launch_bounds__(kThreads, kBlocks) beam_rows_kernel(const Args a) {
+  __shared__ uint64_t bars[kWarps][kStages];
+  extern __shared__ __align__(128) uint8_t dyn[];
+  const int warp = threadIdx.x >> 5;
+  ready(bars[warp]);
+  mtf::chain_wait();
+  walk<T, kAligned>(a, dyn + warp * kStages * kStage, bars[warp], blockIdx.x * kWarps + warp, gridDim.x * kWarps, 0, (int)a.rows);
 }
 
 // What a sentence's choice is made from.
@@ -597,15 +605,11 @@ __device__ __noinline__ int narrowed(const Args& a, long long row0, Room& m, con
   return max(above, at);
 }
 
-// A block a sentence.
+// A sentence's choice.  All threads of a block; the room's counters are 0.
 template <typename T, bool kAligned>
-__global__ void __launch_bounds__(kChoosers, 1) beam_choose_kernel(const Args a) {
-  __shared__ Room m;
-  if (threadIdx.x == 0) m.count = m.n_runs = m.far = 0;
-  __syncthreads();
-  mtf::chain_wait_only();
+__device__ __forceinline__ void choose(const Args& a, Room& m, long long sentence) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const long long sentence = blockIdx.x, row0 = sentence * a.beams;
+  const long long row0 = sentence * a.beams;
   float first[kFirst];
 #pragma unroll
   for (int e = 0; e < kFirst; ++e) first[e] = tid + e * kChoosers < a.beams * a.runs ? a.of_run[row0 * a.runs + tid + e * kChoosers].x : -INFINITY;
@@ -717,6 +721,32 @@ __global__ void __launch_bounds__(kChoosers, 1) beam_choose_kernel(const Args a)
   }
 }
 
+// A block a sentence.
+template <typename T, bool kAligned>
+__global__ void __launch_bounds__(kChoosers, 1) beam_choose_kernel(const Args a) {
+  __shared__ Room m;
+  if (threadIdx.x == 0) m.count = m.n_runs = m.far = 0;
+  __syncthreads();
+  mtf::chain_wait_only();
+  choose<T, kAligned>(a, m, blockIdx.x);
+}
+
+// Few and short rows: a cluster of blocks a sentence, which walk over its rows, and one of which chooses.  (launch_beam_select has the rule.)
+template <typename T, bool kAligned>
+__global__ void __launch_bounds__(kChoosers, 1) beam_few_kernel(const Args a) {
+  __shared__ uint64_t bars[kChooserWarps][kStages];
+  __shared__ Room m;
+  extern __shared__ __align__(128) uint8_t dyn[];
+  const int warp = threadIdx.x >> 5, sentence = blockIdx.x / kCluster, rank = blockIdx.x - sentence * kCluster;
+  if (threadIdx.x == 0) m.count = m.n_runs = m.far = 0;
+  ready(bars[warp]);
+  mtf::chain_wait();
+  walk<T, kAligned>(a, dyn + warp * kStages * kStage, bars[warp], rank * kChooserWarps + warp, kCluster * kChooserWarps, sentence * a.beams, (sentence + 1) * a.beams);
+  __syncwarp();
+  mtf::cluster_barrier();                            // (all runs' sums are written)
+  if (rank == 0) choose<T, kAligned>(a, m, sentence);
+}
+
 int runs_of(int vocab, bool bf16) {
   const int words = kRun * (bf16 ? 8 : 4);
   return (vocab + words - 1) / words;
@@ -752,18 +782,26 @@ mtf_status launch_beam_select(const BeamSelect& b, void* stream) {
   // (rows, with a step of the grid beyond the last, and a sentence's words are counted in 32 bits: the entry's checks keep them below 2^31)
   cudaStream_t st = (cudaStream_t)stream;
   const bool aligned = (long long)b.vocab * (b.bf16 ? 2 : 4) % 16 == 0;
-  const auto rows = b.bf16 ? (aligned ? beam_rows_kernel<__nv_bfloat16, true> : beam_rows_kernel<__nv_bfloat16, false>)
-                           : (aligned ? beam_rows_kernel<float, true> : beam_rows_kernel<float, false>);
-  const auto choose = b.bf16 ? (aligned ? beam_choose_kernel<__nv_bfloat16, true> : beam_choose_kernel<__nv_bfloat16, false>)
-                             : (aligned ? beam_choose_kernel<float, true> : beam_choose_kernel<float, false>);
-  static mtf::KnownPerDevice limit[4];
-  const cudaError_t set = shared_memory_limit(limit[(b.bf16 ? 2 : 0) + (aligned ? 1 : 0)], rows, kRing);
-  if (set != cudaSuccess) return fail(MTF_ERR_CUDA, "beam_rows_kernel: %s", cudaGetErrorString(set));
-  const long long blocks = (a.rows * a.runs + kWarps - 1) / kWarps;
-  launch_chained(rows, (unsigned)std::min<long long>(blocks, (long long)device_sm_count() * kBlocks), kThreads, kRing, st, a);
+  static KnownPerDevice limits[2][4];
+  // One launch instead of two where a cluster's warps have at most a run each and half of the SMs hold the clusters: it saves the host 2.5 us a call, and costs the GPU what a cluster
+  // is slower than the whole of it.  (Calls in a row / in a graph, two launches -> one: 1 x 4 rows of 32768 in bf16 9.5 / 6.5 -> 7.0 / 6.8 us, 8 x 4 9.5 / 6.8 -> 7.2 / 7.0, 16 x 4
+  // 9.6 / 7.0 -> 9.6 / 9.6; two runs a warp, 1 x 8 rows, 9.5 / 6.9 -> 8.0 / 7.9; eight, 1 x 8 of 131072, 9.6 / 7.3 -> 13.8 / 13.8.)
+  const bool few = b.sentences * kCluster * 2 <= device_sm_count() && a.beams * a.runs <= kCluster * kChooserWarps;
+  const auto walking = few ? (b.bf16 ? (aligned ? beam_few_kernel<__nv_bfloat16, true> : beam_few_kernel<__nv_bfloat16, false>) : (aligned ? beam_few_kernel<float, true> : beam_few_kernel<float, false>))
+                           : (b.bf16 ? (aligned ? beam_rows_kernel<__nv_bfloat16, true> : beam_rows_kernel<__nv_bfloat16, false>) : (aligned ? beam_rows_kernel<float, true> : beam_rows_kernel<float, false>));
+  const cudaError_t set = shared_memory_limit(limits[few][(b.bf16 ? 2 : 0) + (aligned ? 1 : 0)], walking, few ? kFewRing : kRing);
+  if (set != cudaSuccess) return fail(MTF_ERR_CUDA, "beam_select kernels: %s", cudaGetErrorString(set));
   count_launch();
-  launch_chained(choose, (unsigned)b.sentences, kChoosers, 0, st, a);
-  count_launch();
+  if (few) {
+    launch_clusters(walking, dim3((unsigned)(b.sentences * kCluster)), kChoosers, kFewRing, kCluster, st, a);
+  } else {
+    const auto choosing = b.bf16 ? (aligned ? beam_choose_kernel<__nv_bfloat16, true> : beam_choose_kernel<__nv_bfloat16, false>)
+                                 : (aligned ? beam_choose_kernel<float, true> : beam_choose_kernel<float, false>);
+    const long long blocks = (a.rows * a.runs + kWarps - 1) / kWarps;
+    launch_chained(walking, (unsigned)std::min<long long>(blocks, (long long)device_sm_count() * kBlocks), kThreads, kRing, st, a);
+    count_launch();
+    launch_chained(choosing, (unsigned)b.sentences, kChoosers, 0, st, a);
+  }
   const cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess) return fail(MTF_ERR_CUDA, "beam_select kernels: %s", cudaGetErrorString(e));
   return MTF_OK;

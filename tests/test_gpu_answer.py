@@ -488,6 +488,16 @@ def test_selection(mtf, dtype, S, K, V, slots):
     select(mtf, z, sc, fin.astype(np.int32), min(2, V - 1), slots, dtype)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("S,K,V,slots", [(9, 4, 8192, 4), (10, 4, 8192, 4), (2, 4, 16384, 4), (2, 4, 32768, 4), (2, 4, 32776, 4), (1, 64, 2049, 33), (9, 3, 4099, 32)])
+def test_selection_where_one_launch_becomes_two(mtf, dtype, S, K, V, slots):
+    """Numbers of sentences and of runs on both sides of what a cluster a sentence takes, some beams not there, some finished."""
+    z, sc = logits(S, K, V, seed=S * V)
+    sc[0, -1], sc[-1, 0] = -np.inf, np.nan
+    fin = np.random.RandomState(7).rand(S, K) < 0.2
+    select(mtf, z, sc, fin.astype(np.int32), 3, slots, dtype)
+
+
 @pytest.mark.parametrize("V", [4096, 9001])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_selection_ties_masks_and_empty_beams(mtf, dtype, V):

@@ -29,7 +29,7 @@ def selection(m, dtype, V):
     return lambda: m.mtf_beam_select(lay, nz, ns, None, 1, outs[0], outs[1], nnew, outs[2], w), outs, guard
 
 
-# attention: a block an item, clusters, the even cut; selection: copies of whole runs, at and off 16 bytes
+# attention: a block an item, clusters, the even cut; selection: copies of whole runs, at and off 16 bytes, in two launches and in one
 CALLS = {
     "block": lambda m, t: attention(m, t, [100, 30], 7, 64),
     "clusters": lambda m, t: attention(m, t, [700, 300], 44, 64),
@@ -37,11 +37,13 @@ CALLS = {
     "shares": lambda m, t: attention(m, t, [3000, 300, 0], 1100, 64),
     "aligned": lambda m, t: selection(m, t, 32768),
     "odd": lambda m, t: selection(m, t, 40001),
+    "few": lambda m, t: selection(m, t, 8000),
+    "few odd": lambda m, t: selection(m, t, 8001),
 }
 
 
 @pytest.mark.parametrize("what,dtype,code", [(w, t, "0xb01") for w in ("block", "clusters", "wide", "shares") for t in ("bf16", "e4m3")]
-                         + [(w, t, "0xb11") for w in ("aligned", "odd") for t in ("bf16", "f32")])
+                         + [(w, t, "0xb11") for w in ("aligned", "odd", "few", "few odd") for t in ("bf16", "f32")])
 def test_a_wait_runs_out_and_the_next_call_is_correct(mtf, what, dtype, code):  # noqa: F811
     import torch
     call, outs, guard = CALLS[what](mtf, dtype)
