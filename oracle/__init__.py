@@ -15,6 +15,8 @@ Contents
   chooser.py      exhaustive search for the cheapest legal layout under those counts (Section 11's future work)
   update.py       Algorithm 1 line 3: the parameter update (reading: SGD with momentum and weight decay)
   vocab.py        embedding, logits einsum and softmax cross-entropy over a (split) vocab dimension
+  losses.py       distillation, policy and preference losses on stored logits
+  answer.py       paged caches and their 8-bit rows, attention of one new token, beam search's selection and reordering
   rounding.py     the one rounding step applied where the method stores an intermediate in bf16
 
 Pins (tests that tie each part to something other than itself) are listed in the test files named
