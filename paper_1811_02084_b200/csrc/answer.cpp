@@ -211,7 +211,7 @@ mtf_status mtf_attention_decode(const mtf_layout_t* layout, const mtf_tensor* q,
     c.dims_like(o, q, 0, q->ndim - 1, 1, "o");
     if (c.ok() && !same(o->dims[o->ndim - 1], cache->v->dims[3])) c.wrong(MTF_ERR_SIZE_MISMATCH, "o's last dimension is not that of the cache's v");
     if (c.ok() && o->dtype != MTF_BF16) c.wrong(MTF_ERR_UNSUPPORTED, "o must be bf16");
-    if (c.ok() && !std::isfinite(scale)) c.wrong(MTF_ERR_INVALID_ARG, "scale must be finite");
+    if (c.ok() && !std::isfinite(scale * 1.5f)) c.wrong(MTF_ERR_INVALID_ARG, "scale must be finite, and in powers of two, too");
     if (!c.ok()) return c.st;
     c.memory(q->data, numel(*q) * 2, 16, false, "q");
     c.memory(o->data, numel(*o) * 2, 16, true, "o");

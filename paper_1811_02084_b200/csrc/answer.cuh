@@ -43,20 +43,14 @@ __device__ __forceinline__ uint32_t in_block(uint32_t at, int rank) {
   asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(x) : "r"(at), "r"(rank));
   return x;
 }
-__device__ __forceinline__ uint32_t far_word(uint32_t at) {
-  uint32_t x;
-  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(x) : "r"(at) : "memory");
+__device__ __forceinline__ float far(uint32_t at) {
+  float x;
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(x) : "r"(at) : "memory");
   return x;
 }
-__device__ __forceinline__ float far(uint32_t at) { return __uint_as_float(far_word(at)); }
 __device__ __forceinline__ float2 far2(uint32_t at) {
   float2 x;
   asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(x.x), "=f"(x.y) : "r"(at) : "memory");
-  return x;
-}
-__device__ __forceinline__ double far_double(uint32_t at) {
-  double x;
-  asm volatile("ld.shared::cluster.f64 %0, [%1];" : "=d"(x) : "r"(at) : "memory");
   return x;
 }
 __device__ __forceinline__ void cluster_barrier() {

@@ -9,7 +9,7 @@
 //     S^T [16 keys x 8 heads] = K [16 x d] q^T [d x 8],   O^T [d x 8 heads] += V^T [d x 16 keys] P^T [16 keys x 8]
 // The order of a sum's terms is free, so a lane reads 16 bytes of a row at a time and what it has of d, and of the keys, is what it multiplies; V's pairs of keys are put together by
 // byte permutes.  (64 sequences of up to 4096 positions in bf16, 1.1 GB, whole call: loads into registers 252 us, copies by the lanes into shared memory 244, TMA 199,
-// of warps that look the pages up a step ahead and join in fours 180: 6.2 TB/s.  4 sequences of up to 65536 in e4m3, 0.4 GB: 74 to 77, half of the issue slots used, two thirds of them to
+// of warps that look the pages up a step ahead and join in fours 180: 6.2 TB/s.  4 sequences of up to 65536 in e4m3, 0.4 GB: 74 to 77, half of the issue slots used, a third of them to
 // make f16 of e4m3, and 5 for joining.)
 //
 // What is shared out are units, 64 to 256 keys of an item (a sequence's head) that the block's warps take a chunk each: a block or a cluster of blocks an item, or, where sequences may be
@@ -21,6 +21,7 @@
 #include <cuda_runtime.h>
 
 #include <algorithm>
+#include <cfloat>
 #include <mutex>
 
 #include "answer.cuh"
@@ -316,6 +317,10 @@ __global__ void __launch_bounds__(kThreads, Shape<kE4m3, DC>::kBlocks) attention
       // the lane's results are those of heads 2t and 2t + 1
       factor[nt][0] = kE4m3 ? a.scale_log2 * __shfl_sync(0xffffffffu, f, 8 * t) : f;
       factor[nt][1] = kE4m3 ? a.scale_log2 * __shfl_sync(0xffffffffu, f, 8 * t + 4) : f;
+      // (a factor beyond f32 stays finite: a product of 0 stays 0, and others are as far apart as weights can tell)
+      if (kE4m3)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) factor[nt][h] = fminf(fmaxf(factor[nt][h], -FLT_MAX), FLT_MAX);
     }
 
     float o[NT][kMT][4], ml[NT][2], mo[NT][2], l[NT][2];

@@ -177,7 +177,7 @@ def test_attention():
     refused("decode", lambda n: {"q": renamed(n["q"], "heads", "h")}, "MTF_ERR_SIZE_MISMATCH")
     refused("decode", lambda n: {"o": renamed(n["o"], "group", "g")}, "MTF_ERR_SIZE_MISMATCH")
     refused("decode", lambda n: {"o": mtf.named(tensor((B, H, G, D), torch.bfloat16), n["o"].names)}, "MTF_ERR_SIZE_MISMATCH")
-    for x in (float("nan"), float("inf")):
+    for x in (float("nan"), float("inf"), -3e38):
         refused("decode", {"scale": x})
     for name in ("q", "o"):
         refused("decode", lambda n: {name: mtf.Named(n[name].dims, n[name].dtype, n[name].ptr + 8, n[name].owner)}, "MTF_ERR_UNSUPPORTED")
