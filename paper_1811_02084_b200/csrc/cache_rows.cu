@@ -76,11 +76,11 @@ __device__ __forceinline__ int place(const RowsArgs& a, int unit) {
   return page * a.rows_page + ((int)m - index * a.slots) * a.row_slot;
 }
 
-// A position's rows of all heads are together in the dense tensor, and their place is one look at the table.  kLanes lanes take a head, 8 values each (d up to 8 kLanes); the
+// A position's rows of all heads are together in the dense tensor, and their place is one look at the table.  kLanes lanes take a head, 8 or 16 values each (d up to as many times kLanes); the
 // 32 / kLanes heads of a warp are an item, and a warp has kEach items' loads under way at once: of one position, or of several where it has few heads.  Their places
 // are looked up by a lane each, those of the next items while these ones' rows are under way.  blockIdx.y: K or V.
-// (A look at the table a row, whole calls: 32 x 512 prompts of 16 heads of 64 written in e4m3 and read back 63 us, 8 x 16384 positions of 8 heads of 128 read back 138; this way 40 and 122, 4.4 and 5.6 TB/s.  Reading is near
-// HBM's rate; writing spends its issue slots, 70 % of them, on finding the rows' largest values and on the conversions.)
+// (A look at the table a row, whole calls: 32 x 512 prompts of 16 heads of 64 written in e4m3 and read back 63 us, 8 x 16384 positions of 8 heads of 128 read back 138; this way 36 and 120, 4.9 and 5.8 TB/s.  Reading is near
+// HBM's rate; writing spends its issue slots on finding the rows' largest values and on the conversions, of 8 values a lane 70 % of them.)
 constexpr int kRowBlocks = 4;          // an SM holds; K's come first
 template <int kEach>
 struct Items {
@@ -97,11 +97,11 @@ struct Items {
   }
 };
 
-template <int kLanes, bool kBf16, bool kE4m3, int kEach>
+template <int kLanes, int kValues, bool kBf16, bool kE4m3, int kEach>
 __global__ void __launch_bounds__(256, kRowBlocks) cache_write_kernel(const RowsArgs a) {
   mtf::chain_wait();
-  const int side = blockIdx.y, d = a.d[side], lane = threadIdx.x & 31, col = lane % kLanes * 8, group = lane / kLanes;
-  constexpr int kHeads = 32 / kLanes;
+  const int side = blockIdx.y, d = a.d[side], lane = threadIdx.x & 31, col = lane % kLanes * kValues, group = lane / kLanes;
+  constexpr int kHeads = 32 / kLanes, kPieces = kValues * (kBf16 ? 2 : 4) / 16;
   const long long step = (long long)gridDim.x * 8 * kEach;
   long long first = ((long long)blockIdx.x * 8 + (threadIdx.x >> 5)) * kEach;
   Items<kEach> next;
@@ -109,33 +109,26 @@ __global__ void __launch_bounds__(256, kRowBlocks) cache_write_kernel(const Rows
   for (; first < a.items; first += step) {
     const Items<kEach> now = next;
     if (now.row == -2 && lane < kEach) atomicExch(&g_bad_place, 1);
-    uint4 w[kEach][2];
+    uint4 w[kEach][kPieces];
     int row[kEach];                                  // -1: nothing to be done by this lane
 #pragma unroll
     for (int e = 0; e < kEach; ++e) {
       const int unit = __shfl_sync(0xffffffffu, now.unit, e), head = __shfl_sync(0xffffffffu, now.head, e) + group, here = __shfl_sync(0xffffffffu, now.row, e);
       row[e] = here >= 0 && head < a.heads && col < d ? here + head * a.row_head : -1;
-      w[e][0] = w[e][1] = make_uint4(0u, 0u, 0u, 0u);
-      if (row[e] >= 0) {
-        const uint4* const p = reinterpret_cast<const uint4*>(a.dense[side] + (((long long)unit * a.heads + head) * d + col) * (kBf16 ? 2 : 4));
-        w[e][0] = p[0];
-        if (!kBf16) w[e][1] = p[1];
-      }
+      const uint4* const p = reinterpret_cast<const uint4*>(a.dense[side] + (((long long)unit * a.heads + head) * d + col) * (kBf16 ? 2 : 4));
+#pragma unroll
+      for (int i = 0; i < kPieces; ++i) w[e][i] = row[e] >= 0 ? p[i] : make_uint4(0u, 0u, 0u, 0u);
     }
     next.look(a, first + step, kHeads);
 #pragma unroll
     for (int e = 0; e < kEach; ++e) {
       const long long at = (long long)row[e] * d + col;
-      float x[8];
-      if (kBf16) {
-        const uint32_t u[4] = {w[e][0].x, w[e][0].y, w[e][0].z, w[e][0].w};
+      uint32_t u[4 * kPieces];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) { x[2 * j] = lo16(u[j]); x[2 * j + 1] = hi16(u[j]); }
-      } else {
-        const uint32_t u[8] = {w[e][0].x, w[e][0].y, w[e][0].z, w[e][0].w, w[e][1].x, w[e][1].y, w[e][1].z, w[e][1].w};
+      for (int i = 0; i < kPieces; ++i) { u[4 * i] = w[e][i].x; u[4 * i + 1] = w[e][i].y; u[4 * i + 2] = w[e][i].z; u[4 * i + 3] = w[e][i].w; }
+      float x[kValues];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] = __uint_as_float(u[j]);
-      }
+      for (int j = 0; j < kValues; ++j) x[j] = kBf16 ? (j & 1 ? hi16(u[j / 2]) : lo16(u[j / 2])) : __uint_as_float(u[j]);
       if (!kE4m3) {
         if (row[e] >= 0)
           *reinterpret_cast<uint4*>(a.pool[side] + at * 2) = kBf16 ? w[e][0] : make_uint4(two_bf16(x[0], x[1]), two_bf16(x[2], x[3]), two_bf16(x[4], x[5]), two_bf16(x[6], x[7]));
@@ -144,12 +137,12 @@ __global__ void __launch_bounds__(256, kRowBlocks) cache_write_kernel(const Rows
       // the row's largest magnitude as bits, in whose order infinities and NaN come last
       uint32_t top = 0;
       if (kBf16) {
-        const uint32_t u[4] = {w[e][0].x & 0x7fff7fffu, w[e][0].y & 0x7fff7fffu, w[e][0].z & 0x7fff7fffu, w[e][0].w & 0x7fff7fffu};
-        const uint32_t m = __vmaxu2(__vmaxu2(u[0], u[1]), __vmaxu2(u[2], u[3]));
-        top = max(m << 16, m & 0xffff0000u);
+#pragma unroll
+        for (int i = 0; i < 4 * kPieces; ++i) top = __vmaxu2(top, u[i] & 0x7fff7fffu);
+        top = max(top << 16, top & 0xffff0000u);
       } else {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(x[j]) & 0x7fffffffu);
+        for (int j = 0; j < kValues; ++j) top = max(top, __float_as_uint(x[j]) & 0x7fffffffu);
       }
 #pragma unroll
       for (int o = kLanes / 2; o > 0; o /= 2) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
@@ -157,7 +150,7 @@ __global__ void __launch_bounds__(256, kRowBlocks) cache_write_kernel(const Rows
         // NaN and infinities: all to NaN, and the largest of the others
         top = 0;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
+        for (int j = 0; j < kValues; ++j) {
           const uint32_t m = __float_as_uint(x[j]) & 0x7fffffffu;
           if (m < 0x7f800000u) top = max(top, m);
           else x[j] = __uint_as_float(0x7fc00000u);
@@ -170,18 +163,20 @@ __global__ void __launch_bounds__(256, kRowBlocks) cache_write_kernel(const Rows
       if (top == 0) field = 127;
       if (row[e] < 0) continue;
       const float up = __uint_as_float((uint32_t)(254 - field) << 23);
+      uint32_t four[kValues / 4];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) x[j] *= up;
-      *reinterpret_cast<uint2*>(a.pool[side] + at) = make_uint2(two_e4m3(x[0], x[1]) | two_e4m3(x[2], x[3]) << 16, two_e4m3(x[4], x[5]) | two_e4m3(x[6], x[7]) << 16);
+      for (int i = 0; i < kValues / 4; ++i) four[i] = two_e4m3(x[4 * i] * up, x[4 * i + 1] * up) | two_e4m3(x[4 * i + 2] * up, x[4 * i + 3] * up) << 16;
+      if constexpr (kValues == 16) *reinterpret_cast<uint4*>(a.pool[side] + at) = make_uint4(four[0], four[1], four[2], four[3]);
+      else *reinterpret_cast<uint2*>(a.pool[side] + at) = make_uint2(four[0], four[1]);
       if (col == 0) a.scale[side][row[e]] = __uint_as_float((uint32_t)field << 23);
     }
   }
 }
 
-template <int kLanes, bool kBf16, bool kE4m3, int kEach>
+template <int kLanes, int kValues, bool kBf16, bool kE4m3, int kEach>
 __global__ void __launch_bounds__(256, kRowBlocks) cache_read_kernel(const RowsArgs a) {
   mtf::chain_wait();
-  const int side = blockIdx.y, d = a.d[side], lane = threadIdx.x & 31, col = lane % kLanes * 8, group = lane / kLanes;
+  const int side = blockIdx.y, d = a.d[side], lane = threadIdx.x & 31, col = lane % kLanes * kValues, group = lane / kLanes;
   constexpr int kHeads = 32 / kLanes;
   const long long step = (long long)gridDim.x * 8 * kEach;
   long long first = ((long long)blockIdx.x * 8 + (threadIdx.x >> 5)) * kEach;
@@ -200,14 +195,14 @@ __global__ void __launch_bounds__(256, kRowBlocks) cache_read_kernel(const RowsA
       if (here < 0 || head >= a.heads || col >= d) continue;
       const int row = here + head * a.row_head;
       const long long at = (long long)row * d + col;
-      if (kE4m3) {
+      if (kE4m3 && kValues == 8) {
         const uint2 v = *reinterpret_cast<const uint2*>(a.pool[side] + at);
         w[e].x = v.x;
         w[e].y = v.y;
-        scale[e] = a.scale[side][row];
       } else {
-        w[e] = *reinterpret_cast<const uint4*>(a.pool[side] + at * 2);
+        w[e] = *reinterpret_cast<const uint4*>(a.pool[side] + at * (kE4m3 ? 1 : 2));
       }
+      if (kE4m3) scale[e] = a.scale[side][row];
     }
     next.look(a, first + step, kHeads);
 #pragma unroll
@@ -216,23 +211,23 @@ __global__ void __launch_bounds__(256, kRowBlocks) cache_read_kernel(const RowsA
       if (unit < 0 || head >= a.heads || col >= d) continue;
       uint4* const p = reinterpret_cast<uint4*>(a.dense[side] + (((long long)unit * a.heads + head) * d + col) * (kBf16 ? 2 : 4));
       if (!kE4m3 && kBf16) { p[0] = w[e]; continue; }
-      float x[8];
+      const uint32_t u[4] = {w[e].x, w[e].y, w[e].z, w[e].w};
+      float x[kValues];
       if (kE4m3) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const float2 v = of_e4m3((j < 2 ? w[e].x : w[e].y) >> (16 * (j & 1)));
+        for (int j = 0; j < kValues / 2; ++j) {
+          const float2 v = of_e4m3(u[j / 2] >> (16 * (j & 1)));
           x[2 * j] = v.x * scale[e];
           x[2 * j + 1] = v.y * scale[e];
         }
       } else {
-        const uint32_t u[4] = {w[e].x, w[e].y, w[e].z, w[e].w};
 #pragma unroll
-        for (int j = 0; j < 4; ++j) { x[2 * j] = lo16(u[j]); x[2 * j + 1] = hi16(u[j]); }
+        for (int j = 0; j < kValues; ++j) x[j] = j & 1 ? hi16(u[j / 2]) : lo16(u[j / 2]);
       }
-      if (kBf16) p[0] = make_uint4(two_bf16(x[0], x[1]), two_bf16(x[2], x[3]), two_bf16(x[4], x[5]), two_bf16(x[6], x[7]));
-      else {
-        p[0] = make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
-        p[1] = make_uint4(__float_as_uint(x[4]), __float_as_uint(x[5]), __float_as_uint(x[6]), __float_as_uint(x[7]));
+#pragma unroll
+      for (int i = 0; i < kValues * (kBf16 ? 2 : 4) / 16; ++i) {
+        if constexpr (kBf16) p[i] = make_uint4(two_bf16(x[8 * i], x[8 * i + 1]), two_bf16(x[8 * i + 2], x[8 * i + 3]), two_bf16(x[8 * i + 4], x[8 * i + 5]), two_bf16(x[8 * i + 6], x[8 * i + 7]));
+        else p[i] = make_uint4(__float_as_uint(x[4 * i]), __float_as_uint(x[4 * i + 1]), __float_as_uint(x[4 * i + 2]), __float_as_uint(x[4 * i + 3]));
       }
     }
   }
@@ -353,22 +348,32 @@ RowsArgs rows_args(const mtf::CachePool& c, const mtf::CacheRows& r) {
   return a;
 }
 
-template <int kLanes, bool kBf16, bool kE4m3>
+template <int kLanes, int kValues, bool kBf16, bool kE4m3>
 void rows_launch(RowsArgs a, bool write, cudaStream_t st) {
   const int passes = (a.heads + 32 / kLanes - 1) / (32 / kLanes);
-  constexpr int kWrite = 4, kRead = kE4m3 ? 8 : 4;       // items at once (8-bit rows are half as long)
+  // items at once: 16 to 32 registers of what is loaded.  (Half as many: prompts 37.8 us for 35.5, the long read 127 for 120; twice as many 39.7 and 132.)
+  constexpr int kWrite = kValues == 16 && !kBf16 ? 2 : 4, kRead = kValues == 8 && kE4m3 ? 8 : 4;
   const int each = write ? kWrite : kRead;
   a.items = (long long)a.units * passes;
   a.by_passes = divide_by(passes);
   const long long blocks = std::min<long long>((a.items + 8 * each - 1) / (8 * each), (long long)mtf::device_sm_count() * kRowBlocks);
-  mtf::launch_clusters(write ? cache_write_kernel<kLanes, kBf16, kE4m3, kWrite> : cache_read_kernel<kLanes, kBf16, kE4m3, kRead>, dim3((unsigned)blocks, 2, 1), 256, 0, 1, st, a);
+  mtf::launch_clusters(write ? cache_write_kernel<kLanes, kValues, kBf16, kE4m3, kWrite> : cache_read_kernel<kLanes, kValues, kBf16, kE4m3, kRead>, dim3((unsigned)blocks, 2, 1), 256, 0, 1, st, a);
 }
 template <bool kBf16, bool kE4m3>
 void rows_lanes(const RowsArgs& a, bool write, cudaStream_t st) {
-  const int d = std::max(a.d[0], a.d[1]);
-  if (d <= 64) rows_launch<8, kBf16, kE4m3>(a, write, st);
-  else if (d <= 128) rows_launch<16, kBf16, kE4m3>(a, write, st);
-  else rows_launch<32, kBf16, kE4m3>(a, write, st);
+  const int d = std::max(a.d[0], a.d[1]), lanes = d <= 64 ? 8 : d <= 128 ? 16 : 32;
+  // 8-bit rows: 16 values a lane where that saves a pass over the heads, 8 where lanes would stand idle.  (8 -> 16 values, rows of 64: written and read back, 2 heads 19.6 -> 24.9 us, 4 12.0 -> 15.1,
+  // 6 15.1 -> 12.5, 8 12.1 -> 11.5, 16 heads of 32 x 512 positions 39.6 -> 35.5; read, 8 x 16384 positions of 4 heads 32 -> 41, of 6 60 -> 46, of 8 65 -> 63.)
+  if constexpr (kE4m3)
+    if (a.heads > 32 / lanes) {
+      if (lanes == 8) rows_launch<4, 16, kBf16, true>(a, write, st);
+      else if (lanes == 16) rows_launch<8, 16, kBf16, true>(a, write, st);
+      else rows_launch<16, 16, kBf16, true>(a, write, st);
+      return;
+    }
+  if (lanes == 8) rows_launch<8, 8, kBf16, kE4m3>(a, write, st);
+  else if (lanes == 16) rows_launch<16, 8, kBf16, kE4m3>(a, write, st);
+  else rows_launch<32, 8, kBf16, kE4m3>(a, write, st);
 }
 mtf_status after(const char* what) {
   mtf::count_launch();

@@ -354,7 +354,7 @@ def bf16_of(x):
 @pytest.mark.parametrize("slot_first", [True, False])
 @pytest.mark.parametrize("source", ["bf16", "f32"])
 @pytest.mark.parametrize("dtype", ["bf16", "e4m3"])
-@pytest.mark.parametrize("heads,dk,dv,slots,length", [(1, 64, 64, 16, 1), (3, 80, 48, 20, 13), (2, 256, 144, 5, 37), (5, 128, 16, 64, 70), (1, 16, 256, 1, 3)])
+@pytest.mark.parametrize("heads,dk,dv,slots,length", [(1, 64, 64, 16, 1), (3, 80, 48, 20, 13), (2, 256, 144, 5, 37), (5, 128, 16, 64, 70), (1, 16, 256, 1, 3), (9, 64, 48, 16, 21)])
 def test_rows_there_and_back(mtf, dtype, source, heads, dk, dv, slots, length, slot_first):
     import torch
     lay, guard = layout(mtf), Guarded()
