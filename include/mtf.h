@@ -570,8 +570,8 @@ mtf_status mtf_cache_read(const mtf_layout_t* layout, const mtf_cache* cache, co
  *     o[s, h, g, :] = sum_m p_m v[m, h, :],  p = softmax over m < lengths[s] of scale * sum_d q[s, h, g, d] k[m, h, d]
  * q [*sequences, heads, group, d_k] or, for one head of queries to a head of the cache, [*sequences, heads, d_k]; o like q with d_v; both bf16, 16-byte
  * aligned; `heads` and d_k named as in the cache; group up to 4096; |scale| below 2e38.  Where there is no position (length 0, all pages left out), or no weight (every logit -infinity), o is 0.  What
- * lies in slots beyond the last position is not looked at.  Sums are f32; a weight is rounded to bf16 (e4m3: to f16, with the scale of its row of v) before
- * it multiplies a row of v.  workspace: device, 16-byte aligned, at least what the query says (0: may be NULL), contents of no matter before and after; calls that may run at
+ * lies in slots beyond the last position is not looked at.  Sums are f32; a weight multiplies a row of v as the sum of two bf16 values, off by 2^-16 of it (e4m3: as
+ * one f16, with the scale of the row of v; 2^-11).  workspace: device, 16-byte aligned, at least what the query says (0: may be NULL), contents of no matter before and after; calls that may run at
  * the same time need one each. */
 mtf_status mtf_attention_decode(const mtf_layout_t* layout, const mtf_tensor* q, const mtf_cache* cache, const int32_t* lengths, float scale, mtf_tensor* o,
                                 void* workspace, size_t workspace_bytes, void* stream);

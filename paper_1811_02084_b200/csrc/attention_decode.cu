@@ -523,8 +523,11 @@ __global__ void __launch_bounds__(kThreads, Shape<kE4m3, DC>::kBlocks) attention
             }
           }
       }
-      // ---- weights
-      uint32_t pb[S::kTiles][NT][2];
+      // ---- weights.  bf16: two pieces, the nearest value and the nearest of what that leaves, so that a weight is off by 2^-16 of itself at most.  (One piece, 2^-8, puts the results
+      // of the 64 sequences above 2^-9.6 of their size from those of f32 weights, as far as their own rounding; two 2^-13.  The second costs 0.5 us of 180, 1.4 of 82 with 16 heads of queries a head.)
+      // e4m3: one f16 piece, 2^-11, which leaves 2^-12; a second would leave 2^-13.7 and cost 75 -> 77 us for the 4 sequences above, 62 -> 72 with 16 heads of queries to each of 4 heads.
+      constexpr int kPieces = kE4m3 ? 1 : 2;
+      uint32_t pb[S::kTiles][NT][kPieces][2];
 #pragma unroll
       for (int c = 0; c < S::kTiles; ++c)
 #pragma unroll
@@ -545,15 +548,19 @@ __global__ void __launch_bounds__(kThreads, Shape<kE4m3, DC>::kBlocks) attention
             }
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
-            uint32_t two;
             if (kE4m3) {
               const __half2 x = __floats2half2_rn(p[2 * e], p[2 * e + 1]);
-              two = *reinterpret_cast<const uint32_t*>(&x);
+              pb[c][nt][0][e] = transposed(*reinterpret_cast<const uint32_t*>(&x));
             } else {
-              const __nv_bfloat162 x = __floats2bfloat162_rn(p[2 * e], p[2 * e + 1]);
-              two = *reinterpret_cast<const uint32_t*>(&x);
+              float left[2] = {p[2 * e], p[2 * e + 1]};
+#pragma unroll
+              for (int i = 0; i < kPieces; ++i) {
+                const __nv_bfloat162 x = __floats2bfloat162_rn(left[0], left[1]);
+                pb[c][nt][i][e] = transposed(*reinterpret_cast<const uint32_t*>(&x));
+                left[0] -= __low2float(x);
+                left[1] -= __high2float(x);
+              }
             }
-            pb[c][nt][e] = transposed(two);
           }
         }
       // ---- weights . v
@@ -579,7 +586,9 @@ __global__ void __launch_bounds__(kThreads, Shape<kE4m3, DC>::kBlocks) attention
               }
               const int tile = p * (S::kVB / 2) + w * (kE4m3 ? 2 : 1) + i;
 #pragma unroll
-              for (int nt = 0; nt < NT; ++nt) mma<kE4m3>(o[nt][tile], a0, a1, a2, a3, pb[c][nt][0], pb[c][nt][1]);
+              for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int j = 0; j < kPieces; ++j) mma<kE4m3>(o[nt][tile], a0, a1, a2, a3, pb[c][nt][j][0], pb[c][nt][j][1]);
             }
           }
         }

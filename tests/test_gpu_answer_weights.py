@@ -1,0 +1,64 @@
+"""Attention over a paged cache keeps its weights' digits: rows of V that all but cancel leave the error of the weights alone.
+
+Pairs of positions hold x and -x with logits one step of 2^-7 apart, exact in every product: the result is P = sum p |v| times some 2^-9, and a weight rounded once, off by up to 2^-8 (bf16) or
+2^-11 (f16) of itself and by another amount in each of a pair, would show as some 2^-11 or 2^-14 P.  Tolerances count the roundings as those of test_gpu_answer do.  With a bf16 cache a weight is
+two pieces, of which the second rounds what the first leaves: w = (2^-8)^2; with an e4m3 cache it is one f16, w = 2^-11.  The positions that have a value have logits z below 2: theirs is off by delta = (2 d_k u) |z| + 6 u |z| (one product is
+not 0), and a weight by 2 delta + 2^-20; in e4m3 the exponent of V's scale and the lift add three roundings of numbers below 16, 2^-21 each.  The other positions lie 2^17 e lower and have no
+value.  The sums take (n / 32 + 64) 2 u.  So
+    |o - o*| <= 2^-8 |o*| + (P + |o*|) (w + 2 delta + 2^-20 + (n / 32 + 64) 2 u [+ 3 2^-21]) [+ n 2^-33 max |v|]    with e4m3's terms in brackets."""
+import numpy as np
+import pytest
+
+from oracle import answer as oa
+from test_gpu_answer import U, Paged, host, layout, mtf, queries, workspace  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+CAP = 17000
+
+# positions, pages of a sequence of 16: a block an item, clusters, the even cut
+PLANS = {"block": ([40, 17], 3), "clusters": ([700, 333], 44), "shares": ([3000, 40], -(-CAP // 16))}
+
+
+@pytest.mark.parametrize("group", [None, 3, 11])
+@pytest.mark.parametrize("d_v", [64, 128, 256])
+@pytest.mark.parametrize("plan", PLANS)
+@pytest.mark.parametrize("dtype", ["bf16", "e4m3"])
+def test_weights_keep_their_digits(mtf, dtype, plan, d_v, group):  # noqa: F811
+    import torch
+    lengths, per = PLANS[plan]
+    r, d_k, eight = np.random.RandomState(d_v + len(plan)), 16, dtype == "e4m3"
+    p = Paged(mtf, dtype, lengths, 2, d_k, d_v, 16, per=per, seed=1)
+    for s, n in enumerate(lengths):
+        z, v = np.full((n, 2), -16.0), np.zeros((n, 2, d_v))
+        for m in range(0, n - 1, 2 * max(1, n // 40)):
+            z[m] = 1 + r.randint(0, 127, 2) / 128                      # (one step below 2 left for the other)
+            z[m + 1] = z[m] + 2.0 ** -7
+            v[m] = r.randint(-15, 16, (2, d_v)) / 4.0                  # (four digits)
+            v[m + 1] = -v[m]
+        k = np.zeros((n, 2, d_k))
+        k[:, :, 0] = z
+        page, slot = p.table_host[s, np.arange(n) // 16], np.arange(n) % 16
+        if eight:                                                      # (a key's value is its scale's, and negative ones its sign's)
+            p.k_scale[page, slot] = torch.tensor(np.abs(z), dtype=torch.float32, device="cuda")
+            p.v_scale[page, slot] = 1.0
+            for pool, x in ((p.k, k / np.abs(z)[..., None]), (p.v, v)):
+                pool.view(torch.uint8)[page, slot] = torch.tensor(oa.to_e4m3(x), device="cuda")
+        else:
+            p.k[page, slot], p.v[page, slot] = (torch.tensor(x, dtype=torch.bfloat16, device="cuda") for x in (k, v))
+        assert np.array_equal(p.rows("k", s), k) and np.array_equal(p.rows("v", s), v)
+    lay = layout(mtf)
+    q, o, nq, no = queries(mtf, p, group, d_k, d_v)
+    q.zero_()
+    q[..., 0] = 1.0
+    mtf.mtf_attention_decode(lay, nq, p.cache, p.lengths, 1.0, no, workspace(mtf, lay, nq, p))
+    mtf.mtf_device_status()
+    p.guard.check()
+    got = host(o).reshape(len(lengths), 2, -1, d_v)
+    delta = (2 * d_k + 6) * U * 2
+    for s, n in enumerate(lengths):
+        v = p.rows("v", s)
+        want, size, _ = oa.decode(host(q)[s].reshape(2, -1, d_k), p.rows("k", s), v, 1.0)
+        off = (2.0 ** -11 + 3 * 2.0 ** -21 if eight else 2.0 ** -16) + 2 * delta + 2.0 ** -20 + (n / 32 + 64) * 2 * U
+        tol = 2.0 ** -8 * np.abs(want) + (size + np.abs(want)) * off + (n * 2.0 ** -33 * np.abs(v).max() if eight else 0.0)
+        err = np.abs(got[s] - want)
+        assert (err <= tol).all(), (s, n, float((err / np.maximum(tol, 1e-300)).max()))
