@@ -20,6 +20,7 @@
 #include "answer.cuh"
 #include "answer.h"
 #include "launch.cuh"
+#include "row_part.h"
 
 namespace {
 
@@ -174,15 +175,14 @@ struct Part {
   const T* first;
   const uint4* base;           // 16-byte boundary at or in front of `first`
   int off, n;                  // words from there to `first`
-  int whole;                   // pieces that come in whole 16-byte loads: all but the row's last, if it is not full, and, off the boundaries, the logits' last
+  int whole;                   // pieces that come in whole 16-byte loads: all but the row's last, if it is not full, and, where rows may begin anywhere, the logits' last
 
   __device__ __forceinline__ Part(const T* z, long long at, int count, long long total) {
     first = z + at;
     n = count;
     off = kAligned ? 0 : (int)(at % kN);
     base = reinterpret_cast<const uint4*>(z + (at - off));
-    whole = n / kN;
-    if (!kAligned) whole = (int)min((long long)whole, max((total - (at - off)) / kN - (off ? 1 : 0), 0LL));
+    whole = mtf::whole_pieces(at, n, total, kN, kAligned);
   }
   __device__ __forceinline__ int pieces() const { return (n + kN - 1) / kN; }
   // from the 16 bytes that piece p begins in, and those behind
