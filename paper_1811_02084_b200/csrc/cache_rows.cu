@@ -259,12 +259,13 @@ __global__ void __launch_bounds__(256) cache_reorder_kernel(const ReorderArgs a)
   const int n = a.lengths[from], whole = max(n, 0) / a.slots, used = max(n, 0) - whole * a.slots;
   const bool fits = n >= 0 && n <= (long long)a.per_sequence * a.slots;
   const int page = used && fits ? of[whole] : 0, fresh = used && fits ? a.fresh[x] : 0;
-  const bool there = page >= 0 && page < a.pages && fresh >= 0 && fresh < a.pages;
+  const bool source = page >= 0 && page < a.pages, there = source && fresh >= 0 && fresh < a.pages;
   if (tid == 0) {
     a.new_lengths[x] = n;
     if (!fits || !there) atomicExch(&g_bad_place, 1);
   }
-  for (int i = tid; i < a.per_sequence; i += threads) to[i] = i == whole && used && fits ? fresh : of[i];
+  // (a last page that is none stays one: what is left out goes on being left out)
+  for (int i = tid; i < a.per_sequence; i += threads) to[i] = i == whole && used && fits && source ? fresh : of[i];
   if (!used || !fits || !there) return;
   // Rows in use of the page that goes on, `used` slots of every head, K's and V's as one range of 16-byte pieces, four under way a thread.  The inner one of slot and head is
   // contiguous: slots of a head (used of them), or all heads of a slot.
