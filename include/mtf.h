@@ -595,7 +595,9 @@ mtf_status mtf_beam_select_workspace_bytes(const mtf_layout_t* layout, const mtf
 mtf_status mtf_beam_reorder(const mtf_layout_t* layout, const char* beam, const int32_t* parents, const mtf_tensor* states, mtf_tensor* out, void* stream);
 /* And a paged cache: sequence (sentence, i) of the new table goes on from sequence (sentence, parents[sentence, i]) of cache->table
  * [sentences, beams, table_pages].  Whole pages are shared; the last one, if it is not full, is copied (its rows in use) to the page fresh[sentence, i], so that each may go on by itself.
- * new_table int32 [sentences, slots, table_pages], new_lengths int32 [sentences, slots]; lengths int32 [sentences, beams]: positions so far.
+ * new_table int32 [sentences, slots, table_pages], new_lengths int32 [sentences, slots]; lengths int32 [sentences, beams]: positions so far (one below 0, or beyond
+ * what the table has pages for, is reported, and 0 or the table's room in new_lengths).  Of a parent outside the beams nothing goes on: pages -1, length 0; a last page outside the pool stays
+ * in the table as it is.
  * fresh int32 [sentences, slots]: pages that no table of the call has in use, different from each other; one that a full last page leaves no need for is not
  * touched and may be given again. */
 mtf_status mtf_cache_reorder(const mtf_layout_t* layout, const mtf_cache* cache, int64_t sentences, int64_t beams, int64_t slots, const int32_t* parents,

@@ -256,17 +256,16 @@ __global__ void __launch_bounds__(256) cache_reorder_kernel(const ReorderArgs a)
   }
   const int from = group * a.beams + parent;
   const int32_t* const of = a.table + (long long)from * a.per_sequence;
-  const int n = a.lengths[from], whole = max(n, 0) / a.slots, used = max(n, 0) - whole * a.slots;
-  const bool fits = n >= 0 && n <= (long long)a.per_sequence * a.slots;
-  const int page = used && fits ? of[whole] : 0, fresh = used && fits ? a.fresh[x] : 0;
+  const int length = a.lengths[from], n = min(max(length, 0), a.per_sequence * a.slots), whole = n / a.slots, used = n - whole * a.slots;      // (positions that the table has pages for)
+  const int page = used ? of[whole] : 0, fresh = used ? a.fresh[x] : 0;
   const bool source = page >= 0 && page < a.pages, there = source && fresh >= 0 && fresh < a.pages;
   if (tid == 0) {
     a.new_lengths[x] = n;
-    if (!fits || !there) atomicExch(&g_bad_place, 1);
+    if (n != length || !there) atomicExch(&g_bad_place, 1);
   }
   // (a last page that is none stays one: what is left out goes on being left out)
-  for (int i = tid; i < a.per_sequence; i += threads) to[i] = i == whole && used && fits && source ? fresh : of[i];
-  if (!used || !fits || !there) return;
+  for (int i = tid; i < a.per_sequence; i += threads) to[i] = i == whole && used && source ? fresh : of[i];
+  if (!used || !there) return;
   // Rows in use of the page that goes on, `used` slots of every head, K's and V's as one range of 16-byte pieces, four under way a thread.  The inner one of slot and head is
   // contiguous: slots of a head (used of them), or all heads of a slot.
   const int rows = used * a.heads, run = a.row_slot == 1 ? used : a.heads, gap = a.row_slot == 1 ? a.row_head : a.row_slot;

@@ -81,3 +81,25 @@ def test_a_last_page_outside_the_pool_stays_outside(mtf, which, dtype, slot_firs
     mtf.mtf_cache_reorder(lay, cache(mtf, p, new_table), ints([[0, 1, 2], [2, 1, 0]]), ints(lengths), ints(np.full((S, K), p.spare[-1])), again, torch.empty_like(new_lengths))
     reported(mtf)
     assert host(again)[1, [0, 2], LENGTH // SLOTS].tolist() == [bad, bad]
+
+
+@pytest.mark.parametrize("slot_first", [True, False])
+@pytest.mark.parametrize("dtype", ["bf16", "e4m3"])
+def test_lengths_below_0_and_beyond_the_table_become_what_the_table_has(mtf, dtype, slot_first):  # noqa: F811
+    import torch
+    p, pools, fresh, new_table, new_lengths = setting(mtf, dtype, slot_first, per=3)
+    room = 3 * SLOTS
+    lengths = np.array([[-1, room + 1, LENGTH], [-2 ** 31, 2 ** 31 - 1, 0]])
+    parents = np.array([[0, 1, 2], [0, 1, 2]])
+    before = {n: raw(getattr(p, n)) for n in pools}
+    mtf.mtf_cache_reorder(layout(mtf), cache(mtf, p, p.table.view(S, K, -1)), ints(parents), ints(lengths), ints(fresh), new_table, new_lengths)
+    reported(mtf)
+    p.guard.check()
+    assert host(new_lengths).tolist() == [[0, room, LENGTH], [0, room, 0]]
+    want = p.table_host.reshape(S, K, -1).copy()
+    want[0, 2, LENGTH // SLOTS] = fresh[0, 2]                         # (the one that goes on)
+    assert np.array_equal(host(new_table).astype(int), want)
+    for n in pools:
+        now = raw(getattr(p, n))
+        now[fresh[0, 2]] = before[n][fresh[0, 2]]
+        assert torch.equal(now, before[n])
