@@ -139,6 +139,14 @@ __device__ __forceinline__ void copy_box(uint32_t to, const CUtensorMap* map, in
                : "memory");
 }
 
+// What a weighted sum relative to 2^top_o is multiplied by, one factor after the other, where the weights' sum is relative to 2^top_l.  8-bit rows of V may have scales down to the smallest float, and
+// the reference lies 2^-9 below them (kLift), where ex2 gives 0: what lies below 2^-60 is a factor of its own.  (bf16: the references are equal, and the factors 1 / sum and 1.)
+__device__ __forceinline__ float2 last_factors(float top_o, float top_l, float sum) {
+  constexpr float kFar = -60.f;                    // (1 / sum is above 2^-40)
+  const float e = top_o == top_l ? 0.f : top_o - top_l;
+  return make_float2(ex2(fmaxf(e, kFar)) / sum, ex2(fminf(e - kFar, 0.f)));
+}
+
 // first unit of block c, of `units` over `blocks`
 __device__ __forceinline__ long long first_unit(long long units, int blocks, int c) { return units * c / blocks; }
 
@@ -650,9 +658,9 @@ __global__ void __launch_bounds__(kThreads, Shape<kE4m3, DC>::kBlocks) attention
       }
       if (whole) {
         if (g < here && d < a.dv) {
-          const float f = sum == 0.f ? 0.f : (kE4m3 ? ex2(top_o - top_l) : 1.f) / sum;
+          const float2 f = last_factors(top_o, top_l, sum);
           __nv_bfloat162* const to = reinterpret_cast<__nv_bfloat162*>(a.o + ((((long long)seq * a.heads + head) * a.group + g0 + g) * a.dv + d));
-          *to = __floats2bfloat162_rn(sum == 0.f ? 0.f : x * f, sum == 0.f ? 0.f : y * f);
+          *to = __floats2bfloat162_rn(sum == 0.f ? 0.f : x * f.x * f.y, sum == 0.f ? 0.f : y * f.x * f.y);
         }
       } else if (a.balanced) {
         *reinterpret_cast<float2*>(a.part_o + ((long long)slot * kHeads + g) * DC + d) = make_float2(x, y);
@@ -691,9 +699,9 @@ __global__ void __launch_bounds__(kThreads, Shape<kE4m3, DC>::kBlocks) attention
             x += v[c].x * f;
             y += v[c].y * f;
           }
-        const float f = sum == 0.f ? 0.f : (top_o == top_l ? 1.f : ex2(top_o - top_l)) / sum;
+        const float2 f = last_factors(top_o, top_l, sum);
         __nv_bfloat162* const to = reinterpret_cast<__nv_bfloat162*>(a.o + ((((long long)seq * a.heads + head) * a.group + g0 + g) * a.dv + d));
-        *to = __floats2bfloat162_rn(sum == 0.f ? 0.f : x * f, sum == 0.f ? 0.f : y * f);
+        *to = __floats2bfloat162_rn(sum == 0.f ? 0.f : x * f.x * f.y, sum == 0.f ? 0.f : y * f.x * f.y);
       }
       cluster_barrier();                             // (no block leaves while others read what it has)
     }
@@ -784,10 +792,11 @@ __global__ void __launch_bounds__(256, 4) attention_decode_join_kernel(const Arg
   for (int j = 0; j < kFours; ++j) {
     const int at = (j * 256 + tid) * 4, g = at / DC, d = at % DC;
     if (g >= here || d >= a.dv) continue;
-    const float l = sums[g], f = l == 0.f ? 0.f : (tops[g][1] == tops[g][0] ? 1.f : ex2(tops[g][1] - tops[g][0])) / l;
+    const float l = sums[g];
+    const float2 f = last_factors(tops[g][1], tops[g][0], l);
     __nv_bfloat162* const to = reinterpret_cast<__nv_bfloat162*>(a.o + ((((long long)piece.x * a.heads + head) * a.group + g0 + g) * a.dv + d));
-    to[0] = __floats2bfloat162_rn(l == 0.f ? 0.f : sum[j].x * f, l == 0.f ? 0.f : sum[j].y * f);
-    to[1] = __floats2bfloat162_rn(l == 0.f ? 0.f : sum[j].z * f, l == 0.f ? 0.f : sum[j].w * f);
+    to[0] = __floats2bfloat162_rn(l == 0.f ? 0.f : sum[j].x * f.x * f.y, l == 0.f ? 0.f : sum[j].y * f.x * f.y);
+    to[1] = __floats2bfloat162_rn(l == 0.f ? 0.f : sum[j].z * f.x * f.y, l == 0.f ? 0.f : sum[j].w * f.x * f.y);
   }
 }
 

@@ -62,3 +62,32 @@ def test_weights_keep_their_digits(mtf, dtype, plan, d_v, group):  # noqa: F811
         tol = 2.0 ** -8 * np.abs(want) + (size + np.abs(want)) * off + (n * 2.0 ** -33 * np.abs(v).max() if eight else 0.0)
         err = np.abs(got[s] - want)
         assert (err <= tol).all(), (s, n, float((err / np.maximum(tol, 1e-300)).max()))
+
+
+@pytest.mark.parametrize("plan", PLANS)
+@pytest.mark.parametrize("far", [-110, -117, -120, -126])
+@pytest.mark.parametrize("some_zero", [False, True])
+def test_rows_of_v_with_the_smallest_scales(mtf, some_zero, far, plan):  # noqa: F811
+    """Scales of V down to the smallest normal float, all of them or all but every fifth, which is 0: results that a bf16 still holds."""
+    lengths, per = PLANS[plan]
+    p = Paged(mtf, "e4m3", lengths, 2, 64, 64, 16, per=per, seed=far + 200)
+    for s, n in enumerate(lengths):
+        page, slot = p.table_host[s, np.arange(n) // 16], np.arange(n) % 16
+        p.v_scale[page, slot] = 2.0 ** far
+        if some_zero:
+            p.v_scale[page[::5], slot[::5]] = 0.0
+    lay = layout(mtf)
+    q, o, nq, no = queries(mtf, p, 3, 64, 64)
+    mtf.mtf_attention_decode(lay, nq, p.cache, p.lengths, 0.125, no, workspace(mtf, lay, nq, p))
+    mtf.mtf_device_status()
+    p.guard.check()
+    got = host(o)
+    for s, n in enumerate(lengths):
+        k, v, qs = p.rows("k", s), p.rows("v", s), host(q)[s]
+        want, size, z = oa.decode(qs, k, v, 0.125)
+        assert np.abs(want).max() > 2.0 ** (far + 2)
+        A = 0.125 * np.einsum("hgd,mhd->hgm", np.abs(qs), np.abs(k)).max(-1)
+        delta = (2 * 64 * U * A + 6 * U * np.abs(z).max(-1))[..., None]
+        # the tolerance of test_gpu_answer; a weight as small as 2^-34 of the largest that a scale goes with; and half of the smallest step of bf16
+        tol = 2.0 ** -8 * np.abs(want) + size * (2.0 ** -11 + 4 * delta + 2.0 ** -20 + (n / 32 + 64) * 4 * U) + n * 2.0 ** -33 * np.abs(v).max() + 2.0 ** -134
+        assert (np.abs(got[s] - want) <= tol).all(), (s, float((np.abs(got[s] - want) / tol).max()))
