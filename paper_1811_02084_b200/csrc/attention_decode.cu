@@ -504,6 +504,37 @@ __global__ void __launch_bounds__(kThreads, Shape<kE4m3, DC>::kBlocks) attention
           if (kE4m3) rise |= xo[nt][h] > mo[nt][h] + kSlack;
         }
       if (__any_sync(0xffffffffu, rise)) {
+        if (kE4m3) {
+          // Rows of zeros of V take part in the sum of weights alone: their scale, which is 1 where they were written, would else put the reference so far above rows of small values
+          // that these have no digits left.  Looked at where a reference rises, the only place where it matters.
+          uint32_t zeros[S::kIndexes];
+#pragma unroll
+          for (int i = 0; i < S::kIndexes; ++i) {
+            const int key = S::kKeys < 32 ? lane & (S::kKeys - 1) : i * 32 + lane;
+            uint32_t any = 0;
+#pragma unroll
+            for (int box = 0; box < S::kBoxes; ++box)
+#pragma unroll
+              for (int j = 0; j < S::kRow / 16; ++j) {
+                const uint4 x = *reinterpret_cast<const uint4*>(stage + S::kSide + (((key >> 4) * S::kBoxes + box) * 16 + (key & 15)) * S::kRow + ((j + lane) & (S::kRow / 16 - 1)) * 16);
+                any |= x.x | x.y | x.z | x.w;
+              }
+            zeros[i] = __ballot_sync(0xffffffffu, (any & 0x7f7f7f7fu) == 0);
+          }
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) xo[nt][0] = xo[nt][1] = -INFINITY;
+#pragma unroll
+          for (int c = 0; c < S::kTiles; ++c)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              const int key = c * 16 + e * 8;
+              if (zeros[key / 32] >> (key % 32 + key_r) & 1) tv[c][e] = -INFINITY;
+#pragma unroll
+              for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) xo[nt][h] = fmaxf(xo[nt][h], s[c][nt][2 * e + h] + tv[c][e]);
+            }
+        }
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll

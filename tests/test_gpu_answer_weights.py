@@ -10,7 +10,7 @@ import numpy as np
 import pytest
 
 from oracle import answer as oa
-from test_gpu_answer import U, Paged, host, layout, mtf, queries, workspace  # noqa: F401
+from test_gpu_answer import U, Paged, check_attention, host, layout, mtf, queries, workspace  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 CAP = 17000
@@ -91,3 +91,32 @@ def test_rows_of_v_with_the_smallest_scales(mtf, some_zero, far, plan):  # noqa:
         # the tolerance of test_gpu_answer; a weight as small as 2^-34 of the largest that a scale goes with; and half of the smallest step of bf16
         tol = 2.0 ** -8 * np.abs(want) + size * (2.0 ** -11 + 4 * delta + 2.0 ** -20 + (n / 32 + 64) * 4 * U) + n * 2.0 ** -33 * np.abs(v).max() + 2.0 ** -134
         assert (np.abs(got[s] - want) <= tol).all(), (s, float((np.abs(got[s] - want) / tol).max()))
+
+
+@pytest.mark.parametrize("plan", PLANS)
+@pytest.mark.parametrize("size", [1.0, 1e-4, 1e-6, 1e-12, 1e-30])
+@pytest.mark.parametrize("order", ["first", "last", "between"])
+def test_rows_of_zeros_leave_the_others_their_digits(mtf, order, size, plan):  # noqa: F811
+    """A row of zeros of V is stored with the scale 1: beside rows of small values that must not take the range of the weights, whether it comes before them, behind them or among them."""
+    import torch
+    lengths, per = PLANS[plan]
+    p = Paged(mtf, "e4m3", lengths, 2, 64, 128, 16, per=per, seed=3)
+    lay, n0 = layout(mtf), max(lengths)
+    g = torch.Generator(device="cuda").manual_seed(7)
+    kk, vv = (torch.randn(len(lengths), n0, 2, d, generator=g, device="cuda") for d in (64, 128))
+    vv *= size
+    for s, n in enumerate(lengths):
+        zero = {"first": np.arange(n) < n // 4, "last": np.arange(n) >= n - n // 4, "between": np.arange(n) % 7 == 3}[order]
+        vv[s, :n][torch.tensor(zero, device="cuda")] = 0.0
+        vv[s, 1 if order == "first" else n - 2, :, ::2] *= -0.0        # (zeros of both signs)
+    dims = ["batch", "length", "heads"]
+    mtf.mtf_cache_write(lay, mtf.named(kk, dims + ["d_k"]), mtf.named(vv, dims + ["d_v"]), None, p.lengths, p.cache)
+    q, o, nq, no = queries(mtf, p, 3, 64, 128)
+    mtf.mtf_attention_decode(lay, nq, p.cache, p.lengths, 0.125, no, workspace(mtf, lay, nq, p))
+    mtf.mtf_device_status()
+    p.guard.check()
+    for s, n in enumerate(lengths):
+        scales = oa.gather(host(p.v_scale), p.table_host[s], n, 16, True)
+        zero = ~p.rows("v", s).any(-1)
+        assert zero.any() and (scales[zero] == 1).all()
+    check_attention(p, q, o, 0.125)
