@@ -562,8 +562,9 @@ __global__ void __launch_bounds__(kThreads, Shape<kE4m3, DC>::kBlocks) attention
             }
           }
       }
-      // ---- weights.  bf16: two pieces, the nearest value and the nearest of what that leaves, so that a weight is off by 2^-16 of itself at most.  (One piece, 2^-8, puts the results
-      // of the 64 sequences above 2^-9.6 of their size from those of f32 weights, as far as their own rounding; two 2^-13.  The second costs 0.5 us of 180, 1.4 of 82 with 16 heads of queries a head.)
+      // ---- weights.  bf16: two pieces, the bits in front and the nearest value of what they leave, so that a weight is off by 2^-16 of itself at most.  The first is the next value below even where
+      // that would leave nothing: both are above 0, and what they make of an infinity in V is one.  (One piece, 2^-8, puts the results of the 64 sequences above 2^-9.6 of their size from
+      // those of f32 weights, as far as their own rounding; two 2^-13.  The second costs 0.7 us of 181, 1 of 82 with 16 heads of queries a head.)
       // e4m3: one f16 piece, 2^-11, which leaves 2^-12; a second would leave 2^-13.7 and cost 75 -> 77 us for the 4 sequences above, 62 -> 72 with 16 heads of queries to each of 4 heads.
       constexpr int kPieces = kE4m3 ? 1 : 2;
       uint32_t pb[S::kTiles][NT][kPieces][2];
@@ -591,14 +592,10 @@ __global__ void __launch_bounds__(kThreads, Shape<kE4m3, DC>::kBlocks) attention
               const __half2 x = __floats2half2_rn(p[2 * e], p[2 * e + 1]);
               pb[c][nt][0][e] = transposed(*reinterpret_cast<const uint32_t*>(&x));
             } else {
-              float left[2] = {p[2 * e], p[2 * e + 1]};
-#pragma unroll
-              for (int i = 0; i < kPieces; ++i) {
-                const __nv_bfloat162 x = __floats2bfloat162_rn(left[0], left[1]);
-                pb[c][nt][i][e] = transposed(*reinterpret_cast<const uint32_t*>(&x));
-                left[0] -= __low2float(x);
-                left[1] -= __high2float(x);
-              }
+              const uint32_t f0 = max(__float_as_uint(p[2 * e]), 1u) - 1u, f1 = max(__float_as_uint(p[2 * e + 1]), 1u) - 1u;
+              const __nv_bfloat162 x = __floats2bfloat162_rn(p[2 * e] - __uint_as_float(f0 & 0xffff0000u), p[2 * e + 1] - __uint_as_float(f1 & 0xffff0000u));
+              pb[c][nt][0][e] = transposed(prmt(f0, f1, 0x7632));
+              pb[c][nt][kPieces - 1][e] = transposed(*reinterpret_cast<const uint32_t*>(&x));
             }
           }
         }
