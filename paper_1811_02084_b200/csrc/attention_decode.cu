@@ -528,7 +528,7 @@ __global__ void __launch_bounds__(kThreads, Shape<kE4m3, DC>::kBlocks) attention
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
               const int key = c * 16 + e * 8;
-              if (zeros[key / 32] >> (key % 32 + key_r) & 1) tv[c][e] = -INFINITY;
+              if (zeros[key / 32] >> (key % 32 + key_r) & 1 && tv[c][e] < INFINITY) tv[c][e] = -INFINITY;      // (0 times a scale that is none is NaN)
 #pragma unroll
               for (int nt = 0; nt < NT; ++nt)
 #pragma unroll

@@ -1,4 +1,5 @@
-"""Infinities in V in attention over a paged cache: what the sum of products gives.  (A weight that multiplies V as two values must not make inf - inf or 0 inf of one.)"""
+"""Infinities in V in attention over a paged cache: what the sum of products gives.  (A weight that multiplies V as two values must not make inf - inf or 0 inf of one.)
+And scales of an e4m3 cache's rows of zeros that are not numbers: what is left out of a reference is not left out of the result."""
 import numpy as np
 import pytest
 
@@ -50,3 +51,17 @@ def test_infinities_in_rows_of_v(mtf, plan, d_v, group):  # noqa: F811
     again = host(o).reshape(got.shape)
     assert np.array_equal(again[~odd], got[~odd])
     check_attention(p, q, o, 0.125)
+
+
+@pytest.mark.parametrize("plan", PLANS)
+@pytest.mark.parametrize("scale", [float("nan"), float("inf")])
+def test_rows_of_zeros_with_scales_that_are_not_numbers(mtf, scale, plan):  # noqa: F811
+    n, per = PLANS[plan]
+    p = Paged(mtf, "e4m3", [n], 2, 64, 64, 16, per=per, seed=5)
+
+    def change():
+        import torch
+        p.v.view(torch.uint8)[p.table_host[0, 1], 4, 0] = 0
+        p.v_scale[p.table_host[0, 1], 4, 0] = scale
+    q, o = attend(mtf, p, 3, 64, change)
+    assert np.isnan(host(o)[0, 0]).all() and np.isfinite(host(o)[0, 1]).all()
