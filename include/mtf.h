@@ -584,7 +584,10 @@ mtf_status mtf_attention_decode_workspace_bytes(const mtf_layout_t* layout, cons
  * [*sentences, any name: slots], new_finished (may be NULL): 1 where the parent was finished or the token is end_id.  parents, tokens and new_finished are int32 of as many.
  * Words with a logit of -infinity, beams whose score is not finite (a beam that is not yet one: -infinity), and those with a NaN, a +infinity or
  * no finite logit offer nothing; slots without an offer have parent 0, token end_id, score -infinity, finished 1.
- * beams and slots up to 64, below 2^31 words in a sentence's beams.  A beam's words are compared by their logits, offers of different beams in 64 bits, from f32 exponentials summed in f32 by threads and in 64 bits across them.
+ * beams and slots up to 64, slots not more than beams times vocab, below 2^31 words in a sentence's beams.  A beam's words are compared by their logits, offers of different beams in 64 bits, from exponentials
+ * in f32 that are summed in f32 within a run of 2 KB of the row (by its threads, then across them) and in 64 bits, with one f32 factor a run, across runs: a row's sum is off by some 2^-18 at most.
+ * Where the beams that are neither finished nor none have more than 1024 words, but fewer such runs than there are slots (a search's first step, short vocabularies), or where more than 1024 words
+ * come as high as the best, the best are found by counting over whole rows, which takes ten times as long and more.
  * workspace as above; it is always needed. */
 mtf_status mtf_beam_select(const mtf_layout_t* layout, const mtf_tensor* logits, const mtf_tensor* scores, const int32_t* finished, int32_t end_id,
                            int32_t* parents, int32_t* tokens, mtf_tensor* new_scores, int32_t* new_finished, void* workspace, size_t workspace_bytes,
@@ -594,10 +597,12 @@ mtf_status mtf_beam_select_workspace_bytes(const mtf_layout_t* layout, const mtf
  * parents int32, one per index of the dimensions in front of `beam` and of out's `beam`.  f32, bf16 or e4m3, any dims and alignment of whole elements. */
 mtf_status mtf_beam_reorder(const mtf_layout_t* layout, const char* beam, const int32_t* parents, const mtf_tensor* states, mtf_tensor* out, void* stream);
 /* And a paged cache: sequence (sentence, i) of the new table goes on from sequence (sentence, parents[sentence, i]) of cache->table
- * [sentences, beams, table_pages].  Whole pages are shared; the last one, if it is not full, is copied (its rows in use) to the page fresh[sentence, i], so that each may go on by itself.
+ * [sentences, beams, table_pages].  Whole pages are shared; the last one, if it is not full, is copied (its rows in use) to the page fresh[sentence, i], so that each may go on in it by itself.
  * new_table int32 [sentences, slots, table_pages], new_lengths int32 [sentences, slots]; lengths int32 [sentences, beams]: positions so far (one below 0, or beyond
  * what the table has pages for, is reported, and 0 or the table's room in new_lengths).  Of a parent outside the beams nothing goes on: pages -1, length 0; a last page outside the pool stays
  * in the table as it is.
+ * Entries behind the last page in use are the parent's, and so the same for all that go on from it: before positions are written there, which is at once where the length is a multiple of a page's
+ * slots, each answer needs a page of its own put into its new table.
  * fresh int32 [sentences, slots]: pages that no table of the call has in use, different from each other; one that a full last page leaves no need for is not
  * touched and may be given again. */
 mtf_status mtf_cache_reorder(const mtf_layout_t* layout, const mtf_cache* cache, int64_t sentences, int64_t beams, int64_t slots, const int32_t* parents,

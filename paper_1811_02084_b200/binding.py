@@ -865,7 +865,8 @@ def mtf_beam_reorder(layout, beam: str, parents, states: Named, out: Named, stre
 
 def mtf_cache_reorder(layout, cache: Cache, parents, lengths, fresh, new_table, new_lengths, stream=None) -> None:
     """parents and fresh [*sentences, slots], lengths [*sentences, beams] of a cache whose table is [*sentences, beams, pages]; new_table [*sentences, slots, pages] and
-    new_lengths [*sentences, slots] are written.  All contiguous int32 device tensors."""
+    new_lengths [*sentences, slots] are written.  All contiguous int32 device tensors.  Entries of new_table behind the last page in use are the parent's: an answer needs pages of its own
+    there before positions are written to them, at once where its length is a multiple of a page's slots."""
     if cache is None or cache.table is None or cache.table.dim() < 2 or parents is None or parents.dim() != cache.table.dim() - 1 or parents.dim() < 1:
         raise MtfError(1, "cache_reorder: a table [*sentences, beams, pages] and parents [*sentences, slots]")
     beams, slots = int(cache.table.shape[-2]), int(parents.shape[-1])

@@ -4,13 +4,15 @@
 //
 // One read of the logits (HBM is the bound, close behind it the exponentials' unit) gives the sums, and of every run of 128 16-byte pieces the largest word.  A sentence's best
 // words lie in runs whose largest words are among its best: the slots-th largest of the maxima of 64 groups of runs is a value that `slots` words at least
-// reach, and a second launch looks only into the runs that reach it, hardly more than `slots` of 1 or 2 KB.  So the first launch is a walk and nothing else: its warps are streams of
+// reach, and a second launch looks only into the runs that reach it, hardly more than `slots` of 2 KB.  So the first launch is a walk and nothing else: its warps are streams of
 // their own, with bulk copies into a ring each, and wait for nobody.  (64 x 8 rows of 131072 in bf16, a tenth of them finished, calls in a graph: lists of the best words kept for each part of a row,
-// by blocks that stop to sort them, 47 us; by a warp of their own, 82; the walk with as many groups as slots, in 64 bits, 35.2; as it is 28.9, of which the walk is 24.  It
-// would take 18.8 without its exponentials; 1 x 4 rows of 32768 take 6.8 us in one launch, 2.3 of them the walk, and the rest is the choice's chain of some ten dependent steps.)
+// by blocks that stop to sort them, 47 us; by a warp of their own, 82; the walk with as many groups as slots, in 64 bits, 35.2; as it is 29.3, of which the walk is 24.  It
+// would take 18.8 without its exponentials; 1 x 4 rows of 32768 take 6.4 us in one launch, 2.3 of them the walk, and the rest is the choice's chain of some ten dependent steps.)
+// Runs are the finest groups: where fewer than `slots` of them are live there is no bar, and more than 1024 words then go by counting, one block a sentence.  (16 sentences of 8 beams over 4096 words, 8
+// slots: 7.3 us with all beams live, 82 in a search's first step; 12 beams over 1000, 24 slots: 225 in every step.  Finer groups of the few runs would give a bar there; not written.)
 //
-// What decides between beams is held in 64 bits: sums of a thread are f32 sums of f32 exponentials relative to an entry of its own, so that
-// the entries that weigh are exact or nearly so; they are joined in 64 bits.  Which thread takes which word goes by the word's index alone, not by
+// What decides between beams is held in 64 bits across runs.  Within one, exponentials relative to its largest word are f32 (of differences that are exact for the words that weigh), are added up in f32
+// by the lanes and then across them, and the run's factor is an f32 exponential: a row's sum is off by some 2^-18 at most, and offers of different beams nearer than that may change places.  Which thread takes which word goes by the word's index alone, not by
 // how the row is aligned: rows that are equal have equal sums to the bit, and their words tie as they should.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>

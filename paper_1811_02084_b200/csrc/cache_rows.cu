@@ -80,7 +80,8 @@ __device__ __forceinline__ int place(const RowsArgs& a, int unit) {
 // 32 / kLanes heads of a warp are an item, and a warp has kEach items' loads under way at once: of one position, or of several where it has few heads.  Their places
 // are looked up by a lane each, those of the next items while these ones' rows are under way.  blockIdx.y: K or V.
 // (A look at the table a row, whole calls: 32 x 512 prompts of 16 heads of 64 written in e4m3 and read back 63 us, 8 x 16384 positions of 8 heads of 128 read back 138; this way 36 and 120, 4.9 and 5.8 TB/s.  Reading is near
-// HBM's rate; writing spends its issue slots on finding the rows' largest values and on the conversions, of 8 values a lane 70 % of them.)
+// HBM's rate; writing waits for its loads and spends issue slots, 62 % of them, on finding the rows' largest values and on the conversions, of 16 values a lane with some spills: 64 registers are what
+// four blocks an SM leave a thread.)
 constexpr int kRowBlocks = 4;          // an SM holds; K's come first
 template <int kEach>
 struct Items {
